@@ -65,7 +65,13 @@ typedef enum {
     GACER_ACT = 11,       /* y = act(x)                                                      */
     GACER_SCALE = 12,     /* y[n,c,h,w] = act(in0[n,c,h,w] * in1[n,c]): squeeze-and-excitation gate */
     GACER_CONCAT = 13,    /* y[:, :cin] = in0, y[:, cin:] = in1 (channel concatenation)      */
-    GACER_AVGPOOL = 14    /* unpadded window mean (kh = kw, stride)                          */
+    GACER_AVGPOOL = 14,   /* unpadded window mean (kh = kw, stride)                          */
+    /* operators of a decoding tenant; `w` is a HOST pointer to their descriptor, see gacer_rope / gacer_cache / gacer_sampling */
+    GACER_QKNORM_ROPE = 15,     /* RMS norm of every query and key head, then rotation by position */
+    GACER_CACHE_WRITE = 16,     /* keys and values of new tokens into a paged 4-bit cache          */
+    GACER_CACHE_READ = 17,      /* keys and values of cached tokens back in the tenant's type      */
+    GACER_CACHE_ATTENTION = 18, /* causal attention of new tokens over that cache                  */
+    GACER_SAMPLE = 19           /* next token of every row of logits                               */
 } gacer_opkind;
 
 /* HSWISH(v) = v * HSIGMOID(v), HSIGMOID(v) = min(max(v + 3, 0), 6) / 6 */
@@ -114,7 +120,7 @@ typedef struct {
 typedef struct {
     gacer_opkind kind;
     int in0, in1, res, out;
-    const void *w;      /* device: weights (dtype of the tenant)           */
+    const void *w;      /* device: weights (dtype of the tenant); kinds from QKNORM_ROPE on: host, their descriptor */
     const float *bias;  /* device: [cout] or NULL                          */
     const float *scale; /* device: [c]   AFFINE_ACT scale / LAYERNORM gamma */
     const float *shift; /* device: [c]   AFFINE_ACT shift / LAYERNORM beta  */
@@ -122,6 +128,92 @@ typedef struct {
     gacer_act act;
     float alpha;
 } gacer_op;
+
+/*
+ * Descriptors of the operators of a decoding tenant.  gacer_op.w points to one of them in HOST memory (no alignment asked);
+ * gacer_load_tenants copies it.  The pointers inside are DEVICE pointers owned by the caller; what they point to is read
+ * when a round runs, so lengths, positions, page tables and filters may change between rounds (or between replays of a
+ * captured round) without loading anything again.  Device values out of range are never followed: see each operator.
+ * Pools and tables are 16-byte aligned, arrays with a value per row, token or sequence as their type.
+ *
+ * Tokens: a qkv tensor is (n=batch, c=(heads+2*kv_heads)*head_dim, h=S, w=1): S new tokens of each of `batch` sequences, each
+ * [query heads | key heads | value heads].  heads is a multiple of kv_heads; query head i reads key/value head
+ * i / (heads/kv_heads).  These operators split along the batch (GACER_AXIS_BATCH); act must be NONE, in1 and res -1.
+ */
+
+/*
+ * QKNORM_ROPE: in0 = qkv, out = a tensor of the same shape (its memory may be in0's: in place, then the values are left alone).
+ * Every query head x becomes x * rsqrt(mean(x^2) + alpha) * scale (scale = device [head_dim], NULL: the query heads are not
+ * normed), every key head likewise with `shift`; then the first rotary_dims features are rotated in pairs: pair i is
+ * features (i, i + rotary_dims/2), interleaved != 0: (2i, 2i+1), and (a, b) becomes (a*c - b*s, b*c + a*s) with
+ * (c, s) = table[positions[b][t][axis of i]][i].  Pairs belong to axes in order: sections[0] pairs to axis 0, and so on
+ * (text: one axis; images and video: height and width, or time, height and width).  Value heads are copied.
+ * head_dim: a multiple of 8, 8..512.  rotary_dims: a multiple of 16, 0..head_dim.  1 <= n_axes <= 3, sections sum to rotary_dims/2.
+ * A position outside [0, n_positions) turns its pairs into NaN.  All arithmetic in fp32, one rounding at the end.
+ */
+typedef struct {
+    int heads, kv_heads, head_dim;
+    int rotary_dims, interleaved;
+    int n_axes, sections[3];
+    int n_positions;
+    const float *table;   /* device [n_positions][rotary_dims/2][2]: cosine, sine; NULL with rotary_dims == 0 */
+    const int *positions; /* device [batch][S][n_axes];                            NULL with rotary_dims == 0 */
+} gacer_rope;
+
+/*
+ * A paged cache of keys and values in 4 bits, shared by CACHE_WRITE, CACHE_READ and CACHE_ATTENTION.
+ * Token p of sequence b lies in page page_table[b][p / page_tokens], at p % page_tokens.  A page outside [0, n_pages) is absent:
+ * its tokens are not written, read back as zeros and are not attended to; so are positions from max_pages * page_tokens on.
+ * Per call, sequence b has start[b] tokens before the S new ones, of which the first count[b] are real (count NULL: all S;
+ * count is taken as 0..S; a negative start or one beyond the pages makes it 0).
+ *   Codes: groups of GACER_CACHE_GROUP features of one head and token share a pair of bf16 numbers (scale, minimum) in one
+ * 32-bit word (scale in the low half); a code c in 0..15 stands for c * scale + minimum.  Writing a group of x takes
+ * minimum = bf16(min x), scale = bf16((max x - min x) / 15), c = round((x - minimum) / scale) clamped to 0..15 (ties to even; 0 where scale
+ * is 0), in fp32.  A group that holds an infinity or a NaN, or whose scale or minimum overflows, gets a NaN scale (0x7FC0) and reads back as NaN.
+ *   Layout: k_codes [page][kv head][token][head_dim/8 words], word i = features 8i..8i+7; v_codes [page][kv head][token / 32][feature][4 words],
+ * word i = tokens 8i..8i+7 of the block of 32; the eight codes of a word start at bits 0, 16, 4, 20, 8, 24, 12, 28.
+ * k_scales and v_scales [page][kv head][token][head_dim/GACER_CACHE_GROUP].
+ *   CACHE_WRITE: in0 = qkv; out = -1.  Writes tokens start[b] .. start[b]+count[b]-1; every other code of a page keeps its value.  No two
+ * sequences may write to one page in the same call.
+ *   CACHE_READ: in0 = -1; out = (n=batch, c=2*kv_heads*head_dim, h=S, w=1): row t = [key heads | value heads] of token start[b]+t; rows
+ * from count[b] on are zeros.
+ *   CACHE_ATTENTION: in0 = qkv (only its query heads are read), out = (n=batch, c=heads*head_dim, h=S, w=1): query t stands at
+ * p = start[b]+t and sees the present keys j <= p, with window > 0 only those with j > p - window:
+ * out = sum_j softmax_j(alpha * q.k_j) v_j.  Rows from count[b] on, and rows that see no key, are zeros.  CACHE_WRITE of the same tokens
+ * comes first.  Scores, softmax and sums in fp32.
+ * head_dim: 64 or 128.  page_tokens: a power of two, 32..4096.  heads/kv_heads <= 64.
+ */
+#define GACER_CACHE_GROUP 64
+typedef struct {
+    int heads, kv_heads, head_dim; /* heads is not looked at by CACHE_READ */
+    int page_tokens, n_pages, max_pages;
+    int window;                    /* CACHE_ATTENTION: 0 = all keys */
+    void *k_codes, *v_codes;       /* device pools, see above */
+    unsigned int *k_scales, *v_scales;
+    const int *page_table;         /* device [batch][max_pages] */
+    const int *start, *count;      /* device [batch]; count may be NULL */
+} gacer_cache;
+
+/*
+ * SAMPLE: in0 = logits (any n, h, w; c = vocabulary, at most 2^24); out = -1.  For every row (position) of logits x, in fp32, NaN taken as -inf:
+ *   m = max x; e_i = 1 where x_i = m, else exp((x_i - m) / temperature); weight w_i = floor(e_i * 2^31), a whole number;
+ *   order: larger x first, equal x by lower index.  Of this order top_k keeps the first top_k entries (<= 0: all); top_p the shortest
+ *   prefix of those whose weights sum to at least top_p of theirs (>= 1: all; <= 0: the first entry); min_p the entries with
+ *   e_i >= min_p (and the first).  temperature <= 0 keeps the first entry only.
+ *   token = the first i, by index, at which the sum of the kept weights up to and with i exceeds floor(u * total) (at most total - 1).
+ * Weights being whole numbers, their sums are the same in any order, and the token does not depend on how the work is split.
+ * logp = (x_token - m) / temperature - ln(total / 2^31), the logarithm of the probability it was drawn with.
+ * A row without a number above -inf gives token -1 and logp -inf.
+ * Parameters are device arrays with a value per row; NULL: temperature 1, top_k 0, top_p 1, min_p 0.
+ */
+typedef struct {
+    const float *u;           /* device [rows], in [0, 1) */
+    const float *temperature;
+    const int *top_k;
+    const float *top_p, *min_p;
+    int *tokens;              /* device [rows]: the result */
+    float *logp;              /* device [rows] or NULL */
+} gacer_sampling;
 
 /* One tenant: its operator list in execution order, its tensors, and the stream it runs on. */
 typedef struct {
@@ -242,6 +334,16 @@ gacer_status gacer_run(gacer_ctx *ctx, int mode, int rounds, float *ms_per_round
  * Returns after all rounds have finished.
  */
 gacer_status gacer_run_static(gacer_ctx *ctx, int mode, int rounds);
+
+/*
+ * One round of one tenant in the stream of the caller's own work: issues the tenant's operators, unsplit and fused as
+ * gacer_set_fuse_affine says, on `stream` (a hipStream_t; NULL = null stream) and returns without waiting; ordinary stream order makes
+ * the inputs' producers and the outputs' readers correct.  For decoding loops, where the host prepares the next step while this one
+ * runs, and for callers that capture a step into a graph of their own (nothing is allocated, no event is recorded).  The tenant's
+ * split-K and attention workspaces belong to the context: two rounds of one tenant must not overlap, whichever calls issued them.  The
+ * plan, the tenant's own stream and captured graphs play no part.  gacer_destroy and gacer_load_tenants do not wait for `stream`.
+ */
+gacer_status gacer_enqueue(gacer_ctx *ctx, int tenant, void *stream);
 
 /*
  * Measurement aid: like gacer_run (same issue loop, one thread or one per tenant as set), but every kernel

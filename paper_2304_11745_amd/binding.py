@@ -16,7 +16,9 @@ LIB_PATH = os.path.join(_HERE, "libgacer.so")
 GACER_OK, GACER_EINVAL, GACER_ESHAPE, GACER_EPLAN, GACER_ESTATE, GACER_ENOMEM, GACER_EHIP = range(7)
 GACER_F32, GACER_BF16 = 0, 1
 (GACER_CONV2D, GACER_DWCONV2D, GACER_GEMM, GACER_BGEMM_QK, GACER_BGEMM_PV, GACER_MAXPOOL, GACER_GAVGPOOL,
- GACER_AFFINE_ACT, GACER_ADD, GACER_LAYERNORM, GACER_SOFTMAX, GACER_ACT, GACER_SCALE, GACER_CONCAT, GACER_AVGPOOL) = range(15)
+ GACER_AFFINE_ACT, GACER_ADD, GACER_LAYERNORM, GACER_SOFTMAX, GACER_ACT, GACER_SCALE, GACER_CONCAT, GACER_AVGPOOL,
+ GACER_QKNORM_ROPE, GACER_CACHE_WRITE, GACER_CACHE_READ, GACER_CACHE_ATTENTION, GACER_SAMPLE) = range(20)
+GACER_CACHE_GROUP = 64
 GACER_ACT_NONE, GACER_ACT_RELU, GACER_ACT_RELU6, GACER_ACT_GELU, GACER_ACT_HSWISH, GACER_ACT_HSIGMOID = range(6)
 GACER_AXIS_NONE, GACER_AXIS_BATCH, GACER_AXIS_COUT = range(3)
 GACER_MODE_PLAN, GACER_MODE_SEQUENTIAL, GACER_MODE_STREAM_PARALLEL = range(3)
@@ -25,7 +27,7 @@ EXPORTS = ["gacer_create", "gacer_destroy", "gacer_load_tenants", "gacer_set_pla
            "gacer_run", "gacer_profile", "gacer_search", "gacer_model_residue", "gacer_plan_free",
            "gacer_last_error", "gacer_launch_count", "gacer_trace_run", "gacer_issue_stats", "gacer_capture",
            "gacer_release_graphs", "gacer_set_issue_threads", "gacer_set_sync_every_launch", "gacer_set_fuse_affine", "gacer_probe_stream_queues", "gacer_place_streams",
-           "gacer_refine", "gacer_run_static", "gacer_plan_to_text",
+           "gacer_refine", "gacer_run_static", "gacer_enqueue", "gacer_plan_to_text",
            "gacer_plan_from_text"]
 
 
@@ -39,6 +41,22 @@ class gacer_op(C.Structure):
                 ("w", C.c_void_p), ("bias", C.c_void_p), ("scale", C.c_void_p), ("shift", C.c_void_p),
                 ("cin", C.c_int), ("cout", C.c_int), ("kh", C.c_int), ("kw", C.c_int), ("stride", C.c_int),
                 ("pad", C.c_int), ("groups", C.c_int), ("act", C.c_int), ("alpha", C.c_float)]
+
+
+class gacer_rope(C.Structure):
+    _fields_ = [("heads", C.c_int), ("kv_heads", C.c_int), ("head_dim", C.c_int), ("rotary_dims", C.c_int), ("interleaved", C.c_int),
+                ("n_axes", C.c_int), ("sections", C.c_int * 3), ("n_positions", C.c_int), ("table", C.c_void_p), ("positions", C.c_void_p)]
+
+
+class gacer_cache(C.Structure):
+    _fields_ = [("heads", C.c_int), ("kv_heads", C.c_int), ("head_dim", C.c_int), ("page_tokens", C.c_int), ("n_pages", C.c_int),
+                ("max_pages", C.c_int), ("window", C.c_int), ("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_scales", C.c_void_p),
+                ("v_scales", C.c_void_p), ("page_table", C.c_void_p), ("start", C.c_void_p), ("count", C.c_void_p)]
+
+
+class gacer_sampling(C.Structure):
+    _fields_ = [("u", C.c_void_p), ("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p),
+                ("tokens", C.c_void_p), ("logp", C.c_void_p)]
 
 
 class gacer_tenant(C.Structure):
@@ -87,6 +105,7 @@ def _load():
     lib.gacer_plan_from_pointers.argtypes = [ctx, C.POINTER(C.c_int), C.c_int, C.POINTER(C.POINTER(gacer_plan))]
     lib.gacer_run.argtypes = [ctx, C.c_int, C.c_int, C.POINTER(C.c_float)]
     lib.gacer_run_static.argtypes = [ctx, C.c_int, C.c_int]
+    lib.gacer_enqueue.argtypes = [ctx, C.c_int, C.c_void_p]
     lib.gacer_profile.argtypes = [ctx, C.POINTER(gacer_prof), C.c_size_t, C.POINTER(C.c_size_t)]
     lib.gacer_search.argtypes = [ctx, C.POINTER(gacer_prof), C.c_size_t, C.c_int, C.POINTER(C.POINTER(gacer_plan)),
                                  C.POINTER(C.c_int), C.POINTER(C.c_int), C.POINTER(C.c_double)]
@@ -123,6 +142,7 @@ gacer_set_plan = lib.gacer_set_plan
 gacer_plan_from_pointers = lib.gacer_plan_from_pointers
 gacer_run = lib.gacer_run
 gacer_run_static = lib.gacer_run_static
+gacer_enqueue = lib.gacer_enqueue
 gacer_profile = lib.gacer_profile
 gacer_search = lib.gacer_search
 gacer_model_residue = lib.gacer_model_residue

@@ -11,20 +11,25 @@ namespace gacer {
 
 // LK_EXPAND_DW: a pointwise convolution (`g`) and the depthwise convolution behind it (`s`); LK_ABSORBED: the operator's work is done by
 // the launch of an operator before it
-enum LaunchKind { LK_IGEMM, LK_DWCONV, LK_MAXPOOL, LK_GAVGPOOL, LK_ELTWISE, LK_LAYERNORM, LK_SOFTMAX, LK_CONCAT, LK_EXPAND_DW, LK_ABSORBED };
+enum LaunchKind { LK_IGEMM, LK_DWCONV, LK_MAXPOOL, LK_GAVGPOOL, LK_ELTWISE, LK_LAYERNORM, LK_SOFTMAX, LK_CONCAT, LK_EXPAND_DW, LK_ABSORBED, LK_TOKENS };
 
 struct Launch {
     LaunchKind kind;
     GemmArgs g;
     StreamArgs s;
+    TokenArgs k;
     size_t ws_off = 0;      // floats into the tenant's split-K workspace: chunks of one operator own disjoint parts
 };
 
 // the cut of one operator's K range (see GemmArgs)
 struct KSplit { int ksplit = 1, kb_per_slice = 1 << 28, kwaves = 0, kb_per_wave = 0; bool stem = false, halo = false; };
 
+// descriptor of an operator of a decoding tenant (gacer_op.w), copied when the tenants are loaded; one of the three by the operator's kind
+struct TokenDesc { gacer_rope rope; gacer_cache cache; gacer_sampling sampling; };
+
 struct Tenant {
     std::vector<gacer_op> ops;
+    std::vector<TokenDesc> token;                   // one per operator
     std::vector<gacer_tensor> tensors;
     int input = 0, output = 0, batch = 1;
     gacer_dtype dtype = GACER_F32;
@@ -90,6 +95,7 @@ struct Ctx {
 
 // axis extent and legality of a decomposition
 int axis_extent(const Tenant &t, int op, gacer_axis axis);
+inline bool is_token_op(gacer_opkind kind) { return kind >= GACER_QKNORM_ROPE; }
 bool axis_legal(gacer_opkind kind, gacer_axis axis);
 void chunk_range(int extent, int factor, int j, int *lo, int *hi);
 // builds the launch of operator `op` restricted to batch items [b_lo,b_hi) and channels [c_lo,c_hi)

@@ -24,6 +24,7 @@
 #include "conv3_geom.h"
 #include "expand_geom.h"
 #include "stem_geom.h"
+#include "tokens_geom.h"
 
 using namespace gacer;
 
@@ -110,9 +111,55 @@ void chunk_range(int extent, int factor, int j, int *lo, int *hi)
 
 static int dt(const Tenant &t) { return t.dtype == GACER_BF16 ? DT_BF16 : DT_F32; }
 
+// channels of an operator's output; an operator that writes none of the tenant's tensors counts as one channel
+static int out_channels(const Tenant &t, int oi) { return t.ops[oi].out < 0 ? 1 : (int)t.tensors[t.ops[oi].out].c; }
+
+// The launch of an operator of a decoding tenant, sequences [b_lo, b_hi)
+static Launch make_token_launch(const Tenant &t, int oi, int b_lo, int b_hi)
+{
+    const gacer_op &op = t.ops[oi];
+    const TokenDesc &d = t.token[oi];
+    const gacer_tensor *in = op.in0 >= 0 ? &t.tensors[op.in0] : nullptr, *out = op.out >= 0 ? &t.tensors[op.out] : nullptr;
+    Launch l;
+    std::memset(&l, 0, sizeof l);
+    l.kind = LK_TOKENS;
+    TokenArgs &k = l.k;
+    k.dtype = dt(t);
+    k.b_lo = b_lo; k.b_hi = b_hi;
+    k.x = in ? in->dptr : nullptr;
+    k.y = out ? out->dptr : nullptr;
+    k.S = (int)(in ? in->h : out->h);
+    k.alpha = op.alpha;
+    if (op.kind == GACER_QKNORM_ROPE) {
+        k.op = TK_QKNORM_ROPE;
+        k.heads = d.rope.heads; k.kv_heads = d.rope.kv_heads; k.D = d.rope.head_dim;
+        k.gamma_q = op.scale; k.gamma_k = op.shift; k.eps = op.alpha;
+        k.table = d.rope.table; k.positions = d.rope.positions;
+        k.R = d.rope.rotary_dims; k.interleaved = d.rope.interleaved; k.axes = d.rope.n_axes; k.n_positions = d.rope.n_positions;
+        for (int i = 0; i < 3; ++i) k.sections[i] = i < d.rope.n_axes ? d.rope.sections[i] : 0;
+    } else if (op.kind == GACER_SAMPLE) {
+        k.op = TK_SAMPLE;
+        k.vocab = (int)in->c;
+        k.S = (int)((in->n / t.batch) * in->h * in->w);
+        k.u = d.sampling.u; k.temperature = d.sampling.temperature; k.top_k = d.sampling.top_k; k.top_p = d.sampling.top_p; k.min_p = d.sampling.min_p;
+        k.tokens = d.sampling.tokens; k.logp = d.sampling.logp;
+    } else {
+        const gacer_cache &c = d.cache;
+        k.op = op.kind == GACER_CACHE_WRITE ? TK_CACHE_WRITE : op.kind == GACER_CACHE_READ ? TK_CACHE_READ : TK_CACHE_ATTENTION;
+        k.heads = c.heads; k.kv_heads = c.kv_heads; k.D = c.head_dim; k.window = c.window;
+        k.cache.k_codes = (unsigned char *)c.k_codes; k.cache.v_codes = (unsigned char *)c.v_codes;
+        k.cache.k_scales = c.k_scales; k.cache.v_scales = c.v_scales;
+        k.cache.page_table = c.page_table; k.cache.start = c.start; k.cache.count = c.count;
+        k.cache.kv_heads = c.kv_heads; k.cache.D = c.head_dim; k.cache.n_pages = c.n_pages; k.cache.max_pages = c.max_pages;
+        while ((1 << k.cache.page_shift) < c.page_tokens) ++k.cache.page_shift;
+    }
+    return l;
+}
+
 Launch make_launch(const Tenant &t, int oi, int b_lo, int b_hi, int c_lo, int c_hi)
 {
     const gacer_op &op = t.ops[oi];
+    if (is_token_op(op.kind)) return make_token_launch(t, oi, b_lo, b_hi);
     const gacer_tensor &in = t.tensors[op.in0];
     const gacer_tensor &out = t.tensors[op.out];
     Launch l;
@@ -247,6 +294,11 @@ LaunchInfo enqueue(const Launch &l, hipStream_t s, bool dry, int phase, float *w
         return launch_igemm(g, s, dry, phase);
     }
     case LK_ABSORBED: return {0, 0, 0, 1, "absorbed", 0};
+    case LK_TOKENS: {
+        TokenArgs k = l.k;
+        k.ws = ws;
+        return launch_tokens(k, s, dry || (!ws && token_ws_floats(k)), phase);   // never without its workspace
+    }
     default: return launch_eltwise(l.s, s, dry);
     }
 }
@@ -312,7 +364,90 @@ struct Written {
     }
 };
 
-static gacer_status check_op(Ctx *c, int ti, const gacer_tenant &t, int oi, const Written &written)
+// An operator of a decoding tenant: its descriptor against its tensors; copies the descriptor to *desc.
+static gacer_status check_token_op(Ctx *c, int ti, const gacer_tenant &t, int oi, const Written &written, TokenDesc *desc)
+{
+    const gacer_op &op = t.ops[oi];
+    auto bad = [&](const char *why) { return fail(c, GACER_ESHAPE, "tenant %d op %d: %s", ti, oi, why); };
+    auto inval = [&](const char *why) { return fail(c, GACER_EINVAL, "tenant %d op %d: %s", ti, oi, why); };
+    auto misaligned = [](const void *p, uintptr_t to) { return ((uintptr_t)p) % to != 0; };
+    if (!launch_tokens) return inval("this build holds no kernels for operators of a decoding tenant");
+    if (!op.w) return inval("null descriptor (w)");
+    if (op.act != GACER_ACT_NONE || op.in1 >= 0 || op.res >= 0) return bad("operators of a decoding tenant take no activation, in1 or res");
+    if (op.kind == GACER_CACHE_READ) {
+        if (op.in0 >= 0) return bad("cache read takes no in0");
+    } else if (op.in0 < 0 || op.in0 >= t.n_tensors || !written.all(op.in0)) return bad("in0 missing or not written by an earlier operator");
+    const bool writes = op.kind != GACER_CACHE_WRITE && op.kind != GACER_SAMPLE;
+    if (writes && (op.out < 0 || op.out >= t.n_tensors)) return bad("out index out of range");
+    if (!writes && op.out >= 0) return bad("this operator writes none of the tenant's tensors: out must be -1");
+    if (writes && !written.none(op.out)) return bad("out tensor is written twice");
+    const gacer_tensor *in = op.in0 >= 0 ? &t.tensors[op.in0] : nullptr, *out = writes ? &t.tensors[op.out] : nullptr;
+    if ((in && in->pitch) || (out && out->pitch)) return bad("operators of a decoding tenant do not take channel windows");
+    const int64_t esz = t.dtype == GACER_BF16 ? 2 : 4;
+    // whether in and out share memory
+    auto overlap = [&] {
+        const uintptr_t a = (uintptr_t)in->dptr, b = (uintptr_t)out->dptr;
+        return a < b + (uintptr_t)(out->n * out->c * out->h * out->w * esz) && b < a + (uintptr_t)(in->n * in->c * in->h * in->w * esz);
+    };
+    if (op.kind == GACER_SAMPLE) {
+        const gacer_sampling d = *(const gacer_sampling *)op.w;
+        if (in->n % t.batch) return bad("tensor n is not a multiple of the tenant batch");
+        if (in->c > (1 << 24)) return bad("a vocabulary of more than 2^24 entries");
+        if (!d.u || !d.tokens) return inval("null random numbers or token array");
+        for (const void *p : {(const void *)d.u, (const void *)d.temperature, (const void *)d.top_k, (const void *)d.top_p, (const void *)d.min_p, (const void *)d.tokens, (const void *)d.logp})
+            if (misaligned(p, 4)) return inval("misaligned array");
+        desc->sampling = d;
+        return GACER_OK;
+    }
+    for (const gacer_tensor *x : {in, out})
+        if (x && (x->n != t.batch || x->w != 1)) return bad("token tensors are (n=batch, c, h=tokens, w=1)");
+    if (op.kind == GACER_QKNORM_ROPE) {
+        const gacer_rope d = *(const gacer_rope *)op.w;
+        if (d.heads < 1 || d.kv_heads < 1 || d.heads > 4096 || d.kv_heads > 4096 || d.heads % d.kv_heads) return bad("heads must be a positive multiple of kv_heads");
+        if (d.head_dim < 8 || d.head_dim > 512 || d.head_dim % 8) return bad("head_dim must be a multiple of 8, 8..512");
+        if (in->c != (int64_t)(d.heads + 2 * d.kv_heads) * d.head_dim || !same_shape(*in, *out)) return bad("in0 and out must be (batch, (heads+2*kv_heads)*head_dim, tokens, 1)");
+        if (d.rotary_dims < 0 || d.rotary_dims > d.head_dim || d.rotary_dims % 16) return bad("rotary_dims must be a multiple of 16, at most head_dim");
+        if (!(op.alpha >= 0.f) || op.alpha > 1e30f) return bad("alpha (the norms' epsilon) must be a finite number, not negative");
+        if (d.rotary_dims) {
+            if (d.n_axes < 1 || d.n_axes > 3) return bad("n_axes must be 1..3");
+            int64_t sum = 0;
+            for (int i = 0; i < d.n_axes; ++i) {
+                if (d.sections[i] < 0) return bad("negative section");
+                sum += d.sections[i];
+            }
+            if (sum != d.rotary_dims / 2) return bad("sections must sum to rotary_dims / 2");
+            if (!d.table || !d.positions || d.n_positions < 1) return inval("null table or positions");
+            if (misaligned(d.table, 16) || misaligned(d.positions, 4)) return inval("misaligned table or positions");
+        }
+        if (misaligned(op.scale, 16) || misaligned(op.shift, 16)) return inval("parameter pointer not 16-byte aligned");
+        if (in->dptr != out->dptr && overlap()) return bad("out overlaps in0 without being it");
+        desc->rope = d;
+        return GACER_OK;
+    }
+    const gacer_cache d = *(const gacer_cache *)op.w;
+    if (d.kv_heads < 1 || d.kv_heads > 4096) return bad("kv_heads must be 1..4096");
+    if (op.kind != GACER_CACHE_READ && (d.heads < d.kv_heads || d.heads % d.kv_heads || d.heads / d.kv_heads > CACHE_HEADS_PER_KV_MAX)) return bad("heads must be a multiple of kv_heads, at most 64 times as many");
+    if (d.head_dim != 64 && d.head_dim != 128) return bad("the cache holds heads of 64 or 128 features");
+    if (d.page_tokens < 32 || d.page_tokens > 4096 || (d.page_tokens & (d.page_tokens - 1))) return bad("page_tokens must be a power of two, 32..4096");
+    if (d.n_pages < 1 || d.max_pages < 1 || (int64_t)d.max_pages * d.page_tokens > (1 << 30)) return bad("n_pages and max_pages must be positive, max_pages * page_tokens at most 2^30");
+    if (!d.k_codes || !d.v_codes || !d.k_scales || !d.v_scales || !d.page_table || !d.start) return inval("null cache pointer");
+    if (misaligned(d.k_codes, 16) || misaligned(d.v_codes, 16) || misaligned(d.k_scales, 16) || misaligned(d.v_scales, 16)) return inval("cache pools must be 16-byte aligned");
+    if (misaligned(d.page_table, 4) || misaligned(d.start, 4) || misaligned(d.count, 4)) return inval("misaligned array");
+    const int64_t kv = (int64_t)d.kv_heads * d.head_dim, q = (int64_t)d.heads * d.head_dim;
+    if (op.kind == GACER_CACHE_READ) {
+        if (out->c != 2 * kv) return bad("out must be (batch, 2*kv_heads*head_dim, tokens, 1)");
+    } else if (in->c != q + 2 * kv) return bad("in0 must be (batch, (heads+2*kv_heads)*head_dim, tokens, 1)");
+    if (op.kind == GACER_CACHE_ATTENTION) {
+        if (out->c != q || out->h != in->h) return bad("out must be (batch, heads*head_dim, tokens, 1)");
+        if (d.window < 0) return bad("negative window");
+        if (!(op.alpha - op.alpha == 0.f)) return bad("alpha (the scores' scale) is not finite");
+        if (overlap()) return bad("out shares memory with in0");
+    }
+    desc->cache = d;
+    return GACER_OK;
+}
+
+static gacer_status check_op(Ctx *c, int ti, const gacer_tenant &t, int oi, const Written &written, TokenDesc *desc)
 {
     const gacer_op &op = t.ops[oi];
     auto bad = [&](const char *why) { return fail(c, GACER_ESHAPE, "tenant %d op %d: %s", ti, oi, why); };
@@ -320,8 +455,9 @@ static gacer_status check_op(Ctx *c, int ti, const gacer_tenant &t, int oi, cons
         if (i < 0) return !required;
         return i < t.n_tensors && written.all(i);
     };
-    if ((int)op.kind < 0 || (int)op.kind > (int)GACER_AVGPOOL) return fail(c, GACER_EINVAL, "tenant %d op %d: unknown kind", ti, oi);
+    if ((int)op.kind < 0 || (int)op.kind > (int)GACER_SAMPLE) return fail(c, GACER_EINVAL, "tenant %d op %d: unknown kind", ti, oi);
     if ((int)op.act < 0 || (int)op.act > (int)GACER_ACT_HSIGMOID) return fail(c, GACER_EINVAL, "tenant %d op %d: unknown activation", ti, oi);
+    if (is_token_op(op.kind)) return check_token_op(c, ti, t, oi, written, desc);
     if (!idx_ok(op.in0, true)) return bad("in0 missing or not written by an earlier operator");
     if (!idx_ok(op.in1, false) || !idx_ok(op.res, false)) return bad("in1/res not written by an earlier operator");
     if (op.out < 0 || op.out >= t.n_tensors) return bad("out index out of range");
@@ -415,6 +551,7 @@ static gacer_status check_op(Ctx *c, int ti, const gacer_tenant &t, int oi, cons
     case GACER_ACT:
         if (!same_shape(in, out)) return bad("in/out shapes differ");
         break;
+    default: break;                              // the operators of a decoding tenant are checked above
     }
     if (in.n % B || out.n % B) return bad("tensor n is not a multiple of the tenant batch");
     return GACER_OK;
@@ -536,6 +673,7 @@ static void plan_workspaces(Ctx *c, std::vector<Tenant> &ts)
         t.ws_floats = 0;
         for (size_t i = 0; i < t.ops.size(); ++i) {
             const gacer_op &op = t.ops[i];
+            if (is_token_op(op.kind)) t.ws_floats = std::max<size_t>(t.ws_floats, token_ws_floats(make_token_launch(t, (int)i, 0, t.batch).k));
             if (op.kind != GACER_CONV2D && op.kind != GACER_GEMM) continue;
             const gacer_tensor &in = t.tensors[op.in0], &out = t.tensors[op.out];
             const int64_t M = out.n * out.h * out.w, N = out.c;
@@ -718,7 +856,7 @@ static void expand_plain(Ctx *c)
         const Tenant &T = c->tenants[t];
         c->plain_exec[t].resize(T.ops.size());
         for (size_t i = 0; i < T.ops.size(); ++i)
-            c->plain_exec[t][i].chunks.push_back(make_launch(T, (int)i, 0, T.batch, 0, (int)T.tensors[T.ops[i].out].c));
+            c->plain_exec[t][i].chunks.push_back(make_launch(T, (int)i, 0, T.batch, 0, out_channels(T, (int)i)));
         longest = std::max(longest, T.ops.size());
     }
     fuse_affine_pairs(c, c->plain_exec, [](int, int) { return false; }, [](int, int) { return false; });
@@ -808,7 +946,7 @@ static gacer_status install_plan(Ctx *c, const std::vector<gacer_split> &splits,
         const Tenant &T = c->tenants[t];
         ex[t].resize(T.ops.size());
         for (int i = 0; i < (int)T.ops.size(); ++i) {
-            const int cout = (int)T.tensors[T.ops[i].out].c;
+            const int cout = out_channels(T, i);
             auto it = smap.find({t, i});
             const int f = (it == smap.end()) ? 1 : it->second.factor;
             const gacer_axis ax = (it == smap.end() || f == 1) ? GACER_AXIS_NONE : it->second.axis;
@@ -945,17 +1083,24 @@ gacer_status gacer_load_tenants(gacer_ctx *c, const gacer_tenant *tenants, int n
         }
         Written written(t);
         written.mark(t.input);
+        Tenant &T = fresh[ti];
+        T.token.assign((size_t)t.n_ops, TokenDesc());
         for (int oi = 0; oi < t.n_ops; ++oi) {
-            gacer_status st = check_op(c, ti, t, oi, written);
+            gacer_status st = check_op(c, ti, t, oi, written, &T.token[oi]);
             if (st != GACER_OK) return st;
             const gacer_op &op = t.ops[oi];
+            if (is_token_op(op.kind)) {
+                if (op.out >= 0) written.mark(op.out);
+                continue;
+            }
             for (const void *p : {(const void *)op.w, (const void *)op.bias, (const void *)op.scale, (const void *)op.shift})
                 if (((uintptr_t)p) % 16) return fail(c, GACER_EINVAL, "tenant %d op %d: parameter pointer not 16-byte aligned", ti, oi);
             written.mark(op.out);
         }
         if (!written.all(t.output)) return fail(c, GACER_ESHAPE, "tenant %d: output tensor is never written", ti);
-        Tenant &T = fresh[ti];
         T.ops.assign(t.ops, t.ops + t.n_ops);
+        for (gacer_op &op : T.ops)
+            if (is_token_op(op.kind)) op.w = nullptr;            // the caller's descriptor, copied above
         T.tensors.assign(t.tensors, t.tensors + t.n_tensors);
         T.input = t.input; T.output = t.output; T.batch = t.batch; T.dtype = t.dtype;
         T.stream = (hipStream_t)t.stream;
@@ -1618,11 +1763,43 @@ gacer_status gacer_run_static(gacer_ctx *c, int mode, int rounds)
     return GACER_OK;
 }
 
+gacer_status gacer_enqueue(gacer_ctx *c, int tenant, void *stream)
+{
+    if (!c) return GACER_EINVAL;
+    if (!c->loaded) return fail(c, GACER_ESTATE, "gacer_enqueue before gacer_load_tenants");
+    if (tenant < 0 || tenant >= (int)c->tenants.size()) return fail(c, GACER_EINVAL, "gacer_enqueue: no tenant %d", tenant);
+    if (!c->has_device) return fail(c, GACER_ESTATE, "the context was created without a GPU");
+    if (c->ws_missing) return fail(c, GACER_EHIP, "split-K workspace could not be allocated when the tenants were loaded");
+    c->ws_run[tenant] = c->tenants[tenant].ws;
+    const auto &ex = c->plain_exec[tenant];
+    for (int i = 0; i < (int)ex.size(); ++i)
+        ISSUE(c, issue_op(c, tenant, i, ex[i], (hipStream_t)stream, false, 0, nullptr));
+    HIPCHK(c, hipGetLastError());
+    return GACER_OK;
+}
+
 // Algorithmic work of one launch (sub-range only).
 static void launch_work(const Launch &l, double *flops, double *bytes)
 {
     *flops = *bytes = 0;
     if (l.kind == LK_ABSORBED) return;
+    if (l.kind == LK_TOKENS) {                              // lengths live on the device: caches count as full, which is an upper bound
+        const TokenArgs &k = l.k;
+        const double esz = k.dtype == DT_BF16 ? 2.0 : 4.0, rows = (double)(k.b_hi - k.b_lo) * k.S, kv = (double)k.kv_heads * k.D, q = (double)k.heads * k.D;
+        const double cached = 2.0 * kv * (0.5 + 4.0 / CACHE_GROUP), most = (double)k.cache.max_pages * (1 << k.cache.page_shift);
+        switch (k.op) {
+        case TK_QKNORM_ROPE: *bytes = rows * 2.0 * esz * (k.x == k.y ? q + kv : q + 2.0 * kv); break;
+        case TK_CACHE_WRITE: case TK_CACHE_READ: *bytes = rows * (2.0 * kv * esz + cached); break;
+        case TK_CACHE_ATTENTION: {
+            const double keys = k.window > 0 ? std::min(most, (double)k.window) : most;
+            *flops = 4.0 * rows * q * keys;
+            *bytes = rows * 2.0 * q * esz + (double)(k.b_hi - k.b_lo) * std::min(most, keys + k.S) * cached;
+            break;
+        }
+        default: *bytes = rows * (k.vocab * esz + 8.0); break;
+        }
+        return;
+    }
     if (l.kind == LK_IGEMM && l.g.attn_scores) {            // both products; qkv read once, scores, probabilities and context written once
         const double rows = (double)l.g.zb * l.g.zh * l.g.H;
         *flops = 4.0 * rows * l.g.H * l.g.K;
@@ -1709,7 +1886,7 @@ gacer_status gacer_trace_run(gacer_ctx *c, int mode, int rounds, gacer_launch_st
                 row.workgroups = li.workgroups;
                 row.flops = row.bytes = 0.0;
                 if (ph == 1) launch_work(e.chunks[j], &row.flops, &row.bytes);   // the operator's work is booked on its main kernel
-                else {                          // the finishing pass moves the partial tiles in and the output out
+                else if (e.chunks[j].kind != LK_TOKENS) {   // the finishing pass moves the partial tiles in and the output out
                     const GemmArgs &g = e.chunks[j].g;
                     const double mn = (double)(g.m_hi - g.m_lo) * (g.n_hi - g.n_lo) * g.zb * g.zh;
                     row.bytes = mn * (4.0 * g.ksplit + (g.dtype == DT_BF16 ? 2.0 : 4.0) * (g.res ? 2.0 : 1.0));
@@ -1838,7 +2015,7 @@ gacer_status gacer_profile(gacer_ctx *c, gacer_prof *out, size_t cap, size_t *n_
     size_t k = 0;
     for (const Variant &v : vars) {
         const Tenant &T = c->tenants[v.t];
-        const int cout = (int)T.tensors[T.ops[v.op].out].c;
+        const int cout = out_channels(T, v.op);
         std::vector<Launch> ch;
         for (int j = 0; j < v.f; ++j) {
             int lo, hi;

@@ -100,6 +100,43 @@ struct StreamArgs {
     unsigned div_cv[2], div_w[2], div_h[2];
 };
 
+// Operators of a decoding tenant.  Sub-range: sequences (SAMPLE: items) [b_lo, b_hi).
+enum TokenOp { TK_QKNORM_ROPE, TK_CACHE_WRITE, TK_CACHE_READ, TK_CACHE_ATTENTION, TK_SAMPLE };
+// most query heads per key/value head
+enum { CACHE_GROUP = 64, CACHE_HEADS_PER_KV_MAX = 64 };
+
+// What the cache operators know of a paged cache (gacer_cache)
+struct CacheView {
+    unsigned char *k_codes, *v_codes;
+    unsigned *k_scales, *v_scales;
+    const int *page_table, *start, *count;
+    int kv_heads, D, page_shift, n_pages, max_pages;
+};
+
+struct TokenArgs {
+    int op, dtype;
+    const void *x;
+    void *y;
+    int b_lo, b_hi, S;         // S: tokens per sequence (SAMPLE: rows per item)
+    int heads, kv_heads, D;
+    // QKNORM_ROPE
+    const float *gamma_q, *gamma_k, *table;
+    const int *positions;
+    float eps;
+    int R, interleaved, axes, sections[3], n_positions;
+    // cache operators
+    CacheView cache;
+    int window;
+    float alpha;
+    // SAMPLE
+    int vocab;
+    const float *u, *temperature, *top_p, *min_p;
+    const int *top_k;
+    int *tokens;
+    float *logp;
+    float *ws;                 // set per call: token_ws_floats() of the unsplit operator, indexed by sequence (chunks own disjoint parts)
+};
+
 // Per-kernel timing (measurement aid): while `launch_timer` points at an event pair on the calling thread, every
 // launcher below hands the pair to the runtime together with its kernel, and the pair then reads the kernel's own
 // begin and end on the device clock (the interval a profiler reports for the dispatch), without changing what is
@@ -128,6 +165,14 @@ LaunchInfo launch_eltwise(const StreamArgs &a, hipStream_t s, bool dry);   // af
 LaunchInfo launch_concat(const StreamArgs &a, hipStream_t s, bool dry);
 LaunchInfo launch_layernorm(const StreamArgs &a, hipStream_t s, bool dry);
 LaunchInfo launch_softmax(const StreamArgs &a, hipStream_t s, bool dry);
+// Operators of a decoding tenant.  Weak, because host-only builds of the executor (its sanitizer tests) are linked without these kernels:
+// there it is null, and loading such an operator is refused.
+__attribute__((weak)) LaunchInfo launch_tokens(const TokenArgs &a, hipStream_t s, bool dry, int phase);
+LaunchInfo launch_qknorm_rope(const TokenArgs &a, hipStream_t s, bool dry);
+LaunchInfo launch_cache_write(const TokenArgs &a, hipStream_t s, bool dry);
+LaunchInfo launch_cache_read(const TokenArgs &a, hipStream_t s, bool dry);
+LaunchInfo launch_cache_attention(const TokenArgs &a, hipStream_t s, bool dry, int phase);
+LaunchInfo launch_sample(const TokenArgs &a, hipStream_t s, bool dry, int phase);
 // one wavefront that spins for `ticks` of the constant 100 MHz clock (stream placement probe)
 void launch_spin(hipStream_t s, unsigned long long ticks);
 

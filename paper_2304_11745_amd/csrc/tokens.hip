@@ -1,0 +1,365 @@
+// Operators of a decoding tenant that stream over tokens: norm and rotation of queries and keys, writing a 4-bit cache and reading it back.
+#include <hip/hip_runtime.h>
+#include <algorithm>
+#include "cache_util.h"
+#include "device_util.h"
+#include "kernels.h"
+#include "tokens_geom.h"
+
+namespace gacer {
+
+static LaunchInfo info(const char *name, int64_t workgroups, int lds)
+{
+    LaunchInfo li;
+    li.workgroups = (int)workgroups; li.threads = 256; li.lds_bytes = lds; li.wg_per_cu = 8; li.kernel = name; li.phases = 1;
+    return li;
+}
+
+// ---- RMS norm and rotation ---------------------------------------------------------------------------------------------------------
+// y = x * rsqrt(mean(x^2) + eps) * gamma for every query and key head, then (a, b) -> (a c - b s, b c + a s) for its pairs.
+//
+// A head is held by LPH lanes, eight features each: two runs of four, which are the two halves of the lane's pairs (i, i + R/2), so that
+// the rotation needs no other lane; beyond the rotated features, and for interleaved pairs, the two runs are neighbours.  Cosine and sine
+// depend on the token and the lane alone and are loaded once for all heads that a workgroup takes.
+struct RopeArgs {
+    const void *x;
+    void *y;
+    const float *gamma_q, *gamma_k, *table;
+    const int *positions;
+    float eps, inv_d;
+    int D, R, interleaved, axes, s1, s2, n_positions;
+    int width, heads, normed, all;      // elements per token; query heads; query and key heads; heads to write (values too unless in place)
+    int t_lo;                           // first token
+};
+
+__device__ __forceinline__ void load4(const float *p, float *v)
+{
+    const float4 a = *(const float4 *)p;
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+}
+__device__ __forceinline__ void load4(const unsigned short *p, float *v)
+{
+    const uint2 a = *(const uint2 *)p;
+    v[0] = __uint_as_float(a.x << 16); v[1] = __uint_as_float(a.x & 0xFFFF0000u);
+    v[2] = __uint_as_float(a.y << 16); v[3] = __uint_as_float(a.y & 0xFFFF0000u);
+}
+__device__ __forceinline__ void store4(float *p, const float *v) { *(float4 *)p = make_float4(v[0], v[1], v[2], v[3]); }
+__device__ __forceinline__ void store4(unsigned short *p, const float *v) { *(uint2 *)p = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])); }
+
+template <typename T, int LPH, int IT> __global__ __launch_bounds__(256) void qknorm_rope_kernel(RopeArgs a)
+{
+    constexpr int SLOTS = 256 / LPH;
+    const int tid = threadIdx.x, sub = tid % LPH, slot = tid / LPH;
+    const int64_t token = a.t_lo + (int64_t)blockIdx.x;
+    const int h0 = (int)blockIdx.y * (SLOTS * IT) + slot;
+    const T *x = (const T *)a.x + token * a.width;
+    T *y = (T *)a.y + token * a.width;
+    const bool on = sub * 8 < a.D, turned = sub * 8 < a.R, halves = turned && !a.interleaved;
+    const int f0 = halves ? sub * 4 : sub * 8, f1 = halves ? a.R / 2 + sub * 4 : sub * 8 + 4;
+
+    float v[IT][8];
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+        const int h = h0 + i * SLOTS;
+        if (on && h < a.all) {
+            load4(x + h * a.D + f0, v[i]);
+            load4(x + h * a.D + f1, v[i] + 4);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
+        }
+    }
+    float c[4], s[4];
+    if (turned) {
+        const int pair = sub * 4, half = a.R / 2;
+        const int *pos = a.positions + token * a.axes;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int at = pos[pair + e < a.s1 ? 0 : pair + e < a.s2 ? 1 : 2];
+            const bool known = (unsigned)at < (unsigned)a.n_positions;
+            const float2 cs = *(const float2 *)(a.table + ((int64_t)(known ? at : 0) * half + pair + e) * 2);
+            c[e] = known ? cs.x : NAN;
+            s[e] = known ? cs.y : NAN;
+        }
+    }
+    float gq[8], gk[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) gq[e] = gk[e] = 1.f;
+    if (on && a.gamma_q) { load4(a.gamma_q + f0, gq); load4(a.gamma_q + f1, gq + 4); }
+    if (on && a.gamma_k) { load4(a.gamma_k + f0, gk); load4(a.gamma_k + f1, gk + 4); }
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+        const int h = h0 + i * SLOTS;
+        const bool query = h < a.heads;
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum = fmaf(v[i][e], v[i][e], sum);
+#pragma unroll
+        for (int o = LPH / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+        if (!on || h >= a.all) continue;
+        if (h < a.normed) {
+            if (query ? a.gamma_q != nullptr : a.gamma_k != nullptr) {
+                const float r = rsqrtf(fmaf(sum, a.inv_d, a.eps));
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[i][e] = v[i][e] * r * (query ? gq[e] : gk[e]);
+            }
+            if (turned) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float p = a.interleaved ? v[i][2 * e] : v[i][e], q = a.interleaved ? v[i][2 * e + 1] : v[i][e + 4];
+                    const float lo = p * c[e] - q * s[e], hi = q * c[e] + p * s[e];
+                    if (a.interleaved) { v[i][2 * e] = lo; v[i][2 * e + 1] = hi; }
+                    else { v[i][e] = lo; v[i][e + 4] = hi; }
+                }
+            }
+        }
+        store4(y + h * a.D + f0, v[i]);
+        store4(y + h * a.D + f1, v[i] + 4);
+    }
+}
+
+template <typename T, int LPH> static void rope_launch(RopeArgs b, int64_t tokens, bool few, hipStream_t s)
+{
+    const int slots = 256 / LPH;
+    for (int64_t at = 0; at < tokens; at += 1 << 22, b.t_lo += 1 << 22) {        // a grid holds fewer than 2^32 threads
+        const unsigned n = (unsigned)std::min<int64_t>(tokens - at, 1 << 22);
+        if (few) GACER_LAUNCH((qknorm_rope_kernel<T, LPH, 1>), dim3(n, (b.all + slots - 1) / slots), dim3(256), 0, s, b);
+        else GACER_LAUNCH((qknorm_rope_kernel<T, LPH, 4>), dim3(n, (b.all + 4 * slots - 1) / (4 * slots)), dim3(256), 0, s, b);
+    }
+}
+
+LaunchInfo launch_qknorm_rope(const TokenArgs &a, hipStream_t s, bool dry)
+{
+    RopeArgs b;
+    b.x = a.x; b.y = a.y; b.gamma_q = a.gamma_q; b.gamma_k = a.gamma_k; b.table = a.table; b.positions = a.positions;
+    b.eps = a.eps; b.inv_d = 1.f / (float)a.D;
+    b.D = a.D; b.R = a.R; b.interleaved = a.interleaved; b.axes = a.axes; b.n_positions = a.n_positions;
+    b.s1 = a.axes > 1 ? a.sections[0] : a.R; b.s2 = a.axes > 2 ? a.sections[0] + a.sections[1] : a.R;
+    b.width = (a.heads + 2 * a.kv_heads) * a.D;
+    b.heads = a.heads; b.normed = a.heads + a.kv_heads; b.all = b.normed + (a.x == a.y ? 0 : a.kv_heads);
+    b.t_lo = a.b_lo * a.S;
+    const int64_t tokens = (int64_t)(a.b_hi - a.b_lo) * a.S;
+    int lph = 1;
+    while (lph * 8 < a.D) lph *= 2;
+    const int slots = 256 / lph;
+    const bool few = tokens * ((b.all + slots - 1) / slots) <= 2048;
+    LaunchInfo li = info(a.dtype == DT_BF16 ? "qknorm_rope_bf16" : "qknorm_rope_f32", tokens * ((b.all + slots * (few ? 1 : 4) - 1) / (slots * (few ? 1 : 4))), 0);
+    if (dry || !tokens) return li;
+#define ROPE(L)                                                                              \
+    case L:                                                                                  \
+        if (a.dtype == DT_BF16) rope_launch<unsigned short, L>(b, tokens, few, s);           \
+        else rope_launch<float, L>(b, tokens, few, s);                                       \
+        break
+    switch (lph) {
+        ROPE(1); ROPE(2); ROPE(4); ROPE(8); ROPE(16); ROPE(32); ROPE(64);
+    }
+#undef ROPE
+    return li;
+}
+
+// ---- into the cache and out of it --------------------------------------------------------------------------------------------------
+// A workgroup owns one block of 32 cache positions of one kv head (a block never crosses a page).  Writing: half of its threads quantise
+// keys, half values, eight features of a token per lane; a group's minimum and maximum go over the eight lanes that hold it.  Key codes
+// are one word per lane as they stand; value codes are gathered in LDS, where the words of eight tokens are put together, on top
+// of the codes that tokens outside the call left there.
+struct CacheArgs {
+    const void *x;
+    void *y;
+    CacheView c;
+    int b_lo, S, blocks, width, k_off;  // blocks: of 32 positions, per sequence and kv head; k_off: first key feature of a token
+};
+
+struct Block { int b, head, p0; Span span; };
+__device__ __forceinline__ Block block_of(const CacheArgs &a)
+{
+    Block k;
+    const int z = (int)blockIdx.x / a.blocks;
+    k.b = a.b_lo + z / a.c.kv_heads;
+    k.head = z % a.c.kv_heads;
+    k.span = span_of(a.c, k.b, a.S);
+    k.p0 = (k.span.start / 32 + (int)blockIdx.x % a.blocks) * 32;
+    return k;
+}
+
+// eight values of one lane -> their code word; `pair` receives scale and minimum of the group of eight lanes (a minimum of zero without a
+// sign: which of two zeros a minimum returns is not defined)
+__device__ __forceinline__ unsigned quantise(const float *v, unsigned &pair)
+{
+    float lo = INFINITY, hi = -INFINITY;
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        bad |= v[e] != v[e];
+        lo = fminf(lo, v[e]);
+        hi = fmaxf(hi, v[e]);
+    }
+    if (bad) lo = -INFINITY;
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) {
+        lo = fminf(lo, __shfl_xor(lo, o, 64));
+        hi = fmaxf(hi, __shfl_xor(hi, o, 64));
+    }
+    const unsigned short low = to_bf16(lo), step = to_bf16(__fdiv_rn(__fsub_rn(hi, lo), 15.f));
+    const float m = ld_f32(&low, 0) + 0.f, s = ld_f32(&step, 0);
+    if (!(fabsf(s) < INFINITY && fabsf(m) < INFINITY)) {
+        pair = 0x7FC0u;
+        return 0u;
+    }
+    pair = (unsigned)step | __float_as_uint(m);
+    unsigned word = 0u;
+    if (s > 0.f) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float q = __builtin_amdgcn_fmed3f(rintf(__fdiv_rn(__fsub_rn(v[e], m), s)), 0.f, 15.f);
+            word |= (unsigned)q << code_shift(e);
+        }
+    }
+    return word;
+}
+
+template <typename T, int D> __global__ __launch_bounds__(256) void cache_write_kernel(CacheArgs a)
+{
+    constexpr int LPT = D / 8, PER = 128 / LPT, PASSES = 32 / PER, NG = D / CACHE_GROUP;     // lanes per token, tokens per pass of a half
+    __shared__ unsigned vw[8 * LPT * 4];               // value words: [feature % 8][feature / 8][word]
+    const int tid = threadIdx.x, half = tid >> 7, sub = tid & (LPT - 1), row = (tid & 127) / LPT;
+    const Block k = block_of(a);
+    const int lo = max(k.p0, k.span.start), hi = min(k.p0 + 32, k.span.start + k.span.count);
+    if (lo >= hi) return;
+    const int page = page_of(a.c, k.b, k.p0);
+    if (page < 0) return;
+    const int64_t first = page_row(a.c, page, k.head) + (k.p0 & ((1 << a.c.page_shift) - 1));
+    const T *x = (const T *)a.x + ((int64_t)k.b * a.S - k.span.start) * a.width + a.k_off + (half * a.c.kv_heads + k.head) * D + sub * 8;
+    float v[PASSES][8];
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+        const int p = k.p0 + i * PER + row;
+        if (p >= lo && p < hi) load8(x + (int64_t)p * a.width, v[i]);
+        else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
+        }
+    }
+    // what stays of the words that the call writes in part
+    unsigned *global = (unsigned *)a.c.v_codes + first * (D / 8);
+    for (int i = tid; i < D * 4; i += 256) {
+        const int f = i >> 2, w = i & 3, q0 = k.p0 + w * 8;
+        unsigned keep = 0u;
+        if (q0 < hi && q0 + 8 > lo && (q0 < lo || q0 + 8 > hi)) {
+            keep = global[i];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (q0 + e >= lo && q0 + e < hi) keep &= ~(15u << code_shift(e));
+        }
+        vw[((f & 7) * LPT + (f >> 3)) * 4 + w] = keep;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+        const int t = i * PER + row, p = k.p0 + t;
+        unsigned pair;
+        const unsigned word = quantise(v[i], pair);
+        if (p < lo || p >= hi) continue;
+        if (!half) ((unsigned *)a.c.k_codes)[(first + t) * LPT + sub] = word;
+        else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                atomicOr(&vw[(e * LPT + sub) * 4 + (t >> 3)], ((word >> code_shift(e)) & 15u) << code_shift(t & 7));
+        }
+        if (sub % 8 == 0) (half ? a.c.v_scales : a.c.k_scales)[(first + t) * NG + sub / 8] = pair;
+    }
+    __syncthreads();
+    for (int i = tid; i < D * 4; i += 256) {
+        const int f = i >> 2, w = i & 3, q0 = k.p0 + w * 8;
+        if (q0 < hi && q0 + 8 > lo) global[i] = vw[((f & 7) * LPT + (f >> 3)) * 4 + w];
+    }
+}
+
+template <typename T, int D> __global__ __launch_bounds__(256) void cache_read_kernel(CacheArgs a)
+{
+    constexpr int LPT = D / 8, PER = 256 / LPT, PASSES = 32 / PER, NG = D / CACHE_GROUP;
+    __shared__ __align__(8) unsigned char codes[32][D + 8];      // value codes, a row per token
+    const int tid = threadIdx.x, sub = tid & (LPT - 1), row = tid / LPT;
+    const Block k = block_of(a);
+    const int page = k.p0 < k.span.start + k.span.count ? page_of(a.c, k.b, k.p0) : -1;
+    const int64_t first = page < 0 ? 0 : page_row(a.c, page, k.head) + (k.p0 & ((1 << a.c.page_shift) - 1));
+    if (page >= 0) {
+        const unsigned *w = (const unsigned *)a.c.v_codes + first * LPT;
+        for (int i = tid; i < D * 4; i += 256) {
+            const unsigned word = w[i];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) codes[(i & 3) * 8 + e][i >> 2] = (unsigned char)((word >> code_shift(e)) & 15u);
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+        const int t = i * PER + row, p = k.p0 + t;
+        if (p < k.span.start || p >= k.span.start + a.S) continue;
+        T *y = (T *)a.y + ((int64_t)k.b * a.S + (p - k.span.start)) * a.width + k.head * D + sub * 8;
+        float kv[8], vv[8];
+        if (page >= 0 && p < k.span.start + k.span.count) {
+            const unsigned word = ((const unsigned *)a.c.k_codes)[(first + t) * LPT + sub];
+            const unsigned kp = a.c.k_scales[(first + t) * NG + sub / 8], vp = a.c.v_scales[(first + t) * NG + sub / 8];
+            const uint2 c8 = *(const uint2 *)&codes[t][sub * 8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                kv[e] = fmaf((float)((word >> code_shift(e)) & 15u), scale_of(kp), minimum_of(kp));
+                vv[e] = fmaf((float)(((e < 4 ? c8.x : c8.y) >> (e & 3) * 8) & 255u), scale_of(vp), minimum_of(vp));
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) kv[e] = vv[e] = 0.f;
+        }
+        store8(y, kv);
+        store8(y + a.c.kv_heads * D, vv);
+    }
+}
+
+static CacheArgs cache_args(const TokenArgs &a, bool read)
+{
+    CacheArgs b;
+    b.x = a.x; b.y = a.y; b.c = a.cache; b.b_lo = a.b_lo; b.S = a.S;
+    b.blocks = (a.S + 30) / 32 + 1;                    // blocks that S positions from anywhere on can touch
+    b.width = (read ? 2 : a.heads / a.kv_heads + 2) * a.kv_heads * a.D;
+    b.k_off = a.heads * a.D;
+    return b;
+}
+
+LaunchInfo launch_cache_write(const TokenArgs &a, hipStream_t s, bool dry)
+{
+    const CacheArgs b = cache_args(a, false);
+    LaunchInfo li = info(a.dtype == DT_BF16 ? "cache_write_bf16" : "cache_write_f32", (int64_t)(a.b_hi - a.b_lo) * a.kv_heads * b.blocks, a.D * 16);
+    if (dry || !li.workgroups) return li;
+    const dim3 grid(li.workgroups), block(256);
+    if (a.dtype == DT_BF16 && a.D == 64) GACER_LAUNCH((cache_write_kernel<unsigned short, 64>), grid, block, 0, s, b);
+    else if (a.dtype == DT_BF16) GACER_LAUNCH((cache_write_kernel<unsigned short, 128>), grid, block, 0, s, b);
+    else if (a.D == 64) GACER_LAUNCH((cache_write_kernel<float, 64>), grid, block, 0, s, b);
+    else GACER_LAUNCH((cache_write_kernel<float, 128>), grid, block, 0, s, b);
+    return li;
+}
+
+LaunchInfo launch_cache_read(const TokenArgs &a, hipStream_t s, bool dry)
+{
+    const CacheArgs b = cache_args(a, true);
+    LaunchInfo li = info(a.dtype == DT_BF16 ? "cache_read_bf16" : "cache_read_f32", (int64_t)(a.b_hi - a.b_lo) * a.kv_heads * b.blocks, 32 * (a.D + 8));
+    if (dry || !li.workgroups) return li;
+    const dim3 grid(li.workgroups), block(256);
+    if (a.dtype == DT_BF16 && a.D == 64) GACER_LAUNCH((cache_read_kernel<unsigned short, 64>), grid, block, 0, s, b);
+    else if (a.dtype == DT_BF16) GACER_LAUNCH((cache_read_kernel<unsigned short, 128>), grid, block, 0, s, b);
+    else if (a.D == 64) GACER_LAUNCH((cache_read_kernel<float, 64>), grid, block, 0, s, b);
+    else GACER_LAUNCH((cache_read_kernel<float, 128>), grid, block, 0, s, b);
+    return li;
+}
+
+LaunchInfo launch_tokens(const TokenArgs &a, hipStream_t s, bool dry, int phase)
+{
+    switch (a.op) {
+    case TK_QKNORM_ROPE: return launch_qknorm_rope(a, s, dry);
+    case TK_CACHE_WRITE: return launch_cache_write(a, s, dry);
+    case TK_CACHE_READ: return launch_cache_read(a, s, dry);
+    case TK_CACHE_ATTENTION: return launch_cache_attention(a, s, dry, phase);
+    default: return launch_sample(a, s, dry, phase);
+    }
+}
+
+}  // namespace gacer

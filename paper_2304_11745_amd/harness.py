@@ -28,20 +28,22 @@ def _ptr(t):
 class Session:
     """One gacer context with its tenants resident in HBM."""
 
-    def __init__(self, tenants, data, device="cuda:0", shared_stream=False, place_streams=True):
+    def __init__(self, tenants, data, device="cuda:0", shared_stream=False, place_streams=True, extra=()):
+        """``extra``: operator lists over the caller's own tensors (``tokens.OpList``), loaded as further tenants behind ``tenants``."""
         if not torch.cuda.is_available():
             raise RuntimeError("a GPU is required: the library has no CPU fallback")
         self.dev = torch.device(device)
         torch.cuda.set_device(self.dev)
-        self.tenants = tenants
+        extra = list(extra)
+        self.tenants = list(tenants) + extra
         self.ctx = C.c_void_p()
         B.check(self.ctx, B.gacer_create(C.byref(self.ctx)))
         self._keep = []
         self.streams = []
         self.sibling_streams = []
-        place = place_streams and not shared_stream and len(tenants) > 1
+        place = place_streams and not shared_stream and len(self.tenants) > 1
         self.acts = []          # per tenant: list of device tensors (channels-last)
-        descs = (B.gacer_tenant * len(tenants))()
+        descs = (B.gacer_tenant * len(self.tenants))()
         for ti, (t, (x, params)) in enumerate(zip(tenants, data)):
             tdt = torch.bfloat16 if t.dtype == "bf16" else torch.float32
             views = getattr(t, "views", {})
@@ -95,11 +97,16 @@ class Session:
                                        B.GACER_BF16 if t.dtype == "bf16" else B.GACER_F32, t.batch,
                                        C.c_void_p(s.cuda_stream))
             self._keep += [tens, ops, dev_params]
+        for ti, ops in enumerate(extra, len(tenants)):
+            s = self.streams[0] if (shared_stream and self.streams) else torch.cuda.Stream(device=self.dev)
+            self.streams.append(s)
+            descs[ti] = ops.descriptor(s.cuda_stream)
+            self.acts.append(ops.activations())
         torch.cuda.synchronize(self.dev)
         if place:
-            self._place_streams(descs, len(tenants))
+            self._place_streams(descs, len(self.tenants))
         self._descs = descs
-        B.check(self.ctx, B.gacer_load_tenants(self.ctx, descs, len(tenants)))
+        B.check(self.ctx, B.gacer_load_tenants(self.ctx, descs, len(self.tenants)))
 
     # -- stream placement --------------------------------------------------------------------------
     def _place_streams(self, descs, n):
@@ -234,7 +241,7 @@ class Session:
         """Overwrite every non-input tensor with NaN so stale results cannot pass for fresh ones."""
         for t, acts in zip(self.tenants, self.acts):
             for i, a in enumerate(acts):
-                if i != t.input:
+                if i != t.input and a.data_ptr() != acts[t.input].data_ptr():
                     a.fill_(float("nan"))
         torch.cuda.synchronize(self.dev)
 
