@@ -1,7 +1,25 @@
-// Attention of new tokens over a paged 4-bit cache.  One wave per query row: a lane scores one key at a time with the queries in LDS, the
-// running maximum and sum of the softmax are per wave, and each lane keeps D / 64 features of the result.
+// Attention of new tokens over a paged 4-bit cache, on the matrix cores.
+//
+// The queries of one key/value head (heads/kv_heads heads x S tokens) are the rows of its products.  A wave takes 64 keys at a time: scores =
+// rows x keys, lane = key, so that the scales of a key stand in the lane that scores it and each register is one row; the values' product
+// has the same rows, lane = feature.  Codes enter the products as whole numbers k = c - BIAS (times a power of two), exact in bf16, and
+// the scales are applied to the scores and to the softmax weights in fp32:
+//   q.k_j = sum over groups g of  s_jg * (sum_d q_d k_jd) + (m_jg + BIAS s_jg) * sum_d q_d
+//   out_d = sum_j (p_j s_jg) k_jd + sum_j p_j (m_jg + BIAS s_jg)
+// so neither keys nor values are ever rounded.  In bf16 tenants k = 16 + c, which is a shift and a mask per pair of codes; fp32 tenants pay more
+// instructions for k = c - 8, because sums of numbers that do not lie around zero lose what their differences need (attention over 1000 keys: relative
+// error 6.8e-6 with 16 + c).  Operands that are not whole numbers are split into bf16 parts: queries of fp32 tenants into
+// three, weights p_j s_jg into two (bf16 tenants: an error of 2^-16 against the result's own rounding of 2^-9; one part would add as much as
+// that) or three.  Where rows leave room in the products' 32, the parts are rows of one product.  Weights pass through a patch of LDS, from
+// lane = key to the layout of an operand.
+//
+// The softmax keeps a reference per row that only moves when a score passes it by more than 2^8: weights are 2^(score - reference), sums are per
+// lane and joined at the end.  Waves of a workgroup take parts of its keys and are joined in LDS; where there are too few workgroups
+// the keys are also cut into splits, joined by a second kernel.
 #include <hip/hip_runtime.h>
+#include <limits.h>
 #include "cache_util.h"
+#include "gemm_util.h"
 #include "kernels.h"
 #include "tokens_geom.h"
 
@@ -10,78 +28,451 @@ namespace gacer {
 struct AttendArgs {
     const void *x;
     void *y;
+    float *ws;
     CacheView c;
-    int b_lo, S, heads, per_kv, window;
-    float alpha;
+    int b_lo, S, heads, per_kv, window, row_tiles, splits;
+    float scale;               // alpha * log2(e)
 };
 
-template <typename T, int D> __global__ __launch_bounds__(64) void cache_attention_rows_kernel(AttendArgs a)
+// fewest 64-key tiles of a split, and the tiles of each of `splits` parts of n tiles
+enum { SPLIT_TILES_MIN = 8 };
+__device__ __forceinline__ int split_tiles(int n, int splits) { return max((int)SPLIT_TILES_MIN, (n + splits - 1) / splits); }
+
+// The tiles of 64 keys that rows [r0, r1) of a sequence see, and the first and last of its tokens among them (t1 < t0: none)
+struct Range { int t0, t1, lo, hi; };
+__device__ __forceinline__ Range range_of(const AttendArgs &a, const Span &s, int r0, int r1)
 {
-    constexpr int NG = D / CACHE_GROUP;
-    __shared__ float q[D], p[64];
-    __shared__ int at[64];
-    const int lane = threadIdx.x, h = blockIdx.x % a.heads, g = h / a.per_kv;
-    const int64_t row = (int64_t)blockIdx.x / a.heads;
-    const int b = a.b_lo + (int)(row / a.S), t = (int)(row % a.S);
-    const Span span = span_of(a.c, b, a.S);
-    const T *x = (const T *)a.x + ((int64_t)b * a.S + t) * (a.heads + 2 * a.c.kv_heads) * D + h * D;
-    T *y = (T *)a.y + (((int64_t)b * a.S + t) * a.heads + h) * D;
-    for (int i = lane; i < D; i += 64) q[i] = ld_f32(x, i);
-    const int pos = span.start + t, first = a.window > 0 ? max(0, pos - a.window + 1) : 0;
-    float acc[NG] = {}, m = -INFINITY, l = 0.f;
-    for (int j0 = first & ~63; t < span.count && j0 <= pos; j0 += 64) {
-        __syncthreads();
-        const int j = j0 + lane, page = j >= first && j <= pos ? page_of(a.c, b, j) : -1;
-        const int64_t r = page < 0 ? 0 : page_row(a.c, page, g) + (j & ((1 << a.c.page_shift) - 1));
-        float s = -INFINITY;
-        if (page >= 0) {
-            s = 0.f;
-            for (int w = 0; w < D / 8; ++w) {
-                const unsigned word = ((const unsigned *)a.c.k_codes)[r * (D / 8) + w], kp = a.c.k_scales[r * NG + w / 8];
-                for (int e = 0; e < 8; ++e) s = fmaf(q[w * 8 + e], fmaf((float)((word >> code_shift(e)) & 15u), scale_of(kp), minimum_of(kp)), s);
-            }
-            s *= a.alpha;
-        }
-        float top = s;
-        for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-        const float now = fmaxf(m, top);
-        if (now == -INFINITY) continue;
-        const float scale = expf(m - now), e = expf(s - now);
-        float sum = e;
-        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-        l = l * scale + sum;
-        m = now;
-        p[lane] = e;
-        at[lane] = page < 0 ? -1 : page;
-        __syncthreads();
-        for (int i = 0; i < NG; ++i) acc[i] *= scale;
-        for (int k = 0; k < 64; ++k) {
-            if (at[k] < 0) continue;
-            const int64_t base = page_row(a.c, at[k], g), o = (j0 + k) & ((1 << a.c.page_shift) - 1);
-            for (int i = 0; i < NG; ++i) {
-                const unsigned word = ((const unsigned *)a.c.v_codes)[(base + (o & ~31)) * (D / 8) + (i * 64 + lane) * 4 + ((o & 31) >> 3)];
-                const unsigned vp = a.c.v_scales[(base + o) * NG + i];
-                acc[i] = fmaf(p[k], fmaf((float)((word >> code_shift(o & 7)) & 15u), scale_of(vp), minimum_of(vp)), acc[i]);
-            }
-        }
+    Range g;
+    g.t0 = r0 / a.per_kv;
+    g.t1 = min((r1 - 1) / a.per_kv, s.count - 1);
+    g.lo = g.hi = 0;
+    if (g.t1 >= g.t0) {
+        const int first = a.window > 0 ? max(0, s.start + g.t0 - a.window + 1) : 0;
+        const int last = min(s.start + g.t1, (a.c.max_pages << a.c.page_shift) - 1);
+        g.lo = first >> 6;
+        g.hi = max(g.lo, (last >> 6) + 1);
     }
-    for (int i = 0; i < NG; ++i) st_f32(y, i * 64 + lane, l > 0.f ? acc[i] / l : 0.f);
+    return g;
 }
 
-LaunchInfo launch_cache_attention(const TokenArgs &a, hipStream_t s, bool dry, int)
+// eight codes of a word as the bf16 numbers 16 + c
+__device__ __forceinline__ unsigned and_or(unsigned a, unsigned mask, unsigned bits)
 {
+    unsigned r;                                        // one instruction; from plain operators the compiler makes two, each with a literal
+    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "s"(mask), "v"(bits));
+    return r;
+}
+__device__ __forceinline__ bf16x8 codes_above(unsigned w, unsigned sixteen)
+{
+    constexpr unsigned MASK = 0x00780078u;
+    return __builtin_bit_cast(bf16x8, make_uint4(and_or(w << 3, MASK, sixteen), and_or(w >> 1, MASK, sixteen), and_or(w >> 5, MASK, sixteen), and_or(w >> 9, MASK, sixteen)));
+}
+// and as (c - 8) / 16: the hardware's conversion of a signed 4-bit number
+__device__ __forceinline__ bf16x8 codes_around(unsigned w)
+{
+    const unsigned x = w ^ 0x88888888u;
+    unsigned r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const unsigned lo = __float_as_uint(__builtin_amdgcn_cvt_off_f32_i4((int)(x >> (4 * i)))), hi = __float_as_uint(__builtin_amdgcn_cvt_off_f32_i4((int)(x >> (4 * i + 16))));
+        r[i] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+    }
+    return __builtin_bit_cast(bf16x8, make_uint4(r[0], r[1], r[2], r[3]));
+}
+
+__device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+
+// v as a sum of PARTS numbers whose upper 16 bits are bf16, each but the last the largest that does not pass it
+template <int PARTS> __device__ __forceinline__ void split_bf16(float v, unsigned *p)
+{
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) {
+        p[i] = __float_as_uint(v);
+        v -= __uint_as_float(p[i] & 0xFFFF0000u);
+    }
+}
+
+// Two blocks of 32 keys and values as loaded: lane & 31 = key of its block (keys, scales) or feature (values), lane >> 5 = half of the group's
+// features (keys) or of the block's keys (values)
+template <int D> struct Tile {
+    uint4 k[2][D / 64];
+    uint2 v[2][D / 32];
+    unsigned ks[2][D / 64], vs[2][D / 64];
+    int page[2];
+};
+
+// the reference of a row that has seen no key yet; scores lie above it
+static constexpr float NO_SCORE = -1e38f;
+
+// a branch that stays one (uniform over the wave): as selects, every tile would pay for what only the first and the last need
+#define RARELY(cond) if (cond) if (([] { asm volatile(""); return true; })())
+
+template <typename T, int D, int ROWS, int NW> __global__ __launch_bounds__(NW * 64) void cache_attention_kernel(AttendArgs a)
+{
+    constexpr bool F32 = sizeof(T) == 4;
+    constexpr int NG = D / 64, R4 = ROWS / 2, QP = F32 ? 3 : 1, PP = F32 ? 3 : 2, PROW = 128 + 16;    // bytes of a row of weights
+    constexpr int STACK = 32 / ROWS < PP ? 32 / ROWS : PP, PM = (PP + STACK - 1) / STACK;              // parts in one product, products
+    constexpr int QSTACK = 32 / ROWS < QP ? 32 / ROWS : QP, QM = (QP + QSTACK - 1) / QSTACK;
+    constexpr float TIMES = F32 ? 16.f : 1.f, BIAS = F32 ? 8.f : -16.f;
+    constexpr int PGROUP = PP * ROWS * PROW, PWAVE = NG * PGROUP, MROW = D + 2;
+    constexpr int BYTES = NW * PWAVE > NW * ROWS * MROW * 4 ? NW * PWAVE : NW * ROWS * MROW * 4;
+    __shared__ __align__(16) unsigned char lds[BYTES];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
+    const int sp = (int)blockIdx.x % a.splits, u = (int)blockIdx.x / a.splits, rt = u % a.row_tiles, z = u / a.row_tiles;
+    const int g = z % a.c.kv_heads, b = a.b_lo + z / a.c.kv_heads;
+    const int rows = a.S * a.per_kv, r0 = rt * ROWS;
+    const Span span = span_of(a.c, b, a.S);
+    const Range rg = range_of(a, span, r0, min(r0 + ROWS, rows));
+    int lo = rg.lo, hi = rg.hi;
+    if (a.splits > 1) {
+        const int n = split_tiles(rg.hi - rg.lo, a.splits);
+        lo = rg.lo + sp * n;
+        hi = min(rg.hi, lo + n);
+        if (lo >= hi) return;
+    }
+    const int per = (hi - lo + NW - 1) / NW, w_lo = lo + wave * per, w_hi = min(hi, w_lo + per);
+
+    const unsigned k_at = l32 * (D / 2) + half * 16, s_at = l32 * NG * 4, v_at = l32 * 16 + half * 8;
+    int pages = -1, pages_at = INT_MIN / 2;            // lane i: page of block pages_at + i
+    auto load = [&](int tile, Tile<D> &x) {
+        const int blk = tile * 2;
+        if (blk - pages_at >= 64 || blk < pages_at) {
+            pages_at = blk;
+            pages = page_of(a.c, b, min(blk + lane, 1 << 25) << 5);
+        }
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            x.page[m] = __builtin_amdgcn_readlane(pages, blk - pages_at + m);
+            const int64_t row = page_row(a.c, max(x.page[m], 0), g) + (((blk + m) << 5) & ((1 << a.c.page_shift) - 1));
+            const unsigned char *k = a.c.k_codes + row * (D / 2), *v = a.c.v_codes + row * (D / 2);
+            const unsigned char *ks = (const unsigned char *)(a.c.k_scales + row * NG), *vs = (const unsigned char *)(a.c.v_scales + row * NG);
+#pragma unroll
+            for (int i = 0; i < NG; ++i) {
+                x.k[m][i] = *(const uint4 *)(k + k_at + i * 32);
+                x.ks[m][i] = *(const unsigned *)(ks + s_at + i * 4);
+                x.vs[m][i] = *(const unsigned *)(vs + s_at + i * 4);
+            }
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) x.v[m][c] = *(const uint2 *)(v + v_at + c * 512);
+        }
+    };
+    Tile<D> even, odd;
+    if (w_lo < w_hi) load(w_lo, even);
+
+    // queries: lane & 31 = row (and part: see STACK); features 64 g + 32 half + 8 j .. of step (g, j)
+    bf16x8 q[QM][NG * 4];
+    const unsigned sixteen = 0x41804180u;
+#pragma unroll
+    for (int n = 0; n < QM; ++n) {
+        const int part = n * QSTACK + l32 / ROWS, r = r0 + (l32 & (ROWS - 1)), t = r / a.per_kv;
+        const bool on = l32 < ROWS * QSTACK && part < QP && r < rows;
+        const T *x = (const T *)a.x + ((int64_t)b * a.S + (on ? t : 0)) * (a.heads + 2 * a.c.kv_heads) * D + (g * a.per_kv + (on ? r - t * a.per_kv : 0)) * D + half * 32;
+#pragma unroll
+        for (int i = 0; i < NG * 4; ++i) {
+            uint4 raw;
+            if constexpr (F32) {
+                float v[8];
+                load8(x + (i >> 2) * 64 + (i & 3) * 8, v);
+                unsigned w[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    unsigned p[QP];
+                    split_bf16<QP>(v[e], p);
+                    w[e] = part == 0 ? p[0] : part == 1 ? p[1] : p[2];
+                }
+                raw = make_uint4(__builtin_amdgcn_perm(w[1], w[0], 0x07060302u), __builtin_amdgcn_perm(w[3], w[2], 0x07060302u),
+                                 __builtin_amdgcn_perm(w[5], w[4], 0x07060302u), __builtin_amdgcn_perm(w[7], w[6], 0x07060302u));
+            } else raw = *(const uint4 *)(x + (i >> 2) * 64 + (i & 3) * 8);
+            q[n][i] = __builtin_bit_cast(bf16x8, on ? raw : make_uint4(0u, 0u, 0u, 0u));
+        }
+    }
+    // a product's register of row e, parts added
+    auto over_parts = [](const f32x16 &d, int e) {
+        float v = d[e];
+#pragma unroll
+        for (int k = 1; k < QSTACK; ++k) v += d[e + k * R4];
+        return v;
+    };
+    const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    float qs[NG][R4];                                  // sums of the queries over each group, in the registers of their rows
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+        f32x16 d = zero;
+#pragma unroll
+        for (int n = 0; n < QM; ++n)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) d = mfma(q[n][i * 4 + j], __builtin_bit_cast(bf16x8, make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u)), d);
+#pragma unroll
+        for (int e = 0; e < R4; ++e) qs[i][e] = over_parts(d, e);
+    }
+    int at[R4];                                        // position of a register's row, -1: nothing to compute
+#pragma unroll
+    for (int e = 0; e < R4; ++e) {
+        const int r = r0 + 8 * (e >> 2) + 4 * half + (e & 3), t = r / a.per_kv;
+        at[e] = r < rows && t < span.count ? span.start + t : -1;
+    }
+    // every row sees all keys in [all_lo, all_hi)
+    const int all_lo = a.window > 0 ? span.start + rg.t1 - a.window + 1 : 0, all_hi = span.start + rg.t0 + 1;
+
+    float base[R4], l[R4], corr[NG][R4];               // base: the reference
+    f32x16 o[D / 32];
+#pragma unroll
+    for (int e = 0; e < R4; ++e) {
+        base[e] = NO_SCORE;
+        l[e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < NG; ++i) corr[i][e] = 0.f;
+    }
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) o[c] = zero;
+    unsigned char *pw = lds + wave * PWAVE;
+
+    auto step = [&](const Tile<D> &x, int tile) {
+        const int p0 = tile * 64;
+        const bool edge = p0 < all_lo || p0 + 64 > all_hi || x.page[0] < 0 || x.page[1] < 0;
+        float s[2][R4];
+        bool over = false;
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            float sc[NG], mm[NG];
+#pragma unroll
+            for (int i = 0; i < NG; ++i) {
+                const float t = scale_of(x.ks[m][i]) * a.scale;
+                sc[i] = t * TIMES;
+                mm[i] = fmaf(BIAS, t, minimum_of(x.ks[m][i]) * a.scale);
+            }
+#pragma unroll
+            for (int e = 0; e < R4; ++e) s[m][e] = 0.f;
+#pragma unroll
+            for (int i = 0; i < NG; ++i) {
+                f32x16 d = zero;
+                const unsigned w[4] = {x.k[m][i].x, x.k[m][i].y, x.k[m][i].z, x.k[m][i].w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const bf16x8 kj = F32 ? codes_around(w[j]) : codes_above(w[j], sixteen);
+#pragma unroll
+                    for (int n = 0; n < QM; ++n) d = mfma(q[n][i * 4 + j], kj, d);
+                }
+#pragma unroll
+                for (int e = 0; e < R4; ++e) s[m][e] = fmaf(sc[i], over_parts(d, e), fmaf(mm[i], qs[i][e], s[m][e]));
+            }
+            RARELY(edge) {
+                const int p = p0 + m * 32 + l32;
+#pragma unroll
+                for (int e = 0; e < R4; ++e)
+                    if (x.page[m] < 0 || p > at[e] || (a.window > 0 && p <= at[e] - a.window)) s[m][e] = -INFINITY;
+            }
+#pragma unroll
+            for (int e = 0; e < R4; ++e) over |= s[m][e] - base[e] > 8.f;
+        }
+        RARELY(__any(over)) {                          // some score is far above its row's reference: the tile's largest becomes the reference
+#pragma unroll
+            for (int e = 0; e < R4; ++e) {
+                float top = fmaxf(s[0][e], s[1][e]);
+#pragma unroll
+                for (int k = 16; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor(top, k, 64));
+                top = fmaxf(top, base[e]);
+                const float f = __builtin_amdgcn_exp2f(base[e] - top);
+                base[e] = top;
+                l[e] *= f;
+#pragma unroll
+                for (int i = 0; i < NG; ++i) corr[i][e] *= f;
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+                    for (int k = 0; k < STACK; ++k) o[c][e + k * R4] *= f;
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            float p[R4];
+#pragma unroll
+            for (int e = 0; e < R4; ++e) {
+                p[e] = __builtin_amdgcn_exp2f(s[m][e] - base[e]);
+                l[e] += p[e];
+            }
+#pragma unroll
+            for (int i = 0; i < NG; ++i) {
+                const float v = scale_of(x.vs[m][i]), sv = v * TIMES, mv = fmaf(BIAS, v, minimum_of(x.vs[m][i]));
+                float ps[R4], pm[R4];
+#pragma unroll
+                for (int e = 0; e < R4; ++e) {
+                    ps[e] = p[e] * sv;
+                    pm[e] = p[e] * mv;
+                }
+                RARELY(edge) {                         // whatever the scales of a key that is not seen hold
+#pragma unroll
+                    for (int e = 0; e < R4; ++e)
+                        if (s[m][e] == -INFINITY) ps[e] = pm[e] = 0.f;
+                }
+#pragma unroll
+                for (int e = 0; e < R4; ++e) {
+                    corr[i][e] += pm[e];
+                    unsigned part[PP];
+                    split_bf16<PP>(ps[e], part);
+                    const int row = 8 * (e >> 2) + 4 * half + (e & 3);
+#pragma unroll
+                    for (int k = 0; k < PP; ++k) *(unsigned short *)(pw + i * PGROUP + (k * ROWS + row) * PROW + (m * 32 + l32) * 2) = (unsigned short)(part[k] >> 16);
+                }
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < NG; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {              // eight keys of each half of block j / 2
+                bf16x8 pa[PM];
+#pragma unroll
+                for (int n = 0; n < PM; ++n) {         // rows beyond the parts: repeated where nothing reads their sums, zeros where a second product would add them
+                    const bool real = n * 32 + l32 < PP * ROWS;
+                    pa[n] = *(const bf16x8 *)(pw + i * PGROUP + (real ? n * 32 + l32 : l32 & (ROWS - 1)) * PROW + (j >> 1) * 64 + half * 32 + (j & 1) * 16);
+                    if (PM > 1 && !real) pa[n] = __builtin_bit_cast(bf16x8, make_uint4(0u, 0u, 0u, 0u));
+                }
+#pragma unroll
+                for (int c = 2 * i; c < 2 * i + 2; ++c) {
+                    const unsigned w = j & 1 ? x.v[j >> 1][c].y : x.v[j >> 1][c].x;
+                    const bf16x8 vj = F32 ? codes_around(w) : codes_above(w, sixteen);
+#pragma unroll
+                    for (int n = 0; n < PM; ++n) o[c] = mfma(pa[n], vj, o[c]);
+                }
+            }
+        mfma_settle<DT_BF16>();
+        __builtin_amdgcn_wave_barrier();
+        asm volatile("" ::: "memory");
+    };
+    // The next tile is always loaded, at the end the last one again: where a load may or may not have been issued, the wait for an older one
+    // waits for it too.
+    for (int tile = w_lo; tile < w_hi; tile += 2) {
+        load(min(tile + 1, w_hi - 1), odd);
+        step(even, tile);
+        if (tile + 1 >= w_hi) break;
+        load(min(tile + 2, w_hi - 1), even);
+        step(odd, tile + 1);
+    }
+
+    // the waves' results, relative to their references, are joined in LDS
+#pragma unroll
+    for (int e = 0; e < R4; ++e) {
+#pragma unroll
+        for (int k = 16; k > 0; k >>= 1) {
+            l[e] += __shfl_xor(l[e], k, 64);
+#pragma unroll
+            for (int i = 0; i < NG; ++i) corr[i][e] += __shfl_xor(corr[i][e], k, 64);
+        }
+    }
+    __syncthreads();
+    float *mo = (float *)lds;
+#pragma unroll
+    for (int e = 0; e < R4; ++e) {
+        float *row = mo + (wave * ROWS + 8 * (e >> 2) + 4 * half + (e & 3)) * MROW;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+            float v = o[c][e] + corr[c / 2][e];
+#pragma unroll
+            for (int k = 1; k < STACK; ++k) v += o[c][e + k * R4];
+            row[c * 32 + l32] = v;
+        }
+        if (l32 == 0) {
+            row[D] = base[e];
+            row[D + 1] = l[e];
+        }
+    }
+    __syncthreads();
+    for (int i = tid; i < ROWS * D; i += NW * 64) {
+        const int row = i / D, d = i % D, r = r0 + row, t = r / a.per_kv;
+        float top = NO_SCORE;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) top = fmaxf(top, mo[(w * ROWS + row) * MROW + D]);
+        float sum = 0.f, acc = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float *m = mo + (w * ROWS + row) * MROW;
+            const float f = __builtin_amdgcn_exp2f(m[D] - top);
+            sum = fmaf(f, m[D + 1], sum);
+            acc = fmaf(f, m[d], acc);
+        }
+        if (a.splits > 1) {
+            float *ws = a.ws + ((((int64_t)b * a.c.kv_heads + g) * a.row_tiles + rt) * a.splits + sp) * (ROWS * MROW) + row * MROW;
+            ws[d] = acc;
+            if (d == 0) {
+                ws[D] = top;
+                ws[D + 1] = sum;
+            }
+        } else if (r < rows) {
+            const bool on = t < span.count && sum != 0.f;
+            st_f32((T *)a.y, (((int64_t)b * a.S + t) * a.heads + g * a.per_kv + (r - t * a.per_kv)) * D + d, on ? acc / sum : 0.f);
+        }
+    }
+}
+
+// Joins the splits of one row: a workgroup per row, its threads over features and, D at a time, over splits.
+template <typename T, int D, int ROWS> __global__ __launch_bounds__(256) void cache_attention_join_kernel(AttendArgs a)
+{
+    constexpr int MROW = D + 2, GROUPS = 256 / D;
+    __shared__ float acc_s[256], sum_s[GROUPS];
+    const int tid = threadIdx.x, d = tid % D, grp = tid / D;
+    const int h = (int)blockIdx.x % a.heads, g = h / a.per_kv;
+    const int64_t bt = (int64_t)blockIdx.x / a.heads;
+    const int t = (int)(bt % a.S), b = a.b_lo + (int)(bt / a.S);
+    const int r = t * a.per_kv + (h - g * a.per_kv), rt = r / ROWS, row = r % ROWS, rows = a.S * a.per_kv;
+    const Span span = span_of(a.c, b, a.S);
+    const Range rg = range_of(a, span, rt * ROWS, min(rt * ROWS + ROWS, rows));
+    const int tiles = rg.hi - rg.lo, n = t < span.count && tiles > 0 ? (tiles + split_tiles(tiles, a.splits) - 1) / split_tiles(tiles, a.splits) : 0;
+    const float *ws = a.ws + (((int64_t)b * a.c.kv_heads + g) * a.row_tiles + rt) * a.splits * (ROWS * MROW) + row * MROW;
+    float top = NO_SCORE;
+    for (int i = tid & 63; i < n; i += 64) top = fmaxf(top, ws[(int64_t)i * (ROWS * MROW) + D]);
+    for (int k = 32; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor(top, k, 64));
+    float acc = 0.f, sum = 0.f;
+#pragma unroll 4
+    for (int i = grp; i < n; i += GROUPS) {
+        const float *w = ws + (int64_t)i * (ROWS * MROW);
+        const float f = __builtin_amdgcn_exp2f(w[D] - top);
+        sum = fmaf(f, w[D + 1], sum);
+        acc = fmaf(f, w[d], acc);
+    }
+    acc_s[tid] = acc;
+    if (d == 0) sum_s[grp] = sum;
+    __syncthreads();
+    if (grp) return;
+    sum = 0.f;
+    acc = 0.f;
+    for (int i = 0; i < GROUPS; ++i) {
+        sum += sum_s[i];
+        acc += acc_s[i * D + d];
+    }
+    st_f32((T *)a.y, (bt + (int64_t)a.b_lo * a.S) * a.heads * D + h * D + d, sum != 0.f ? acc / sum : 0.f);
+}
+
+template <typename T, int D, int ROWS, int NW> static void attend(const AttendArgs &b, int grid, int joins, hipStream_t s, int phase)
+{
+    if (phase != 2) GACER_LAUNCH((cache_attention_kernel<T, D, ROWS, NW>), dim3(grid), dim3(NW * 64), 0, s, b);
+    if (b.splits > 1 && phase != 1) GACER_LAUNCH((cache_attention_join_kernel<T, D, ROWS>), dim3(joins), dim3(256), 0, s, b);
+}
+
+LaunchInfo launch_cache_attention(const TokenArgs &a, hipStream_t s, bool dry, int phase)
+{
+    const AttendGeom g = attend_geom(a);
     AttendArgs b;
-    b.x = a.x; b.y = a.y; b.c = a.cache; b.b_lo = a.b_lo; b.S = a.S; b.heads = a.heads; b.per_kv = a.heads / a.kv_heads;
-    b.window = a.window; b.alpha = a.alpha;
+    b.x = a.x; b.y = a.y; b.ws = a.ws; b.c = a.cache; b.b_lo = a.b_lo; b.S = a.S; b.heads = a.heads; b.per_kv = a.heads / a.kv_heads;
+    b.window = a.window; b.row_tiles = g.row_tiles; b.splits = g.splits;
+    b.scale = a.alpha * 1.4426950408889634f;
+    const int n = a.b_hi - a.b_lo, grid = n * a.kv_heads * g.row_tiles * g.splits, joins = n * a.S * a.heads;
     LaunchInfo li;
-    li.workgroups = (a.b_hi - a.b_lo) * a.S * a.heads;
-    li.threads = 64; li.lds_bytes = 1024; li.wg_per_cu = 32; li.kernel = a.dtype == DT_BF16 ? "cache_attention_bf16" : "cache_attention_f32"; li.phases = 1;
-    if (dry || !li.workgroups) return li;
-    const dim3 grid(li.workgroups), block(64);
-    if (a.dtype == DT_BF16 && a.D == 64) GACER_LAUNCH((cache_attention_rows_kernel<unsigned short, 64>), grid, block, 0, s, b);
-    else if (a.dtype == DT_BF16) GACER_LAUNCH((cache_attention_rows_kernel<unsigned short, 128>), grid, block, 0, s, b);
-    else if (a.D == 64) GACER_LAUNCH((cache_attention_rows_kernel<float, 64>), grid, block, 0, s, b);
-    else GACER_LAUNCH((cache_attention_rows_kernel<float, 128>), grid, block, 0, s, b);
+    li.workgroups = phase == 2 ? joins : grid;
+    li.threads = phase == 2 ? 256 : g.waves * 64; li.lds_bytes = g.waves * g.rows * (a.D + 2) * 4; li.wg_per_cu = phase == 2 ? 8 : 8 / g.waves;
+    li.kernel = phase == 2 ? "cache_attention_join" : a.dtype == DT_BF16 ? "cache_attention_bf16" : "cache_attention_f32";
+    li.phases = g.splits > 1 ? 2 : 1;
+    if (dry || !grid) return li;
+#define ATTEND(TYPE, DIM, ROWS, NW) if (a.D == DIM && g.rows == ROWS && g.waves == NW) attend<TYPE, DIM, ROWS, NW>(b, grid, joins, s, phase)
+    if (a.dtype == DT_BF16) {
+        ATTEND(unsigned short, 64, 8, 8); ATTEND(unsigned short, 64, 16, 4); ATTEND(unsigned short, 64, 32, 4);
+        ATTEND(unsigned short, 128, 8, 8); ATTEND(unsigned short, 128, 16, 4); ATTEND(unsigned short, 128, 32, 4);
+    } else {
+        ATTEND(float, 64, 8, 4); ATTEND(float, 64, 16, 4); ATTEND(float, 64, 32, 4);
+        ATTEND(float, 128, 8, 4); ATTEND(float, 128, 16, 4); ATTEND(float, 128, 32, 4);
+    }
+#undef ATTEND
     return li;
 }
 

@@ -125,7 +125,7 @@ static Launch make_token_launch(const Tenant &t, int oi, int b_lo, int b_hi)
     l.kind = LK_TOKENS;
     TokenArgs &k = l.k;
     k.dtype = dt(t);
-    k.b_lo = b_lo; k.b_hi = b_hi;
+    k.b_lo = b_lo; k.b_hi = b_hi; k.batch = t.batch;
     k.x = in ? in->dptr : nullptr;
     k.y = out ? out->dptr : nullptr;
     k.S = (int)(in ? in->h : out->h);

@@ -117,7 +117,7 @@ struct TokenArgs {
     int op, dtype;
     const void *x;
     void *y;
-    int b_lo, b_hi, S;         // S: tokens per sequence (SAMPLE: rows per item)
+    int b_lo, b_hi, batch, S;  // batch: of the unsplit operator; S: tokens per sequence (SAMPLE: rows per item)
     int heads, kv_heads, D;
     // QKNORM_ROPE
     const float *gamma_q, *gamma_k, *table;
