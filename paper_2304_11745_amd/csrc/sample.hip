@@ -1,9 +1,17 @@
 // Sampling: one token per row of logits (gacer_sampling in include/gacer.h has the definition).
 //
-// A workgroup owns a row.  Weights are whole numbers, so every sum is exact and the same in any order.  The entries that the filters keep are
-// a prefix of the order "larger first, equal ones by index", described by a key (the logit's bits in an order of unsigned
-// numbers) and a number of entries with that key; both top-k (by count) and top-p (by weight) find it digit by digit, eight bits of the key at
-// a time, from a histogram in LDS.  The draw halves in on its index by sums over ranges.
+// A workgroup owns a row.  Weights are whole numbers, so every sum is exact and the same in any order, whatever adds it.  The entries that the
+// filters keep are a prefix of the order "larger first, equal ones by index"; it ends at a key (the logit's bits in an order of
+// unsigned numbers) and, among the entries with that key, at an index.
+//   The row's largest logit comes first.  Then one pass puts every entry into one of 2048 bins by its distance from the largest, 1/64 of a
+// temperature each (weights vanish 21.5 temperatures below), counting entries (top-k) or adding weights (top-p); the bin in which
+// the prefix ends is found by a scan.  For top-k the entries up to this bin go into a list in LDS, and everything else happens on the list: ranks
+// by counting, the nucleus by a scan over ranks, the draw by sums over smaller indexes.  For top-p alone only the bin's own entries need
+// ranks; the draw then adds the kept weights of the row, a part per wave, and looks for its index in one of the parts.
+//   Where more entries end up in the list than it holds (a flat row), the prefix's end is found digit by digit of the key instead.
+//
+// What bounds it: instructions.  A weight is a correctly rounded division, an exponential and a conversion, some 25 instructions, for every
+// entry of the row under top-p, and the row's workgroup runs on one compute unit.
 #include <hip/hip_runtime.h>
 #include "device_util.h"
 #include "kernels.h"
@@ -22,6 +30,8 @@ struct SampleArgs {
     float *logp;
 };
 
+static constexpr int THREADS = 1024, WAVES = THREADS / 64, BINS = 2048, LIST = 2048;
+
 // numbers in an order of unsigned integers: -inf and NaN lowest, both zeros alike
 __device__ __forceinline__ unsigned key_of(float x)
 {
@@ -31,156 +41,365 @@ __device__ __forceinline__ unsigned key_of(float x)
 }
 __device__ __forceinline__ float value_of(unsigned key) { return __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xFFFFFFFFu)); }
 
-template <typename T> struct Row {
-    static constexpr int THREADS = 1024, WAVES = THREADS / 64;
-    const T *x;
-    int V;
-    float top, temperature;
-    u64 *shared;               // WAVES + 1
+// Weights of a row
+struct Weights {
+    float top, temperature, inverse, lowest;           // inverse: 1 / temperature, rounded; lowest: a distance at which every weight is 0
+    bool plain;                                        // the temperature is so small or large that only a division is safe
+    __device__ void set(float t, float temp)
+    {
+        top = t;
+        temperature = temp;
+        inverse = __fdiv_rn(1.f, temp);
+        lowest = -120.f * temp;
+        plain = !(temp > 1e-18f && temp < 1e18f);
+    }
+    // (x - top) / temperature, correctly rounded: a product with the rounded inverse is within two units in the last place, a step
+    // with the exact remainder within one, and from there another step rounds correctly.
+    __device__ __forceinline__ float distance(float x) const
+    {
+        const float a = fmaxf(__fsub_rn(x, top), lowest);
+        if (plain) return x == top ? 0.f : __fdiv_rn(a, temperature);
+        float q = __fmul_rn(a, inverse);
+        q = __fmaf_rn(__fmaf_rn(-q, temperature, a), inverse, q);
+        q = __fmaf_rn(__fmaf_rn(-q, temperature, a), inverse, q);
+        return x == top ? 0.f : q;                     // an infinite top
+    }
+    static __device__ __forceinline__ unsigned weight(float part) { return (unsigned)(part * 2147483648.f); }
+    __device__ __forceinline__ float part(unsigned key) const { return expf(distance(value_of(key))); }
+};
+__device__ __forceinline__ int bin_of(float distance) { return min(BINS - 1, (int)(distance * -64.f)); }
 
+__device__ __forceinline__ u64 wave_sum(u64 v)
+{
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+// sum over lanes 0..lane
+__device__ __forceinline__ u64 wave_scan(u64 v)
+{
+    const int lane = threadIdx.x & 63;
+    for (int o = 1; o < 64; o <<= 1) {
+        const u64 n = __shfl_up(v, o, 64);
+        if (lane >= o) v += n;
+    }
+    return v;
+}
+
+template <typename T> struct Row {
+    static constexpr int VEC = 16 / sizeof(T), DEPTH = 4;
+    const T *x;
+    int V, head, vectors, per;                         // entries before the first 16-byte boundary, vectors after it, vectors of a wave's part
+
+    __device__ void set(const T *row, int v)
+    {
+        x = row;
+        V = v;
+        head = min(v, (int)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(T));
+        vectors = (v - head) / VEC;
+        per = (vectors + WAVES - 1) / WAVES;
+    }
     __device__ unsigned key(int i) const { return key_of(ld_f32(x, i)); }
-    __device__ float part(unsigned k) const
+    __device__ int part_begin(int w) const { return w == 0 ? 0 : head + min(w * per, vectors) * VEC; }
+    __device__ int part_end(int w) const { return w == WAVES - 1 ? V : head + min((w + 1) * per, vectors) * VEC; }
+    // f(index, key) for the entries of the wave's part, DEPTH vectors of a lane in flight
+    template <typename F> __device__ __forceinline__ void each(F f) const
     {
-        const float v = value_of(k);
-        return v == top ? 1.f : expf(__fdiv_rn(__fsub_rn(v, top), temperature));
-    }
-    static __device__ u64 weight(float part) { return (u64)(part * 2147483648.f); }
-    __device__ u64 sum(u64 v)
-    {
-        for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-        __syncthreads();
-        if (threadIdx.x % 64 == 0) shared[threadIdx.x / 64] = v;
-        __syncthreads();
-        u64 s = 0;
-        for (int w = 0; w < WAVES; ++w) s += shared[w];
-        return s;
-    }
-    // The first index at which the sum of f over 0..i exceeds `goal` (goal < sum of all).
-    template <typename F> __device__ int locate(u64 goal, F f)
-    {
-        int lo = 0, hi = V;
-        const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
-        while (hi - lo > 64) {
-            const int per = ((hi - lo + WAVES - 1) / WAVES + 63) & ~63;
-            const int a = min(hi, lo + wave * per), b = min(hi, a + per);
-            u64 v = 0;
-            for (int i = a + lane; i < b; i += 64) v += f(i);
-            for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-            __syncthreads();
-            if (lane == 0) shared[wave] = v;
-            __syncthreads();
-            int w = 0;
-            while (w < WAVES - 1 && shared[w] <= goal) goal -= shared[w++];
-            const int end = hi;
-            lo = min(end, lo + w * per);
-            hi = min(end, lo + per);
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+        const int b = min(vectors, (wave + 1) * per);
+        const T *body = x + head;
+        for (int v = wave * per + lane; v < b; v += 64 * DEPTH) {
+            Vec<T, VEC> in[DEPTH];
+#pragma unroll
+            for (int k = 0; k < DEPTH; ++k) in[k] = ld_vec<T, VEC>(body, (int64_t)min(v + 64 * k, b - 1) * VEC);
+#pragma unroll
+            for (int k = 0; k < DEPTH; ++k) {
+                if (v + 64 * k >= b) break;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) f(head + (v + 64 * k) * VEC + e, key_of(in[k].get(e)));
+            }
         }
-        u64 v = lo + lane < hi ? f(lo + lane) : 0;
-        for (int o = 1; o < 64; o <<= 1) {
-            const u64 n = __shfl_up(v, o, 64);
-            if (lane >= o) v += n;
-        }
-        return lo + __popcll(__ballot(v <= goal && lo + lane < hi));
+        const int rest = V - head - vectors * VEC;
+        if (wave == 0 && lane < head) f(lane, key(lane));
+        if (wave == WAVES - 1 && lane < rest) f(V - rest + lane, key(V - rest + lane));
     }
 };
 
+struct Shared {
+    u64 sums[WAVES], bins[BINS], list[LIST];           // list: key, then the index's complement, so that larger numbers come first in the order
+    unsigned weight[LIST];                             // of the list's entries, by rank
+    int place[LIST];                                   // and their indexes
+    unsigned peak;
+    int entries, found, digit;
+    u64 before;
+};
+
+__device__ __forceinline__ u64 entry_of(unsigned key, int i) { return (u64)key << 32 | (unsigned)~i; }
+__device__ __forceinline__ unsigned entry_key(u64 e) { return (unsigned)(e >> 32); }
+__device__ __forceinline__ int entry_index(u64 e) { return (int)~(unsigned)e; }
+
+// sum over the workgroup
+__device__ u64 block_sum(Shared &s, u64 v)
+{
+    v = wave_sum(v);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) s.sums[threadIdx.x >> 6] = v;
+    __syncthreads();
+    u64 all = 0;
+    for (int w = 0; w < WAVES; ++w) all += s.sums[w];
+    return all;
+}
+
+// The first bin, from 0 on, at which the sum passes the line: done(sum up to and with it).  `before` receives the sum in front of it.
+template <typename D> __device__ int first_bin(Shared &s, D done, u64 *before)
+{
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const u64 a = s.bins[2 * tid], b = s.bins[2 * tid + 1];
+    u64 v = wave_scan(a + b);
+    __syncthreads();
+    if (lane == 63) s.sums[wave] = v;
+    if (tid == 0) s.found = BINS - 1;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) v += s.sums[w];
+    if (done(v) && !done(v - a - b)) {
+        const bool first = done(v - b);
+        s.found = 2 * tid + (first ? 0 : 1);
+        s.before = first ? v - a - b : v - b;
+    }
+    __syncthreads();
+    *before = s.before;
+    return s.found;
+}
+
+// entries of the list in order: place[r] and weight[r] of rank r
+__device__ void rank_list(Shared &s, const Weights &w, int n)
+{
+    for (int i = threadIdx.x; i < n; i += THREADS) {
+        const u64 me = s.list[i];
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += s.list[j] > me;
+        s.place[rank] = i;
+        s.weight[rank] = Weights::weight(w.part(entry_key(me)));
+    }
+    __syncthreads();
+}
+
+// The number of ranks, at most n, up to and with the first at which `before` and the weights so far reach the line; by one wave, told to all.
+__device__ int ranks_to(Shared &s, int n, u64 before, double reach)
+{
+    if (threadIdx.x < 64) {
+        int r = n;
+        for (int i = 0; i < n; i += 64) {
+            const int at = i + (int)threadIdx.x;
+            const u64 v = before + wave_scan(at < n ? s.weight[at] : 0u);
+            const u64 hit = __ballot(at < n && (double)v >= reach);
+            if (hit) {
+                r = i + __builtin_ctzll(hit) + 1;
+                break;
+            }
+            before = __shfl(v, 63, 64);
+        }
+        if (threadIdx.x == 0) s.found = r;
+    }
+    __syncthreads();
+    return s.found;
+}
+
+// end of the kept prefix by the digits of the key, for rows whose entries crowd in one bin
+template <typename T, typename M> __device__ void prefix_by_digits(Shared &s, const Row<T> &row, double reach, M measure, unsigned &cut, int &last)
+{
+    const int tid = threadIdx.x;
+    u64 before = 0;                                    // measure of the keys above the digits found so far
+    unsigned prefix = 0u;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        __syncthreads();
+        if (tid < 256) s.bins[tid] = 0;
+        __syncthreads();
+        row.each([&](int i, unsigned k) {
+            if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) {
+                const u64 m = measure(i, k);
+                if (m) atomicAdd(&s.bins[(k >> shift) & 255u], m);
+            }
+        });
+        __syncthreads();
+        int digit = 255;
+        for (; digit > 0 && (double)(before + s.bins[digit]) < reach; --digit) before += s.bins[digit];
+        prefix |= (unsigned)digit << shift;
+    }
+    // entries of this very key are taken by index until the line is reached: halve in on the last one's index
+    auto same = [&](int i, unsigned k) -> u64 { return k == prefix ? measure(i, k) : 0; };
+    int lo = 0, hi = row.V;                            // the last one lies in [lo, hi)
+    while (hi - lo > 1) {
+        const int mid = lo + (hi - lo) / 2;
+        u64 v = 0;
+        for (int i = lo + tid; i < mid; i += THREADS) v += same(i, row.key(i));
+        v = block_sum(s, v);
+        if ((double)(before + v) >= reach) hi = mid;
+        else {
+            before += v;
+            lo = mid;
+        }
+    }
+    cut = prefix;
+    last = lo;
+}
+
 template <typename T> __global__ __launch_bounds__(1024) void sample_kernel(SampleArgs a)
 {
-    __shared__ u64 shared[Row<T>::WAVES + 1], bins[256];
-    __shared__ unsigned topmost;
-    const int tid = threadIdx.x;
+    __shared__ Shared s;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int64_t r = a.row_lo + blockIdx.x;
-    Row<T> row = {(const T *)a.x + r * a.V, a.V, 0.f, 1.f, shared};
-    if (tid == 0) topmost = 0u;
+    Row<T> row;
+    row.set((const T *)a.x + r * a.V, a.V);
+    const unsigned none = key_of(-INFINITY);
+    unsigned peak = none;
+    row.each([&](int, unsigned k) { peak = max(peak, k); });
+    for (int o = 32; o > 0; o >>= 1) peak = max(peak, (unsigned)__shfl_xor((int)peak, o, 64));
+    if (lane == 0) s.sums[wave] = peak;
+    for (int i = tid; i < BINS; i += THREADS) s.bins[i] = 0;
+    if (tid == 0) s.entries = 0;
     __syncthreads();
-    unsigned best = 0u;
-    for (int i = tid; i < a.V; i += 1024) best = max(best, row.key(i));
-    atomicMax(&topmost, best);
-    __syncthreads();
-    const unsigned none = key_of(-INFINITY), peak = topmost;
-    if (peak <= none) {
+    for (int w = 0; w < WAVES; ++w) peak = max(peak, (unsigned)s.sums[w]);
+    if (peak == none) {
         if (tid == 0) {
             a.tokens[r] = -1;
             if (a.logp) a.logp[r] = -INFINITY;
         }
         return;
     }
-    row.top = value_of(peak);
-    row.temperature = a.temperature ? a.temperature[r] : 1.f;
-    const float top_p = a.top_p ? a.top_p[r] : 1.f, min_p = a.min_p ? a.min_p[r] : 0.f;
+    const float temperature = a.temperature ? a.temperature[r] : 1.f, top_p = a.top_p ? a.top_p[r] : 1.f, min_p = a.min_p ? a.min_p[r] : 0.f;
     int top_k = a.top_k ? a.top_k[r] : 0;
-    if (!(row.temperature > 0.f) || !(top_p > 0.f) || !(min_p <= 1.f)) top_k = 1;
-    if (top_k <= 0 || top_k > a.V) top_k = a.V;
-
-    // kept: keys above `cut`, and the first `ties` entries (by index, up to `last`) with that key
-    unsigned cut = 0u;
-    int last = a.V;
-    for (int pass = 0; pass < 2; ++pass) {
-        const bool by_weight = pass == 1;
-        if (by_weight ? !(top_p < 1.f) || top_k == 1 : top_k == a.V) continue;
-        auto measure = [&](int i, unsigned k) -> u64 {
-            if (!by_weight) return 1;
-            return k > cut || (k == cut && i <= last) ? Row<T>::weight(row.part(k)) : 0;
-        };
-        double reach = (double)top_k;
-        if (by_weight) {
-            u64 v = 0;
-            for (int i = tid; i < a.V; i += 1024) v += measure(i, row.key(i));
-            reach = (double)top_p * (double)row.sum(v);
+    const bool one = top_k == 1 || !(temperature > 0.f) || !(top_p > 0.f) || !(min_p <= 1.f);
+    Weights w;
+    w.set(value_of(peak), one ? 1.f : temperature);
+    if (one) {                                         // the first of the largest
+        int first = a.V;
+        row.each([&](int i, unsigned k) { if (k == peak) first = min(first, i); });
+        for (int o = 32; o > 0; o >>= 1) first = min(first, __shfl_xor(first, o, 64));
+        __syncthreads();
+        if (lane == 0) s.sums[wave] = first;
+        __syncthreads();
+        if (tid == 0) {
+            for (int v = 0; v < WAVES; ++v) first = min(first, (int)s.sums[v]);
+            a.tokens[r] = first;
+            if (a.logp) a.logp[r] = 0.f;
         }
-        u64 before = 0;                              // measure of the keys above the digits found so far
-        unsigned prefix = 0u;
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            __syncthreads();
-            if (tid < 256) bins[tid] = 0;
-            __syncthreads();
-            for (int i = tid; i < a.V; i += 1024) {
-                const unsigned k = row.key(i);
-                if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) {
-                    const u64 m = measure(i, k);
-                    if (m) atomicAdd(&bins[(k >> shift) & 255u], m);
-                }
-            }
-            __syncthreads();
-            int digit = 255;
-            for (; digit > 0 && (double)(before + bins[digit]) < reach; --digit) before += bins[digit];
-            prefix |= (unsigned)digit << shift;
-        }
-        // entries of this very key that the prefix still takes, one by one
-        const u64 each = by_weight ? Row<T>::weight(row.part(prefix)) : 1;
-        u64 ties = 1;
-        if (each) {
-            const double more = reach - (double)before;
-            ties = (u64)(more / (double)each);
-            while ((double)(before + ties * each) < reach) ++ties;
-            while (ties > 1 && (double)(before + (ties - 1) * each) >= reach) --ties;
-        }
-        u64 equal = 0;
-        const unsigned old_cut = cut;
-        const int old_last = last;
-        auto same = [&](int i) -> u64 { return row.key(i) == prefix && (prefix > old_cut || i <= old_last); };
-        for (int i = tid; i < a.V; i += 1024) equal += same(i);
-        equal = row.sum(equal);
-        last = ties < equal ? row.locate(ties - 1, same) : (prefix > old_cut ? a.V : old_last);
-        cut = prefix;
+        return;
     }
-    auto kept = [&](int i) -> u64 {
-        const unsigned k = row.key(i);
-        if (k < cut || (k == cut && i > last) || k <= none) return 0;
-        const float part = row.part(k);
-        return part >= min_p || top_k == 1 ? Row<T>::weight(part) : 0;
-    };
-    u64 total = 0;
-    for (int i = tid; i < a.V; i += 1024) total += kept(i);
-    total = row.sum(total);
-    const double goal = floor((double)a.u[r] * (double)total);
-    const u64 g = goal > 0. ? (goal >= (double)total ? total - 1 : (u64)goal) : 0;
-    const int token = row.locate(g, kept);
-    if (tid == 0) {
+    if (top_k <= 0 || top_k > a.V) top_k = a.V;
+    auto write = [&](int token, unsigned key, u64 total) {
         a.tokens[r] = token;
-        if (a.logp) {
-            const float v = value_of(row.key(token));
-            a.logp[r] = (v == row.top ? 0.f : __fdiv_rn(__fsub_rn(v, row.top), row.temperature)) - logf((float)total * 0x1p-31f);
+        if (a.logp) a.logp[r] = w.distance(value_of(key)) - logf((float)total * 0x1p-31f);
+    };
+    auto goal_of = [&](u64 total) -> u64 {
+        const double goal = floor((double)a.u[r] * (double)total);
+        return goal > 0. ? (goal >= (double)total ? total - 1 : (u64)goal) : 0;
+    };
+
+    unsigned cut = 0u;                                 // kept: keys above `cut`, and those equal to it up to index `last`
+    int last = a.V;
+    if (top_k < a.V) {
+        row.each([&](int, unsigned k) { atomicAdd(&s.bins[bin_of(w.distance(value_of(k)))], 1ull); });
+        __syncthreads();
+        u64 before;
+        const u64 k64 = (u64)top_k;
+        const int bin = first_bin(s, [&](u64 v) { return v >= k64; }, &before);
+        const u64 in_list = before + s.bins[bin];
+        if (in_list <= LIST) {
+            row.each([&](int i, unsigned k) {
+                if (bin_of(w.distance(value_of(k))) <= bin) s.list[atomicAdd(&s.entries, 1)] = entry_of(k, i);
+            });
+            __syncthreads();
+            rank_list(s, w, (int)in_list);
+            int n = top_k;
+            if (top_p < 1.f) {
+                u64 v = 0;
+                for (int i = tid; i < n; i += THREADS) v += s.weight[i];
+                n = ranks_to(s, n, 0, (double)top_p * (double)block_sum(s, v));
+            }
+            // the kept ones' indexes and weights, then the draw: whose weight the goal falls on, smaller indexes before it
+            u64 v = 0;
+            for (int i = tid; i < n; i += THREADS) {
+                const u64 e = s.list[s.place[i]];
+                const unsigned m = i == 0 || w.part(entry_key(e)) >= min_p ? s.weight[i] : 0u;
+                s.bins[i] = (u64)(unsigned)entry_index(e) << 32 | m;
+                v += m;
+            }
+            const u64 total = block_sum(s, v), goal = goal_of(total);
+            __syncthreads();
+            for (int i = tid; i < n; i += THREADS) {
+                const u64 me = s.bins[i];
+                u64 sum = 0;
+                for (int j = 0; j < n; ++j) sum += (s.bins[j] >> 32) < (me >> 32) ? (unsigned)s.bins[j] : 0u;
+                if (sum <= goal && goal < sum + (unsigned)me) write((int)(me >> 32), entry_key(s.list[s.place[i]]), total);
+            }
+            return;
+        }
+        prefix_by_digits(s, row, (double)top_k, [&](int, unsigned) -> u64 { return 1; }, cut, last);
+        __syncthreads();
+        for (int i = tid; i < BINS; i += THREADS) s.bins[i] = 0;
+        __syncthreads();
+    }
+    if (top_p < 1.f) {
+        const unsigned cut_k = cut;
+        const int last_k = last;
+        auto measure = [&](int i, unsigned k) -> u64 { return k > cut_k || (k == cut_k && i <= last_k) ? Weights::weight(w.part(k)) : 0u; };
+        row.each([&](int i, unsigned k) {
+            const float q = w.distance(value_of(k));
+            const unsigned m = k > cut_k || (k == cut_k && i <= last_k) ? Weights::weight(expf(q)) : 0u;
+            if (m) atomicAdd(&s.bins[bin_of(q)], (u64)m);
+        });
+        __syncthreads();
+        u64 all = 0, before;
+        for (int i = tid; i < BINS; i += THREADS) all += s.bins[i];
+        const double reach = (double)top_p * (double)block_sum(s, all);
+        const int bin = first_bin(s, [&](u64 v) { return (double)v >= reach; }, &before);
+        row.each([&](int i, unsigned k) {
+            if (bin_of(w.distance(value_of(k))) == bin && (k > cut_k || (k == cut_k && i <= last_k))) {
+                const int at = atomicAdd(&s.entries, 1);
+                if (at < LIST) s.list[at] = entry_of(k, i);
+            }
+        });
+        __syncthreads();
+        const int n = s.entries;
+        if (n <= LIST) {
+            rank_list(s, w, n);
+            const u64 e = s.list[s.place[max(1, ranks_to(s, n, before, reach)) - 1]];
+            cut = entry_key(e);
+            last = entry_index(e);
+        } else prefix_by_digits(s, row, reach, measure, cut, last);
+    }
+    // the draw: sums of the kept weights by the waves' parts, then by threads within the part that the goal falls into
+    const float near = min_p > 0.f ? w.top + w.temperature * (logf(min_p) - 0.01f) : -INFINITY;      // certainly below min_p
+    const unsigned cut_min = max(max(cut, none + 1u), key_of(near));
+    auto kept = [&](int i, unsigned k) -> unsigned {
+        if (k < cut_min || (k == cut && i > last)) return 0u;
+        const float part = w.part(k);
+        return part >= min_p || k == peak ? Weights::weight(part) : 0u;
+    };
+    u64 mine = 0;
+    row.each([&](int i, unsigned k) { mine += kept(i, k); });
+    const u64 total = block_sum(s, mine);
+    u64 goal = goal_of(total);
+    int p = 0;
+    while (p < WAVES - 1 && s.sums[p] <= goal) goal -= s.sums[p++];
+    const int lo = row.part_begin(p), hi = row.part_end(p), each = (hi - lo + THREADS - 1) / THREADS;
+    const int b = min(hi, lo + tid * each), e = min(hi, b + each);
+    u64 v = 0;
+    for (int i = b; i < e; ++i) v += kept(i, row.key(i));
+    u64 sum = wave_scan(v);
+    __syncthreads();
+    if (lane == 63) s.sums[wave] = sum;
+    __syncthreads();
+    for (int k = 0; k < wave; ++k) sum += s.sums[k];
+    if (sum > goal && sum - v <= goal) {
+        u64 at = sum - v;
+        for (int i = b; i < e; ++i) {
+            const unsigned k = row.key(i);
+            at += kept(i, k);
+            if (at > goal) {
+                write(i, k, total);
+                break;
+            }
         }
     }
 }
@@ -192,10 +411,10 @@ LaunchInfo launch_sample(const TokenArgs &a, hipStream_t s, bool dry, int)
     b.top_k = a.top_k; b.tokens = a.tokens; b.logp = a.logp;
     LaunchInfo li;
     li.workgroups = (a.b_hi - a.b_lo) * a.S;
-    li.threads = 1024; li.lds_bytes = 2304; li.wg_per_cu = 2; li.kernel = a.dtype == DT_BF16 ? "sample_bf16" : "sample_f32"; li.phases = 1;
+    li.threads = THREADS; li.lds_bytes = (int)sizeof(Shared); li.wg_per_cu = 2; li.kernel = a.dtype == DT_BF16 ? "sample_bf16" : "sample_f32"; li.phases = 1;
     if (dry || !li.workgroups) return li;
-    if (a.dtype == DT_BF16) GACER_LAUNCH(sample_kernel<unsigned short>, dim3(li.workgroups), dim3(1024), 0, s, b);
-    else GACER_LAUNCH(sample_kernel<float>, dim3(li.workgroups), dim3(1024), 0, s, b);
+    if (a.dtype == DT_BF16) GACER_LAUNCH(sample_kernel<unsigned short>, dim3(li.workgroups), dim3(THREADS), 0, s, b);
+    else GACER_LAUNCH(sample_kernel<float>, dim3(li.workgroups), dim3(THREADS), 0, s, b);
     return li;
 }
 
