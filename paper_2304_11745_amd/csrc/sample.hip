@@ -31,6 +31,9 @@ struct SampleArgs {
 };
 
 static constexpr int THREADS = 1024, WAVES = THREADS / 64, BINS = 2048, LIST = 2048;
+// Entries that a list may hold where the alternative is another pass over the row: ranks by counting take n steps of a thread and more, a pass over 131072
+// entries what 600 of them take.
+static constexpr int SHORT = 512;
 
 // numbers in an order of unsigned integers: -inf and NaN lowest, both zeros alike
 __device__ __forceinline__ unsigned key_of(float x)
@@ -41,31 +44,26 @@ __device__ __forceinline__ unsigned key_of(float x)
 }
 __device__ __forceinline__ float value_of(unsigned key) { return __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xFFFFFFFFu)); }
 
-// Weights of a row
-struct Weights {
+__device__ __forceinline__ unsigned weight_of(float part) { return (unsigned)(part * 2147483648.f); }
+
+// Weights of a row.  PLAIN: only a division is safe (a temperature very small or large, an infinite top).
+template <bool PLAIN> struct Weights {
     float top, temperature, inverse, lowest;           // inverse: 1 / temperature, rounded; lowest: a distance at which every weight is 0
-    bool plain;                                        // the temperature is so small or large that only a division is safe
-    __device__ void set(float t, float temp)
-    {
-        top = t;
-        temperature = temp;
-        inverse = __fdiv_rn(1.f, temp);
-        lowest = -120.f * temp;
-        plain = !(temp > 1e-18f && temp < 1e18f);
-    }
+    __device__ Weights(float t, float temp) : top(t), temperature(temp), inverse(__fdiv_rn(1.f, temp)), lowest(-120.f * temp) {}
     // (x - top) / temperature, correctly rounded: a product with the rounded inverse is within two units in the last place, a step
-    // with the exact remainder within one, and from there another step rounds correctly.
+    // with the exact remainder within one, and from there another step rounds correctly (no difference to a division in 4 x 2^30 pairs,
+    // significands near one and two among them).  NaN counts as -inf.
     __device__ __forceinline__ float distance(float x) const
     {
         const float a = fmaxf(__fsub_rn(x, top), lowest);
-        if (plain) return x == top ? 0.f : __fdiv_rn(a, temperature);
+        if constexpr (PLAIN) return x == top ? 0.f : __fdiv_rn(a, temperature);
         float q = __fmul_rn(a, inverse);
         q = __fmaf_rn(__fmaf_rn(-q, temperature, a), inverse, q);
-        q = __fmaf_rn(__fmaf_rn(-q, temperature, a), inverse, q);
-        return x == top ? 0.f : q;                     // an infinite top
+        return __fmaf_rn(__fmaf_rn(-q, temperature, a), inverse, q);
     }
-    static __device__ __forceinline__ unsigned weight(float part) { return (unsigned)(part * 2147483648.f); }
     __device__ __forceinline__ float part(unsigned key) const { return expf(distance(value_of(key))); }
+    // a logit that stands `d` temperatures (d <= 0) and a little below the top: no entry whose distance is d or more is smaller
+    __device__ __forceinline__ float below(float d) const { return top + temperature * (d * 1.0001f - 0.001f); }
 };
 __device__ __forceinline__ int bin_of(float distance) { return min(BINS - 1, (int)(distance * -64.f)); }
 
@@ -101,7 +99,7 @@ template <typename T> struct Row {
     __device__ unsigned key(int i) const { return key_of(ld_f32(x, i)); }
     __device__ int part_begin(int w) const { return w == 0 ? 0 : head + min(w * per, vectors) * VEC; }
     __device__ int part_end(int w) const { return w == WAVES - 1 ? V : head + min((w + 1) * per, vectors) * VEC; }
-    // f(index, key) for the entries of the wave's part, DEPTH vectors of a lane in flight
+    // f(index, logit) for the entries of the wave's part, DEPTH vectors of a lane in flight
     template <typename F> __device__ __forceinline__ void each(F f) const
     {
         const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -115,12 +113,12 @@ template <typename T> struct Row {
             for (int k = 0; k < DEPTH; ++k) {
                 if (v + 64 * k >= b) break;
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) f(head + (v + 64 * k) * VEC + e, key_of(in[k].get(e)));
+                for (int e = 0; e < VEC; ++e) f(head + (v + 64 * k) * VEC + e, in[k].get(e));
             }
         }
         const int rest = V - head - vectors * VEC;
-        if (wave == 0 && lane < head) f(lane, key(lane));
-        if (wave == WAVES - 1 && lane < rest) f(V - rest + lane, key(V - rest + lane));
+        if (wave == 0 && lane < head) f(lane, ld_f32(x, lane));
+        if (wave == WAVES - 1 && lane < rest) f(V - rest + lane, ld_f32(x, V - rest + lane));
     }
 };
 
@@ -136,6 +134,12 @@ struct Shared {
 __device__ __forceinline__ u64 entry_of(unsigned key, int i) { return (u64)key << 32 | (unsigned)~i; }
 __device__ __forceinline__ unsigned entry_key(u64 e) { return (unsigned)(e >> 32); }
 __device__ __forceinline__ int entry_index(u64 e) { return (int)~(unsigned)e; }
+
+__device__ __forceinline__ u64 goal_of(float u, u64 total)
+{
+    const double goal = floor((double)u * (double)total);
+    return goal > 0. ? (goal >= (double)total ? total - 1 : (u64)goal) : 0;
+}
 
 // sum over the workgroup
 __device__ u64 block_sum(Shared &s, u64 v)
@@ -171,14 +175,14 @@ template <typename D> __device__ int first_bin(Shared &s, D done, u64 *before)
 }
 
 // entries of the list in order: place[r] and weight[r] of rank r
-__device__ void rank_list(Shared &s, const Weights &w, int n)
+template <typename W> __device__ void rank_list(Shared &s, const W &w, int n)
 {
     for (int i = threadIdx.x; i < n; i += THREADS) {
         const u64 me = s.list[i];
         int rank = 0;
         for (int j = 0; j < n; ++j) rank += s.list[j] > me;
         s.place[rank] = i;
-        s.weight[rank] = Weights::weight(w.part(entry_key(me)));
+        s.weight[rank] = weight_of(w.part(entry_key(me)));
     }
     __syncthreads();
 }
@@ -214,7 +218,8 @@ template <typename T, typename M> __device__ void prefix_by_digits(Shared &s, co
         __syncthreads();
         if (tid < 256) s.bins[tid] = 0;
         __syncthreads();
-        row.each([&](int i, unsigned k) {
+        row.each([&](int i, float x) {
+            const unsigned k = key_of(x);
             if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) {
                 const u64 m = measure(i, k);
                 if (m) atomicAdd(&s.bins[(k >> shift) & 255u], m);
@@ -243,149 +248,151 @@ template <typename T, typename M> __device__ void prefix_by_digits(Shared &s, co
     last = lo;
 }
 
-template <typename T> __global__ __launch_bounds__(1024) void sample_kernel(SampleArgs a)
+struct Filters { float top_p, min_p, u; int top_k; };
+
+// The draw from a list that holds every kept entry (and perhaps more): the first n ranks, of them those of at least min_p
+template <typename W, typename F> __device__ void draw_from_list(Shared &s, const W &w, const Filters &f, int n, F write)
 {
-    __shared__ Shared s;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-    const int64_t r = a.row_lo + blockIdx.x;
-    Row<T> row;
-    row.set((const T *)a.x + r * a.V, a.V);
-    const unsigned none = key_of(-INFINITY);
-    unsigned peak = none;
-    row.each([&](int, unsigned k) { peak = max(peak, k); });
-    for (int o = 32; o > 0; o >>= 1) peak = max(peak, (unsigned)__shfl_xor((int)peak, o, 64));
-    if (lane == 0) s.sums[wave] = peak;
-    for (int i = tid; i < BINS; i += THREADS) s.bins[i] = 0;
-    if (tid == 0) s.entries = 0;
+    const int tid = threadIdx.x;
+    u64 v = 0;
+    for (int i = tid; i < n; i += THREADS) {
+        const u64 e = s.list[s.place[i]];
+        const unsigned m = i == 0 || w.part(entry_key(e)) >= f.min_p ? s.weight[i] : 0u;
+        s.bins[i] = (u64)(unsigned)entry_index(e) << 32 | m;
+        v += m;
+    }
+    const u64 total = block_sum(s, v), goal = goal_of(f.u, total);
     __syncthreads();
-    for (int w = 0; w < WAVES; ++w) peak = max(peak, (unsigned)s.sums[w]);
-    if (peak == none) {
-        if (tid == 0) {
-            a.tokens[r] = -1;
-            if (a.logp) a.logp[r] = -INFINITY;
-        }
-        return;
+    for (int i = tid; i < n; i += THREADS) {           // whose weight does the goal fall on, smaller indexes before it
+        const u64 me = s.bins[i];
+        u64 sum = 0;
+        for (int j = 0; j < n; ++j) sum += (s.bins[j] >> 32) < (me >> 32) ? (unsigned)s.bins[j] : 0u;
+        if (sum <= goal && goal < sum + (unsigned)me) write((int)(me >> 32), value_of(entry_key(s.list[s.place[i]])), total);
     }
-    const float temperature = a.temperature ? a.temperature[r] : 1.f, top_p = a.top_p ? a.top_p[r] : 1.f, min_p = a.min_p ? a.min_p[r] : 0.f;
-    int top_k = a.top_k ? a.top_k[r] : 0;
-    const bool one = top_k == 1 || !(temperature > 0.f) || !(top_p > 0.f) || !(min_p <= 1.f);
-    Weights w;
-    w.set(value_of(peak), one ? 1.f : temperature);
-    if (one) {                                         // the first of the largest
-        int first = a.V;
-        row.each([&](int i, unsigned k) { if (k == peak) first = min(first, i); });
-        for (int o = 32; o > 0; o >>= 1) first = min(first, __shfl_xor(first, o, 64));
-        __syncthreads();
-        if (lane == 0) s.sums[wave] = first;
-        __syncthreads();
-        if (tid == 0) {
-            for (int v = 0; v < WAVES; ++v) first = min(first, (int)s.sums[v]);
-            a.tokens[r] = first;
-            if (a.logp) a.logp[r] = 0.f;
-        }
-        return;
-    }
-    if (top_k <= 0 || top_k > a.V) top_k = a.V;
-    auto write = [&](int token, unsigned key, u64 total) {
+}
+
+template <typename T, bool PLAIN> __device__ __forceinline__ void sample_row(const SampleArgs &a, Shared &s, const Row<T> &row, int64_t r, float top, float temperature, Filters f)
+{
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const Weights<PLAIN> w(top, temperature);
+    const unsigned none = key_of(-INFINITY), peak = key_of(top);
+    auto write = [&](int token, float x, u64 total) {
         a.tokens[r] = token;
-        if (a.logp) a.logp[r] = w.distance(value_of(key)) - logf((float)total * 0x1p-31f);
+        if (a.logp) a.logp[r] = w.distance(x) - logf((float)total * 0x1p-31f);
     };
-    auto goal_of = [&](u64 total) -> u64 {
-        const double goal = floor((double)a.u[r] * (double)total);
-        return goal > 0. ? (goal >= (double)total ? total - 1 : (u64)goal) : 0;
+    // a logit below which nothing is kept, whatever the other filters say: min_p, and weights of 0 (21.5 temperatures below)
+    const float floor_p = w.below(f.min_p > 0.f ? logf(f.min_p) : -22.f);
+    auto clear = [&] {
+        __syncthreads();
+        for (int i = tid; i < BINS; i += THREADS) s.bins[i] = 0;
+        if (tid == 0) s.entries = 0;
+        __syncthreads();
     };
+    // entries of at least `least`, and `in(x, i)`, into the list; their number, which may be more than it holds
+    auto gather = [&](float least, auto in) {
+        row.each([&](int i, float x) {
+            if (x < least || !in(x, i)) return;
+            const int at = atomicAdd(&s.entries, 1);
+            if (at < LIST) s.list[at] = entry_of(key_of(x), i);
+        });
+        __syncthreads();
+        return s.entries;
+    };
+    auto bin_floor = [&](int bin) { return bin < BINS - 1 ? w.below((bin + 1) * (-1.f / 64.f)) : -INFINITY; };
 
     unsigned cut = 0u;                                 // kept: keys above `cut`, and those equal to it up to index `last`
     int last = a.V;
-    if (top_k < a.V) {
-        row.each([&](int, unsigned k) { atomicAdd(&s.bins[bin_of(w.distance(value_of(k)))], 1ull); });
+    if (f.top_k < a.V) {
+        // the last bin takes the far end of the row; it is not counted one by one, at one address, but taken to hold everything
+        row.each([&](int, float x) {
+            const int bin = bin_of(w.distance(x));
+            if (bin < BINS - 1) atomicAdd(&s.bins[bin], 1ull);
+        });
+        if (tid == 0) s.bins[BINS - 1] = (u64)a.V;
         __syncthreads();
         u64 before;
-        const u64 k64 = (u64)top_k;
+        const u64 k64 = (u64)f.top_k;
         const int bin = first_bin(s, [&](u64 v) { return v >= k64; }, &before);
-        const u64 in_list = before + s.bins[bin];
-        if (in_list <= LIST) {
-            row.each([&](int i, unsigned k) {
-                if (bin_of(w.distance(value_of(k))) <= bin) s.list[atomicAdd(&s.entries, 1)] = entry_of(k, i);
-            });
-            __syncthreads();
-            rank_list(s, w, (int)in_list);
-            int n = top_k;
-            if (top_p < 1.f) {
+        if (before + s.bins[bin] <= LIST) {
+            const int n = gather(bin_floor(bin), [&](float x, int) { return bin_of(w.distance(x)) <= bin; });
+            rank_list(s, w, n);
+            int kept = f.top_k;
+            if (f.top_p < 1.f) {
                 u64 v = 0;
-                for (int i = tid; i < n; i += THREADS) v += s.weight[i];
-                n = ranks_to(s, n, 0, (double)top_p * (double)block_sum(s, v));
+                for (int i = tid; i < kept; i += THREADS) v += s.weight[i];
+                kept = ranks_to(s, kept, 0, (double)f.top_p * (double)block_sum(s, v));
             }
-            // the kept ones' indexes and weights, then the draw: whose weight the goal falls on, smaller indexes before it
-            u64 v = 0;
-            for (int i = tid; i < n; i += THREADS) {
-                const u64 e = s.list[s.place[i]];
-                const unsigned m = i == 0 || w.part(entry_key(e)) >= min_p ? s.weight[i] : 0u;
-                s.bins[i] = (u64)(unsigned)entry_index(e) << 32 | m;
-                v += m;
-            }
-            const u64 total = block_sum(s, v), goal = goal_of(total);
-            __syncthreads();
-            for (int i = tid; i < n; i += THREADS) {
-                const u64 me = s.bins[i];
-                u64 sum = 0;
-                for (int j = 0; j < n; ++j) sum += (s.bins[j] >> 32) < (me >> 32) ? (unsigned)s.bins[j] : 0u;
-                if (sum <= goal && goal < sum + (unsigned)me) write((int)(me >> 32), entry_key(s.list[s.place[i]]), total);
-            }
+            draw_from_list(s, w, f, kept, write);
             return;
         }
-        prefix_by_digits(s, row, (double)top_k, [&](int, unsigned) -> u64 { return 1; }, cut, last);
-        __syncthreads();
-        for (int i = tid; i < BINS; i += THREADS) s.bins[i] = 0;
-        __syncthreads();
+        prefix_by_digits(s, row, (double)f.top_k, [&](int, unsigned) -> u64 { return 1; }, cut, last);
+        clear();
     }
-    if (top_p < 1.f) {
+    if (f.top_p < 1.f) {
         const unsigned cut_k = cut;
         const int last_k = last;
-        auto measure = [&](int i, unsigned k) -> u64 { return k > cut_k || (k == cut_k && i <= last_k) ? Weights::weight(w.part(k)) : 0u; };
-        row.each([&](int i, unsigned k) {
-            const float q = w.distance(value_of(k));
-            const unsigned m = k > cut_k || (k == cut_k && i <= last_k) ? Weights::weight(expf(q)) : 0u;
-            if (m) atomicAdd(&s.bins[bin_of(q)], (u64)m);
-        });
+        auto allowed = [&](int i, unsigned k) { return k > cut_k || (k == cut_k && i <= last_k); };
+        auto measure = [&](int i, unsigned k) -> u64 { return allowed(i, k) ? weight_of(w.part(k)) : 0u; };
+        if (cut_k == 0u)
+            row.each([&](int, float x) {
+                const float q = w.distance(x);
+                const unsigned m = weight_of(expf(q));
+                if (m) atomicAdd(&s.bins[bin_of(q)], (u64)m);
+            });
+        else
+            row.each([&](int i, float x) {
+                const u64 m = measure(i, key_of(x));
+                if (m) atomicAdd(&s.bins[bin_of(w.distance(x))], m);
+            });
         __syncthreads();
         u64 all = 0, before;
         for (int i = tid; i < BINS; i += THREADS) all += s.bins[i];
-        const double reach = (double)top_p * (double)block_sum(s, all);
+        const double reach = (double)f.top_p * (double)block_sum(s, all);
         const int bin = first_bin(s, [&](u64 v) { return (double)v >= reach; }, &before);
-        row.each([&](int i, unsigned k) {
-            if (bin_of(w.distance(value_of(k))) == bin && (k > cut_k || (k == cut_k && i <= last_k))) {
-                const int at = atomicAdd(&s.entries, 1);
-                if (at < LIST) s.list[at] = entry_of(k, i);
+        // few kept entries (min_p, or a peaked row): all of them go into the list.  How many they are follows from the bins, whose entries weigh
+        // the same within 1/64.
+        const float least = fmaxf(bin_floor(bin), floor_p);
+        const int last_bin = min(bin, bin_of(w.distance(least)));
+        float many = 0.f;
+        for (int i = tid; i <= last_bin; i += THREADS) many += (float)s.bins[i] * 0x1p-31f * expf((i + 0.5f) * (1.f / 64.f));
+        if (block_sum(s, (u64)(many * 1024.f)) >> 10 < (u64)(SHORT - SHORT / 16)) {
+            const int n = gather(least, [&](float x, int i) { return allowed(i, key_of(x)); });
+            if (n <= LIST) {
+                rank_list(s, w, n);
+                draw_from_list(s, w, f, ranks_to(s, n, 0, reach), write);
+                return;
             }
-        });
-        __syncthreads();
-        const int n = s.entries;
-        if (n <= LIST) {
-            rank_list(s, w, n);
-            const u64 e = s.list[s.place[max(1, ranks_to(s, n, before, reach)) - 1]];
+            __syncthreads();
+            if (tid == 0) s.entries = 0;
+            __syncthreads();
+        }
+        const int m = gather(bin_floor(bin), [&](float x, int i) { return bin_of(w.distance(x)) == bin && allowed(i, key_of(x)); });
+        if (m <= LIST) {
+            rank_list(s, w, m);
+            const u64 e = s.list[s.place[max(1, ranks_to(s, m, before, reach)) - 1]];
             cut = entry_key(e);
             last = entry_index(e);
         } else prefix_by_digits(s, row, reach, measure, cut, last);
     }
     // the draw: sums of the kept weights by the waves' parts, then by threads within the part that the goal falls into
-    const float near = min_p > 0.f ? w.top + w.temperature * (logf(min_p) - 0.01f) : -INFINITY;      // certainly below min_p
-    const unsigned cut_min = max(max(cut, none + 1u), key_of(near));
-    auto kept = [&](int i, unsigned k) -> unsigned {
-        if (k < cut_min || (k == cut && i > last)) return 0u;
+    const float least = fmaxf(value_of(max(cut, none + 1u)), floor_p);
+    auto kept = [&](int i, float x) -> unsigned {
+        if (!(x >= least)) return 0u;
+        const unsigned k = key_of(x);
+        if (k < cut || (k == cut && i > last)) return 0u;
         const float part = w.part(k);
-        return part >= min_p || k == peak ? Weights::weight(part) : 0u;
+        return part >= f.min_p || k == peak ? weight_of(part) : 0u;
     };
     u64 mine = 0;
-    row.each([&](int i, unsigned k) { mine += kept(i, k); });
+    row.each([&](int i, float x) { mine += kept(i, x); });
     const u64 total = block_sum(s, mine);
-    u64 goal = goal_of(total);
+    u64 goal = goal_of(f.u, total);
     int p = 0;
     while (p < WAVES - 1 && s.sums[p] <= goal) goal -= s.sums[p++];
     const int lo = row.part_begin(p), hi = row.part_end(p), each = (hi - lo + THREADS - 1) / THREADS;
     const int b = min(hi, lo + tid * each), e = min(hi, b + each);
     u64 v = 0;
-    for (int i = b; i < e; ++i) v += kept(i, row.key(i));
+    for (int i = b; i < e; ++i) v += kept(i, ld_f32(row.x, i));
     u64 sum = wave_scan(v);
     __syncthreads();
     if (lane == 63) s.sums[wave] = sum;
@@ -394,14 +401,58 @@ template <typename T> __global__ __launch_bounds__(1024) void sample_kernel(Samp
     if (sum > goal && sum - v <= goal) {
         u64 at = sum - v;
         for (int i = b; i < e; ++i) {
-            const unsigned k = row.key(i);
-            at += kept(i, k);
+            const float x = ld_f32(row.x, i);
+            at += kept(i, x);
             if (at > goal) {
-                write(i, k, total);
+                write(i, x, total);
                 break;
             }
         }
     }
+}
+
+template <typename T> __global__ __launch_bounds__(1024) void sample_kernel(SampleArgs a)
+{
+    __shared__ Shared s;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const int64_t r = a.row_lo + blockIdx.x;
+    Row<T> row;
+    row.set((const T *)a.x + r * a.V, a.V);
+    const float temperature = a.temperature ? a.temperature[r] : 1.f;
+    Filters f = {a.top_p ? a.top_p[r] : 1.f, a.min_p ? a.min_p[r] : 0.f, a.u[r], a.top_k ? a.top_k[r] : 0};
+    if (f.top_k <= 0 || f.top_k > a.V) f.top_k = a.V;
+    for (int i = tid; i < BINS; i += THREADS) s.bins[i] = 0;
+    if (tid == 0) s.entries = 0;
+    float top = -INFINITY;
+    row.each([&](int, float x) { top = fmaxf(top, x); });
+    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    if (lane == 0) s.sums[wave] = __float_as_uint(top);
+    __syncthreads();
+    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, __uint_as_float((unsigned)s.sums[w]));
+    top += 0.f;
+    if (top == -INFINITY) {
+        if (tid == 0) {
+            a.tokens[r] = -1;
+            if (a.logp) a.logp[r] = -INFINITY;
+        }
+        return;
+    }
+    if (f.top_k == 1 || !(temperature > 0.f) || !(f.top_p > 0.f) || !(f.min_p <= 1.f)) {       // the first of the largest
+        int first = a.V;
+        row.each([&](int i, float x) { if (x == top) first = min(first, i); });
+        for (int o = 32; o > 0; o >>= 1) first = min(first, __shfl_xor(first, o, 64));
+        __syncthreads();
+        if (lane == 0) s.sums[wave] = first;
+        __syncthreads();
+        if (tid == 0) {
+            for (int w = 0; w < WAVES; ++w) first = min(first, (int)s.sums[w]);
+            a.tokens[r] = first;
+            if (a.logp) a.logp[r] = 0.f;
+        }
+        return;
+    }
+    if (temperature > 1e-18f && temperature < 1e18f && top < INFINITY) sample_row<T, false>(a, s, row, r, top, temperature, f);
+    else sample_row<T, true>(a, s, row, r, top, temperature, f);
 }
 
 LaunchInfo launch_sample(const TokenArgs &a, hipStream_t s, bool dry, int)
