@@ -1,0 +1,84 @@
+// What the attention kernels over a 4-bit cache share: their arguments, the range of keys of some rows, codes as operands of matrix instructions.
+#pragma once
+#include "cache_util.h"
+#include "gemm_util.h"
+#include "kernels.h"
+
+namespace gacer {
+
+struct AttendArgs {
+    const void *x;
+    void *y;
+    float *ws;
+    CacheView c;
+    int b_lo, S, heads, per_kv, window, rows, row_tiles, splits;     // rows: of a row tile
+    float scale;               // alpha * log2(e)
+};
+
+// fewest 64-key tiles of a split, and the tiles of each of `splits` parts of n tiles
+enum { SPLIT_TILES_MIN = 8 };
+__device__ __forceinline__ int split_tiles(int n, int splits) { return max((int)SPLIT_TILES_MIN, (n + splits - 1) / splits); }
+
+// The tiles of 64 keys that rows [r0, r1) of a sequence see, and the first and last of its tokens among them (t1 < t0: none)
+struct Range { int t0, t1, lo, hi; };
+__device__ __forceinline__ Range range_of(const AttendArgs &a, const Span &s, int r0, int r1)
+{
+    Range g;
+    g.t0 = r0 / a.per_kv;
+    g.t1 = min((r1 - 1) / a.per_kv, s.count - 1);
+    g.lo = g.hi = 0;
+    if (g.t1 >= g.t0) {
+        const int first = a.window > 0 ? max(0, s.start + g.t0 - a.window + 1) : 0;
+        const int last = min(s.start + g.t1, (a.c.max_pages << a.c.page_shift) - 1);
+        g.lo = first >> 6;
+        g.hi = max(g.lo, (last >> 6) + 1);
+    }
+    return g;
+}
+
+// eight codes of a word as the bf16 numbers 16 + c
+__device__ __forceinline__ unsigned and_or(unsigned a, unsigned mask, unsigned bits)
+{
+    unsigned r;                                        // one instruction; from plain operators the compiler makes two, each with a literal
+    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "s"(mask), "v"(bits));
+    return r;
+}
+__device__ __forceinline__ bf16x8 codes_above(unsigned w, unsigned sixteen)
+{
+    constexpr unsigned MASK = 0x00780078u;
+    return __builtin_bit_cast(bf16x8, make_uint4(and_or(w << 3, MASK, sixteen), and_or(w >> 1, MASK, sixteen), and_or(w >> 5, MASK, sixteen), and_or(w >> 9, MASK, sixteen)));
+}
+// and as (c - 8) / 16: the hardware's conversion of a signed 4-bit number
+__device__ __forceinline__ bf16x8 codes_around(unsigned w)
+{
+    const unsigned x = w ^ 0x88888888u;
+    unsigned r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const unsigned lo = __float_as_uint(__builtin_amdgcn_cvt_off_f32_i4((int)(x >> (4 * i)))), hi = __float_as_uint(__builtin_amdgcn_cvt_off_f32_i4((int)(x >> (4 * i + 16))));
+        r[i] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+    }
+    return __builtin_bit_cast(bf16x8, make_uint4(r[0], r[1], r[2], r[3]));
+}
+
+__device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+
+// v as a sum of PARTS numbers whose upper 16 bits are bf16, each but the last the largest that does not pass it
+template <int PARTS> __device__ __forceinline__ void split_bf16(float v, unsigned *p)
+{
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) {
+        p[i] = __float_as_uint(v);
+        v -= __uint_as_float(p[i] & 0xFFFF0000u);
+    }
+}
+
+// the reference of a row that has seen no key yet; scores lie above it
+static constexpr float NO_SCORE = -1e38f;
+
+// a branch that stays one (uniform over the wave): as selects, every tile would pay for what only the first and the last need
+#define RARELY(cond) if (cond) if (([] { asm volatile(""); return true; })())
+
+void launch_cache_attention_wide(const AttendArgs &b, int D, int grid, hipStream_t s);      // rows of 128, bf16
+
+}  // namespace gacer

@@ -18,79 +18,10 @@
 // the keys are also cut into splits, joined by a second kernel.
 #include <hip/hip_runtime.h>
 #include <limits.h>
-#include "cache_util.h"
-#include "gemm_util.h"
-#include "kernels.h"
+#include "cache_attention.h"
 #include "tokens_geom.h"
 
 namespace gacer {
-
-struct AttendArgs {
-    const void *x;
-    void *y;
-    float *ws;
-    CacheView c;
-    int b_lo, S, heads, per_kv, window, row_tiles, splits;
-    float scale;               // alpha * log2(e)
-};
-
-// fewest 64-key tiles of a split, and the tiles of each of `splits` parts of n tiles
-enum { SPLIT_TILES_MIN = 8 };
-__device__ __forceinline__ int split_tiles(int n, int splits) { return max((int)SPLIT_TILES_MIN, (n + splits - 1) / splits); }
-
-// The tiles of 64 keys that rows [r0, r1) of a sequence see, and the first and last of its tokens among them (t1 < t0: none)
-struct Range { int t0, t1, lo, hi; };
-__device__ __forceinline__ Range range_of(const AttendArgs &a, const Span &s, int r0, int r1)
-{
-    Range g;
-    g.t0 = r0 / a.per_kv;
-    g.t1 = min((r1 - 1) / a.per_kv, s.count - 1);
-    g.lo = g.hi = 0;
-    if (g.t1 >= g.t0) {
-        const int first = a.window > 0 ? max(0, s.start + g.t0 - a.window + 1) : 0;
-        const int last = min(s.start + g.t1, (a.c.max_pages << a.c.page_shift) - 1);
-        g.lo = first >> 6;
-        g.hi = max(g.lo, (last >> 6) + 1);
-    }
-    return g;
-}
-
-// eight codes of a word as the bf16 numbers 16 + c
-__device__ __forceinline__ unsigned and_or(unsigned a, unsigned mask, unsigned bits)
-{
-    unsigned r;                                        // one instruction; from plain operators the compiler makes two, each with a literal
-    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "s"(mask), "v"(bits));
-    return r;
-}
-__device__ __forceinline__ bf16x8 codes_above(unsigned w, unsigned sixteen)
-{
-    constexpr unsigned MASK = 0x00780078u;
-    return __builtin_bit_cast(bf16x8, make_uint4(and_or(w << 3, MASK, sixteen), and_or(w >> 1, MASK, sixteen), and_or(w >> 5, MASK, sixteen), and_or(w >> 9, MASK, sixteen)));
-}
-// and as (c - 8) / 16: the hardware's conversion of a signed 4-bit number
-__device__ __forceinline__ bf16x8 codes_around(unsigned w)
-{
-    const unsigned x = w ^ 0x88888888u;
-    unsigned r[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const unsigned lo = __float_as_uint(__builtin_amdgcn_cvt_off_f32_i4((int)(x >> (4 * i)))), hi = __float_as_uint(__builtin_amdgcn_cvt_off_f32_i4((int)(x >> (4 * i + 16))));
-        r[i] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
-    }
-    return __builtin_bit_cast(bf16x8, make_uint4(r[0], r[1], r[2], r[3]));
-}
-
-__device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-
-// v as a sum of PARTS numbers whose upper 16 bits are bf16, each but the last the largest that does not pass it
-template <int PARTS> __device__ __forceinline__ void split_bf16(float v, unsigned *p)
-{
-#pragma unroll
-    for (int i = 0; i < PARTS; ++i) {
-        p[i] = __float_as_uint(v);
-        v -= __uint_as_float(p[i] & 0xFFFF0000u);
-    }
-}
 
 // Two blocks of 32 keys and values as loaded: lane & 31 = key of its block (keys, scales) or feature (values), lane >> 5 = half of the group's
 // features (keys) or of the block's keys (values)
@@ -100,12 +31,6 @@ template <int D> struct Tile {
     unsigned ks[2][D / 64], vs[2][D / 64];
     int page[2];
 };
-
-// the reference of a row that has seen no key yet; scores lie above it
-static constexpr float NO_SCORE = -1e38f;
-
-// a branch that stays one (uniform over the wave): as selects, every tile would pay for what only the first and the last need
-#define RARELY(cond) if (cond) if (([] { asm volatile(""); return true; })())
 
 template <typename T, int D, int ROWS, int NW> __global__ __launch_bounds__(NW * 64) void cache_attention_kernel(AttendArgs a)
 {
@@ -407,7 +332,7 @@ template <typename T, int D, int ROWS, int NW> __global__ __launch_bounds__(NW *
 }
 
 // Joins the splits of one row: a workgroup per row, its threads over features and, D at a time, over splits.
-template <typename T, int D, int ROWS> __global__ __launch_bounds__(256) void cache_attention_join_kernel(AttendArgs a)
+template <typename T, int D> __global__ __launch_bounds__(256) void cache_attention_join_kernel(AttendArgs a)
 {
     constexpr int MROW = D + 2, GROUPS = 256 / D;
     __shared__ float acc_s[256], sum_s[GROUPS];
@@ -415,18 +340,18 @@ template <typename T, int D, int ROWS> __global__ __launch_bounds__(256) void ca
     const int h = (int)blockIdx.x % a.heads, g = h / a.per_kv;
     const int64_t bt = (int64_t)blockIdx.x / a.heads;
     const int t = (int)(bt % a.S), b = a.b_lo + (int)(bt / a.S);
-    const int r = t * a.per_kv + (h - g * a.per_kv), rt = r / ROWS, row = r % ROWS, rows = a.S * a.per_kv;
+    const int r = t * a.per_kv + (h - g * a.per_kv), rt = r / a.rows, row = r % a.rows, rows = a.S * a.per_kv;
     const Span span = span_of(a.c, b, a.S);
-    const Range rg = range_of(a, span, rt * ROWS, min(rt * ROWS + ROWS, rows));
+    const Range rg = range_of(a, span, rt * a.rows, min(rt * a.rows + a.rows, rows));
     const int tiles = rg.hi - rg.lo, n = t < span.count && tiles > 0 ? (tiles + split_tiles(tiles, a.splits) - 1) / split_tiles(tiles, a.splits) : 0;
-    const float *ws = a.ws + (((int64_t)b * a.c.kv_heads + g) * a.row_tiles + rt) * a.splits * (ROWS * MROW) + row * MROW;
+    const float *ws = a.ws + (((int64_t)b * a.c.kv_heads + g) * a.row_tiles + rt) * a.splits * (a.rows * MROW) + row * MROW;
     float top = NO_SCORE;
-    for (int i = tid & 63; i < n; i += 64) top = fmaxf(top, ws[(int64_t)i * (ROWS * MROW) + D]);
+    for (int i = tid & 63; i < n; i += 64) top = fmaxf(top, ws[(int64_t)i * (a.rows * MROW) + D]);
     for (int k = 32; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor(top, k, 64));
     float acc = 0.f, sum = 0.f;
 #pragma unroll 4
     for (int i = grp; i < n; i += GROUPS) {
-        const float *w = ws + (int64_t)i * (ROWS * MROW);
+        const float *w = ws + (int64_t)i * (a.rows * MROW);
         const float f = __builtin_amdgcn_exp2f(w[D] - top);
         sum = fmaf(f, w[D + 1], sum);
         acc = fmaf(f, w[d], acc);
@@ -446,8 +371,11 @@ template <typename T, int D, int ROWS> __global__ __launch_bounds__(256) void ca
 
 template <typename T, int D, int ROWS, int NW> static void attend(const AttendArgs &b, int grid, int joins, hipStream_t s, int phase)
 {
-    if (phase != 2) GACER_LAUNCH((cache_attention_kernel<T, D, ROWS, NW>), dim3(grid), dim3(NW * 64), 0, s, b);
-    if (b.splits > 1 && phase != 1) GACER_LAUNCH((cache_attention_join_kernel<T, D, ROWS>), dim3(joins), dim3(256), 0, s, b);
+    if (phase != 2) {
+        if constexpr (ROWS <= 32) GACER_LAUNCH((cache_attention_kernel<T, D, ROWS, NW>), dim3(grid), dim3(NW * 64), 0, s, b);
+        else launch_cache_attention_wide(b, D, grid, s);
+    }
+    if (b.splits > 1 && phase != 1) GACER_LAUNCH((cache_attention_join_kernel<T, D>), dim3(joins), dim3(256), 0, s, b);
 }
 
 LaunchInfo launch_cache_attention(const TokenArgs &a, hipStream_t s, bool dry, int phase)
@@ -455,7 +383,7 @@ LaunchInfo launch_cache_attention(const TokenArgs &a, hipStream_t s, bool dry, i
     const AttendGeom g = attend_geom(a);
     AttendArgs b;
     b.x = a.x; b.y = a.y; b.ws = a.ws; b.c = a.cache; b.b_lo = a.b_lo; b.S = a.S; b.heads = a.heads; b.per_kv = a.heads / a.kv_heads;
-    b.window = a.window; b.row_tiles = g.row_tiles; b.splits = g.splits;
+    b.window = a.window; b.rows = g.rows; b.row_tiles = g.row_tiles; b.splits = g.splits;
     b.scale = a.alpha * 1.4426950408889634f;
     const int n = a.b_hi - a.b_lo, grid = n * a.kv_heads * g.row_tiles * g.splits, joins = n * a.S * a.heads;
     LaunchInfo li;
@@ -466,8 +394,8 @@ LaunchInfo launch_cache_attention(const TokenArgs &a, hipStream_t s, bool dry, i
     if (dry || !grid) return li;
 #define ATTEND(TYPE, DIM, ROWS, NW) if (a.D == DIM && g.rows == ROWS && g.waves == NW) attend<TYPE, DIM, ROWS, NW>(b, grid, joins, s, phase)
     if (a.dtype == DT_BF16) {
-        ATTEND(unsigned short, 64, 8, 8); ATTEND(unsigned short, 64, 16, 4); ATTEND(unsigned short, 64, 32, 4);
-        ATTEND(unsigned short, 128, 8, 8); ATTEND(unsigned short, 128, 16, 4); ATTEND(unsigned short, 128, 32, 4);
+        ATTEND(unsigned short, 64, 8, 8); ATTEND(unsigned short, 64, 16, 4); ATTEND(unsigned short, 64, 32, 4); ATTEND(unsigned short, 64, 128, 4);
+        ATTEND(unsigned short, 128, 8, 8); ATTEND(unsigned short, 128, 16, 4); ATTEND(unsigned short, 128, 32, 4); ATTEND(unsigned short, 128, 128, 4);
     } else {
         ATTEND(float, 64, 8, 4); ATTEND(float, 64, 16, 4); ATTEND(float, 64, 32, 4);
         ATTEND(float, 128, 8, 4); ATTEND(float, 128, 16, 4); ATTEND(float, 128, 32, 4);

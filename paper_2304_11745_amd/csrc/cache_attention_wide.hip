@@ -1,0 +1,303 @@
+// Attention of many rows (prompts) over a paged 4-bit cache, bf16.
+//
+// A workgroup takes 128 rows (heads x tokens of one key/value head), 32 to a wave, and 64 keys at a time.  The codes are turned into bf16 once
+// for all four waves and stand in LDS as the whole numbers c - 8: keys row by row, values feature by feature.  Scores are keys x rows (lane =
+// row), so a row's weights stay in its lanes' registers and are the operand of the values' product, features x rows, as they are; the
+// order of the keys within that product is the one in which a lane holds them, and the values are stored in it.  As in the kernel for
+// few rows the scales are applied in fp32,
+//   q.k_j = sum over groups g of  s_jg * (sum_d q_d (c_jd - 8)) + (m_jg + 8 s_jg) * sum_d q_d
+//   out_d = sum_j (p_j s_jg) (c_jd - 8) + sum_j p_j (m_jg + 8 s_jg)
+// with the second sums as further matrix instructions: the pair (s, m) of a key, two bf16 numbers, times the sums of the queries in three bf16
+// parts, and the weights times m + 8 s in two.  The weights p_j s_jg are rounded to bf16 once: with codes around zero that is as
+// much as the result's own rounding adds (2.3e-3 of the result together, 1.7e-3 for the latter alone), and a second part would be
+// 16 more matrix instructions per 64 keys and two more operations per weight.
+#include <hip/hip_runtime.h>
+#include <limits.h>
+#include "cache_attention.h"
+
+namespace gacer {
+
+template <int D> __global__ __launch_bounds__(256, 2) void cache_attention_wide_kernel(AttendArgs a)
+{
+    constexpr int NG = D / 64, ROWS = 128, KROW = D * 2 + 16, VROW = 128 + 16, KROWS = 64 * KROW, VROWS = D * VROW;
+    constexpr int EXT_K = 64 * 32, EXT_V = 2 * NG * VROW, SCALES = 2 * NG * 64 * 4, BUF = KROWS + VROWS + EXT_K + EXT_V + SCALES;
+    constexpr int ITEMS = 64 * D / 32;                 // 16-byte pieces of a tile's key codes, and of its value codes
+    __shared__ __align__(16) unsigned char lds[2 * BUF];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
+    // last rows first: they see the most keys; neighbours in the grid, which run on different XCDs, are different heads
+    const int groups = (int)gridDim.x / a.row_tiles / a.splits, zs = (int)blockIdx.x % (groups * a.splits), z = zs % groups, sp = zs / groups;
+    const int rt = a.row_tiles - 1 - (int)blockIdx.x / (groups * a.splits), g = z % a.c.kv_heads, b = a.b_lo + z / a.c.kv_heads;
+    const int rows = a.S * a.per_kv, r0 = rt * ROWS;
+    const Span span = span_of(a.c, b, a.S);
+    const Range rg = range_of(a, span, r0, min(r0 + ROWS, rows));
+    int lo = rg.lo, hi = rg.hi;
+    if (a.splits > 1) {
+        const int n = split_tiles(rg.hi - rg.lo, a.splits);
+        lo = rg.lo + sp * n;
+        hi = min(rg.hi, lo + n);
+        if (lo >= hi) return;
+    }
+    const int r = r0 + wave * 32 + l32, t = r / a.per_kv, head = g * a.per_kv + (r - t * a.per_kv);
+    const int at = r < rows && t < span.count ? span.start + t : -1;
+    // what the wave's rows see: every row all of [all_lo, all_hi), none anything outside [any_lo, any_hi)
+    const int w0 = r0 + wave * 32, w1 = min(w0 + 32, rows), t0 = w0 / a.per_kv, t1 = min((w1 - 1) / a.per_kv, span.count - 1);
+    const bool idle = w0 >= rows || t0 > t1;
+    const int all_lo = a.window > 0 ? span.start + t1 - a.window + 1 : 0, all_hi = span.start + t0 + 1;
+    const int any_lo = a.window > 0 ? span.start + t0 - a.window + 1 : 0, any_hi = span.start + t1 + 1;
+
+    // -- a tile's codes and scales: loaded into registers, later turned into operands in LDS -------------------------------------------
+    int pages = -1, pages_at = INT_MIN / 2;            // lane i: page of block pages_at + i
+    uint4 kin, vin;
+    unsigned sin[NG];
+    int page_in[2], page_now[2];
+    const bool k_mine = tid < ITEMS, v_mine = ITEMS == 256 || tid >= 256 - ITEMS, s_mine = tid < 128;
+    const int ki = tid & (ITEMS - 1), kkey = ki / (D / 32), kpart = ki % (D / 32), vblk = ki / D, vd = ki % D, skey = tid & 63;
+    auto load = [&](int tile) {
+        const int blk = tile * 2;
+        if (blk - pages_at >= 64 || blk < pages_at) {
+            pages_at = blk;
+            pages = page_of(a.c, b, min(blk + lane, 1 << 25) << 5);
+        }
+        int64_t row[2];
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            page_in[m] = __builtin_amdgcn_readlane(pages, blk - pages_at + m);
+            row[m] = page_row(a.c, max(page_in[m], 0), g) + (((blk + m) << 5) & ((1 << a.c.page_shift) - 1));
+        }
+        kin = *(const uint4 *)(a.c.k_codes + ((kkey >> 5 ? row[1] : row[0]) + (kkey & 31)) * (D / 2) + kpart * 16);
+        vin = *(const uint4 *)(a.c.v_codes + (vblk ? row[1] : row[0]) * (D / 2) + vd * 16);
+        const unsigned *sc = (tid & 64 ? a.c.v_scales : a.c.k_scales) + ((skey >> 5 ? row[1] : row[0]) + (skey & 31)) * NG;
+#pragma unroll
+        for (int i = 0; i < NG; ++i) sin[i] = sc[i];
+    };
+    auto unpack = [&](unsigned char *buf) {
+        if (k_mine) {
+            const unsigned w[4] = {kin.x, kin.y, kin.z, kin.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) *(bf16x8 *)(buf + kkey * KROW + kpart * 64 + i * 16) = codes_around(w[i]);
+        }
+        if (v_mine) {                                  // of each 16 keys first those that half 0 of a wave holds: 0..3 and 8..11, then 4..7 and 12..15
+            const unsigned w[4] = {vin.x, vin.y, vin.z, vin.w};
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint4 p = __builtin_bit_cast(uint4, codes_around(w[2 * i])), q = __builtin_bit_cast(uint4, codes_around(w[2 * i + 1]));
+                unsigned char *v = buf + KROWS + vd * VROW + (vblk * 2 + i) * 32;
+                *(uint4 *)v = make_uint4(p.x, p.y, q.x, q.y);
+                *(uint4 *)(v + 16) = make_uint4(p.z, p.w, q.z, q.w);
+            }
+        }
+        if (s_mine) {
+            float *scales = (float *)(buf + KROWS + VROWS + EXT_K + EXT_V);
+            const int slot = (skey & 32) + (skey & 16) + ((skey >> 2) & 1) * 8 + ((skey >> 3) & 1) * 4 + (skey & 3);        // as the values' keys
+            unsigned e[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int i = 0; i < NG; ++i) {
+                const float sc = scale_of(sin[i]), m = minimum_of(sin[i]);
+                if (tid < 64) {
+                    scales[i * 64 + skey] = sc * 16.f * a.scale;
+                    e[i] = sin[i];
+                } else {
+                    scales[(NG + i) * 64 + skey] = sc * 16.f;
+                    const float mm = fmaf(8.f, sc, m);
+                    const unsigned short hi16 = f32_to_bf16(mm), lo16 = f32_to_bf16(mm - bf16_to_f32(hi16));
+                    unsigned char *x = buf + KROWS + VROWS + EXT_K + 2 * i * VROW + slot * 2;
+                    *(unsigned short *)x = hi16;
+                    *(unsigned short *)(x + VROW) = lo16;
+                }
+            }
+            if (tid < 64) {                            // slots 0..7: the pairs of the groups, twice; 8..15: once more and zeros
+                unsigned char *x = buf + KROWS + VROWS + skey * 32;
+                *(uint4 *)x = NG == 2 ? make_uint4(e[0], e[1], e[0], e[1]) : make_uint4(e[0], e[0], e[0], 0u);
+                *(uint4 *)(x + 16) = NG == 2 ? make_uint4(e[0], e[1], 0u, 0u) : make_uint4(0u, 0u, 0u, 0u);
+            }
+        }
+    };
+    if (lo < hi) load(lo);
+
+    // -- queries: lane & 31 = row; features 16 t + 8 half .. of step t, and the sums of each group as the operand of the pairs -----------
+    bf16x8 q[NG * 4], qx;
+    {
+        const bool on = r < rows;
+        const unsigned short *x = (const unsigned short *)a.x + ((int64_t)b * a.S + (on ? t : 0)) * (a.heads + 2 * a.c.kv_heads) * D + (on ? head : 0) * D + half * 8;
+        float sum[NG];
+#pragma unroll
+        for (int i = 0; i < NG; ++i) sum[i] = 0.f;
+#pragma unroll
+        for (int i = 0; i < NG * 4; ++i) {
+            const uint4 raw = *(const uint4 *)(x + i * 16);
+            q[i] = __builtin_bit_cast(bf16x8, on ? raw : make_uint4(0u, 0u, 0u, 0u));
+            float v[8];
+            load8((const unsigned short *)&q[i], v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[i / 4] += v[e];
+        }
+        unsigned pair[NG][3];                          // parts of (8 sum, sum) of each group, as they meet (scale, minimum)
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+            const float all = (sum[i] + __shfl_xor(sum[i], 32, 64)) * a.scale;
+            unsigned p8[3], p1[3];
+            split_bf16<3>(8.f * all, p8);
+            split_bf16<3>(all, p1);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) pair[i][k] = __builtin_amdgcn_perm(p1[k], p8[k], 0x07060302u);
+        }
+        const uint4 first = NG == 2 ? make_uint4(pair[0][0], pair[NG - 1][0], pair[0][1], pair[NG - 1][1]) : make_uint4(pair[0][0], pair[0][1], pair[0][2], 0u);
+        const uint4 second = NG == 2 ? make_uint4(pair[0][2], pair[NG - 1][2], 0u, 0u) : make_uint4(0u, 0u, 0u, 0u);
+        qx = __builtin_bit_cast(bf16x8, half ? second : first);
+    }
+    const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    f32x16 o[D / 32], corr = zero;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) o[c] = zero;
+    float base = NO_SCORE, l = 0.f;
+
+    // -- 32 keys of a tile: scores, weights, their product with the values ------------------------------------------------------------
+    auto block = [&](const unsigned char *buf, int m, int p0, bool edge, bool gone) {
+        f32x16 d[NG], x;
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+            d[i] = zero;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) d[i] = mfma(*(const bf16x8 *)(buf + (m * 32 + l32) * KROW + (i * 4 + j) * 32 + half * 16), q[i * 4 + j], d[i]);
+        }
+        x = mfma(*(const bf16x8 *)(buf + KROWS + VROWS + (m * 32 + l32) * 32 + half * 16), qx, zero);
+        const float *scales = (const float *)(buf + KROWS + VROWS + EXT_K + EXT_V) + m * 32 + half * 4;
+        float s[16], top = NO_SCORE;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float4 sc[NG];
+#pragma unroll
+            for (int i = 0; i < NG; ++i) sc[i] = *(const float4 *)(scales + i * 64 + k * 8);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float v = x[4 * k + e];
+#pragma unroll
+                for (int i = 0; i < NG; ++i) v = fmaf(e == 0 ? sc[i].x : e == 1 ? sc[i].y : e == 2 ? sc[i].z : sc[i].w, d[i][4 * k + e], v);
+                s[4 * k + e] = v;
+            }
+        }
+        RARELY(edge) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int p = p0 + 8 * (e >> 2) + 4 * half + (e & 3);
+                if (gone || p > at || (a.window > 0 && p <= at - a.window)) s[e] = -INFINITY;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[e]);
+        RARELY(__any(top - base > 8.f)) {              // the largest score so far becomes the reference
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            top = fmaxf(top, base);
+            const float f = __builtin_amdgcn_exp2f(base - top);
+            base = top;
+            l *= f;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                corr[e] *= f;
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) o[c][e] *= f;
+            }
+        }
+        float p[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            p[e] = __builtin_amdgcn_exp2f(s[e] - base);
+            l += p[e];
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {                  // 16 keys
+            uint4 w[NG], wp;
+#pragma unroll
+            for (int i = 0; i < NG; ++i) {
+                const float4 s0 = *(const float4 *)(scales + (NG + i) * 64 + k * 16), s1 = *(const float4 *)(scales + (NG + i) * 64 + k * 16 + 8);
+                float v[8] = {p[8 * k] * s0.x, p[8 * k + 1] * s0.y, p[8 * k + 2] * s0.z, p[8 * k + 3] * s0.w,
+                              p[8 * k + 4] * s1.x, p[8 * k + 5] * s1.y, p[8 * k + 6] * s1.z, p[8 * k + 7] * s1.w};
+                RARELY(edge) {                         // whatever the scales of a key that is not seen hold
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (s[8 * k + e] == -INFINITY) v[e] = 0.f;
+                }
+                w[i] = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+            }
+            wp = make_uint4(pack_bf16(p[8 * k], p[8 * k + 1]), pack_bf16(p[8 * k + 2], p[8 * k + 3]), pack_bf16(p[8 * k + 4], p[8 * k + 5]), pack_bf16(p[8 * k + 6], p[8 * k + 7]));
+            const int at_key = (m * 2 + k) * 32 + half * 16;
+            bf16x8 mx = *(const bf16x8 *)(buf + KROWS + VROWS + EXT_K + min(l32, 2 * NG - 1) * VROW + at_key);
+            RARELY(edge) {                             // the same for their minima: an operand that holds no NaN
+                uint4 u = __builtin_bit_cast(uint4, mx);
+                unsigned *e = (unsigned *)&u;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if ((e[i] & 0x7F80u) == 0x7F80u) e[i] &= 0xFFFF0000u;
+                    if ((e[i] & 0x7F800000u) == 0x7F800000u) e[i] &= 0xFFFFu;
+                }
+                mx = __builtin_bit_cast(bf16x8, u);
+            }
+            corr = mfma(mx, __builtin_bit_cast(bf16x8, wp), corr);
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c)
+                o[c] = mfma(*(const bf16x8 *)(buf + KROWS + (c * 32 + l32) * VROW + at_key), __builtin_bit_cast(bf16x8, w[c / 2]), o[c]);
+        }
+        mfma_settle<DT_BF16>();
+    };
+    for (int tile = lo; tile < hi; ++tile) {
+        unsigned char *buf = lds + ((tile - lo) & 1) * BUF;
+        unpack(buf);
+        page_now[0] = page_in[0];
+        page_now[1] = page_in[1];
+        __syncthreads();
+        load(min(tile + 1, hi - 1));
+        if (idle) continue;
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const int p0 = tile * 64 + m * 32;
+            if (p0 >= any_hi || p0 + 32 <= any_lo) continue;
+            const bool gone = page_now[m] < 0;
+            block(buf, m, p0, gone || p0 < all_lo || p0 + 32 > all_hi, gone);
+        }
+    }
+
+    l += __shfl_xor(l, 32, 64);
+    float cr[NG];                                      // the minima's part of the result, rows 0..3 of the product: in lanes of half 0
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+        const float v = corr[2 * i] + corr[2 * i + 1], other = __shfl_xor(v, 32, 64);
+        cr[i] = half ? other : v;
+    }
+    if (r >= rows) return;
+    if (a.splits > 1) {
+        float *ws = a.ws + ((((int64_t)b * a.c.kv_heads + g) * a.row_tiles + rt) * a.splits + sp) * (ROWS * (D + 2)) + (r - r0) * (D + 2);
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                float *y = ws + c * 32 + k * 8 + half * 4;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = o[c][4 * k + e] + cr[c / 2];
+            }
+        if (!half) {
+            ws[D] = base;
+            ws[D + 1] = l;
+        }
+        return;
+    }
+    const bool seen = at >= 0 && l != 0.f;
+    const float inv = 1.f / l;
+    unsigned short *y = (unsigned short *)a.y + (((int64_t)b * a.S + t) * a.heads + head) * D + half * 4;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = seen ? (o[c][4 * k + e] + cr[c / 2]) * inv : 0.f;
+            *(uint2 *)(y + c * 32 + k * 8) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+        }
+}
+
+void launch_cache_attention_wide(const AttendArgs &b, int D, int grid, hipStream_t s)
+{
+    if (D == 64) GACER_LAUNCH(cache_attention_wide_kernel<64>, dim3(grid), dim3(256), 0, s, b);
+    else GACER_LAUNCH(cache_attention_wide_kernel<128>, dim3(grid), dim3(256), 0, s, b);
+}
+
+}  // namespace gacer

@@ -13,7 +13,7 @@ inline AttendGeom attend_geom(const TokenArgs &a)
 {
     AttendGeom g;
     const int64_t all = (int64_t)a.S * (a.heads / a.kv_heads);
-    g.rows = all <= 8 ? 8 : all <= 16 ? 16 : 32;
+    g.rows = all <= 8 ? 8 : all <= 16 ? 16 : all < 128 || a.dtype != DT_BF16 ? 32 : 128;
     g.waves = g.rows == 8 && a.dtype == DT_BF16 ? 8 : 4;
     g.row_tiles = (int)((all + g.rows - 1) / g.rows);
     const int64_t groups = (int64_t)a.batch * a.kv_heads * g.row_tiles;
