@@ -11,13 +11,12 @@ struct AttendArgs {
     void *y;
     float *ws;
     CacheView c;
-    int b_lo, S, heads, per_kv, window, rows, row_tiles, splits;     // rows: of a row tile
+    int b_lo, S, heads, per_kv, window, rows, row_tiles, splits, split_min;      // rows: of a row tile; split_min: fewest tiles of 64 keys in a split
     float scale;               // alpha * log2(e)
 };
 
-// fewest 64-key tiles of a split, and the tiles of each of `splits` parts of n tiles
-enum { SPLIT_TILES_MIN = 8 };
-__device__ __forceinline__ int split_tiles(int n, int splits) { return max((int)SPLIT_TILES_MIN, (n + splits - 1) / splits); }
+// the tiles of each split of n tiles
+__device__ __forceinline__ int split_tiles(const AttendArgs &a, int n) { return max(a.split_min, (n + a.splits - 1) / a.splits); }
 
 // The tiles of 64 keys that rows [r0, r1) of a sequence see, and the first and last of its tokens among them (t1 < t0: none)
 struct Range { int t0, t1, lo, hi; };
@@ -79,6 +78,6 @@ static constexpr float NO_SCORE = -1e38f;
 // a branch that stays one (uniform over the wave): as selects, every tile would pay for what only the first and the last need
 #define RARELY(cond) if (cond) if (([] { asm volatile(""); return true; })())
 
-void launch_cache_attention_wide(const AttendArgs &b, int D, int grid, hipStream_t s);      // rows of 128, bf16
+void launch_cache_attention_wide(const AttendArgs &b, int dtype, int D, int grid, hipStream_t s);      // rows of 128
 
 }  // namespace gacer

@@ -50,7 +50,7 @@ template <typename T, int D, int ROWS, int NW> __global__ __launch_bounds__(NW *
     const Range rg = range_of(a, span, r0, min(r0 + ROWS, rows));
     int lo = rg.lo, hi = rg.hi;
     if (a.splits > 1) {
-        const int n = split_tiles(rg.hi - rg.lo, a.splits);
+        const int n = split_tiles(a, rg.hi - rg.lo);
         lo = rg.lo + sp * n;
         hi = min(rg.hi, lo + n);
         if (lo >= hi) return;
@@ -318,12 +318,9 @@ template <typename T, int D, int ROWS, int NW> __global__ __launch_bounds__(NW *
             acc = fmaf(f, m[d], acc);
         }
         if (a.splits > 1) {
-            float *ws = a.ws + ((((int64_t)b * a.c.kv_heads + g) * a.row_tiles + rt) * a.splits + sp) * (ROWS * MROW) + row * MROW;
-            ws[d] = acc;
-            if (d == 0) {
-                ws[D] = top;
-                ws[D + 1] = sum;
-            }
+            float *ws = a.ws + ((((int64_t)b * a.c.kv_heads + g) * a.row_tiles + rt) * a.splits + sp) * (ROWS * (D + 2));
+            ws[i] = acc;
+            if (d == 0) *(float2 *)(ws + ROWS * D + row * 2) = make_float2(top, sum);
         } else if (r < rows) {
             const bool on = t < span.count && sum != 0.f;
             st_f32((T *)a.y, (((int64_t)b * a.S + t) * a.heads + g * a.per_kv + (r - t * a.per_kv)) * D + d, on ? acc / sum : 0.f);
@@ -331,51 +328,63 @@ template <typename T, int D, int ROWS, int NW> __global__ __launch_bounds__(NW *
     }
 }
 
-// Joins the splits of one row: a workgroup per row, its threads over features and, D at a time, over splits.
-template <typename T, int D> __global__ __launch_bounds__(256) void cache_attention_join_kernel(AttendArgs a)
+// Joins the splits: D / 4 lanes to a row, and GROUPS of them where there are many splits, each over every GROUPS-th.  A split holds its rows'
+// sums [rows][D], relative to their references, then [rows][reference, sum of the weights].
+template <typename T, int D, int GROUPS> __global__ __launch_bounds__(256) void cache_attention_join_kernel(AttendArgs a, int64_t outputs)
 {
-    constexpr int MROW = D + 2, GROUPS = 256 / D;
-    __shared__ float acc_s[256], sum_s[GROUPS];
-    const int tid = threadIdx.x, d = tid % D, grp = tid / D;
-    const int h = (int)blockIdx.x % a.heads, g = h / a.per_kv;
-    const int64_t bt = (int64_t)blockIdx.x / a.heads;
-    const int t = (int)(bt % a.S), b = a.b_lo + (int)(bt / a.S);
-    const int r = t * a.per_kv + (h - g * a.per_kv), rt = r / a.rows, row = r % a.rows, rows = a.S * a.per_kv;
-    const Span span = span_of(a.c, b, a.S);
-    const Range rg = range_of(a, span, rt * a.rows, min(rt * a.rows + a.rows, rows));
-    const int tiles = rg.hi - rg.lo, n = t < span.count && tiles > 0 ? (tiles + split_tiles(tiles, a.splits) - 1) / split_tiles(tiles, a.splits) : 0;
-    const float *ws = a.ws + (((int64_t)b * a.c.kv_heads + g) * a.row_tiles + rt) * a.splits * (a.rows * MROW) + row * MROW;
-    float top = NO_SCORE;
-    for (int i = tid & 63; i < n; i += 64) top = fmaxf(top, ws[(int64_t)i * (a.rows * MROW) + D]);
-    for (int k = 32; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor(top, k, 64));
-    float acc = 0.f, sum = 0.f;
-#pragma unroll 4
-    for (int i = grp; i < n; i += GROUPS) {
-        const float *w = ws + (int64_t)i * (a.rows * MROW);
-        const float f = __builtin_amdgcn_exp2f(w[D] - top);
-        sum = fmaf(f, w[D + 1], sum);
-        acc = fmaf(f, w[d], acc);
+    constexpr int LANES = D / 4, ROWS = 256 / (LANES * GROUPS);                // rows of a workgroup
+    __shared__ float4 acc_s[GROUPS > 1 ? 256 : 1];
+    __shared__ float2 ml_s[GROUPS > 1 ? GROUPS : 1];
+    const int tid = threadIdx.x, lane = tid % LANES, grp = tid / LANES % GROUPS;
+    const int64_t out = (int64_t)blockIdx.x * ROWS + tid / (LANES * GROUPS);   // (sequence, token, head), counted from the first sequence of the call
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float top = NO_SCORE, sum = 0.f;
+    auto add = [&](float m, float l, const float4 &v) {
+        const float now = fmaxf(top, m), f0 = __builtin_amdgcn_exp2f(top - now), f1 = __builtin_amdgcn_exp2f(m - now);
+        top = now;
+        sum = fmaf(sum, f0, l * f1);
+        acc = make_float4(fmaf(acc.x, f0, v.x * f1), fmaf(acc.y, f0, v.y * f1), fmaf(acc.z, f0, v.z * f1), fmaf(acc.w, f0, v.w * f1));
+    };
+    if (out < outputs) {
+        const int h = (int)(out % a.heads), g = h / a.per_kv;
+        const int t = (int)(out / a.heads % a.S), b = a.b_lo + (int)(out / a.heads / a.S);
+        const int r = t * a.per_kv + (h - g * a.per_kv), rt = r / a.rows, row = r - rt * a.rows;
+        const Span span = span_of(a.c, b, a.S);
+        const Range rg = range_of(a, span, rt * a.rows, min(rt * a.rows + a.rows, a.S * a.per_kv));
+        const int tiles = rg.hi - rg.lo, per = split_tiles(a, tiles), n = t < span.count && tiles > 0 ? (tiles + per - 1) / per : 0;
+        const int64_t step = (int64_t)a.rows * (D + 2);
+        const float *ws = a.ws + (((int64_t)b * a.c.kv_heads + g) * a.row_tiles + rt) * a.splits * step;
+#pragma unroll 8
+        for (int i = grp; i < n; i += GROUPS) {
+            const float *x = ws + i * step;
+            const float2 ml = *(const float2 *)(x + a.rows * D + row * 2);
+            add(ml.x, ml.y, *(const float4 *)(x + row * D + lane * 4));
+        }
     }
-    acc_s[tid] = acc;
-    if (d == 0) sum_s[grp] = sum;
-    __syncthreads();
-    if (grp) return;
-    sum = 0.f;
-    acc = 0.f;
-    for (int i = 0; i < GROUPS; ++i) {
-        sum += sum_s[i];
-        acc += acc_s[i * D + d];
+    if constexpr (GROUPS > 1) {
+        acc_s[tid] = acc;
+        if (lane == 0) ml_s[grp] = make_float2(top, sum);
+        __syncthreads();
+        if (grp) return;
+#pragma unroll
+        for (int i = 1; i < GROUPS; ++i) add(ml_s[i].x, ml_s[i].y, acc_s[i * LANES + lane]);
     }
-    st_f32((T *)a.y, (bt + (int64_t)a.b_lo * a.S) * a.heads * D + h * D + d, sum != 0.f ? acc / sum : 0.f);
+    if (out >= outputs) return;
+    const float inv = sum != 0.f ? 1.f / sum : 0.f;
+    const float v[4] = {acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv};
+    store_vec4((T *)a.y + (out + (int64_t)a.b_lo * a.S * a.heads) * D + lane * 4, v);
 }
 
-template <typename T, int D, int ROWS, int NW> static void attend(const AttendArgs &b, int grid, int joins, hipStream_t s, int phase)
+template <typename T, int D, int ROWS, int NW> static void attend(const AttendArgs &b, int grid, int64_t outputs, hipStream_t s, int phase)
 {
     if (phase != 2) {
         if constexpr (ROWS <= 32) GACER_LAUNCH((cache_attention_kernel<T, D, ROWS, NW>), dim3(grid), dim3(NW * 64), 0, s, b);
-        else launch_cache_attention_wide(b, D, grid, s);
+        else launch_cache_attention_wide(b, sizeof(T) == 4 ? DT_F32 : DT_BF16, D, grid, s);
     }
-    if (b.splits > 1 && phase != 1) GACER_LAUNCH((cache_attention_join_kernel<T, D>), dim3(joins), dim3(256), 0, s, b);
+    if (b.splits > 1 && phase != 1) {
+        if (b.splits > 8) GACER_LAUNCH((cache_attention_join_kernel<T, D, 1024 / D>), dim3((unsigned)outputs), dim3(256), 0, s, b, outputs);
+        else GACER_LAUNCH((cache_attention_join_kernel<T, D, 1>), dim3((unsigned)((outputs + 1024 / D - 1) / (1024 / D))), dim3(256), 0, s, b, outputs);
+    }
 }
 
 LaunchInfo launch_cache_attention(const TokenArgs &a, hipStream_t s, bool dry, int phase)
@@ -383,22 +392,23 @@ LaunchInfo launch_cache_attention(const TokenArgs &a, hipStream_t s, bool dry, i
     const AttendGeom g = attend_geom(a);
     AttendArgs b;
     b.x = a.x; b.y = a.y; b.ws = a.ws; b.c = a.cache; b.b_lo = a.b_lo; b.S = a.S; b.heads = a.heads; b.per_kv = a.heads / a.kv_heads;
-    b.window = a.window; b.rows = g.rows; b.row_tiles = g.row_tiles; b.splits = g.splits;
+    b.window = a.window; b.rows = g.rows; b.row_tiles = g.row_tiles; b.splits = g.splits; b.split_min = g.split_min;
     b.scale = a.alpha * 1.4426950408889634f;
-    const int n = a.b_hi - a.b_lo, grid = n * a.kv_heads * g.row_tiles * g.splits, joins = n * a.S * a.heads;
+    const int n = a.b_hi - a.b_lo, grid = n * a.kv_heads * g.row_tiles * g.splits;
+    const int64_t outputs = (int64_t)n * a.S * a.heads;
     LaunchInfo li;
-    li.workgroups = phase == 2 ? joins : grid;
+    li.workgroups = phase == 2 ? (int)(b.splits > 8 ? outputs : (outputs * a.D + 1023) / 1024) : grid;
     li.threads = phase == 2 ? 256 : g.waves * 64; li.lds_bytes = g.waves * g.rows * (a.D + 2) * 4; li.wg_per_cu = phase == 2 ? 8 : 8 / g.waves;
     li.kernel = phase == 2 ? "cache_attention_join" : a.dtype == DT_BF16 ? "cache_attention_bf16" : "cache_attention_f32";
     li.phases = g.splits > 1 ? 2 : 1;
     if (dry || !grid) return li;
-#define ATTEND(TYPE, DIM, ROWS, NW) if (a.D == DIM && g.rows == ROWS && g.waves == NW) attend<TYPE, DIM, ROWS, NW>(b, grid, joins, s, phase)
+#define ATTEND(TYPE, DIM, ROWS, NW) if (a.D == DIM && g.rows == ROWS && g.waves == NW) attend<TYPE, DIM, ROWS, NW>(b, grid, outputs, s, phase)
     if (a.dtype == DT_BF16) {
         ATTEND(unsigned short, 64, 8, 8); ATTEND(unsigned short, 64, 16, 4); ATTEND(unsigned short, 64, 32, 4); ATTEND(unsigned short, 64, 128, 4);
         ATTEND(unsigned short, 128, 8, 8); ATTEND(unsigned short, 128, 16, 4); ATTEND(unsigned short, 128, 32, 4); ATTEND(unsigned short, 128, 128, 4);
     } else {
-        ATTEND(float, 64, 8, 4); ATTEND(float, 64, 16, 4); ATTEND(float, 64, 32, 4);
-        ATTEND(float, 128, 8, 4); ATTEND(float, 128, 16, 4); ATTEND(float, 128, 32, 4);
+        ATTEND(float, 64, 8, 4); ATTEND(float, 64, 16, 4); ATTEND(float, 64, 32, 4); ATTEND(float, 64, 128, 4);
+        ATTEND(float, 128, 8, 4); ATTEND(float, 128, 16, 4); ATTEND(float, 128, 32, 4); ATTEND(float, 128, 128, 4);
     }
 #undef ATTEND
     return li;

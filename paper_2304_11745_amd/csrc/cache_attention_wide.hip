@@ -1,4 +1,4 @@
-// Attention of many rows (prompts) over a paged 4-bit cache, bf16.
+// Attention of many rows (prompts) over a paged 4-bit cache.
 //
 // A workgroup takes 128 rows (heads x tokens of one key/value head), 32 to a wave, and 64 keys at a time.  The codes are turned into bf16 once
 // for all four waves and stand in LDS as the whole numbers c - 8: keys row by row, values feature by feature.  Scores are keys x rows (lane =
@@ -7,9 +7,10 @@
 // few rows the scales are applied in fp32,
 //   q.k_j = sum over groups g of  s_jg * (sum_d q_d (c_jd - 8)) + (m_jg + 8 s_jg) * sum_d q_d
 //   out_d = sum_j (p_j s_jg) (c_jd - 8) + sum_j p_j (m_jg + 8 s_jg)
-// with the second sums as further matrix instructions: the pair (s, m) of a key, two bf16 numbers, times the sums of the queries in three bf16
-// parts, and the weights times m + 8 s in two.  The weights p_j s_jg are rounded to bf16 once: with codes around zero that is as
-// much as the result's own rounding adds (2.3e-3 of the result together, 1.7e-3 for the latter alone), and a second part would be
+// with the second sum of the scores as a further matrix instruction: the pair (s, m) of a key, two bf16 numbers, times the sums of the queries in
+// three bf16 parts; that of the result likewise in bf16 tenants, the weights times m + 8 s in two parts.  fp32 tenants have their queries and
+// weights in three bf16 parts each, every part a matrix instruction, and add p_j (m + 8 s) as it is.  In bf16 tenants the weights p_j s_jg are rounded to bf16 once: with codes around zero that is as
+// much as the result's own rounding adds (2.2e-3 of the result together, 1.7e-3 for the latter alone), and a second part would be
 // 16 more matrix instructions per 64 keys and two more operations per weight.
 #include <hip/hip_runtime.h>
 #include <limits.h>
@@ -17,10 +18,32 @@
 
 namespace gacer {
 
-template <int D> __global__ __launch_bounds__(256, 2) void cache_attention_wide_kernel(AttendArgs a)
+// eight numbers whose upper 16 bits are bf16, as an operand
+__device__ __forceinline__ bf16x8 operand(unsigned a, unsigned b, unsigned c, unsigned d, unsigned e, unsigned f, unsigned g, unsigned h)
 {
+    return __builtin_bit_cast(bf16x8, make_uint4(__builtin_amdgcn_perm(b, a, 0x07060302u), __builtin_amdgcn_perm(d, c, 0x07060302u),
+                                                 __builtin_amdgcn_perm(f, e, 0x07060302u), __builtin_amdgcn_perm(h, g, 0x07060302u)));
+}
+// eight numbers as PARTS operands, one: rounded
+template <int PARTS> __device__ __forceinline__ void operands(const float *v, bf16x8 *out)
+{
+    if constexpr (PARTS == 1) {
+        out[0] = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])));
+    } else {
+        unsigned p[8][PARTS];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) split_bf16<PARTS>(v[e], p[e]);
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k) out[k] = operand(p[0][k], p[1][k], p[2][k], p[3][k], p[4][k], p[5][k], p[6][k], p[7][k]);
+    }
+}
+
+template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void cache_attention_wide_kernel(AttendArgs a)
+{
+    constexpr bool F32 = sizeof(T) == 4;
+    constexpr int QP = F32 ? 3 : 1, PP = F32 ? 3 : 1, MP = 2;                  // bf16 parts of queries, weights, and of the minima m + 8 s
     constexpr int NG = D / 64, ROWS = 128, KROW = D * 2 + 16, VROW = 128 + 16, KROWS = 64 * KROW, VROWS = D * VROW;
-    constexpr int EXT_K = 64 * 32, EXT_V = 2 * NG * VROW, SCALES = 2 * NG * 64 * 4, BUF = KROWS + VROWS + EXT_K + EXT_V + SCALES;
+    constexpr int EXT_K = 64 * 32, EXT_V = F32 ? NG * 64 * 4 : MP * NG * VROW, SCALES = 2 * NG * 64 * 4, BUF = KROWS + VROWS + EXT_K + EXT_V + SCALES;
     constexpr int ITEMS = 64 * D / 32;                 // 16-byte pieces of a tile's key codes, and of its value codes
     __shared__ __align__(16) unsigned char lds[2 * BUF];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
@@ -32,7 +55,7 @@ template <int D> __global__ __launch_bounds__(256, 2) void cache_attention_wide_
     const Range rg = range_of(a, span, r0, min(r0 + ROWS, rows));
     int lo = rg.lo, hi = rg.hi;
     if (a.splits > 1) {
-        const int n = split_tiles(rg.hi - rg.lo, a.splits);
+        const int n = split_tiles(a, rg.hi - rg.lo);
         lo = rg.lo + sp * n;
         hi = min(rg.hi, lo + n);
         if (lo >= hi) return;
@@ -99,10 +122,14 @@ template <int D> __global__ __launch_bounds__(256, 2) void cache_attention_wide_
                 } else {
                     scales[(NG + i) * 64 + skey] = sc * 16.f;
                     const float mm = fmaf(8.f, sc, m);
-                    const unsigned short hi16 = f32_to_bf16(mm), lo16 = f32_to_bf16(mm - bf16_to_f32(hi16));
-                    unsigned char *x = buf + KROWS + VROWS + EXT_K + 2 * i * VROW + slot * 2;
-                    *(unsigned short *)x = hi16;
-                    *(unsigned short *)(x + VROW) = lo16;
+                    if constexpr (F32) {
+                        ((float *)(buf + KROWS + VROWS + EXT_K))[i * 64 + skey] = mm;
+                        continue;
+                    }
+                    unsigned part[MP];
+                    split_bf16<MP>(mm, part);
+#pragma unroll
+                    for (int k = 0; k < MP; ++k) *(unsigned short *)(buf + KROWS + VROWS + EXT_K + (MP * i + k) * VROW + slot * 2) = (unsigned short)(part[k] >> 16);
                 }
             }
             if (tid < 64) {                            // slots 0..7: the pairs of the groups, twice; 8..15: once more and zeros
@@ -115,21 +142,26 @@ template <int D> __global__ __launch_bounds__(256, 2) void cache_attention_wide_
     if (lo < hi) load(lo);
 
     // -- queries: lane & 31 = row; features 16 t + 8 half .. of step t, and the sums of each group as the operand of the pairs -----------
-    bf16x8 q[NG * 4], qx;
+    bf16x8 q[QP][NG * 4], qx;
     {
         const bool on = r < rows;
-        const unsigned short *x = (const unsigned short *)a.x + ((int64_t)b * a.S + (on ? t : 0)) * (a.heads + 2 * a.c.kv_heads) * D + (on ? head : 0) * D + half * 8;
+        const T *x = (const T *)a.x + ((int64_t)b * a.S + (on ? t : 0)) * (a.heads + 2 * a.c.kv_heads) * D + (on ? head : 0) * D + half * 8;
         float sum[NG];
 #pragma unroll
         for (int i = 0; i < NG; ++i) sum[i] = 0.f;
 #pragma unroll
         for (int i = 0; i < NG * 4; ++i) {
-            const uint4 raw = *(const uint4 *)(x + i * 16);
-            q[i] = __builtin_bit_cast(bf16x8, on ? raw : make_uint4(0u, 0u, 0u, 0u));
             float v[8];
-            load8((const unsigned short *)&q[i], v);
+            load8(x + i * 16, v);
+            unsigned part[8][QP];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum[i / 4] += v[e];
+            for (int e = 0; e < 8; ++e) {
+                if (!on) v[e] = 0.f;
+                sum[i / 4] += v[e];
+                split_bf16<QP>(v[e], part[e]);
+            }
+#pragma unroll
+            for (int k = 0; k < QP; ++k) q[k][i] = operand(part[0][k], part[1][k], part[2][k], part[3][k], part[4][k], part[5][k], part[6][k], part[7][k]);
         }
         unsigned pair[NG][3];                          // parts of (8 sum, sum) of each group, as they meet (scale, minimum)
 #pragma unroll
@@ -146,10 +178,14 @@ template <int D> __global__ __launch_bounds__(256, 2) void cache_attention_wide_
         qx = __builtin_bit_cast(bf16x8, half ? second : first);
     }
     const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    f32x16 o[D / 32], corr = zero;
+    f32x16 o[D / 32], small[F32 ? D / 32 : 1], corr = zero;             // small: of the weights' second and third parts
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) o[c] = zero;
-    float base = NO_SCORE, l = 0.f;
+#pragma unroll
+    for (int c = 0; c < (F32 ? D / 32 : 1); ++c) small[c] = zero;
+    float base = 0.f, l = 0.f, cr[NG];             // cr: the minima's part of the result, of the lane's keys (fp32) or at the end
+#pragma unroll
+    for (int i = 0; i < NG; ++i) cr[i] = 0.f;
 
     // -- 32 keys of a tile: scores, weights, their product with the values ------------------------------------------------------------
     auto block = [&](const unsigned char *buf, int m, int p0, bool edge, bool gone) {
@@ -157,12 +193,17 @@ template <int D> __global__ __launch_bounds__(256, 2) void cache_attention_wide_
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
             d[i] = zero;
+            bf16x8 k8[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) d[i] = mfma(*(const bf16x8 *)(buf + (m * 32 + l32) * KROW + (i * 4 + j) * 32 + half * 16), q[i * 4 + j], d[i]);
+            for (int j = 0; j < 4; ++j) k8[j] = *(const bf16x8 *)(buf + (m * 32 + l32) * KROW + (i * 4 + j) * 32 + half * 16);
+#pragma unroll
+            for (int k = QP - 1; k >= 0; --k)          // the small parts first: their sums are rounded before they are large
+#pragma unroll
+                for (int j = 0; j < 4; ++j) d[i] = mfma(k8[j], q[k][i * 4 + j], d[i]);
         }
         x = mfma(*(const bf16x8 *)(buf + KROWS + VROWS + (m * 32 + l32) * 32 + half * 16), qx, zero);
         const float *scales = (const float *)(buf + KROWS + VROWS + EXT_K + EXT_V) + m * 32 + half * 4;
-        float s[16], top = NO_SCORE;
+        float s[16], top = -INFINITY;                  // scores above the reference: subtracted first, so that those that count are small when they are rounded
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             float4 sc[NG];
@@ -170,7 +211,7 @@ template <int D> __global__ __launch_bounds__(256, 2) void cache_attention_wide_
             for (int i = 0; i < NG; ++i) sc[i] = *(const float4 *)(scales + i * 64 + k * 8);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                float v = x[4 * k + e];
+                float v = x[4 * k + e] - base;
 #pragma unroll
                 for (int i = 0; i < NG; ++i) v = fmaf(e == 0 ? sc[i].x : e == 1 ? sc[i].y : e == 2 ? sc[i].z : sc[i].w, d[i][4 * k + e], v);
                 s[4 * k + e] = v;
@@ -185,28 +226,35 @@ template <int D> __global__ __launch_bounds__(256, 2) void cache_attention_wide_
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) top = fmaxf(top, s[e]);
-        RARELY(__any(top - base > 8.f)) {              // the largest score so far becomes the reference
+        RARELY(__any(top > 8.f || (l == 0.f && top > -INFINITY))) {      // the largest score so far becomes the reference, and the first one
+            const bool first = l + __shfl_xor(l, 32, 64) == 0.f;
             top = fmaxf(top, __shfl_xor(top, 32, 64));
-            top = fmaxf(top, base);
-            const float f = __builtin_amdgcn_exp2f(base - top);
-            base = top;
+            const float up = top == -INFINITY ? 0.f : first ? top : fmaxf(top, 0.f), f = first ? 1.f : __builtin_amdgcn_exp2f(-up);
+            base += up;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] -= up;
             l *= f;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                corr[e] *= f;
+            for (int i = 0; i < NG; ++i) cr[i] *= f;
 #pragma unroll
-                for (int c = 0; c < D / 32; ++c) o[c][e] *= f;
+            for (int e = 0; e < 16; ++e) {
+                if constexpr (!F32) corr[e] *= f;
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) {
+                    o[c][e] *= f;
+                    if constexpr (F32) small[c][e] *= f;
+                }
             }
         }
-        float p[16];
+        float p[16], sum[8];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            p[e] = __builtin_amdgcn_exp2f(s[e] - base);
-            l += p[e];
-        }
+        for (int e = 0; e < 16; ++e) p[e] = __builtin_amdgcn_exp2f(s[e]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] = p[e] + p[e + 8];
+        l += ((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7]));      // one at a time a thousand keys cost l 1e-6
 #pragma unroll
         for (int k = 0; k < 2; ++k) {                  // 16 keys
-            uint4 w[NG], wp;
+            bf16x8 w[NG][PP];                          // the weights times the groups' scales
 #pragma unroll
             for (int i = 0; i < NG; ++i) {
                 const float4 s0 = *(const float4 *)(scales + (NG + i) * 64 + k * 16), s1 = *(const float4 *)(scales + (NG + i) * 64 + k * 16 + 8);
@@ -217,25 +265,48 @@ template <int D> __global__ __launch_bounds__(256, 2) void cache_attention_wide_
                     for (int e = 0; e < 8; ++e)
                         if (s[8 * k + e] == -INFINITY) v[e] = 0.f;
                 }
-                w[i] = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+                operands<PP>(v, w[i]);
             }
-            wp = make_uint4(pack_bf16(p[8 * k], p[8 * k + 1]), pack_bf16(p[8 * k + 2], p[8 * k + 3]), pack_bf16(p[8 * k + 4], p[8 * k + 5]), pack_bf16(p[8 * k + 6], p[8 * k + 7]));
             const int at_key = (m * 2 + k) * 32 + half * 16;
-            bf16x8 mx = *(const bf16x8 *)(buf + KROWS + VROWS + EXT_K + min(l32, 2 * NG - 1) * VROW + at_key);
-            RARELY(edge) {                             // the same for their minima: an operand that holds no NaN
-                uint4 u = __builtin_bit_cast(uint4, mx);
-                unsigned *e = (unsigned *)&u;
+            if constexpr (F32) {
+                const float *mm = (const float *)(buf + KROWS + VROWS + EXT_K) + m * 32 + half * 4 + k * 16;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if ((e[i] & 0x7F80u) == 0x7F80u) e[i] &= 0xFFFF0000u;
-                    if ((e[i] & 0x7F800000u) == 0x7F800000u) e[i] &= 0xFFFFu;
+                for (int i = 0; i < NG; ++i) {
+                    const float4 m0 = *(const float4 *)(mm + i * 64), m1 = *(const float4 *)(mm + i * 64 + 8);
+                    float v[8] = {p[8 * k] * m0.x, p[8 * k + 1] * m0.y, p[8 * k + 2] * m0.z, p[8 * k + 3] * m0.w,
+                                  p[8 * k + 4] * m1.x, p[8 * k + 5] * m1.y, p[8 * k + 6] * m1.z, p[8 * k + 7] * m1.w};
+                    RARELY(edge) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (s[8 * k + e] == -INFINITY) v[e] = 0.f;
+                    }
+                    cr[i] += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
                 }
-                mx = __builtin_bit_cast(bf16x8, u);
-            }
-            corr = mfma(mx, __builtin_bit_cast(bf16x8, wp), corr);
+            } else {
+                bf16x8 mx = *(const bf16x8 *)(buf + KROWS + VROWS + EXT_K + min(l32, MP * NG - 1) * VROW + at_key);
+                RARELY(edge) {                             // the same for their minima: an operand that holds no NaN
+                    uint4 u = __builtin_bit_cast(uint4, mx);
+                    unsigned *e = (unsigned *)&u;
 #pragma unroll
-            for (int c = 0; c < D / 32; ++c)
-                o[c] = mfma(*(const bf16x8 *)(buf + KROWS + (c * 32 + l32) * VROW + at_key), __builtin_bit_cast(bf16x8, w[c / 2]), o[c]);
+                    for (int i = 0; i < 4; ++i) {
+                        if ((e[i] & 0x7F80u) == 0x7F80u) e[i] &= 0xFFFF0000u;
+                        if ((e[i] & 0x7F800000u) == 0x7F800000u) e[i] &= 0xFFFFu;
+                    }
+                    mx = __builtin_bit_cast(bf16x8, u);
+                }
+                bf16x8 wp[1];
+                operands<1>(p + 8 * k, wp);
+                corr = mfma(mx, wp[0], corr);
+            }
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) {
+                const bf16x8 v8 = *(const bf16x8 *)(buf + KROWS + (c * 32 + l32) * VROW + at_key);
+#pragma unroll
+                for (int n = 0; n < PP; ++n) {
+                    if (F32 && n) small[F32 ? c : 0] = mfma(v8, w[c / 2][n], small[F32 ? c : 0]);
+                    else o[c] = mfma(v8, w[c / 2][n], o[c]);
+                }
+            }
         }
         mfma_settle<DT_BF16>();
     };
@@ -256,33 +327,39 @@ template <int D> __global__ __launch_bounds__(256, 2) void cache_attention_wide_
         }
     }
 
+    if constexpr (F32) {
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[c][e] += small[c][e];
+    }
     l += __shfl_xor(l, 32, 64);
-    float cr[NG];                                      // the minima's part of the result, rows 0..3 of the product: in lanes of half 0
 #pragma unroll
     for (int i = 0; i < NG; ++i) {
-        const float v = corr[2 * i] + corr[2 * i + 1], other = __shfl_xor(v, 32, 64);
-        cr[i] = half ? other : v;
+        if constexpr (F32) cr[i] += __shfl_xor(cr[i], 32, 64);
+        else {                                         // rows 2 i and 2 i + 1 of the product, in half 0
+            const float v = corr[2 * i] + corr[2 * i + 1], other = __shfl_xor(v, 32, 64);
+            cr[i] = half ? other : v;
+        }
     }
     if (r >= rows) return;
     if (a.splits > 1) {
-        float *ws = a.ws + ((((int64_t)b * a.c.kv_heads + g) * a.row_tiles + rt) * a.splits + sp) * (ROWS * (D + 2)) + (r - r0) * (D + 2);
+        float *ws = a.ws + ((((int64_t)b * a.c.kv_heads + g) * a.row_tiles + rt) * a.splits + sp) * (ROWS * (D + 2));
 #pragma unroll
         for (int c = 0; c < D / 32; ++c)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                float *y = ws + c * 32 + k * 8 + half * 4;
+                float v[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] = o[c][4 * k + e] + cr[c / 2];
+                for (int e = 0; e < 4; ++e) v[e] = o[c][4 * k + e] + cr[c / 2];
+                store_vec4(ws + (r - r0) * D + c * 32 + k * 8 + half * 4, v);
             }
-        if (!half) {
-            ws[D] = base;
-            ws[D + 1] = l;
-        }
+        if (!half) *(float2 *)(ws + ROWS * D + (r - r0) * 2) = make_float2(l != 0.f ? base : NO_SCORE, l);
         return;
     }
     const bool seen = at >= 0 && l != 0.f;
     const float inv = 1.f / l;
-    unsigned short *y = (unsigned short *)a.y + (((int64_t)b * a.S + t) * a.heads + head) * D + half * 4;
+    T *y = (T *)a.y + (((int64_t)b * a.S + t) * a.heads + head) * D + half * 4;
 #pragma unroll
     for (int c = 0; c < D / 32; ++c)
 #pragma unroll
@@ -290,14 +367,16 @@ template <int D> __global__ __launch_bounds__(256, 2) void cache_attention_wide_
             float v[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = seen ? (o[c][4 * k + e] + cr[c / 2]) * inv : 0.f;
-            *(uint2 *)(y + c * 32 + k * 8) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+            store_vec4(y + c * 32 + k * 8, v);
         }
 }
 
-void launch_cache_attention_wide(const AttendArgs &b, int D, int grid, hipStream_t s)
+void launch_cache_attention_wide(const AttendArgs &b, int dtype, int D, int grid, hipStream_t s)
 {
-    if (D == 64) GACER_LAUNCH(cache_attention_wide_kernel<64>, dim3(grid), dim3(256), 0, s, b);
-    else GACER_LAUNCH(cache_attention_wide_kernel<128>, dim3(grid), dim3(256), 0, s, b);
+    if (dtype == DT_BF16 && D == 64) GACER_LAUNCH((cache_attention_wide_kernel<unsigned short, 64>), dim3(grid), dim3(256), 0, s, b);
+    else if (dtype == DT_BF16) GACER_LAUNCH((cache_attention_wide_kernel<unsigned short, 128>), dim3(grid), dim3(256), 0, s, b);
+    else if (D == 64) GACER_LAUNCH((cache_attention_wide_kernel<float, 64>), dim3(grid), dim3(256), 0, s, b);
+    else GACER_LAUNCH((cache_attention_wide_kernel<float, 128>), dim3(grid), dim3(256), 0, s, b);
 }
 
 }  // namespace gacer

@@ -7,19 +7,21 @@
 namespace gacer {
 
 // Attention over a cache, by the unsplit operator's shape (so that every decomposition adds in the same order): rows of a key/value head in
-// tiles of `rows`, keys in `splits` parts that a second kernel joins.
-struct AttendGeom { int rows, waves, row_tiles, splits; };
+// tiles of `rows`, keys in `splits` parts of at least `split_min` tiles of 64 that a second kernel joins.
+struct AttendGeom { int rows, waves, row_tiles, splits, split_min; };
 inline AttendGeom attend_geom(const TokenArgs &a)
 {
     AttendGeom g;
     const int64_t all = (int64_t)a.S * (a.heads / a.kv_heads);
-    g.rows = all <= 8 ? 8 : all <= 16 ? 16 : all < 128 || a.dtype != DT_BF16 ? 32 : 128;
+    g.rows = all <= 8 ? 8 : all <= 16 ? 16 : all < 128 ? 32 : 128;
     g.waves = g.rows == 8 && a.dtype == DT_BF16 ? 8 : 4;
     g.row_tiles = (int)((all + g.rows - 1) / g.rows);
     const int64_t groups = (int64_t)a.batch * a.kv_heads * g.row_tiles;
     const int64_t most = std::min((int64_t)a.cache.max_pages << a.cache.page_shift, a.window > 0 ? (int64_t)a.window + a.S : (int64_t)1 << 40);
-    const int64_t want = (256 + groups - 1) / groups, can = std::max<int64_t>(1, most / 1024);
-    g.splits = (int)std::min<int64_t>(std::min(want, can), 128);
+    const bool wide = g.rows == 128;
+    const int want = wide ? 512 : 256, least = wide ? 256 : 1024;      // workgroups, keys of a split
+    g.split_min = wide ? 4 : 8;
+    g.splits = (int)std::min<int64_t>(std::min((want + groups - 1) / groups, std::max<int64_t>(1, most / least)), 128);
     return g;
 }
 

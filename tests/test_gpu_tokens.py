@@ -592,3 +592,47 @@ def test_the_example_decodes_as_if_every_token_were_filled_in_at_once():
     # its group's range; three such steps of one key feature move a logit of size 3 by a few hundredths
     assert (logits[:, 0] - want).abs().max() <= 0.05 * want.abs().max()
     s.close()
+
+
+SPLITS = [  # page, dim, heads, kv, tokens, starts, counts, window: few sequences with room for long ones, so that their keys are cut into parts
+    (64, 128, 8, 2, 1, [2300, 70], None, 0),
+    (256, 64, 2, 2, 1, [1025, 0, 2047], None, 0),
+    (64, 64, 24, 2, 1, [1800], None, 0),
+    (128, 128, 4, 2, 9, [1500, 600], [9, 4], 0),
+    (64, 64, 3, 3, 150, [900, 0], [150, 70], 0),
+    (64, 128, 8, 1, 40, [1100], None, 0),
+    (128, 64, 4, 1, 70, [1200], None, 700),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("page,dim,heads,kv,tokens,starts,counts,window", SPLITS)
+def test_attention_with_the_keys_in_splits(dtype, page, dim, heads, kv, tokens, starts, counts, window):
+    """The whole result, and the same bits from any cut of the batch (every part of it has its own part of the workspace)."""
+    from paper_2304_11745_amd import binding as B
+    ref, qkv, start, count, scale, want, weight = attend_case(dtype, page, dim, heads, kv, tokens, starts, counts, window, False)
+    n = len(starts)
+    used = ref.table.shape[1]
+    ref.table = torch.cat((ref.table, torch.full((n, 32768 // page - used), -1, dtype=torch.int32)), 1)
+    ref.table[0, 1] = -1                                        # an absent page within
+    want, weight = R.attention(ref, qkv, heads, start, count, scale, window)
+    out = torch.full((n, tokens, heads * dim), 7.0, dtype=DT[dtype], device="cuda")
+    s = session(lambda o: o.cache_attention(dev(qkv), out, on_gpu(ref), dev(start), dev(count), heads=heads, scale=scale, window=window), dtype, n)
+    rows = C.c_size_t()
+    B.check(s.ctx, B.gacer_trace_run(s.ctx, B.GACER_MODE_SEQUENTIAL, 1, None, 0, C.byref(rows)))
+    assert rows.value == 2                                      # the parts, and what joins them
+    s.enqueue()
+    torch.cuda.synchronize()
+    check_attention(out, want, weight, dtype, dim)
+    whole = out.clone()
+    for sizes in ([1] * n, [n - 1, 1]):
+        if n == 1:
+            continue
+        arr = (C.c_int * len(sizes))(*sizes)
+        sp = (B.gacer_split * 1)(B.gacer_split(0, 0, B.GACER_AXIS_BATCH, len(sizes), arr, 0))
+        B.check(s.ctx, B.gacer_set_plan(s.ctx, C.byref(B.gacer_plan(1, sp, 0, None))))
+        out.fill_(3.0)
+        torch.cuda.synchronize()
+        s.run(B.GACER_MODE_PLAN)
+        assert torch.equal(out, whole)
+    s.close()
