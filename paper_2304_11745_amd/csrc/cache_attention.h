@@ -13,6 +13,9 @@ struct AttendArgs {
     CacheView c;
     int b_lo, S, heads, per_kv, window, rows, row_tiles, splits, split_min;      // rows: of a row tile; split_min: fewest tiles of 64 keys in a split
     float scale;               // alpha * log2(e)
+    // set by the launcher, see divisor(): heads per kv head, kv heads, heads, tokens, splits, row tiles, (sequence, kv head) pairs, those times splits
+    unsigned div_per_kv[2], div_kv[2], div_heads[2], div_S[2], div_splits[2], div_tiles[2], div_groups[2], div_parts[2];
+    int groups, parts;
 };
 
 // the tiles of each split of n tiles
@@ -23,8 +26,8 @@ struct Range { int t0, t1, lo, hi; };
 __device__ __forceinline__ Range range_of(const AttendArgs &a, const Span &s, int r0, int r1)
 {
     Range g;
-    g.t0 = r0 / a.per_kv;
-    g.t1 = min((r1 - 1) / a.per_kv, s.count - 1);
+    g.t0 = div_by(r0, a.div_per_kv);
+    g.t1 = min(div_by(r1 - 1, a.div_per_kv), s.count - 1);
     g.lo = g.hi = 0;
     if (g.t1 >= g.t0) {
         const int first = a.window > 0 ? max(0, s.start + g.t0 - a.window + 1) : 0;

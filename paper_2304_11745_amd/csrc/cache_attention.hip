@@ -32,6 +32,17 @@ template <int D> struct Tile {
     int page[2];
 };
 
+// sum over the 32 lanes of a half
+template <int CTRL> __device__ __forceinline__ float add_lanes(float v) { return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true)); }
+__device__ __forceinline__ float sum32(float v)
+{
+    v = add_lanes<0xB1>(v);                            // quad_perm 1,0,3,2
+    v = add_lanes<0x4E>(v);                            // quad_perm 2,3,0,1
+    v = add_lanes<0x141>(v);                           // mirrored within 8 lanes
+    v = add_lanes<0x140>(v);                           // mirrored within 16
+    return v + __shfl_xor(v, 16, 64);
+}
+
 template <typename T, int D, int ROWS, int NW> __global__ __launch_bounds__(NW * 64) void cache_attention_kernel(AttendArgs a)
 {
     constexpr bool F32 = sizeof(T) == 4;
@@ -39,12 +50,14 @@ template <typename T, int D, int ROWS, int NW> __global__ __launch_bounds__(NW *
     constexpr int STACK = 32 / ROWS < PP ? 32 / ROWS : PP, PM = (PP + STACK - 1) / STACK;              // parts in one product, products
     constexpr int QSTACK = 32 / ROWS < QP ? 32 / ROWS : QP, QM = (QP + QSTACK - 1) / QSTACK;
     constexpr float TIMES = F32 ? 16.f : 1.f, BIAS = F32 ? 8.f : -16.f;
-    constexpr int PGROUP = PP * ROWS * PROW, PWAVE = NG * PGROUP, MROW = D + 2;
-    constexpr int BYTES = NW * PWAVE > NW * ROWS * MROW * 4 ? NW * PWAVE : NW * ROWS * MROW * 4;
+    constexpr int PGROUP = PP * ROWS * PROW, PWAVE = NG * PGROUP;
+    constexpr int JOIN = NW * ROWS * D * 4, BYTES = NW * PWAVE > JOIN ? NW * PWAVE : JOIN;
     __shared__ __align__(16) unsigned char lds[BYTES];
+    __shared__ float2 ends[NW * ROWS];
+    __shared__ float factor[NW * ROWS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
-    const int sp = (int)blockIdx.x % a.splits, u = (int)blockIdx.x / a.splits, rt = u % a.row_tiles, z = u / a.row_tiles;
-    const int g = z % a.c.kv_heads, b = a.b_lo + z / a.c.kv_heads;
+    const int u = div_by((int)blockIdx.x, a.div_splits), sp = (int)blockIdx.x - u * a.splits, z = div_by(u, a.div_tiles), rt = u - z * a.row_tiles;
+    const int zb = div_by(z, a.div_kv), g = z - zb * a.c.kv_heads, b = a.b_lo + zb;
     const int rows = a.S * a.per_kv, r0 = rt * ROWS;
     const Span span = span_of(a.c, b, a.S);
     const Range rg = range_of(a, span, r0, min(r0 + ROWS, rows));
@@ -89,7 +102,7 @@ template <typename T, int D, int ROWS, int NW> __global__ __launch_bounds__(NW *
     const unsigned sixteen = 0x41804180u;
 #pragma unroll
     for (int n = 0; n < QM; ++n) {
-        const int part = n * QSTACK + l32 / ROWS, r = r0 + (l32 & (ROWS - 1)), t = r / a.per_kv;
+        const int part = n * QSTACK + l32 / ROWS, r = r0 + (l32 & (ROWS - 1)), t = div_by(r, a.div_per_kv);
         const bool on = l32 < ROWS * QSTACK && part < QP && r < rows;
         const T *x = (const T *)a.x + ((int64_t)b * a.S + (on ? t : 0)) * (a.heads + 2 * a.c.kv_heads) * D + (g * a.per_kv + (on ? r - t * a.per_kv : 0)) * D + half * 32;
 #pragma unroll
@@ -133,7 +146,7 @@ template <typename T, int D, int ROWS, int NW> __global__ __launch_bounds__(NW *
     int at[R4];                                        // position of a register's row, -1: nothing to compute
 #pragma unroll
     for (int e = 0; e < R4; ++e) {
-        const int r = r0 + 8 * (e >> 2) + 4 * half + (e & 3), t = r / a.per_kv;
+        const int r = r0 + 8 * (e >> 2) + 4 * half + (e & 3), t = div_by(r, a.div_per_kv);
         at[e] = r < rows && t < span.count ? span.start + t : -1;
     }
     // every row sees all keys in [all_lo, all_hi)
@@ -276,67 +289,73 @@ template <typename T, int D, int ROWS, int NW> __global__ __launch_bounds__(NW *
         step(odd, tile + 1);
     }
 
-    // the waves' results, relative to their references, are joined in LDS
+    // the waves' results are joined in LDS, each relative to its own reference
 #pragma unroll
     for (int e = 0; e < R4; ++e) {
+        l[e] = sum32(l[e]);
 #pragma unroll
-        for (int k = 16; k > 0; k >>= 1) {
-            l[e] += __shfl_xor(l[e], k, 64);
-#pragma unroll
-            for (int i = 0; i < NG; ++i) corr[i][e] += __shfl_xor(corr[i][e], k, 64);
-        }
+        for (int i = 0; i < NG; ++i) corr[i][e] = sum32(corr[i][e]);
     }
-    __syncthreads();
+    __syncthreads();                                   // every wave is done with its patch of weights
     float *mo = (float *)lds;
 #pragma unroll
     for (int e = 0; e < R4; ++e) {
-        float *row = mo + (wave * ROWS + 8 * (e >> 2) + 4 * half + (e & 3)) * MROW;
+        const int row = 8 * (e >> 2) + 4 * half + (e & 3);
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
             float v = o[c][e] + corr[c / 2][e];
 #pragma unroll
             for (int k = 1; k < STACK; ++k) v += o[c][e + k * R4];
-            row[c * 32 + l32] = v;
+            mo[(wave * ROWS + row) * D + c * 32 + l32] = v;
         }
-        if (l32 == 0) {
-            row[D] = base[e];
-            row[D + 1] = l[e];
-        }
+        if (l32 == 0) ends[wave * ROWS + row] = make_float2(base[e], l[e]);
     }
     __syncthreads();
-    for (int i = tid; i < ROWS * D; i += NW * 64) {
-        const int row = i / D, d = i % D, r = r0 + row, t = r / a.per_kv;
-        float top = NO_SCORE;
+    float *part = a.ws + (a.splits > 1 ? ((((int64_t)b * a.c.kv_heads + g) * a.row_tiles + rt) * a.splits + sp) * (ROWS * (D + 2)) : 0);
+    if (tid < ROWS) {                                  // a row: the largest reference, the waves' factors, the sum of the weights
+        float top = NO_SCORE, sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) top = fmaxf(top, mo[(w * ROWS + row) * MROW + D]);
-        float sum = 0.f, acc = 0.f;
+        for (int w = 0; w < NW; ++w) top = fmaxf(top, ends[w * ROWS + tid].x);
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-            const float *m = mo + (w * ROWS + row) * MROW;
-            const float f = __builtin_amdgcn_exp2f(m[D] - top);
-            sum = fmaf(f, m[D + 1], sum);
-            acc = fmaf(f, m[d], acc);
+            const float f = __builtin_amdgcn_exp2f(ends[w * ROWS + tid].x - top);
+            sum = fmaf(f, ends[w * ROWS + tid].y, sum);
+            factor[w * ROWS + tid] = f;
         }
-        if (a.splits > 1) {
-            float *ws = a.ws + ((((int64_t)b * a.c.kv_heads + g) * a.row_tiles + rt) * a.splits + sp) * (ROWS * (D + 2));
-            ws[i] = acc;
-            if (d == 0) *(float2 *)(ws + ROWS * D + row * 2) = make_float2(top, sum);
-        } else if (r < rows) {
-            const bool on = t < span.count && sum != 0.f;
-            st_f32((T *)a.y, (((int64_t)b * a.S + t) * a.heads + g * a.per_kv + (r - t * a.per_kv)) * D + d, on ? acc / sum : 0.f);
+        const int r = r0 + tid, t = div_by(r, a.div_per_kv);
+        if (a.splits > 1) *(float2 *)(part + ROWS * D + tid * 2) = make_float2(top, sum);
+        ends[tid] = make_float2(r < rows && t < span.count && sum != 0.f ? 1.f / sum : 0.f, 0.f);
+    }
+    __syncthreads();
+    for (int i = tid * 4; i < ROWS * D; i += NW * 256) {
+        const int row = i / D, d = i % D, r = r0 + row, t = div_by(r, a.div_per_kv);
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float f = factor[w * ROWS + row];
+            const float4 x = *(const float4 *)(mo + (w * ROWS + row) * D + d);
+            v[0] = fmaf(f, x.x, v[0]); v[1] = fmaf(f, x.y, v[1]); v[2] = fmaf(f, x.z, v[2]); v[3] = fmaf(f, x.w, v[3]);
+        }
+        if (a.splits > 1) store_vec4(part + i, v);
+        else if (r < rows) {
+            const float inv = ends[row].x;
+            const bool none = inv == 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = none ? 0.f : v[e] * inv;
+            store_vec4((T *)a.y + (((int64_t)b * a.S + t) * a.heads + g * a.per_kv + (r - t * a.per_kv)) * D + d, v);
         }
     }
 }
 
 // Joins the splits: D / 4 lanes to a row, and GROUPS of them where there are many splits, each over every GROUPS-th.  A split holds its rows'
 // sums [rows][D], relative to their references, then [rows][reference, sum of the weights].
-template <typename T, int D, int GROUPS> __global__ __launch_bounds__(256) void cache_attention_join_kernel(AttendArgs a, int64_t outputs)
+template <typename T, int D, int GROUPS> __global__ __launch_bounds__(256) void cache_attention_join_kernel(AttendArgs a, int outputs)
 {
     constexpr int LANES = D / 4, ROWS = 256 / (LANES * GROUPS);                // rows of a workgroup
     __shared__ float4 acc_s[GROUPS > 1 ? 256 : 1];
     __shared__ float2 ml_s[GROUPS > 1 ? GROUPS : 1];
     const int tid = threadIdx.x, lane = tid % LANES, grp = tid / LANES % GROUPS;
-    const int64_t out = (int64_t)blockIdx.x * ROWS + tid / (LANES * GROUPS);   // (sequence, token, head), counted from the first sequence of the call
+    const int out = (int)blockIdx.x * ROWS + tid / (LANES * GROUPS);   // (sequence, token, head), counted from the first sequence of the call
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float top = NO_SCORE, sum = 0.f;
     auto add = [&](float m, float l, const float4 &v) {
@@ -346,8 +365,7 @@ template <typename T, int D, int GROUPS> __global__ __launch_bounds__(256) void 
         acc = make_float4(fmaf(acc.x, f0, v.x * f1), fmaf(acc.y, f0, v.y * f1), fmaf(acc.z, f0, v.z * f1), fmaf(acc.w, f0, v.w * f1));
     };
     if (out < outputs) {
-        const int h = (int)(out % a.heads), g = h / a.per_kv;
-        const int t = (int)(out / a.heads % a.S), b = a.b_lo + (int)(out / a.heads / a.S);
+        const int bt = div_by(out, a.div_heads), h = out - bt * a.heads, g = div_by(h, a.div_per_kv), zb = div_by(bt, a.div_S), t = bt - zb * a.S, b = a.b_lo + zb;
         const int r = t * a.per_kv + (h - g * a.per_kv), rt = r / a.rows, row = r - rt * a.rows;
         const Span span = span_of(a.c, b, a.S);
         const Range rg = range_of(a, span, rt * a.rows, min(rt * a.rows + a.rows, a.S * a.per_kv));
@@ -372,10 +390,10 @@ template <typename T, int D, int GROUPS> __global__ __launch_bounds__(256) void 
     if (out >= outputs) return;
     const float inv = sum != 0.f ? 1.f / sum : 0.f;
     const float v[4] = {acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv};
-    store_vec4((T *)a.y + (out + (int64_t)a.b_lo * a.S * a.heads) * D + lane * 4, v);
+    store_vec4((T *)a.y + ((int64_t)out + (int64_t)a.b_lo * a.S * a.heads) * D + lane * 4, v);
 }
 
-template <typename T, int D, int ROWS, int NW> static void attend(const AttendArgs &b, int grid, int64_t outputs, hipStream_t s, int phase)
+template <typename T, int D, int ROWS, int NW> static void attend(const AttendArgs &b, int grid, int outputs, hipStream_t s, int phase)
 {
     if (phase != 2) {
         if constexpr (ROWS <= 32) GACER_LAUNCH((cache_attention_kernel<T, D, ROWS, NW>), dim3(grid), dim3(NW * 64), 0, s, b);
@@ -394,10 +412,13 @@ LaunchInfo launch_cache_attention(const TokenArgs &a, hipStream_t s, bool dry, i
     b.x = a.x; b.y = a.y; b.ws = a.ws; b.c = a.cache; b.b_lo = a.b_lo; b.S = a.S; b.heads = a.heads; b.per_kv = a.heads / a.kv_heads;
     b.window = a.window; b.rows = g.rows; b.row_tiles = g.row_tiles; b.splits = g.splits; b.split_min = g.split_min;
     b.scale = a.alpha * 1.4426950408889634f;
+    b.groups = (a.b_hi - a.b_lo) * a.kv_heads; b.parts = b.groups * g.splits;
+    divisor(b.per_kv, b.div_per_kv); divisor(a.kv_heads, b.div_kv); divisor(a.heads, b.div_heads); divisor(a.S, b.div_S);
+    divisor(g.splits, b.div_splits); divisor(g.row_tiles, b.div_tiles); divisor(b.groups, b.div_groups); divisor(b.parts, b.div_parts);
     const int n = a.b_hi - a.b_lo, grid = n * a.kv_heads * g.row_tiles * g.splits;
-    const int64_t outputs = (int64_t)n * a.S * a.heads;
+    const int outputs = n * a.S * a.heads;
     LaunchInfo li;
-    li.workgroups = phase == 2 ? (int)(b.splits > 8 ? outputs : (outputs * a.D + 1023) / 1024) : grid;
+    li.workgroups = phase == 2 ? (b.splits > 8 ? outputs : (int)(((int64_t)outputs * a.D + 1023) / 1024)) : grid;
     li.threads = phase == 2 ? 256 : g.waves * 64; li.lds_bytes = g.waves * g.rows * (a.D + 2) * 4; li.wg_per_cu = phase == 2 ? 8 : 8 / g.waves;
     li.kernel = phase == 2 ? "cache_attention_join" : a.dtype == DT_BF16 ? "cache_attention_bf16" : "cache_attention_f32";
     li.phases = g.splits > 1 ? 2 : 1;

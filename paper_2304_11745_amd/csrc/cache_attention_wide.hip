@@ -48,8 +48,8 @@ template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 &&
     __shared__ __align__(16) unsigned char lds[2 * BUF];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
     // last rows first: they see the most keys; neighbours in the grid, which run on different XCDs, are different heads
-    const int groups = (int)gridDim.x / a.row_tiles / a.splits, zs = (int)blockIdx.x % (groups * a.splits), z = zs % groups, sp = zs / groups;
-    const int rt = a.row_tiles - 1 - (int)blockIdx.x / (groups * a.splits), g = z % a.c.kv_heads, b = a.b_lo + z / a.c.kv_heads;
+    const int back = div_by((int)blockIdx.x, a.div_parts), part = (int)blockIdx.x - back * a.parts, rt = a.row_tiles - 1 - back;
+    const int sp = div_by(part, a.div_groups), z = part - sp * a.groups, zb = div_by(z, a.div_kv), g = z - zb * a.c.kv_heads, b = a.b_lo + zb;
     const int rows = a.S * a.per_kv, r0 = rt * ROWS;
     const Span span = span_of(a.c, b, a.S);
     const Range rg = range_of(a, span, r0, min(r0 + ROWS, rows));
@@ -60,10 +60,10 @@ template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 &&
         hi = min(rg.hi, lo + n);
         if (lo >= hi) return;
     }
-    const int r = r0 + wave * 32 + l32, t = r / a.per_kv, head = g * a.per_kv + (r - t * a.per_kv);
+    const int r = r0 + wave * 32 + l32, t = div_by(r, a.div_per_kv), head = g * a.per_kv + (r - t * a.per_kv);
     const int at = r < rows && t < span.count ? span.start + t : -1;
     // what the wave's rows see: every row all of [all_lo, all_hi), none anything outside [any_lo, any_hi)
-    const int w0 = r0 + wave * 32, w1 = min(w0 + 32, rows), t0 = w0 / a.per_kv, t1 = min((w1 - 1) / a.per_kv, span.count - 1);
+    const int w0 = r0 + wave * 32, w1 = min(w0 + 32, rows), t0 = div_by(w0, a.div_per_kv), t1 = min(div_by(max(w1 - 1, 0), a.div_per_kv), span.count - 1);
     const bool idle = w0 >= rows || t0 > t1;
     const int all_lo = a.window > 0 ? span.start + t1 - a.window + 1 : 0, all_hi = span.start + t0 + 1;
     const int any_lo = a.window > 0 ? span.start + t0 - a.window + 1 : 0, any_hi = span.start + t1 + 1;

@@ -7,10 +7,12 @@ namespace gacer {
 
 // A sequence's part of a call: `start` tokens before it, `count` new ones; out of range on the device: none.
 struct Span { int start, count; };
+// an integer that nothing writes while the kernel runs: where the index is uniform it comes through the scalar cache
+__device__ __forceinline__ int fixed_int(const int *p, int64_t i) { return ((const __attribute__((address_space(4))) int *)(uintptr_t)p)[i]; }
 __device__ __forceinline__ Span span_of(const CacheView &c, int b, int S)
 {
-    Span s = {c.start[b], S};
-    if (c.count) s.count = max(0, min(c.count[b], S));
+    Span s = {fixed_int(c.start, b), S};
+    if (c.count) s.count = max(0, min(fixed_int(c.count, b), S));
     if (s.start < 0 || s.start > c.max_pages << c.page_shift) s = {0, 0};
     return s;
 }
