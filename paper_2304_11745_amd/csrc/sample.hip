@@ -3,15 +3,19 @@
 // A workgroup owns a row.  Weights are whole numbers, so every sum is exact and the same in any order, whatever adds it.  The entries that the
 // filters keep are a prefix of the order "larger first, equal ones by index"; it ends at a key (the logit's bits in an order of
 // unsigned numbers) and, among the entries with that key, at an index.
-//   The row's largest logit comes first.  Then one pass puts every entry into one of 2048 bins by its distance from the largest, 1/64 of a
-// temperature each (weights vanish 21.5 temperatures below), counting entries (top-k) or adding weights (top-p); the bin in which
-// the prefix ends is found by a scan.  For top-k the entries up to this bin go into a list in LDS, and everything else happens on the list: ranks
-// by counting, the nucleus by a scan over ranks, the draw by sums over smaller indexes.  For top-p alone only the bin's own entries need
-// ranks; the draw then adds the kept weights of the row, a part per wave, and looks for its index in one of the parts.
-//   Where more entries end up in the list than it holds (a flat row), the prefix's end is found digit by digit of the key instead.
+//   bf16 logits are few values: one pass over the row finds the largest and counts the entries by their 16 bits, in 65536 counters of 16 bits
+// that fill 128 KB of LDS.  Scans over the counts, and over the counts times the weights of the some thousand values that occur, give the value at
+// which top-k and the nucleus end and how many of its entries they still take.  The draw then adds the kept weights of the row, from a
+// table, a part of the row per wave, and looks for its index in one of the parts.
+//   fp32 logits: a second pass puts every entry into one of 2048 bins by its distance from the largest, 1/64 of a temperature each (weights vanish
+// 21.5 temperatures below), counting entries (top-k) or adding weights (top-p); the bin in which the prefix ends is found by a
+// scan.  Where few entries can be kept, they go into a list in LDS, and everything else happens on the list: ranks by counting, the nucleus by a scan
+// over ranks, the draw by sums over smaller indexes.  Otherwise only the last bin's entries need ranks, and the draw goes as for bf16.
+//   Where a list would not hold its entries or a counter its count (a flat row), the prefix's end is found digit by digit of the key instead.
 //
-// What bounds it: instructions.  A weight is a correctly rounded division, an exponential and a conversion, some 25 instructions, for every
-// entry of the row under top-p, and the row's workgroup runs on one compute unit.
+// What bounds it: with many rows of bf16 logits the way from memory and the counters, with fp32 instructions (a weight is a correctly rounded
+// division, an exponential and a conversion, some 25 of them, for every entry under top-p), with few rows the chain of passes, barriers
+// and scans.
 #include <hip/hip_runtime.h>
 #include "device_util.h"
 #include "kernels.h"
@@ -30,7 +34,7 @@ struct SampleArgs {
     float *logp;
 };
 
-static constexpr int THREADS = 1024, WAVES = THREADS / 64, BINS = 2048, LIST = 2048;
+static constexpr int THREADS = 1024, WAVES = THREADS / 64, BINS = 2048, LIST = 2048, CODES = 32768, GROUPS = 512;
 // Entries that a list may hold where the alternative is another pass over the row: ranks by counting take n steps of a thread and more, a pass over 131072
 // entries what 600 of them take.
 static constexpr int SHORT = 512;
@@ -123,12 +127,18 @@ template <typename T> struct Row {
 };
 
 struct Shared {
-    u64 sums[WAVES], bins[BINS], list[LIST];           // list: key, then the index's complement, so that larger numbers come first in the order
-    unsigned weight[LIST];                             // of the list's entries, by rank
-    int place[LIST];                                   // and their indexes
-    unsigned peak;
-    int entries, found, digit;
-    u64 before;
+    u64 sums[WAVES], groups[GROUPS], before, all;
+    unsigned equal[WAVES];
+    float value;
+    int entries, found;
+    union {
+        unsigned codes[CODES];                         // entries by the code of their magnitude: positive ones in the upper half, negative ones in the lower
+        struct {
+            u64 bins[BINS], list[LIST];                // list: key, then the index's complement, so that larger numbers come first in the order
+            unsigned weight[LIST];                     // of the list's entries, by rank
+            int place[LIST];                           // and where they stand in it
+        };
+    };
 };
 
 __device__ __forceinline__ u64 entry_of(unsigned key, int i) { return (u64)key << 32 | (unsigned)~i; }
@@ -172,6 +182,88 @@ template <typename D> __device__ int first_bin(Shared &s, D done, u64 *before)
     __syncthreads();
     *before = s.before;
     return s.found;
+}
+
+// bf16 values in the order of unsigned 16-bit numbers
+__device__ __forceinline__ unsigned key16_of(float x)
+{
+    const unsigned h = __float_as_uint(x + 0.f) >> 16;
+    return h ^ (h & 0x8000u ? 0xFFFFu : 0x8000u);
+}
+__device__ __forceinline__ float value16_of(unsigned k) { return __uint_as_float((k & 0x8000u ? k ^ 0x8000u : k ^ 0xFFFFu) << 16); }
+
+// The largest value up to and with which the measure of the counted entries, from the largest value on, reaches the line; `before` receives the measure
+// of larger ones, `all` of the row.  measure(value, entries) of a value; reached(measure, all).  Groups of 128 values are added by a wave
+// each, then scanned; the first 256 groups are those of the positive values.
+template <typename M, typename D> __device__ float first_value(Shared &s, M measure, D reached, u64 *before, u64 *all)
+{
+    constexpr int HALF = GROUPS / 2, EACH = GROUPS / WAVES, AHEAD = 8;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    // the lane's two counters of a group, of the larger value first: magnitudes of positive values fall, of negative ones rise
+    auto counters = [&](int group) {
+        const int m = group < HALF ? (HALF - 1 - group) * 128 + 126 - 2 * lane : (group - HALF) * 128 + 2 * lane;
+        const uint2 c = *(const uint2 *)&s.codes[m];
+        return group < HALF ? make_uint2(c.y >> 16, c.x >> 16) : make_uint2(c.x & 0xFFFFu, c.y & 0xFFFFu);
+    };
+    auto value = [&](int group, int which) {
+        const int m = group < HALF ? (HALF - 1 - group) * 128 + 127 - 2 * lane - which : (group - HALF) * 128 + 2 * lane + which;
+        return __uint_as_float((unsigned)m << 16 | (group < HALF ? 0u : 0x80000000u));
+    };
+    for (int i = 0; i < EACH; i += AHEAD) {
+        uint2 n[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) n[k] = counters(wave + WAVES * (i + k));
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int g = wave + WAVES * (i + k);
+            u64 v = 0;
+            if (__any((n[k].x | n[k].y) != 0u)) {
+                if (n[k].x) v += measure(value(g, 0), n[k].x);
+                if (n[k].y) v += measure(value(g, 1), n[k].y);
+                v = wave_sum(v);
+            }
+            if (lane == 0) s.groups[g] = v;
+        }
+    }
+    __syncthreads();
+    if (wave == 0) {
+        u64 part[GROUPS / 64], v = 0;                  // eight groups of a lane
+#pragma unroll
+        for (int i = 0; i < GROUPS / 64; ++i) {
+            part[i] = s.groups[lane * (GROUPS / 64) + i];
+            v += part[i];
+        }
+        const u64 upto = wave_scan(v), total = __shfl(upto, 63, 64);
+        u64 sum = upto - v, at = 0;
+        int g = 0;
+        bool found = false;
+#pragma unroll
+        for (int i = 0; i < GROUPS / 64; ++i) {
+            if (!found && reached(sum + part[i], total)) {
+                found = true;
+                g = i;
+                at = sum;
+            }
+            sum += part[i];
+        }
+        const u64 mine = __ballot(found);
+        const int l = mine ? __builtin_ctzll(mine) : 63;
+        g = l * (GROUPS / 64) + __shfl(g, l, 64);
+        at = __shfl(at, l, 64);
+        const uint2 n = counters(g);
+        const u64 x = n.x ? measure(value(g, 0), n.x) : 0, y = n.y ? measure(value(g, 1), n.y) : 0, in = at + wave_scan(x + y);
+        const u64 hit = __ballot(reached(in, total));
+        if (lane == (hit ? __builtin_ctzll(hit) : 63)) {
+            const bool first = reached(in - y, total);
+            s.value = value(g, first ? 0 : 1);
+            s.before = first ? in - y - x : in - y;
+            s.all = total;
+        }
+    }
+    __syncthreads();
+    *before = s.before;
+    *all = s.all;
+    return s.value;
 }
 
 // entries of the list in order: place[r] and weight[r] of rank r
@@ -271,25 +363,152 @@ template <typename W, typename F> __device__ void draw_from_list(Shared &s, cons
     }
 }
 
-template <typename T, bool PLAIN> __device__ __forceinline__ void sample_row(const SampleArgs &a, Shared &s, const Row<T> &row, int64_t r, float top, float temperature, Filters f)
+// What the draw needs to know of a kept set: weights, by value, of entries above `cut`, and `ties` entries, by index, that equal it.  Sums over
+// the waves' parts of the row, then over threads within the part that the goal falls into, then one by one.
+template <typename T, typename K, typename F> __device__ __forceinline__ void draw_from_row(Shared &s, const Row<T> &row, float u, float least, float cut, u64 ties, unsigned of_cut, K weight, F write)
 {
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    // entries below `least` (which is not below `cut`) weigh nothing
+    auto add = [&](float x, u64 &sum, unsigned &equal) {
+        if (!(x >= least)) return;
+        if (x > cut) sum += weight(x);
+        else ++equal;
+    };
+    u64 v = 0;
+    unsigned n = 0;
+    row.each([&](int, float x) { add(x, v, n); });
+    v = wave_sum(v);
+    n = (unsigned)wave_sum(n);
+    __syncthreads();
+    if (lane == 0) {
+        s.sums[wave] = v;
+        s.equal[wave] = n;
+    }
+    __syncthreads();
+    u64 total = 0, all = 0;
+    for (int k = 0; k < WAVES; ++k) {
+        total += s.sums[k];
+        all += s.equal[k];
+    }
+    ties = all < ties ? all : ties;
+    total += ties * of_cut;
+    u64 goal = goal_of(u, total);
+    int p = 0;
+    for (; p < WAVES - 1; ++p) {
+        const u64 taken = s.equal[p] < ties ? s.equal[p] : ties, part = s.sums[p] + taken * of_cut;
+        if (goal < part) break;
+        goal -= part;
+        ties -= taken;
+    }
+    const int lo = row.part_begin(p), hi = row.part_end(p), each = (hi - lo + THREADS - 1) / THREADS;
+    const int b = min(hi, lo + tid * each), e = min(hi, b + each);
+    v = 0;
+    n = 0;
+    for (int i = b; i < e; ++i) add(ld_f32(row.x, i), v, n);
+    u64 sum = wave_scan(v), equal = wave_scan(n);
+    __syncthreads();
+    if (lane == 63) {
+        s.sums[wave] = sum;
+        s.equal[wave] = (unsigned)equal;
+    }
+    __syncthreads();
+    for (int k = 0; k < wave; ++k) {
+        sum += s.sums[k];
+        equal += s.equal[k];
+    }
+    auto upto = [&](u64 sums, u64 equals) { return sums + (equals < ties ? equals : ties) * of_cut; };
+    if (upto(sum, equal) > goal && upto(sum - v, equal - n) <= goal) {
+        sum -= v;
+        equal -= n;
+        for (int i = b; i < e; ++i) {
+            const float x = ld_f32(row.x, i);
+            unsigned one = 0;
+            add(x, sum, one);
+            equal += one;
+            if (upto(sum, equal) > goal) {
+                write(i, x, total);
+                break;
+            }
+        }
+    }
+}
+
+// `coded`: the entries have been counted by their values (bf16); `counted`: how many of them there are
+template <typename T, bool PLAIN> __device__ __forceinline__ void sample_row(const SampleArgs &a, Shared &s, const Row<T> &row, int64_t r, float top, float temperature, Filters f, bool coded, u64 counted)
+{
+    const int tid = threadIdx.x;
     const Weights<PLAIN> w(top, temperature);
-    const unsigned none = key_of(-INFINITY), peak = key_of(top);
+    const unsigned none = key_of(-INFINITY);
     auto write = [&](int token, float x, u64 total) {
         a.tokens[r] = token;
         if (a.logp) a.logp[r] = w.distance(x) - logf((float)total * 0x1p-31f);
     };
+    auto full = [&](float x) { return weight_of(expf(w.distance(x))); };           // before min_p
+    auto kept = [&](float x) {
+        const float part = expf(w.distance(x));
+        return part >= f.min_p || x == top ? weight_of(part) : 0u;
+    };
     // a logit below which nothing is kept, whatever the other filters say: min_p, and weights of 0 (21.5 temperatures below)
     const float floor_p = w.below(f.min_p > 0.f ? logf(f.min_p) : -22.f);
+
+    if constexpr (sizeof(T) == 2) {
+        // 16 bits hold a counter unless more than 65535 entries are alike; then the counts add up to less than there are
+        u64 before, all;
+        float cut = -INFINITY;
+        u64 ties = 0;
+        if (coded && f.top_k < a.V) {
+            const u64 k64 = (u64)f.top_k;
+            const float v = first_value(s, [](float, unsigned n) -> u64 { return n; }, [&](u64 m, u64) { return m >= k64; }, &before, &all);
+            coded = all == counted;
+            if (all >= k64) {                          // otherwise top-k keeps every finite entry
+                cut = v;
+                ties = k64 - before;
+            }
+        } else if (coded && a.V > 65535) {
+            u64 v = 0;
+#pragma unroll 8
+            for (int i = tid; i < CODES; i += THREADS) v += (s.codes[i] & 0xFFFFu) + (s.codes[i] >> 16);
+            coded = block_sum(s, v) == counted;
+        }
+        if (coded) {
+            if (f.top_p < 1.f) {
+                const double p = (double)f.top_p;
+                const float cut_k = cut;
+                const u64 ties_k = ties;
+                auto entries = [&](float x, unsigned n) -> u64 { return x > cut_k ? n : x == cut_k ? ties_k : 0; };
+                cut = first_value(s, [&](float x, unsigned n) -> u64 { return full(x) * entries(x, n); }, [&](u64 m, u64 t) { return m != 0 && (double)m >= p * (double)t; }, &before, &all);
+                const double reach = p * (double)all;
+                const u64 each = full(cut);
+                ties = 1;
+                if (each) {                            // the fewest with which the line is reached
+                    ties = (u64)((reach - (double)before) / (double)each);
+                    while ((double)(before + ties * each) < reach) ++ties;
+                    while (ties > 1 && (double)(before + (ties - 1) * each) >= reach) --ties;
+                }
+            }
+            const float least = fmaxf(fmaxf(cut, value_of(none + 1u)), floor_p);
+            const unsigned high = key16_of(top), span = min(high - key16_of(least), (unsigned)(CODES - 1));
+            __syncthreads();
+            for (unsigned i = tid; i <= span; i += THREADS) s.codes[i] = kept(value16_of(high - i));       // the counts are done with
+            __syncthreads();
+            auto weight = [&](float x) -> unsigned {
+                const unsigned d = high - key16_of(x);
+                return d <= span ? s.codes[d] : kept(x);
+            };
+            draw_from_row(s, row, f.u, least, cut, least > cut ? 0 : ties, kept(cut), weight, write);
+            return;
+        }
+    }
     auto clear = [&] {
         __syncthreads();
         for (int i = tid; i < BINS; i += THREADS) s.bins[i] = 0;
-        if (tid == 0) s.entries = 0;
         __syncthreads();
     };
     // entries of at least `least`, and `in(x, i)`, into the list; their number, which may be more than it holds
     auto gather = [&](float least, auto in) {
+        __syncthreads();
+        if (tid == 0) s.entries = 0;
+        __syncthreads();
         row.each([&](int i, float x) {
             if (x < least || !in(x, i)) return;
             const int at = atomicAdd(&s.entries, 1);
@@ -303,6 +522,7 @@ template <typename T, bool PLAIN> __device__ __forceinline__ void sample_row(con
     unsigned cut = 0u;                                 // kept: keys above `cut`, and those equal to it up to index `last`
     int last = a.V;
     if (f.top_k < a.V) {
+        clear();
         // the last bin takes the far end of the row; it is not counted one by one, at one address, but taken to hold everything
         row.each([&](int, float x) {
             const int bin = bin_of(w.distance(x));
@@ -316,23 +536,23 @@ template <typename T, bool PLAIN> __device__ __forceinline__ void sample_row(con
         if (before + s.bins[bin] <= LIST) {
             const int n = gather(bin_floor(bin), [&](float x, int) { return bin_of(w.distance(x)) <= bin; });
             rank_list(s, w, n);
-            int kept = f.top_k;
+            int first = f.top_k;
             if (f.top_p < 1.f) {
                 u64 v = 0;
-                for (int i = tid; i < kept; i += THREADS) v += s.weight[i];
-                kept = ranks_to(s, kept, 0, (double)f.top_p * (double)block_sum(s, v));
+                for (int i = tid; i < first; i += THREADS) v += s.weight[i];
+                first = ranks_to(s, first, 0, (double)f.top_p * (double)block_sum(s, v));
             }
-            draw_from_list(s, w, f, kept, write);
+            draw_from_list(s, w, f, first, write);
             return;
         }
         prefix_by_digits(s, row, (double)f.top_k, [&](int, unsigned) -> u64 { return 1; }, cut, last);
-        clear();
     }
     if (f.top_p < 1.f) {
         const unsigned cut_k = cut;
         const int last_k = last;
         auto allowed = [&](int i, unsigned k) { return k > cut_k || (k == cut_k && i <= last_k); };
         auto measure = [&](int i, unsigned k) -> u64 { return allowed(i, k) ? weight_of(w.part(k)) : 0u; };
+        clear();
         if (cut_k == 0u)
             row.each([&](int, float x) {
                 const float q = w.distance(x);
@@ -362,9 +582,6 @@ template <typename T, bool PLAIN> __device__ __forceinline__ void sample_row(con
                 draw_from_list(s, w, f, ranks_to(s, n, 0, reach), write);
                 return;
             }
-            __syncthreads();
-            if (tid == 0) s.entries = 0;
-            __syncthreads();
         }
         const int m = gather(bin_floor(bin), [&](float x, int i) { return bin_of(w.distance(x)) == bin && allowed(i, key_of(x)); });
         if (m <= LIST) {
@@ -374,41 +591,15 @@ template <typename T, bool PLAIN> __device__ __forceinline__ void sample_row(con
             last = entry_index(e);
         } else prefix_by_digits(s, row, reach, measure, cut, last);
     }
-    // the draw: sums of the kept weights by the waves' parts, then by threads within the part that the goal falls into
-    const float least = fmaxf(value_of(max(cut, none + 1u)), floor_p);
-    auto kept = [&](int i, float x) -> unsigned {
-        if (!(x >= least)) return 0u;
-        const unsigned k = key_of(x);
-        if (k < cut || (k == cut && i > last)) return 0u;
-        const float part = w.part(k);
-        return part >= f.min_p || k == peak ? weight_of(part) : 0u;
-    };
-    u64 mine = 0;
-    row.each([&](int i, float x) { mine += kept(i, x); });
-    const u64 total = block_sum(s, mine);
-    u64 goal = goal_of(f.u, total);
-    int p = 0;
-    while (p < WAVES - 1 && s.sums[p] <= goal) goal -= s.sums[p++];
-    const int lo = row.part_begin(p), hi = row.part_end(p), each = (hi - lo + THREADS - 1) / THREADS;
-    const int b = min(hi, lo + tid * each), e = min(hi, b + each);
-    u64 v = 0;
-    for (int i = b; i < e; ++i) v += kept(i, ld_f32(row.x, i));
-    u64 sum = wave_scan(v);
-    __syncthreads();
-    if (lane == 63) s.sums[wave] = sum;
-    __syncthreads();
-    for (int k = 0; k < wave; ++k) sum += s.sums[k];
-    if (sum > goal && sum - v <= goal) {
-        u64 at = sum - v;
-        for (int i = b; i < e; ++i) {
-            const float x = ld_f32(row.x, i);
-            at += kept(i, x);
-            if (at > goal) {
-                write(i, x, total);
-                break;
-            }
-        }
+    // entries that equal the last one, up to it
+    const float value = cut > none ? value_of(cut) : -INFINITY;
+    u64 ties = 0;
+    if (cut > none) {
+        for (int i = tid; i <= min(last, a.V - 1); i += THREADS) ties += row.key(i) == cut;
+        ties = block_sum(s, ties);
     }
+    const float least = fmaxf(fmaxf(value, value_of(none + 1u)), floor_p);
+    draw_from_row(s, row, f.u, least, value, least > value ? 0 : ties, kept(value), kept, write);
 }
 
 template <typename T> __global__ __launch_bounds__(1024) void sample_kernel(SampleArgs a)
@@ -421,14 +612,31 @@ template <typename T> __global__ __launch_bounds__(1024) void sample_kernel(Samp
     const float temperature = a.temperature ? a.temperature[r] : 1.f;
     Filters f = {a.top_p ? a.top_p[r] : 1.f, a.min_p ? a.min_p[r] : 0.f, a.u[r], a.top_k ? a.top_k[r] : 0};
     if (f.top_k <= 0 || f.top_k > a.V) f.top_k = a.V;
-    for (int i = tid; i < BINS; i += THREADS) s.bins[i] = 0;
-    if (tid == 0) s.entries = 0;
+    const bool one = f.top_k == 1 || !(temperature > 0.f) || !(f.top_p > 0.f) || !(f.min_p <= 1.f);       // the first of the largest
+    const bool coded = sizeof(T) == 2 && !one && (f.top_k < a.V || f.top_p < 1.f);
     float top = -INFINITY;
-    row.each([&](int, float x) { top = fmaxf(top, x); });
+    unsigned counted = 0u;
+    if (coded) {
+        for (int i = tid * 4; i < CODES; i += THREADS * 4) *(uint4 *)&s.codes[i] = make_uint4(0u, 0u, 0u, 0u);
+        __syncthreads();
+        row.each([&](int, float x) {
+            top = fmaxf(top, x);
+            if (x > -INFINITY) {                       // not those that a mask took out: they are alike, and counters that are alike wait for each other
+                const unsigned bits = __float_as_uint(x + 0.f);      // both zeros alike
+                atomicAdd((unsigned *)((char *)s.codes + ((bits >> 14) & 0x1FFFCu)), (int)bits < 0 ? 1u : 0x10000u);
+                ++counted;
+            }
+        });
+    } else row.each([&](int, float x) { top = fmaxf(top, x); });
     for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-    if (lane == 0) s.sums[wave] = __float_as_uint(top);
+    const u64 in_wave = wave_sum(counted);
+    if (lane == 0) s.sums[wave] = (in_wave << 32) | __float_as_uint(top);
     __syncthreads();
-    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, __uint_as_float((unsigned)s.sums[w]));
+    u64 finite = 0;
+    for (int w = 0; w < WAVES; ++w) {
+        top = fmaxf(top, __uint_as_float((unsigned)s.sums[w]));
+        finite += s.sums[w] >> 32;
+    }
     top += 0.f;
     if (top == -INFINITY) {
         if (tid == 0) {
@@ -437,7 +645,7 @@ template <typename T> __global__ __launch_bounds__(1024) void sample_kernel(Samp
         }
         return;
     }
-    if (f.top_k == 1 || !(temperature > 0.f) || !(f.top_p > 0.f) || !(f.min_p <= 1.f)) {       // the first of the largest
+    if (one) {
         int first = a.V;
         row.each([&](int i, float x) { if (x == top) first = min(first, i); });
         for (int o = 32; o > 0; o >>= 1) first = min(first, __shfl_xor(first, o, 64));
@@ -451,8 +659,8 @@ template <typename T> __global__ __launch_bounds__(1024) void sample_kernel(Samp
         }
         return;
     }
-    if (temperature > 1e-18f && temperature < 1e18f && top < INFINITY) sample_row<T, false>(a, s, row, r, top, temperature, f);
-    else sample_row<T, true>(a, s, row, r, top, temperature, f);
+    if (temperature > 1e-18f && temperature < 1e18f && top < INFINITY) sample_row<T, false>(a, s, row, r, top, temperature, f, coded, finite);
+    else sample_row<T, true>(a, s, row, r, top, temperature, f, coded, finite);
 }
 
 LaunchInfo launch_sample(const TokenArgs &a, hipStream_t s, bool dry, int)
@@ -462,7 +670,7 @@ LaunchInfo launch_sample(const TokenArgs &a, hipStream_t s, bool dry, int)
     b.top_k = a.top_k; b.tokens = a.tokens; b.logp = a.logp;
     LaunchInfo li;
     li.workgroups = (a.b_hi - a.b_lo) * a.S;
-    li.threads = THREADS; li.lds_bytes = (int)sizeof(Shared); li.wg_per_cu = 2; li.kernel = a.dtype == DT_BF16 ? "sample_bf16" : "sample_f32"; li.phases = 1;
+    li.threads = THREADS; li.lds_bytes = (int)sizeof(Shared); li.wg_per_cu = 1; li.kernel = a.dtype == DT_BF16 ? "sample_bf16" : "sample_f32"; li.phases = 1;
     if (dry || !li.workgroups) return li;
     if (a.dtype == DT_BF16) GACER_LAUNCH(sample_kernel<unsigned short>, dim3(li.workgroups), dim3(THREADS), 0, s, b);
     else GACER_LAUNCH(sample_kernel<float>, dim3(li.workgroups), dim3(THREADS), 0, s, b);
