@@ -75,11 +75,31 @@ template <int PARTS> __device__ __forceinline__ void split_bf16(float v, unsigne
     }
 }
 
+// eight numbers whose upper 16 bits are bf16, as an operand
+__device__ __forceinline__ bf16x8 operand(unsigned a, unsigned b, unsigned c, unsigned d, unsigned e, unsigned f, unsigned g, unsigned h)
+{
+    return __builtin_bit_cast(bf16x8, make_uint4(__builtin_amdgcn_perm(b, a, 0x07060302u), __builtin_amdgcn_perm(d, c, 0x07060302u),
+                                                 __builtin_amdgcn_perm(f, e, 0x07060302u), __builtin_amdgcn_perm(h, g, 0x07060302u)));
+}
+// eight numbers as PARTS operands, one: rounded
+template <int PARTS> __device__ __forceinline__ void operands(const float *v, bf16x8 *out)
+{
+    if constexpr (PARTS == 1) {
+        out[0] = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])));
+    } else {
+        unsigned p[8][PARTS];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) split_bf16<PARTS>(v[e], p[e]);
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k) out[k] = operand(p[0][k], p[1][k], p[2][k], p[3][k], p[4][k], p[5][k], p[6][k], p[7][k]);
+    }
+}
+
 // the reference of a row that has seen no key yet; scores lie above it
 static constexpr float NO_SCORE = -1e38f;
 
-// a branch that stays one (uniform over the wave): as selects, every tile would pay for what only the first and the last need
-#define RARELY(cond) if (cond) if (([] { asm volatile(""); return true; })())
+// Keeps the (wave-uniform) branch around it a branch: as selects, every tile would pay for what only the first and the last need.
+template <typename V> __device__ __forceinline__ void in_branch(V &v) { asm volatile("" : "+v"(v)); }
 
 void launch_cache_attention_wide(const AttendArgs &b, int dtype, int D, int grid, hipStream_t s);      // rows of 128
 

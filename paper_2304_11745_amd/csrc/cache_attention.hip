@@ -194,8 +194,9 @@ template <typename T, int D, int ROWS, int NW> __global__ __launch_bounds__(NW *
 #pragma unroll
                 for (int e = 0; e < R4; ++e) s[m][e] = fmaf(sc[i], over_parts(d, e), fmaf(mm[i], qs[i][e], s[m][e]));
             }
-            RARELY(edge) {
-                const int p = p0 + m * 32 + l32;
+            if (edge) {
+                int p = p0 + m * 32 + l32;
+                in_branch(p);
 #pragma unroll
                 for (int e = 0; e < R4; ++e)
                     if (x.page[m] < 0 || p > at[e] || (a.window > 0 && p <= at[e] - a.window)) s[m][e] = -INFINITY;
@@ -203,9 +204,10 @@ template <typename T, int D, int ROWS, int NW> __global__ __launch_bounds__(NW *
 #pragma unroll
             for (int e = 0; e < R4; ++e) over |= s[m][e] - base[e] > 8.f;
         }
-        RARELY(__any(over)) {                          // some score is far above its row's reference: the tile's largest becomes the reference
+        if (__any(over)) {                             // some score is far above its row's reference: the tile's largest becomes the reference
 #pragma unroll
             for (int e = 0; e < R4; ++e) {
+                in_branch(s[0][e]);
                 float top = fmaxf(s[0][e], s[1][e]);
 #pragma unroll
                 for (int k = 16; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor(top, k, 64));
@@ -238,10 +240,12 @@ template <typename T, int D, int ROWS, int NW> __global__ __launch_bounds__(NW *
                     ps[e] = p[e] * sv;
                     pm[e] = p[e] * mv;
                 }
-                RARELY(edge) {                         // whatever the scales of a key that is not seen hold
+                if (edge) {                            // whatever the scales of a key that is not seen hold
 #pragma unroll
-                    for (int e = 0; e < R4; ++e)
+                    for (int e = 0; e < R4; ++e) {
+                        in_branch(ps[e]);
                         if (s[m][e] == -INFINITY) ps[e] = pm[e] = 0.f;
+                    }
                 }
 #pragma unroll
                 for (int e = 0; e < R4; ++e) {

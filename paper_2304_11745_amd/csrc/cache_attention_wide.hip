@@ -1,14 +1,15 @@
 // Attention of many rows (prompts) over a paged 4-bit cache.
 //
 // A workgroup takes 128 rows (heads x tokens of one key/value head), 32 to a wave, and 64 keys at a time.  The codes are turned into bf16 once
-// for all four waves and stand in LDS as the whole numbers c - 8: keys row by row, values feature by feature.  Scores are keys x rows (lane =
+// for all four waves and stand in LDS as the whole numbers c - 8 (the keys of bf16 tenants as 16 + c, which is half the work, and whose sums
+// lose less than the rounding of the queries has): keys row by row, values feature by feature.  Scores are keys x rows (lane =
 // row), so a row's weights stay in its lanes' registers and are the operand of the values' product, features x rows, as they are; the
 // order of the keys within that product is the one in which a lane holds them, and the values are stored in it.  As in the kernel for
 // few rows the scales are applied in fp32,
-//   q.k_j = sum over groups g of  s_jg * (sum_d q_d (c_jd - 8)) + (m_jg + 8 s_jg) * sum_d q_d
+//   q.k_j = sum over groups g of  s_jg * (sum_d q_d (c_jd - z)) + (m_jg + z s_jg) * sum_d q_d             (z = 8 or -16)
 //   out_d = sum_j (p_j s_jg) (c_jd - 8) + sum_j p_j (m_jg + 8 s_jg)
 // with the second sum of the scores as a further matrix instruction: the pair (s, m) of a key, two bf16 numbers, times the sums of the queries in
-// three bf16 parts; that of the result likewise in bf16 tenants, the weights times m + 8 s in two parts.  fp32 tenants have their queries and
+// three bf16 parts, and a one times the parts of minus the row's reference; that of the result likewise in bf16 tenants, the weights times m + 8 s in two parts.  fp32 tenants have their queries and
 // weights in three bf16 parts each, every part a matrix instruction, and add p_j (m + 8 s) as it is.  In bf16 tenants the weights p_j s_jg are rounded to bf16 once: with codes around zero that is as
 // much as the result's own rounding adds (2.2e-3 of the result together, 1.7e-3 for the latter alone), and a second part would be
 // 16 more matrix instructions per 64 keys and two more operations per weight.
@@ -18,30 +19,11 @@
 
 namespace gacer {
 
-// eight numbers whose upper 16 bits are bf16, as an operand
-__device__ __forceinline__ bf16x8 operand(unsigned a, unsigned b, unsigned c, unsigned d, unsigned e, unsigned f, unsigned g, unsigned h)
-{
-    return __builtin_bit_cast(bf16x8, make_uint4(__builtin_amdgcn_perm(b, a, 0x07060302u), __builtin_amdgcn_perm(d, c, 0x07060302u),
-                                                 __builtin_amdgcn_perm(f, e, 0x07060302u), __builtin_amdgcn_perm(h, g, 0x07060302u)));
-}
-// eight numbers as PARTS operands, one: rounded
-template <int PARTS> __device__ __forceinline__ void operands(const float *v, bf16x8 *out)
-{
-    if constexpr (PARTS == 1) {
-        out[0] = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])));
-    } else {
-        unsigned p[8][PARTS];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) split_bf16<PARTS>(v[e], p[e]);
-#pragma unroll
-        for (int k = 0; k < PARTS; ++k) out[k] = operand(p[0][k], p[1][k], p[2][k], p[3][k], p[4][k], p[5][k], p[6][k], p[7][k]);
-    }
-}
-
 template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void cache_attention_wide_kernel(AttendArgs a)
 {
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int QP = F32 ? 3 : 1, PP = F32 ? 3 : 1, MP = 2;                  // bf16 parts of queries, weights, and of the minima m + 8 s
+    constexpr float K_UNIT = F32 ? 16.f : 1.f, K_MIDDLE = F32 ? 8.f : -16.f;   // keys in LDS: (c - 8) / 16 or 16 + c; value of a step, of where they are zero
     constexpr int NG = D / 64, ROWS = 128, KROW = D * 2 + 16, VROW = 128 + 16, KROWS = 64 * KROW, VROWS = D * VROW;
     constexpr int EXT_K = 64 * 32, EXT_V = F32 ? NG * 64 * 4 : MP * NG * VROW, SCALES = 2 * NG * 64 * 4, BUF = KROWS + VROWS + EXT_K + EXT_V + SCALES;
     constexpr int ITEMS = 64 * D / 32;                 // 16-byte pieces of a tile's key codes, and of its value codes
@@ -97,7 +79,7 @@ template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 &&
         if (k_mine) {
             const unsigned w[4] = {kin.x, kin.y, kin.z, kin.w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) *(bf16x8 *)(buf + kkey * KROW + kpart * 64 + i * 16) = codes_around(w[i]);
+            for (int i = 0; i < 4; ++i) *(bf16x8 *)(buf + kkey * KROW + kpart * 64 + i * 16) = F32 ? codes_around(w[i]) : codes_above(w[i], 0x41804180u);
         }
         if (v_mine) {                                  // of each 16 keys first those that half 0 of a wave holds: 0..3 and 8..11, then 4..7 and 12..15
             const unsigned w[4] = {vin.x, vin.y, vin.z, vin.w};
@@ -117,7 +99,7 @@ template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 &&
             for (int i = 0; i < NG; ++i) {
                 const float sc = scale_of(sin[i]), m = minimum_of(sin[i]);
                 if (tid < 64) {
-                    scales[i * 64 + skey] = sc * 16.f * a.scale;
+                    scales[i * 64 + skey] = sc * K_UNIT * a.scale;
                     e[i] = sin[i];
                 } else {
                     scales[(NG + i) * 64 + skey] = sc * 16.f;
@@ -132,10 +114,10 @@ template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 &&
                     for (int k = 0; k < MP; ++k) *(unsigned short *)(buf + KROWS + VROWS + EXT_K + (MP * i + k) * VROW + slot * 2) = (unsigned short)(part[k] >> 16);
                 }
             }
-            if (tid < 64) {                            // slots 0..7: the pairs of the groups, twice; 8..15: once more and zeros
+            if (tid < 64) {                            // slots 0..7: the pairs of the groups, twice; 8..11: once more; 12..14: ones, for the reference
                 unsigned char *x = buf + KROWS + VROWS + skey * 32;
                 *(uint4 *)x = NG == 2 ? make_uint4(e[0], e[1], e[0], e[1]) : make_uint4(e[0], e[0], e[0], 0u);
-                *(uint4 *)(x + 16) = NG == 2 ? make_uint4(e[0], e[1], 0u, 0u) : make_uint4(0u, 0u, 0u, 0u);
+                *(uint4 *)(x + 16) = make_uint4(NG == 2 ? e[0] : 0u, NG == 2 ? e[1] : 0u, 0x3F803F80u, 0x3F80u);
             }
         }
     };
@@ -163,18 +145,18 @@ template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 &&
 #pragma unroll
             for (int k = 0; k < QP; ++k) q[k][i] = operand(part[0][k], part[1][k], part[2][k], part[3][k], part[4][k], part[5][k], part[6][k], part[7][k]);
         }
-        unsigned pair[NG][3];                          // parts of (8 sum, sum) of each group, as they meet (scale, minimum)
+        unsigned pair[NG][3];                          // parts of (K_MIDDLE sum, sum) of each group, as they meet (scale, minimum)
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
             const float all = (sum[i] + __shfl_xor(sum[i], 32, 64)) * a.scale;
             unsigned p8[3], p1[3];
-            split_bf16<3>(8.f * all, p8);
+            split_bf16<3>(K_MIDDLE * all, p8);
             split_bf16<3>(all, p1);
 #pragma unroll
             for (int k = 0; k < 3; ++k) pair[i][k] = __builtin_amdgcn_perm(p1[k], p8[k], 0x07060302u);
         }
         const uint4 first = NG == 2 ? make_uint4(pair[0][0], pair[NG - 1][0], pair[0][1], pair[NG - 1][1]) : make_uint4(pair[0][0], pair[0][1], pair[0][2], 0u);
-        const uint4 second = NG == 2 ? make_uint4(pair[0][2], pair[NG - 1][2], 0u, 0u) : make_uint4(0u, 0u, 0u, 0u);
+        const uint4 second = NG == 2 ? make_uint4(pair[0][2], pair[NG - 1][2], 0u, 0u) : make_uint4(0u, 0u, 0u, 0u);       // the reference is 0
         qx = __builtin_bit_cast(bf16x8, half ? second : first);
     }
     const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -203,7 +185,7 @@ template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 &&
         }
         x = mfma(*(const bf16x8 *)(buf + KROWS + VROWS + (m * 32 + l32) * 32 + half * 16), qx, zero);
         const float *scales = (const float *)(buf + KROWS + VROWS + EXT_K + EXT_V) + m * 32 + half * 4;
-        float s[16], top = -INFINITY;                  // scores above the reference: subtracted first, so that those that count are small when they are rounded
+        float s[16], top = -INFINITY;                  // scores above the reference, which the extra product takes off: those that count are small when they are rounded
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             float4 sc[NG];
@@ -211,26 +193,38 @@ template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 &&
             for (int i = 0; i < NG; ++i) sc[i] = *(const float4 *)(scales + i * 64 + k * 8);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                float v = x[4 * k + e] - base;
+                float v = x[4 * k + e];
 #pragma unroll
                 for (int i = 0; i < NG; ++i) v = fmaf(e == 0 ? sc[i].x : e == 1 ? sc[i].y : e == 2 ? sc[i].z : sc[i].w, d[i][4 * k + e], v);
                 s[4 * k + e] = v;
             }
         }
-        RARELY(edge) {
+        if (edge) {
+            int q0 = p0 + 4 * half;
+            in_branch(q0);
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                const int p = p0 + 8 * (e >> 2) + 4 * half + (e & 3);
+                const int p = q0 + 8 * (e >> 2) + (e & 3);
                 if (gone || p > at || (a.window > 0 && p <= at - a.window)) s[e] = -INFINITY;
             }
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) top = fmaxf(top, s[e]);
-        RARELY(__any(top > 8.f || (l == 0.f && top > -INFINITY))) {      // the largest score so far becomes the reference, and the first one
+        if (__any(top > 8.f || (l == 0.f && top > -INFINITY))) {      // the largest score so far becomes the reference, and the first one
+            in_branch(top);
             const bool first = l + __shfl_xor(l, 32, 64) == 0.f;
             top = fmaxf(top, __shfl_xor(top, 32, 64));
             const float up = top == -INFINITY ? 0.f : first ? top : fmaxf(top, 0.f), f = first ? 1.f : __builtin_amdgcn_exp2f(-up);
             base += up;
+            unsigned part[3];
+            split_bf16<3>(-base, part);
+            base = -(__uint_as_float(part[0] & 0xFFFF0000u) + __uint_as_float(part[1] & 0xFFFF0000u) + __uint_as_float(part[2] & 0xFFFF0000u));
+            if (half) {
+                uint4 u = __builtin_bit_cast(uint4, qx);
+                u.z = __builtin_amdgcn_perm(part[1], part[0], 0x07060302u);
+                u.w = part[2] >> 16;
+                qx = __builtin_bit_cast(bf16x8, u);
+            }
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[e] -= up;
             l *= f;
@@ -260,7 +254,9 @@ template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 &&
                 const float4 s0 = *(const float4 *)(scales + (NG + i) * 64 + k * 16), s1 = *(const float4 *)(scales + (NG + i) * 64 + k * 16 + 8);
                 float v[8] = {p[8 * k] * s0.x, p[8 * k + 1] * s0.y, p[8 * k + 2] * s0.z, p[8 * k + 3] * s0.w,
                               p[8 * k + 4] * s1.x, p[8 * k + 5] * s1.y, p[8 * k + 6] * s1.z, p[8 * k + 7] * s1.w};
-                RARELY(edge) {                         // whatever the scales of a key that is not seen hold
+                if (edge) {                            // whatever the scales of a key that is not seen hold
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) in_branch(v[e]);
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
                         if (s[8 * k + e] == -INFINITY) v[e] = 0.f;
@@ -275,7 +271,9 @@ template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 &&
                     const float4 m0 = *(const float4 *)(mm + i * 64), m1 = *(const float4 *)(mm + i * 64 + 8);
                     float v[8] = {p[8 * k] * m0.x, p[8 * k + 1] * m0.y, p[8 * k + 2] * m0.z, p[8 * k + 3] * m0.w,
                                   p[8 * k + 4] * m1.x, p[8 * k + 5] * m1.y, p[8 * k + 6] * m1.z, p[8 * k + 7] * m1.w};
-                    RARELY(edge) {
+                    if (edge) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) in_branch(v[e]);
 #pragma unroll
                         for (int e = 0; e < 8; ++e)
                             if (s[8 * k + e] == -INFINITY) v[e] = 0.f;
@@ -284,9 +282,10 @@ template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 &&
                 }
             } else {
                 bf16x8 mx = *(const bf16x8 *)(buf + KROWS + VROWS + EXT_K + min(l32, MP * NG - 1) * VROW + at_key);
-                RARELY(edge) {                             // the same for their minima: an operand that holds no NaN
+                if (edge) {                                // the same for their minima: an operand that holds no NaN
                     uint4 u = __builtin_bit_cast(uint4, mx);
                     unsigned *e = (unsigned *)&u;
+                    asm volatile("" : "+v"(e[0]));
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         if ((e[i] & 0x7F80u) == 0x7F80u) e[i] &= 0xFFFF0000u;
