@@ -34,7 +34,7 @@ struct SampleArgs {
     float *logp;
 };
 
-static constexpr int THREADS = 1024, WAVES = THREADS / 64, BINS = 2048, LIST = 2048, CODES = 32768, GROUPS = 512;
+static constexpr int THREADS = 1024, WAVES = THREADS / 64, BINS = 2048, LIST = 2048, CODES = 32768, GROUPS = 512, PEAKS = 768;
 // Entries that a list may hold where the alternative is another pass over the row: ranks by counting take n steps of a thread and more, a pass over 131072
 // entries what 600 of them take.
 static constexpr int SHORT = 512;
@@ -49,6 +49,10 @@ __device__ __forceinline__ unsigned key_of(float x)
 __device__ __forceinline__ float value_of(unsigned key) { return __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xFFFFFFFFu)); }
 
 __device__ __forceinline__ unsigned weight_of(float part) { return (unsigned)(part * 2147483648.f); }
+
+// a logit that stands `d` temperatures (d <= 0) and a little below the top: no entry whose distance is d or more is smaller
+__device__ __forceinline__ float below_top(float top, float temperature, float d) { return top + temperature * (d * 1.0001f - 0.001f); }
+static constexpr float WEIGHTLESS = -22.f;             // 2^31 exp(d) < 1 from here down
 
 // Weights of a row.  PLAIN: only a division is safe (a temperature very small or large, an infinite top).
 template <bool PLAIN> struct Weights {
@@ -66,29 +70,58 @@ template <bool PLAIN> struct Weights {
         return __fmaf_rn(__fmaf_rn(-q, temperature, a), inverse, q);
     }
     __device__ __forceinline__ float part(unsigned key) const { return expf(distance(value_of(key))); }
-    // a logit that stands `d` temperatures (d <= 0) and a little below the top: no entry whose distance is d or more is smaller
-    __device__ __forceinline__ float below(float d) const { return top + temperature * (d * 1.0001f - 0.001f); }
+    __device__ __forceinline__ float below(float d) const { return below_top(top, temperature, d); }
 };
 __device__ __forceinline__ int bin_of(float distance) { return min(BINS - 1, (int)(distance * -64.f)); }
 
-__device__ __forceinline__ u64 wave_sum(u64 v)
+// Sums over a wave, all lanes active, by moves within and between its rows of 16 lanes (a shuffle goes through LDS and takes ten times as long)
+template <int MOVE, int ROWS> __device__ __forceinline__ u64 moved(u64 v)
 {
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
+    return (u64)(unsigned)__builtin_amdgcn_update_dpp(0, (int)(v >> 32), MOVE, ROWS, 0xf, false) << 32 | (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, MOVE, ROWS, 0xf, false);
 }
-// sum over lanes 0..lane
+// sum over lanes 0..lane: lanes to the right by 1, 2, 4, 8 in a row, then a row's last lane to the next row, then lane 31 to the upper half
 __device__ __forceinline__ u64 wave_scan(u64 v)
 {
-    const int lane = threadIdx.x & 63;
-    for (int o = 1; o < 64; o <<= 1) {
-        const u64 n = __shfl_up(v, o, 64);
-        if (lane >= o) v += n;
-    }
+    v += moved<0x111, 0xf>(v);
+    v += moved<0x112, 0xf>(v);
+    v += moved<0x114, 0xf>(v);
+    v += moved<0x118, 0xf>(v);
+    v += moved<0x142, 0xa>(v);
+    v += moved<0x143, 0xc>(v);
     return v;
 }
+__device__ __forceinline__ u64 lane_of(u64 v, int lane) { return (u64)(unsigned)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)v, lane); }
+__device__ __forceinline__ u64 wave_sum(u64 v) { return lane_of(wave_scan(v), 63); }
+template <int MOVE, int ROWS> __device__ __forceinline__ float larger(float v)
+{
+    return fmaxf(v, __uint_as_float((unsigned)__builtin_amdgcn_update_dpp((int)0xFF800000u, (int)__float_as_uint(v), MOVE, ROWS, 0xf, false)));
+}
+__device__ __forceinline__ float wave_max(float v)
+{
+    v = larger<0x118, 0xf>(larger<0x114, 0xf>(larger<0x112, 0xf>(larger<0x111, 0xf>(v))));
+    v = larger<0x143, 0xc>(larger<0x142, 0xa>(v));
+    return __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63));
+}
+
+struct Shared {
+    u64 sums[WAVES], groups[GROUPS], before, all;
+    unsigned equal[WAVES];
+    float value;
+    int entries, found;
+    unsigned best, low;                                // keys of the largest logit so far, and of the lowest line from which entries were counted
+    unsigned short peaks[WAVES][PEAKS];                // the upper 16 bits of the largest of each two vectors of a lane, in the order of the first pass
+    union {
+        unsigned codes[CODES];                         // entries by the code of their magnitude: positive ones in the upper half, negative ones in the lower
+        struct {
+            u64 bins[BINS], list[LIST];                // list: key, then the index's complement, so that larger numbers come first in the order
+            unsigned weight[LIST];                     // of the list's entries, by rank
+            int place[LIST];                           // and where they stand in it
+        };
+    };
+};
 
 template <typename T> struct Row {
-    static constexpr int VEC = 16 / sizeof(T), DEPTH = 4;
+    static constexpr int VEC = 16 / sizeof(T), DEPTH = 4, BATCH = 2;
     const T *x;
     int V, head, vectors, per;                         // entries before the first 16-byte boundary, vectors after it, vectors of a wave's part
 
@@ -103,8 +136,9 @@ template <typename T> struct Row {
     __device__ unsigned key(int i) const { return key_of(ld_f32(x, i)); }
     __device__ int part_begin(int w) const { return w == 0 ? 0 : head + min(w * per, vectors) * VEC; }
     __device__ int part_end(int w) const { return w == WAVES - 1 ? V : head + min((w + 1) * per, vectors) * VEC; }
-    // f(index, logit) for the entries of the wave's part, DEPTH vectors of a lane in flight
-    template <typename F> __device__ __forceinline__ void each(F f) const
+    // f(index, logit) for the entries of the wave's part, DEPTH vectors of a lane in flight.  LONG: a body of many instructions stands there once per
+    // element of a vector and not DEPTH times (what a wave runs through once comes from beyond the instruction cache).
+    template <bool LONG = false, typename F> __device__ __forceinline__ void each(F f) const
     {
         const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
         const int b = min(vectors, (wave + 1) * per);
@@ -113,32 +147,116 @@ template <typename T> struct Row {
             Vec<T, VEC> in[DEPTH];
 #pragma unroll
             for (int k = 0; k < DEPTH; ++k) in[k] = ld_vec<T, VEC>(body, (int64_t)min(v + 64 * k, b - 1) * VEC);
+            if constexpr (LONG) {
+#pragma unroll 1
+                for (int k = 0; k < DEPTH; ++k) {
+                    if (v + 64 * k >= b) break;
 #pragma unroll
-            for (int k = 0; k < DEPTH; ++k) {
-                if (v + 64 * k >= b) break;
+                    for (int e = 0; e < VEC; ++e) f(head + (v + 64 * k) * VEC + e, in[0].get(e));
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) f(head + (v + 64 * k) * VEC + e, in[k].get(e));
+                    for (int j = 1; j < DEPTH; ++j) in[j - 1] = in[j];
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < DEPTH; ++k) {
+                    if (v + 64 * k >= b) break;
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) f(head + (v + 64 * k) * VEC + e, in[k].get(e));
+                }
             }
         }
-        const int rest = V - head - vectors * VEC;
-        if (wave == 0 && lane < head) f(lane, ld_f32(x, lane));
-        if (wave == WAVES - 1 && lane < rest) f(V - rest + lane, ld_f32(x, V - rest + lane));
+        if (border() >= 0) f(border(), ld_f32(x, border()));
     }
-};
-
-struct Shared {
-    u64 sums[WAVES], groups[GROUPS], before, all;
-    unsigned equal[WAVES];
-    float value;
-    int entries, found;
-    union {
-        unsigned codes[CODES];                         // entries by the code of their magnitude: positive ones in the upper half, negative ones in the lower
-        struct {
-            u64 bins[BINS], list[LIST];                // list: key, then the index's complement, so that larger numbers come first in the order
-            unsigned weight[LIST];                     // of the list's entries, by rank
-            int place[LIST];                           // and where they stand in it
+    // the lane's entry among those before and behind the vectors, -1: none
+    __device__ __forceinline__ int border() const
+    {
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, rest = V - head - vectors * VEC;
+        return wave == 0 && lane < head ? lane : wave == WAVES - 1 && lane < rest ? V - rest + lane : -1;
+    }
+    // batches of BATCH vectors a lane in a wave's part
+    __device__ int batches() const { return (per + 64 * BATCH - 1) / (64 * BATCH); }
+    __device__ __forceinline__ void fetch(int turn, Vec<T, VEC> *in) const
+    {
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, b = min(vectors, (wave + 1) * per);
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) in[k] = ld_vec<T, VEC>(x + head, (int64_t)max(0, min(wave * per + lane + (turn * BATCH + k) * 64, b - 1)) * VEC);
+    }
+    // The first pass over bf16 logits: the largest, its key in s.best; counters of the entries by value, but for those that weigh nothing even
+    // against the largest so far; peaks of two vectors each.  `in`: the first batch.  Returns the number of the lane's counted entries.
+    __device__ __forceinline__ unsigned count(Shared &s, float temperature, Vec<T, VEC> *in) const
+    {
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+        const int first = wave * per + lane, b = min(vectors, (wave + 1) * per), turns = batches();
+        unsigned counted = 0u;
+        auto line = [&](float most) {                  // from which entries count
+            most = wave_max(most);
+            if (lane == 0) atomicMax(&s.best, key_of(most));
+            const float from = fmaxf(below_top(value_of(*(volatile unsigned *)&s.best), temperature, WEIGHTLESS), -3.4028235e38f);
+            if (lane == 0) atomicMin(&s.low, key_of(from));
+            return from;
         };
-    };
+        auto add = [&](float v, float from) {
+            if (!(v >= from)) return;
+            const unsigned bits = __float_as_uint(v + 0.f);              // both zeros alike
+            atomicAdd((unsigned *)((char *)s.codes + ((bits >> 14) & 0x1FFFCu)), (int)bits < 0 ? 1u : 0x10000u);
+            ++counted;
+        };
+        const bool peaked = turns * (BATCH * 32) <= PEAKS;
+        auto batch = [&](int turn, const Vec<T, VEC> *in) {
+            float peak[BATCH / 2], most = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < BATCH / 2; ++k) {
+                peak[k] = -INFINITY;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) peak[k] = fmaxf(peak[k], fmaxf(in[2 * k].get(e), in[2 * k + 1].get(e)));
+                if (peaked) s.peaks[wave][(turn * (BATCH / 2) + k) * 64 + lane] = (unsigned short)(__float_as_uint(peak[k]) >> 16);
+            }
+#pragma unroll
+            for (int k = 0; k < BATCH / 2; ++k) most = fmaxf(most, peak[k]);
+            const float from = line(most);
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) {
+                if (first + (turn * BATCH + k) * 64 >= b || !(peak[k / 2] >= from)) continue;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) add(in[k].get(e), from);
+            }
+        };
+        Vec<T, VEC> next[BATCH];
+        for (int turn = 0; turn < turns; turn += 2) {  // one batch on its way while the other is counted
+            fetch(turn + 1, next);
+            batch(turn, in);
+            if (turn + 1 == turns) break;
+            fetch(turn + 2, in);
+            batch(turn + 1, next);
+        }
+        if (__any(border() >= 0)) {
+            const float mine = border() >= 0 ? ld_f32(x, border()) : -INFINITY;
+            add(mine, line(mine));
+        }
+        return counted;
+    }
+    // f(logit) for the entries of the wave's part whose peak reaches `least`, and perhaps more
+    template <typename F> __device__ __forceinline__ void each_above(const unsigned short *peaks, float least, F f) const
+    {
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, first = wave * per + lane, b = min(vectors, (wave + 1) * per);
+        unsigned hits = 0u;
+        for (int i = 0; i < batches() * (BATCH / 2); ++i)
+            if (__uint_as_float((unsigned)peaks[i * 64 + lane] << 16) >= least) hits |= 1u << i;
+        while (hits) {
+            const int v = first + __builtin_ctz(hits) * 128;
+            hits &= hits - 1;
+            Vec<T, VEC> in[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) in[k] = ld_vec<T, VEC>(x + head, (int64_t)min(v + 64 * k, b - 1) * VEC);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                if (v + 64 * k >= b) break;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) f(in[k].get(e));
+            }
+        }
+        if (border() >= 0) f(ld_f32(x, border()));
+    }
 };
 
 __device__ __forceinline__ u64 entry_of(unsigned key, int i) { return (u64)key << 32 | (unsigned)~i; }
@@ -192,12 +310,21 @@ __device__ __forceinline__ unsigned key16_of(float x)
 }
 __device__ __forceinline__ float value16_of(unsigned k) { return __uint_as_float((k & 0x8000u ? k ^ 0x8000u : k ^ 0xFFFFu) << 16); }
 
-// The largest value up to and with which the measure of the counted entries, from the largest value on, reaches the line; `before` receives the measure
-// of larger ones, `all` of the row.  measure(value, entries) of a value; reached(measure, all).  Groups of 128 values are added by a wave
-// each, then scanned; the first 256 groups are those of the positive values.
-template <typename M, typename D> __device__ float first_value(Shared &s, M measure, D reached, u64 *before, u64 *all)
+// group of the value with these upper bits of magnitude, see first_value()
+__device__ __forceinline__ int group_of(float x)
 {
-    constexpr int HALF = GROUPS / 2, EACH = GROUPS / WAVES, AHEAD = 8;
+    const unsigned b = __float_as_uint(x);
+    const int m = (int)(b >> 23 & 255u);
+    return b >> 31 ? GROUPS / 2 + m : GROUPS / 2 - 1 - m;
+}
+
+// The largest value up to and with which the measure of the counted entries, from the largest value on, reaches the line; `before` receives the measure
+// of larger ones, `all` of the row, `counted` the sum of the counts.  measure(value, entries) of a value; reached(measure, all).  Groups of 128 values (a
+// power of two and a sign) are added by a wave each, then scanned; the first 256 groups are those of the positive values.  `range`: first and last
+// group that holds any.
+template <typename M, typename D> __device__ __forceinline__ float first_value(Shared &s, int2 range, M measure, D reached, u64 *before, u64 *all, u64 *counted)
+{
+    constexpr int HALF = GROUPS / 2;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     // the lane's two counters of a group, of the larger value first: magnitudes of positive values fall, of negative ones rise
     auto counters = [&](int group) {
@@ -209,22 +336,25 @@ template <typename M, typename D> __device__ float first_value(Shared &s, M meas
         const int m = group < HALF ? (HALF - 1 - group) * 128 + 127 - 2 * lane - which : (group - HALF) * 128 + 2 * lane + which;
         return __uint_as_float((unsigned)m << 16 | (group < HALF ? 0u : 0x80000000u));
     };
-    for (int i = 0; i < EACH; i += AHEAD) {
-        uint2 n[AHEAD];
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) n[k] = counters(wave + WAVES * (i + k));
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            const int g = wave + WAVES * (i + k);
-            u64 v = 0;
-            if (__any((n[k].x | n[k].y) != 0u)) {
-                if (n[k].x) v += measure(value(g, 0), n[k].x);
-                if (n[k].y) v += measure(value(g, 1), n[k].y);
-                v = wave_sum(v);
-            }
-            if (lane == 0) s.groups[g] = v;
+    __syncthreads();                                   // all have read what stands in s.sums and s.groups
+    for (int i = tid; i < GROUPS; i += THREADS) s.groups[i] = 0;
+    __syncthreads();
+    unsigned entries = 0u;
+    for (int g = range.x + ((wave - range.x) & (WAVES - 1)); g <= range.y; g += WAVES) {
+        const uint2 n = counters(g);
+        if (!__any((n.x | n.y) != 0u)) continue;
+        entries += n.x + n.y;
+        u64 v = 0;
+#pragma unroll 1
+        for (int k = 0; k < 2; ++k) {
+            const unsigned c = k ? n.y : n.x;
+            if (c) v += measure(value(g, k), c);
         }
+        v = wave_sum(v);
+        if (lane == 0) s.groups[g] = v;
     }
+    const u64 in_wave = wave_sum(entries);
+    if (lane == 0) s.sums[wave] = in_wave;
     __syncthreads();
     if (wave == 0) {
         u64 part[GROUPS / 64], v = 0;                  // eight groups of a lane
@@ -233,7 +363,7 @@ template <typename M, typename D> __device__ float first_value(Shared &s, M meas
             part[i] = s.groups[lane * (GROUPS / 64) + i];
             v += part[i];
         }
-        const u64 upto = wave_scan(v), total = __shfl(upto, 63, 64);
+        const u64 upto = wave_scan(v), total = lane_of(upto, 63);
         u64 sum = upto - v, at = 0;
         int g = 0;
         bool found = false;
@@ -248,8 +378,8 @@ template <typename M, typename D> __device__ float first_value(Shared &s, M meas
         }
         const u64 mine = __ballot(found);
         const int l = mine ? __builtin_ctzll(mine) : 63;
-        g = l * (GROUPS / 64) + __shfl(g, l, 64);
-        at = __shfl(at, l, 64);
+        g = l * (GROUPS / 64) + __builtin_amdgcn_readlane(g, l);
+        at = lane_of(at, l);
         const uint2 n = counters(g);
         const u64 x = n.x ? measure(value(g, 0), n.x) : 0, y = n.y ? measure(value(g, 1), n.y) : 0, in = at + wave_scan(x + y);
         const u64 hit = __ballot(reached(in, total));
@@ -263,6 +393,8 @@ template <typename M, typename D> __device__ float first_value(Shared &s, M meas
     __syncthreads();
     *before = s.before;
     *all = s.all;
+    *counted = 0;
+    for (int w = 0; w < WAVES; ++w) *counted += s.sums[w];
     return s.value;
 }
 
@@ -292,7 +424,7 @@ __device__ int ranks_to(Shared &s, int n, u64 before, double reach)
                 r = i + __builtin_ctzll(hit) + 1;
                 break;
             }
-            before = __shfl(v, 63, 64);
+            before = lane_of(v, 63);
         }
         if (threadIdx.x == 0) s.found = r;
     }
@@ -365,7 +497,7 @@ template <typename W, typename F> __device__ void draw_from_list(Shared &s, cons
 
 // What the draw needs to know of a kept set: weights, by value, of entries above `cut`, and `ties` entries, by index, that equal it.  Sums over
 // the waves' parts of the row, then over threads within the part that the goal falls into, then one by one.
-template <typename T, typename K, typename F> __device__ __forceinline__ void draw_from_row(Shared &s, const Row<T> &row, float u, float least, float cut, u64 ties, unsigned of_cut, K weight, F write)
+template <bool LONG, typename T, typename K, typename F> __device__ __forceinline__ void draw_from_row(Shared &s, const Row<T> &row, bool peaked, float u, float least, float cut, u64 ties, unsigned of_cut, K weight, F write)
 {
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     // entries below `least` (which is not below `cut`) weigh nothing
@@ -376,7 +508,8 @@ template <typename T, typename K, typename F> __device__ __forceinline__ void dr
     };
     u64 v = 0;
     unsigned n = 0;
-    row.each([&](int, float x) { add(x, v, n); });
+    if (peaked) row.each_above(s.peaks[wave], least, [&](float x) { add(x, v, n); });
+    else row.template each<LONG>([&](int, float x) { add(x, v, n); });
     v = wave_sum(v);
     n = (unsigned)wave_sum(n);
     __syncthreads();
@@ -404,7 +537,27 @@ template <typename T, typename K, typename F> __device__ __forceinline__ void dr
     const int b = min(hi, lo + tid * each), e = min(hi, b + each);
     v = 0;
     n = 0;
-    for (int i = b; i < e; ++i) add(ld_f32(row.x, i), v, n);
+    constexpr int TOGETHER = 8;
+    auto load = [&](int i, float *in) {
+#pragma unroll
+        for (int k = 0; k < TOGETHER; ++k) in[k] = ld_f32(row.x, min(i + k, row.V - 1));
+    };
+    for (int i = b; i < e; i += TOGETHER) {
+        float in[TOGETHER];
+        load(i, in);
+        if constexpr (LONG) {
+#pragma unroll 1
+            for (int k = 0; k < TOGETHER; ++k) {
+                if (i + k < e) add(in[0], v, n);
+#pragma unroll
+                for (int j = 1; j < TOGETHER; ++j) in[j - 1] = in[j];
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < TOGETHER; ++k)
+                if (i + k < e) add(in[k], v, n);
+        }
+    }
     u64 sum = wave_scan(v), equal = wave_scan(n);
     __syncthreads();
     if (lane == 63) {
@@ -420,15 +573,18 @@ template <typename T, typename K, typename F> __device__ __forceinline__ void dr
     if (upto(sum, equal) > goal && upto(sum - v, equal - n) <= goal) {
         sum -= v;
         equal -= n;
+        float in[TOGETHER] = {};
         for (int i = b; i < e; ++i) {
-            const float x = ld_f32(row.x, i);
+            if (((i - b) & (TOGETHER - 1)) == 0) load(i, in);
             unsigned one = 0;
-            add(x, sum, one);
+            add(in[0], sum, one);
             equal += one;
             if (upto(sum, equal) > goal) {
-                write(i, x, total);
+                write(i, in[0], total);
                 break;
             }
+#pragma unroll
+            for (int j = 1; j < TOGETHER; ++j) in[j - 1] = in[j];
         }
     }
 }
@@ -449,53 +605,51 @@ template <typename T, bool PLAIN> __device__ __forceinline__ void sample_row(con
         return part >= f.min_p || x == top ? weight_of(part) : 0u;
     };
     // a logit below which nothing is kept, whatever the other filters say: min_p, and weights of 0 (21.5 temperatures below)
-    const float floor_p = w.below(f.min_p > 0.f ? logf(f.min_p) : -22.f);
+    const float floor_p = w.below(f.min_p > 0.f ? logf(f.min_p) : WEIGHTLESS);
 
     if constexpr (sizeof(T) == 2) {
         // 16 bits hold a counter unless more than 65535 entries are alike; then the counts add up to less than there are
         u64 before, all;
         float cut = -INFINITY;
         u64 ties = 0;
+        const u64 finite = counted;
+        const int2 range = make_int2(group_of(top), group_of(value_of(s.low)));
         if (coded && f.top_k < a.V) {
             const u64 k64 = (u64)f.top_k;
-            const float v = first_value(s, [](float, unsigned n) -> u64 { return n; }, [&](u64 m, u64) { return m >= k64; }, &before, &all);
-            coded = all == counted;
+            const float v = first_value(s, range, [](float, unsigned n) -> u64 { return n; }, [&](u64 m, u64) { return m >= k64; }, &before, &all, &counted);
             if (all >= k64) {                          // otherwise top-k keeps every finite entry
                 cut = v;
                 ties = k64 - before;
             }
-        } else if (coded && a.V > 65535) {
-            u64 v = 0;
-#pragma unroll 8
-            for (int i = tid; i < CODES; i += THREADS) v += (s.codes[i] & 0xFFFFu) + (s.codes[i] >> 16);
-            coded = block_sum(s, v) == counted;
         }
-        if (coded) {
-            if (f.top_p < 1.f) {
-                const double p = (double)f.top_p;
-                const float cut_k = cut;
-                const u64 ties_k = ties;
-                auto entries = [&](float x, unsigned n) -> u64 { return x > cut_k ? n : x == cut_k ? ties_k : 0; };
-                cut = first_value(s, [&](float x, unsigned n) -> u64 { return full(x) * entries(x, n); }, [&](u64 m, u64 t) { return m != 0 && (double)m >= p * (double)t; }, &before, &all);
-                const double reach = p * (double)all;
-                const u64 each = full(cut);
-                ties = 1;
-                if (each) {                            // the fewest with which the line is reached
-                    ties = (u64)((reach - (double)before) / (double)each);
-                    while ((double)(before + ties * each) < reach) ++ties;
-                    while (ties > 1 && (double)(before + (ties - 1) * each) >= reach) --ties;
-                }
+        const float cut_k = cut;
+        const u64 ties_k = ties;
+        if (coded && counted == finite && f.top_p < 1.f) {
+            const double p = (double)f.top_p;
+            auto entries = [&](float x, unsigned n) -> unsigned { return x > cut_k ? n : x == cut_k ? (unsigned)ties_k : 0u; };
+            cut = first_value(s, range, [&](float x, unsigned n) -> u64 { return (u64)full(x) * entries(x, n); }, [&](u64 m, u64 t) { return m != 0 && (double)m >= p * (double)t; }, &before, &all, &counted);
+            const double reach = p * (double)all;
+            const u64 each = full(cut);
+            ties = 1;
+            if (each) {                                // the fewest with which the line is reached
+                ties = (u64)((reach - (double)before) / (double)each);
+                while ((double)(before + ties * each) < reach) ++ties;
+                while (ties > 1 && (double)(before + (ties - 1) * each) >= reach) --ties;
             }
+        }
+        coded = coded && counted == finite;
+        if (coded) {
             const float least = fmaxf(fmaxf(cut, value_of(none + 1u)), floor_p);
-            const unsigned high = key16_of(top), span = min(high - key16_of(least), (unsigned)(CODES - 1));
-            __syncthreads();
-            for (unsigned i = tid; i <= span; i += THREADS) s.codes[i] = kept(value16_of(high - i));       // the counts are done with
-            __syncthreads();
-            auto weight = [&](float x) -> unsigned {
-                const unsigned d = high - key16_of(x);
-                return d <= span ? s.codes[d] : kept(x);
-            };
-            draw_from_row(s, row, f.u, least, cut, least > cut ? 0 : ties, kept(cut), weight, write);
+            const unsigned high = key16_of(top), span = high - key16_of(least);
+            const unsigned of_cut = kept(cut);
+            ties = least > cut ? 0 : ties;
+            if (span < (unsigned)CODES) {              // a table of the kept values' weights, where the counts were
+                __syncthreads();
+#pragma unroll 1
+                for (unsigned i = tid; i <= span; i += THREADS) s.codes[i] = kept(value16_of(high - i));
+                __syncthreads();
+                draw_from_row<false>(s, row, row.batches() * (Row<T>::BATCH * 32) <= PEAKS, f.u, least, cut, ties, of_cut, [&](float x) { return s.codes[high - key16_of(x)]; }, write);
+            } else draw_from_row<true>(s, row, false, f.u, least, cut, ties, of_cut, kept, write);
             return;
         }
     }
@@ -599,7 +753,7 @@ template <typename T, bool PLAIN> __device__ __forceinline__ void sample_row(con
         ties = block_sum(s, ties);
     }
     const float least = fmaxf(fmaxf(value, value_of(none + 1u)), floor_p);
-    draw_from_row(s, row, f.u, least, value, least > value ? 0 : ties, kept(value), kept, write);
+    draw_from_row<true>(s, row, false, f.u, least, value, least > value ? 0 : ties, kept(value), kept, write);
 }
 
 template <typename T> __global__ __launch_bounds__(1024) void sample_kernel(SampleArgs a)
@@ -609,6 +763,11 @@ template <typename T> __global__ __launch_bounds__(1024) void sample_kernel(Samp
     const int64_t r = a.row_lo + blockIdx.x;
     Row<T> row;
     row.set((const T *)a.x + r * a.V, a.V);
+    // on their way while the row's filters are fetched and the counters cleared
+    Vec<T, Row<T>::VEC> in[sizeof(T) == 2 ? Row<T>::BATCH : 1];
+    if constexpr (sizeof(T) == 2) {
+        if (row.vectors) row.fetch(0, in);
+    }
     const float temperature = a.temperature ? a.temperature[r] : 1.f;
     Filters f = {a.top_p ? a.top_p[r] : 1.f, a.min_p ? a.min_p[r] : 0.f, a.u[r], a.top_k ? a.top_k[r] : 0};
     if (f.top_k <= 0 || f.top_k > a.V) f.top_k = a.V;
@@ -616,19 +775,19 @@ template <typename T> __global__ __launch_bounds__(1024) void sample_kernel(Samp
     const bool coded = sizeof(T) == 2 && !one && (f.top_k < a.V || f.top_p < 1.f);
     float top = -INFINITY;
     unsigned counted = 0u;
-    if (coded) {
-        for (int i = tid * 4; i < CODES; i += THREADS * 4) *(uint4 *)&s.codes[i] = make_uint4(0u, 0u, 0u, 0u);
-        __syncthreads();
-        row.each([&](int, float x) {
-            top = fmaxf(top, x);
-            if (x > -INFINITY) {                       // not those that a mask took out: they are alike, and counters that are alike wait for each other
-                const unsigned bits = __float_as_uint(x + 0.f);      // both zeros alike
-                atomicAdd((unsigned *)((char *)s.codes + ((bits >> 14) & 0x1FFFCu)), (int)bits < 0 ? 1u : 0x10000u);
-                ++counted;
+    if constexpr (sizeof(T) == 2) {
+        if (coded) {
+            for (int i = tid * 4; i < CODES; i += THREADS * 4) *(uint4 *)&s.codes[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (tid == 0) {
+                s.best = key_of(-INFINITY);
+                s.low = ~0u;
             }
-        });
-    } else row.each([&](int, float x) { top = fmaxf(top, x); });
-    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+            __syncthreads();
+            counted = row.count(s, temperature, in);
+        }
+    }
+    if (!coded) row.each([&](int, float x) { top = fmaxf(top, x); });
+    top = wave_max(top);
     const u64 in_wave = wave_sum(counted);
     if (lane == 0) s.sums[wave] = (in_wave << 32) | __float_as_uint(top);
     __syncthreads();
@@ -637,6 +796,7 @@ template <typename T> __global__ __launch_bounds__(1024) void sample_kernel(Samp
         top = fmaxf(top, __uint_as_float((unsigned)s.sums[w]));
         finite += s.sums[w] >> 32;
     }
+    if (coded) top = value_of(s.best);
     top += 0.f;
     if (top == -INFINITY) {
         if (tid == 0) {
