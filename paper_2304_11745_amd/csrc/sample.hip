@@ -121,7 +121,7 @@ struct Shared {
 };
 
 template <typename T> struct Row {
-    static constexpr int VEC = 16 / sizeof(T), DEPTH = 4, BATCH = 2;
+    static constexpr int VEC = 16 / sizeof(T), DEPTH = 2, BATCH = 2;        // a lane's vectors in flight: of a pass (4: one row of 32000 fp32 11.5 us against 10.8, 8: 17.5), of the counting one
     const T *x;
     int V, head, vectors, per;                         // entries before the first 16-byte boundary, vectors after it, vectors of a wave's part
 
@@ -589,8 +589,8 @@ template <bool LONG, typename T, typename K, typename F> __device__ __forceinlin
     }
 }
 
-// `coded`: the entries have been counted by their values (bf16); `counted`: how many of them there are
-template <typename T, bool PLAIN> __device__ __forceinline__ void sample_row(const SampleArgs &a, Shared &s, const Row<T> &row, int64_t r, float top, float temperature, Filters f, bool coded, u64 counted)
+// mine: the largest logit that the thread has seen (fp32); `coded`: the entries have been counted by their values (bf16); `counted`: how many of them there are
+template <typename T, bool PLAIN> __device__ __forceinline__ void sample_row(const SampleArgs &a, Shared &s, const Row<T> &row, int64_t r, float top, float temperature, Filters f, float mine, bool coded, u64 counted)
 {
     const int tid = threadIdx.x;
     const Weights<PLAIN> w(top, temperature);
@@ -676,19 +676,13 @@ template <typename T, bool PLAIN> __device__ __forceinline__ void sample_row(con
     unsigned cut = 0u;                                 // kept: keys above `cut`, and those equal to it up to index `last`
     int last = a.V;
     if (f.top_k < a.V) {
-        clear();
-        // the last bin takes the far end of the row; it is not counted one by one, at one address, but taken to hold everything
-        row.each([&](int, float x) {
-            const int bin = bin_of(w.distance(x));
-            if (bin < BINS - 1) atomicAdd(&s.bins[bin], 1ull);
-        });
-        if (tid == 0) s.bins[BINS - 1] = (u64)a.V;
-        __syncthreads();
         u64 before;
         const u64 k64 = (u64)f.top_k;
-        const int bin = first_bin(s, [&](u64 v) { return v >= k64; }, &before);
-        if (before + s.bins[bin] <= LIST) {
-            const int n = gather(bin_floor(bin), [&](float x, int) { return bin_of(w.distance(x)) <= bin; });
+        auto to_bin = [&](float x) {
+            const int bin = bin_of(w.distance(x));
+            if (bin < BINS - 1) atomicAdd(&s.bins[bin], 1ull);
+        };
+        auto draw = [&](int n) {
             rank_list(s, w, n);
             int first = f.top_k;
             if (f.top_p < 1.f) {
@@ -697,6 +691,30 @@ template <typename T, bool PLAIN> __device__ __forceinline__ void sample_row(con
                 first = ranks_to(s, first, 0, (double)f.top_p * (double)block_sum(s, v));
             }
             draw_from_list(s, w, f, first, write);
+        };
+        if (sizeof(T) == 4 && f.top_k <= THREADS / 4) {
+            // top-k entries of the row are no smaller than the top-k of the threads' largest ones, and few others are
+            clear();
+            to_bin(mine);
+            __syncthreads();
+            const int bin = first_bin(s, [&](u64 v) { return v >= k64; }, &before);
+            if (bin < BINS - 1) {
+                const float least = bin_floor(bin);
+                const int n = gather(least, [](float, int) { return true; });
+                if (n <= LIST) {
+                    draw(n);
+                    return;
+                }
+            }
+        }
+        clear();
+        // the last bin takes the far end of the row; it is not counted one by one, at one address, but taken to hold everything
+        row.each([&](int, float x) { to_bin(x); });
+        if (tid == 0) s.bins[BINS - 1] = (u64)a.V;
+        __syncthreads();
+        const int bin = first_bin(s, [&](u64 v) { return v >= k64; }, &before);
+        if (before + s.bins[bin] <= LIST) {
+            draw(gather(bin_floor(bin), [&](float x, int) { return bin_of(w.distance(x)) <= bin; }));
             return;
         }
         prefix_by_digits(s, row, (double)f.top_k, [&](int, unsigned) -> u64 { return 1; }, cut, last);
@@ -786,7 +804,8 @@ template <typename T> __global__ __launch_bounds__(1024) void sample_kernel(Samp
             counted = row.count(s, temperature, in);
         }
     }
-    if (!coded) row.each([&](int, float x) { top = fmaxf(top, x); });
+    if (sizeof(T) == 4 || !coded) row.each([&](int, float x) { top = fmaxf(top, x); });
+    const float mine = top;
     top = wave_max(top);
     const u64 in_wave = wave_sum(counted);
     if (lane == 0) s.sums[wave] = (in_wave << 32) | __float_as_uint(top);
@@ -819,8 +838,8 @@ template <typename T> __global__ __launch_bounds__(1024) void sample_kernel(Samp
         }
         return;
     }
-    if (temperature > 1e-18f && temperature < 1e18f && top < INFINITY) sample_row<T, false>(a, s, row, r, top, temperature, f, coded, finite);
-    else sample_row<T, true>(a, s, row, r, top, temperature, f, coded, finite);
+    if (temperature > 1e-18f && temperature < 1e18f && top < INFINITY) sample_row<T, false>(a, s, row, r, top, temperature, f, mine, coded, finite);
+    else sample_row<T, true>(a, s, row, r, top, temperature, f, mine, coded, finite);
 }
 
 LaunchInfo launch_sample(const TokenArgs &a, hipStream_t s, bool dry, int)
