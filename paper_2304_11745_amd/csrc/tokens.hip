@@ -158,10 +158,10 @@ LaunchInfo launch_qknorm_rope(const TokenArgs &a, hipStream_t s, bool dry)
 }
 
 // ---- into the cache and out of it --------------------------------------------------------------------------------------------------
-// A workgroup owns one block of 32 cache positions of one kv head (a block never crosses a page).  Writing: half of its threads quantise
+// A workgroup owns one block of 32 cache positions of one kv head (a block never crosses a page).  Writing: half of its waves quantise
 // keys, half values, eight features of a token per lane; a group's minimum and maximum go over the eight lanes that hold it.  Key codes
-// are one word per lane as they stand; value codes are gathered in LDS, where the words of eight tokens are put together, on top
-// of the codes that tokens outside the call left there.
+// are one word per lane as they stand.  Of the values a wave takes eight tokens at a time, 64 features of each, and the eight lanes that
+// hold the same features transpose their 8 x 8 codes in three exchanges; where a word also has codes of tokens outside the call, those stay.
 struct CacheArgs {
     const void *x;
     void *y;
@@ -181,96 +181,141 @@ __device__ __forceinline__ Block block_of(const CacheArgs &a)
     return k;
 }
 
+// Over the eight lanes of a group: with the neighbour, the other pair, the other four (in reverse).  One instruction each, after the two wait states that
+// such a move asks for behind the instruction that wrote its source; from builtins the compiler makes three.
+#define GROUP_STEP(op, v, move) asm("s_nop 1\n\t" op "_dpp %0, %1, %1 " move " row_mask:0xf bank_mask:0xf" : "=v"(v) : "v"(v))
+__device__ __forceinline__ float group_min(float v)
+{
+    GROUP_STEP("v_min_f32", v, "quad_perm:[1,0,3,2]");
+    GROUP_STEP("v_min_f32", v, "quad_perm:[2,3,0,1]");
+    GROUP_STEP("v_min_f32", v, "row_half_mirror");
+    return v;
+}
+__device__ __forceinline__ float group_max(float v)
+{
+    GROUP_STEP("v_max_f32", v, "quad_perm:[1,0,3,2]");
+    GROUP_STEP("v_max_f32", v, "quad_perm:[2,3,0,1]");
+    GROUP_STEP("v_max_f32", v, "row_half_mirror");
+    return v;
+}
+#undef GROUP_STEP
+
+// d / s, correctly rounded, for an s of few significant bits (8 at most) and `inverse` within some units of 1 / s: the remainder of the first guess is exact, and the
+// quotient is either half way between two numbers or further from there than 2^-9 of their distance, while the second guess errs by 2^-21 of it.
+__device__ __forceinline__ float divided(float d, float s, float inverse)
+{
+    const float q = __fmul_rn(d, inverse);
+    return __fmaf_rn(__fmaf_rn(-q, s, d), inverse, q);
+}
+
 // eight values of one lane -> their code word; `pair` receives scale and minimum of the group of eight lanes (a minimum of zero without a
 // sign: which of two zeros a minimum returns is not defined)
 __device__ __forceinline__ unsigned quantise(const float *v, unsigned &pair)
 {
-    float lo = INFINITY, hi = -INFINITY;
-    bool bad = false;
+    float lo = v[0], hi = v[0];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        bad |= v[e] != v[e];
-        lo = fminf(lo, v[e]);
+    for (int e = 1; e < 8; ++e) {
+        lo = __builtin_elementwise_minimum(lo, v[e]);  // NaN if there is any
         hi = fmaxf(hi, v[e]);
     }
-    if (bad) lo = -INFINITY;
-#pragma unroll
-    for (int o = 1; o < 8; o <<= 1) {
-        lo = fminf(lo, __shfl_xor(lo, o, 64));
-        hi = fmaxf(hi, __shfl_xor(hi, o, 64));
-    }
-    const unsigned short low = to_bf16(lo), step = to_bf16(__fdiv_rn(__fsub_rn(hi, lo), 15.f));
+    lo = group_min(lo == lo ? lo : -INFINITY);
+    hi = group_max(hi);
+    const unsigned short low = to_bf16(lo), step = to_bf16(divided(__fsub_rn(hi, lo), 15.f, 1.f / 15.f));
     const float m = ld_f32(&low, 0) + 0.f, s = ld_f32(&step, 0);
     if (!(fabsf(s) < INFINITY && fabsf(m) < INFINITY)) {
         pair = 0x7FC0u;
         return 0u;
     }
     pair = (unsigned)step | __float_as_uint(m);
-    unsigned word = 0u;
-    if (s > 0.f) {
+    if (!(s > 0.f)) return 0u;
+    float q[8];
+    if (__any(!(s > 0x1p-100f && s < 0x1p100f))) {     // 1 / s or a remainder may not be a number of full precision
+        asm volatile("");                              // a branch: both sides would cost more than the divisions alone
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float q = __builtin_amdgcn_fmed3f(rintf(__fdiv_rn(__fsub_rn(v[e], m), s)), 0.f, 15.f);
-            word |= (unsigned)q << code_shift(e);
-        }
+        for (int e = 0; e < 8; ++e) q[e] = __fdiv_rn(__fsub_rn(v[e], m), s);
+    } else {
+        const float inverse = __builtin_amdgcn_rcpf(s);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) q[e] = divided(__fsub_rn(v[e], m), s, inverse);
     }
-    return word;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) q[e] = __builtin_amdgcn_fmed3f(rintf(q[e]), 0.f, 15.f);
+    // elements of even and of odd index: sums of codes times powers of 16, whole numbers
+    const float even = fmaf(fmaf(fmaf(q[6], 16.f, q[4]), 16.f, q[2]), 16.f, q[0]), odd = fmaf(fmaf(fmaf(q[7], 16.f, q[5]), 16.f, q[3]), 16.f, q[1]);
+    return (unsigned)even | (unsigned)odd << 16;
+}
+
+// Lane 8 t + s of a wave has the codes of token t, features 8 s ..; lane f receives those of feature f, tokens 0..7.  Three exchanges, one for each
+// bit of the index: halves of a word, then of its bytes, then of its halves' bytes (the order of code_shift()).
+__device__ __forceinline__ unsigned transpose_codes(unsigned w)
+{
+    const int lane = threadIdx.x & 63;
+    auto exchange = [&](int across, unsigned mask, int shift) {
+        const unsigned o = (unsigned)__shfl_xor((int)w, across, 64);
+        w = lane & across ? (w & ~mask) | (o & ~mask) >> shift : (w & mask) | (o & mask) << shift;
+    };
+    exchange(8, 0x0000FFFFu, 16);
+    exchange(16, 0x0F0F0F0Fu, 4);
+    exchange(32, 0x00FF00FFu, 8);
+    return (unsigned)__shfl((int)w, (lane & 7) * 8 + (lane >> 3), 64);       // in the order of the features: neighbours store neighbours
 }
 
 template <typename T, int D> __global__ __launch_bounds__(256) void cache_write_kernel(CacheArgs a)
 {
     constexpr int LPT = D / 8, PER = 128 / LPT, PASSES = 32 / PER, NG = D / CACHE_GROUP;     // lanes per token, tokens per pass of a half
-    __shared__ unsigned vw[8 * LPT * 4];               // value words: [feature % 8][feature / 8][word]
-    const int tid = threadIdx.x, half = tid >> 7, sub = tid & (LPT - 1), row = (tid & 127) / LPT;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6 & 1;
+    const bool values = __builtin_amdgcn_readfirstlane(tid >> 7);
     const Block k = block_of(a);
     const int lo = max(k.p0, k.span.start), hi = min(k.p0 + 32, k.span.start + k.span.count);
     if (lo >= hi) return;
     const int page = page_of(a.c, k.b, k.p0);
     if (page < 0) return;
     const int64_t first = page_row(a.c, page, k.head) + (k.p0 & ((1 << a.c.page_shift) - 1));
-    const T *x = (const T *)a.x + ((int64_t)k.b * a.S - k.span.start) * a.width + a.k_off + (half * a.c.kv_heads + k.head) * D + sub * 8;
+    // the lane's features 8 sub .. and tokens: keys row by row, values eight tokens of 64 features a wave
+    const int sub = !values ? tid & (LPT - 1) : D == 128 ? wave * 8 + (lane & 7) : lane & 7;
+    const int row = !values ? (tid & 127) / LPT : (D == 128 ? 0 : wave * PASSES * 8) + (lane >> 3), next = values ? 8 : PER;
+    const T *x = (const T *)a.x + ((int64_t)k.b * a.S - k.span.start) * a.width + a.k_off + (values * a.c.kv_heads + k.head) * D + sub * 8;
     float v[PASSES][8];
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) {
-        const int p = k.p0 + i * PER + row;
+        const int p = k.p0 + i * next + row;
         if (p >= lo && p < hi) load8(x + (int64_t)p * a.width, v[i]);
         else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
         }
     }
-    // what stays of the words that the call writes in part
-    unsigned *global = (unsigned *)a.c.v_codes + first * (D / 8);
-    for (int i = tid; i < D * 4; i += 256) {
-        const int f = i >> 2, w = i & 3, q0 = k.p0 + w * 8;
-        unsigned keep = 0u;
-        if (q0 < hi && q0 + 8 > lo && (q0 < lo || q0 + 8 > hi)) {
-            keep = global[i];
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (q0 + e >= lo && q0 + e < hi) keep &= ~(15u << code_shift(e));
-        }
-        vw[((f & 7) * LPT + (f >> 3)) * 4 + w] = keep;
-    }
-    __syncthreads();
+    unsigned words[PASSES];
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) {
-        const int t = i * PER + row, p = k.p0 + t;
+        const int t = i * next + row, p = k.p0 + t;
         unsigned pair;
-        const unsigned word = quantise(v[i], pair);
+        words[i] = quantise(v[i], pair);
         if (p < lo || p >= hi) continue;
-        if (!half) ((unsigned *)a.c.k_codes)[(first + t) * LPT + sub] = word;
-        else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                atomicOr(&vw[(e * LPT + sub) * 4 + (t >> 3)], ((word >> code_shift(e)) & 15u) << code_shift(t & 7));
-        }
-        if (sub % 8 == 0) (half ? a.c.v_scales : a.c.k_scales)[(first + t) * NG + sub / 8] = pair;
+        if (!values) ((unsigned *)a.c.k_codes)[(first + t) * LPT + sub] = words[i];
+        if (sub % 8 == 0) (values ? a.c.v_scales : a.c.k_scales)[(first + t) * NG + sub / 8] = pair;
     }
-    __syncthreads();
-    for (int i = tid; i < D * 4; i += 256) {
-        const int f = i >> 2, w = i & 3, q0 = k.p0 + w * 8;
-        if (q0 < hi && q0 + 8 > lo) global[i] = vw[((f & 7) * LPT + (f >> 3)) * 4 + w];
+    if (!values) return;
+    unsigned *out = (unsigned *)a.c.v_codes + first * LPT + ((sub & ~7) * 8 + lane) * 4;       // the feature's four words of eight tokens
+    const int w0 = D == 128 ? 0 : wave * PASSES;
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) words[i] = transpose_codes(words[i]);
+    if (lo == k.p0 && hi == k.p0 + 32) {
+        if constexpr (PASSES == 4) *(uint4 *)out = make_uint4(words[0], words[1], words[2], words[3]);
+        else *(uint2 *)(out + w0) = make_uint2(words[0], words[1]);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+        const int q0 = k.p0 + (w0 + i) * 8;
+        if (q0 >= hi || q0 + 8 <= lo) continue;
+        unsigned mine = 0u;                            // of the word's codes those that the call writes
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (q0 + e >= lo && q0 + e < hi) mine |= 15u << code_shift(e);
+        unsigned w = words[i];
+        if (mine != ~0u) w = (w & mine) | (out[w0 + i] & ~mine);
+        out[w0 + i] = w;
     }
 }
 
@@ -328,7 +373,7 @@ static CacheArgs cache_args(const TokenArgs &a, bool read)
 LaunchInfo launch_cache_write(const TokenArgs &a, hipStream_t s, bool dry)
 {
     const CacheArgs b = cache_args(a, false);
-    LaunchInfo li = info(a.dtype == DT_BF16 ? "cache_write_bf16" : "cache_write_f32", (int64_t)(a.b_hi - a.b_lo) * a.kv_heads * b.blocks, a.D * 16);
+    LaunchInfo li = info(a.dtype == DT_BF16 ? "cache_write_bf16" : "cache_write_f32", (int64_t)(a.b_hi - a.b_lo) * a.kv_heads * b.blocks, 0);
     if (dry || !li.workgroups) return li;
     const dim3 grid(li.workgroups), block(256);
     if (a.dtype == DT_BF16 && a.D == 64) GACER_LAUNCH((cache_write_kernel<unsigned short, 64>), grid, block, 0, s, b);
