@@ -16,6 +16,11 @@
 // The softmax keeps a reference per row that only moves when a score passes it by more than 2^8: weights are 2^(score - reference), sums are per
 // lane and joined at the end.  Waves of a workgroup take parts of its keys and are joined in LDS; where there are too few workgroups
 // the keys are also cut into splits, joined by a second kernel.
+//
+// Up to 8 rows the way from memory bounds it, and the 251 registers of a wave (two tiles of codes among them) that leave room for one workgroup in a
+// unit: 64 sequences of up to 8192 keys, 8 kv heads of 128 features (one token, bf16, 308 MB of cache) 84 us = 3.7 TB/s, of which the loads alone take
+// 65; one of 131072 keys (151 MB) 41 us = 3.7 TB/s, 5 of them the join.  With more rows the instructions that turn codes into operands
+// and scores into weights bound it, and from 33 on (65 in fp32) the kernel for 128 rows takes over.
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include "cache_attention.h"
@@ -427,7 +432,9 @@ LaunchInfo launch_cache_attention(const TokenArgs &a, hipStream_t s, bool dry, i
     const int outputs = n * a.S * a.heads;
     LaunchInfo li;
     li.workgroups = phase == 2 ? (join_by_groups(b, outputs) ? outputs : (int)(((int64_t)outputs * a.D + 1023) / 1024)) : grid;
-    li.threads = phase == 2 ? 256 : g.waves * 64; li.lds_bytes = g.waves * g.rows * (a.D + 2) * 4; li.wg_per_cu = phase == 2 ? 8 : 8 / g.waves;
+    li.threads = phase == 2 ? 256 : g.waves * 64;
+    li.lds_bytes = phase == 2 ? 0 : g.rows == 128 ? 2 * wide_tile_bytes(a.D, a.dtype == DT_F32) : g.waves * g.rows * (a.D + 2) * 4;
+    li.wg_per_cu = phase == 2 ? 8 : g.per_cu;
     li.kernel = phase == 2 ? "cache_attention_join" : a.dtype == DT_BF16 ? "cache_attention_bf16" : "cache_attention_f32";
     li.phases = g.splits > 1 ? 2 : 1;
     if (dry || !grid) return li;

@@ -8,11 +8,18 @@
 // few rows the scales are applied in fp32,
 //   q.k_j = sum over groups g of  s_jg * (sum_d q_d (c_jd - z)) + (m_jg + z s_jg) * sum_d q_d             (z = 8 or -16)
 //   out_d = sum_j (p_j s_jg) (c_jd - 8) + sum_j p_j (m_jg + 8 s_jg)
-// with the second sum of the scores as a further matrix instruction: the pair (s, m) of a key, two bf16 numbers, times the sums of the queries in
-// three bf16 parts, and a one times the parts of minus the row's reference; that of the result likewise in bf16 tenants, the weights times m + 8 s in two parts.  fp32 tenants have their queries and
-// weights in three bf16 parts each, every part a matrix instruction, and add p_j (m + 8 s) as it is.  In bf16 tenants the weights p_j s_jg are rounded to bf16 once: with codes around zero that is as
-// much as the result's own rounding adds (2.2e-3 of the result together, 1.7e-3 for the latter alone), and a second part would be
-// 16 more matrix instructions per 64 keys and two more operations per weight.
+// with the second sum of the scores as a further matrix instruction: the pair (s, m) of a key, two bf16 numbers, times the sums of the queries
+// in three bf16 parts, and a one times the parts of minus the row's reference; that of the result likewise in bf16 tenants, the weights times
+// m + 8 s in two parts.  fp32 tenants have their queries and weights in three bf16 parts each, every part a matrix instruction, and add
+// p_j (m + 8 s) as it is.  In bf16 tenants the weights p_j s_jg are rounded to bf16 once: with codes around zero that is as much as the result's own
+// rounding adds (2.2e-3 of the result together, 1.7e-3 for the latter alone), and a second part would be 16 more matrix instructions per 64
+// keys and two more operations per weight.
+//
+// Bound by the two waves of a SIMD that 238 registers allow: each runs scores, exponentials and products one after another, and vector
+// instructions (52 % of the time), matrix instructions (32 %), LDS (35 %) and waits for LDS and barriers (39 %) fill each other's gaps only in part.  A
+// prompt of 4096 tokens, 32 heads of 128 features over 8 (bf16): 223 us = 617 TFLOP/s, where a large product reaches 1377.  256 rows a workgroup, which
+// halve the unpacking: 212 there, but 98 against 93 at 2048 tokens and 361 against 344 at 16 x 256 tokens after 4096 keys; two groups
+// of waves that take turns at the matrix cores, a barrier after each turn: 263.
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include "cache_attention.h"
@@ -25,7 +32,7 @@ template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 &&
     constexpr int QP = F32 ? 3 : 1, PP = F32 ? 3 : 1, MP = 2;                  // bf16 parts of queries, weights, and of the minima m + 8 s
     constexpr float K_UNIT = F32 ? 16.f : 1.f, K_MIDDLE = F32 ? 8.f : -16.f;   // keys in LDS: (c - 8) / 16 or 16 + c; value of a step, of where they are zero
     constexpr int NG = D / 64, ROWS = 128, KROW = D * 2 + 16, VROW = 128 + 16, KROWS = 64 * KROW, VROWS = D * VROW;
-    constexpr int EXT_K = 64 * 32, EXT_V = F32 ? NG * 64 * 4 : MP * NG * VROW, SCALES = 2 * NG * 64 * 4, BUF = KROWS + VROWS + EXT_K + EXT_V + SCALES;
+    constexpr int EXT_K = 64 * 32, EXT_V = F32 ? NG * 64 * 4 : MP * NG * VROW, BUF = wide_tile_bytes(D, F32);
     constexpr int ITEMS = 64 * D / 32;                 // 16-byte pieces of a tile's key codes, and of its value codes
     __shared__ __align__(16) unsigned char lds[2 * BUF];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;

@@ -4,18 +4,21 @@
 // filters keep are a prefix of the order "larger first, equal ones by index"; it ends at a key (the logit's bits in an order of
 // unsigned numbers) and, among the entries with that key, at an index.
 //   bf16 logits are few values: one pass over the row finds the largest and counts the entries by their 16 bits, in 65536 counters of 16 bits
-// that fill 128 KB of LDS.  Scans over the counts, and over the counts times the weights of the some thousand values that occur, give the value at
-// which top-k and the nucleus end and how many of its entries they still take.  The draw then adds the kept weights of the row, from a
-// table, a part of the row per wave, and looks for its index in one of the parts.
-//   fp32 logits: a second pass puts every entry into one of 2048 bins by its distance from the largest, 1/64 of a temperature each (weights vanish
-// 21.5 temperatures below), counting entries (top-k) or adding weights (top-p); the bin in which the prefix ends is found by a
-// scan.  Where few entries can be kept, they go into a list in LDS, and everything else happens on the list: ranks by counting, the nucleus by a scan
-// over ranks, the draw by sums over smaller indexes.  Otherwise only the last bin's entries need ranks, and the draw goes as for bf16.
+// that fill 128 KB of LDS (entries that weigh nothing even against the largest so far are left out; they can only be kept where that changes
+// no weight).  Scans over the counts, and over the counts times the weights of the some thousand values that occur, give the value at which top-k and
+// the nucleus end and how many of its entries they still take.  The draw then adds the kept weights of the row, from a table, a part of
+// the row per wave, and looks for its index in one of the parts; it reads again only pairs of vectors whose largest entry, noted by the first pass, is kept.
+//   fp32 logits under top-k: the largest entries of the threads' shares give a value that at least k entries reach and few others do; those go
+// into a list in LDS, and everything else happens on the list: ranks by counting, the nucleus by a scan over ranks, the draw by sums over smaller
+// indexes.  Under top-p, or where k is large, a second pass puts every entry into one of 2048 bins by its distance from the largest, 1/64 of a
+// temperature each (weights vanish 21.5 temperatures below), counting entries or adding weights; the bin in which the prefix ends is found by a
+// scan, and few kept entries go into the list.  Otherwise only the last bin's entries need ranks, and the draw goes as for bf16.
 //   Where a list would not hold its entries or a counter its count (a flat row), the prefix's end is found digit by digit of the key instead.
 //
-// What bounds it: with many rows of bf16 logits the way from memory and the counters, with fp32 instructions (a weight is a correctly rounded
-// division, an exponential and a conversion, some 25 of them, for every entry under top-p), with few rows the chain of passes, barriers
-// and scans.
+// What bounds it, and what it takes.  256 rows of 131072 bf16 logits under top-p and min-p (67 MB, one row in each unit): 52 us, of which the first pass
+// takes 24 (20 without its counters; 67 MB at the rate of a large copy are 13), the scans of the counts 8, the draw 10.  One row of 32000 fp32
+// logits, top-k 50 and top-p: 11 us, a chain of two passes, some twenty barriers and instructions that a single workgroup runs through once; by bins
+// 15, through the codes of bf16 as a first digit 21.
 #include <hip/hip_runtime.h>
 #include "device_util.h"
 #include "kernels.h"

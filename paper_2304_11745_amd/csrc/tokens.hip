@@ -20,7 +20,10 @@ static LaunchInfo info(const char *name, int64_t workgroups, int lds)
 //
 // A head is held by LPH lanes, eight features each: two runs of four, which are the two halves of the lane's pairs (i, i + R/2), so that
 // the rotation needs no other lane; beyond the rotated features, and for interleaved pairs, the two runs are neighbours.  Cosine and sine
-// depend on the token and the lane alone and are loaded once for all heads that a workgroup takes.
+// depend on the token and the lane alone and are loaded once for all heads that a workgroup takes; the token's positions come through the scalar
+// cache.  Every element is read and written once: bound by the way to memory and back.  Three heads of a lane in flight: 3 x 4111
+// tokens of 28 + 4 + 4 heads of 128 features (bf16, 227 MB) 53 us = 4.3 TB/s; two 64, four 55 (few models' heads fill them), one 113 against 80 at
+// 16384 tokens of 32 + 8 + 8 heads, and no faster for a single token (5.8 us, a launch).
 struct RopeArgs {
     const void *x;
     void *y;
@@ -69,13 +72,15 @@ template <typename T, int LPH, int IT> __global__ __launch_bounds__(256) void qk
             for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
         }
     }
+    int pos[3];                                        // the token's position on each axis (a missing one is not looked at)
+#pragma unroll
+    for (int i = 0; i < 3; ++i) pos[i] = fixed_int(a.positions, token * a.axes + min(i, a.axes - 1));
     float c[4], s[4];
     if (turned) {
         const int pair = sub * 4, half = a.R / 2;
-        const int *pos = a.positions + token * a.axes;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int at = pos[pair + e < a.s1 ? 0 : pair + e < a.s2 ? 1 : 2];
+            const int at = pair + e < a.s1 ? pos[0] : pair + e < a.s2 ? pos[1] : pos[2];
             const bool known = (unsigned)at < (unsigned)a.n_positions;
             const float2 cs = *(const float2 *)(a.table + ((int64_t)(known ? at : 0) * half + pair + e) * 2);
             c[e] = known ? cs.x : NAN;
@@ -90,6 +95,7 @@ template <typename T, int LPH, int IT> __global__ __launch_bounds__(256) void qk
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
         const int h = h0 + i * SLOTS;
+        if (__builtin_amdgcn_readfirstlane(h) >= a.all) break;         // none of the wave's heads
         const bool query = h < a.heads;
         float sum = 0.f;
 #pragma unroll
@@ -118,13 +124,14 @@ template <typename T, int LPH, int IT> __global__ __launch_bounds__(256) void qk
     }
 }
 
-template <typename T, int LPH> static void rope_launch(RopeArgs b, int64_t tokens, bool few, hipStream_t s)
+static constexpr int HEADS_AT_A_TIME = 3;
+
+template <typename T, int LPH> static void rope_launch(RopeArgs b, int64_t tokens, hipStream_t s)
 {
-    const int slots = 256 / LPH;
+    const int heads = 256 / LPH * HEADS_AT_A_TIME;
     for (int64_t at = 0; at < tokens; at += 1 << 22, b.t_lo += 1 << 22) {        // a grid holds fewer than 2^32 threads
         const unsigned n = (unsigned)std::min<int64_t>(tokens - at, 1 << 22);
-        if (few) GACER_LAUNCH((qknorm_rope_kernel<T, LPH, 1>), dim3(n, (b.all + slots - 1) / slots), dim3(256), 0, s, b);
-        else GACER_LAUNCH((qknorm_rope_kernel<T, LPH, 4>), dim3(n, (b.all + 4 * slots - 1) / (4 * slots)), dim3(256), 0, s, b);
+        GACER_LAUNCH((qknorm_rope_kernel<T, LPH, HEADS_AT_A_TIME>), dim3(n, (b.all + heads - 1) / heads), dim3(256), 0, s, b);
     }
 }
 
@@ -141,14 +148,13 @@ LaunchInfo launch_qknorm_rope(const TokenArgs &a, hipStream_t s, bool dry)
     const int64_t tokens = (int64_t)(a.b_hi - a.b_lo) * a.S;
     int lph = 1;
     while (lph * 8 < a.D) lph *= 2;
-    const int slots = 256 / lph;
-    const bool few = tokens * ((b.all + slots - 1) / slots) <= 2048;
-    LaunchInfo li = info(a.dtype == DT_BF16 ? "qknorm_rope_bf16" : "qknorm_rope_f32", tokens * ((b.all + slots * (few ? 1 : 4) - 1) / (slots * (few ? 1 : 4))), 0);
+    const int heads = 256 / lph * HEADS_AT_A_TIME;
+    LaunchInfo li = info(a.dtype == DT_BF16 ? "qknorm_rope_bf16" : "qknorm_rope_f32", tokens * ((b.all + heads - 1) / heads), 0);
     if (dry || !tokens) return li;
 #define ROPE(L)                                                                              \
     case L:                                                                                  \
-        if (a.dtype == DT_BF16) rope_launch<unsigned short, L>(b, tokens, few, s);           \
-        else rope_launch<float, L>(b, tokens, few, s);                                       \
+        if (a.dtype == DT_BF16) rope_launch<unsigned short, L>(b, tokens, s);           \
+        else rope_launch<float, L>(b, tokens, s);                                       \
         break
     switch (lph) {
         ROPE(1); ROPE(2); ROPE(4); ROPE(8); ROPE(16); ROPE(32); ROPE(64);
@@ -162,6 +168,10 @@ LaunchInfo launch_qknorm_rope(const TokenArgs &a, hipStream_t s, bool dry)
 // keys, half values, eight features of a token per lane; a group's minimum and maximum go over the eight lanes that hold it.  Key codes
 // are one word per lane as they stand.  Of the values a wave takes eight tokens at a time, 64 features of each, and the eight lanes that
 // hold the same features transpose their 8 x 8 codes in three exchanges; where a word also has codes of tokens outside the call, those stay.
+// Nothing goes through LDS but the exchanges.  Bound by vector instructions, some 14 for an element, and the way from memory: 6 prompts of up to 5001
+// tokens, 8 kv heads of 128 features (bf16, 154 MB) 44 us = 3.5 TB/s; by divisions and with the transposition by LDS atomics 65.
+// Reading is a copy that widens: value codes go through LDS to become rows of a token again.  The same prompts 25 us; 8 x 8192 tokens
+// (327 MB) 67 us = 4.9 TB/s, what a large copy reaches.
 struct CacheArgs {
     const void *x;
     void *y;
