@@ -65,12 +65,15 @@ __device__ __forceinline__ bf16x8 codes_around(unsigned w)
 
 __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 
-// v as a sum of PARTS numbers whose upper 16 bits are bf16, each but the last the largest that does not pass it
+// v as a sum of PARTS numbers whose upper 16 bits are bf16, each the largest that does not pass it, but for the second of two, which is rounded: errors
+// that all lie on one side add up over the keys (weights of 131072 keys: an error of 8.5e-3 of the result, which is small against each of its terms).
+// Three hold all of v.
 template <int PARTS> __device__ __forceinline__ void split_bf16(float v, unsigned *p)
 {
 #pragma unroll
     for (int i = 0; i < PARTS; ++i) {
         p[i] = __float_as_uint(v);
+        if (PARTS == 2 && i == 1) p[i] += 0x8000u;
         v -= __uint_as_float(p[i] & 0xFFFF0000u);
     }
 }
