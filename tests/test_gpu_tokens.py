@@ -636,3 +636,36 @@ def test_attention_with_the_keys_in_splits(dtype, page, dim, heads, kv, tokens, 
         s.run(B.GACER_MODE_PLAN)
         assert torch.equal(out, whole)
     s.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens,heads", [(1, 4), (4, 4), (6, 4), (12, 4), (20, 4)])       # rows of 4, 16, 24, 48 and 80: every kernel
+def test_long_caches_are_averaged_without_bias(dtype, tokens, heads):
+    """65536 keys of nearly equal weight: the result is 1/256 of the values, so errors of the weights that all lie on one side would show.
+    bf16: roundings to nearest of the result, of the weights and of the weights times the scales, each at most 2^-9 of a number and 2^-9 / sqrt(3) on
+    average, together 2^-9; twice that is allowed.  fp32: 2^-24 for each of some hundred additions to a sum, 2^-17."""
+    page, dim, n_keys = 256, 64, 65536
+    g = gen(tokens)
+    ref = ref_cache(page, dim, 1, 1, g, n_keys)
+    at = ref.table[0].long()
+    qkv = (0.2 * torch.randn(1, tokens, (heads + 2) * dim, generator=g)).to(DT[dtype])
+
+    def unpacked(codes, pair):                                   # codes [pages, page, D], pair [pages, page]
+        scale, low = (pair.long() << 16).to(torch.int32).view(torch.float32).double(), (pair & -65536).view(torch.float32).double()
+        return (codes.double() * scale[..., None] + low[..., None]).reshape(n_keys, dim)
+    k = unpacked(R.codes_of(ref.k[at][:, 0].contiguous().view(torch.int32)), ref.ks[at][:, 0, :, 0])
+    v = unpacked(R.codes_of(ref.v[at][:, 0].contiguous().view(torch.int32)).transpose(2, 3).reshape(len(at), page, dim), ref.vs[at][:, 0, :, 0])
+    for p in (0, 31, 32, 300, n_keys - 1):
+        assert torch.equal(k[p], ref.value(0, p, "k")[0]) and torch.equal(v[p], ref.value(0, p, "v")[0])
+    q = qkv[0, :, :heads * dim].double().reshape(tokens, heads, dim)
+    seen = torch.arange(n_keys)[None, :] <= n_keys - tokens + torch.arange(tokens)[:, None]
+    score = torch.einsum("thd,kd->thk", q, k) * dim ** -0.5
+    want = torch.softmax(score.masked_fill(~seen[:, None], -float("inf")), -1) @ v
+    start = torch.tensor([n_keys - tokens], dtype=torch.int32)
+    out = torch.empty(1, tokens, heads * dim, dtype=DT[dtype], device="cuda")
+    s = session(lambda o: o.cache_attention(dev(qkv), out, on_gpu(ref), dev(start), None, heads=heads), dtype, 1)
+    s.enqueue()
+    torch.cuda.synchronize()
+    err = (out.cpu().double().reshape(want.shape) - want).norm() / want.norm()
+    assert err <= (2.0 ** -8 if dtype == "bf16" else 2.0 ** -17), float(err)
+    s.close()
