@@ -105,8 +105,9 @@ static constexpr float NO_SCORE = -1e38f;
 template <typename V> __device__ __forceinline__ void in_branch(V &v) { asm volatile("" : "+v"(v)); }
 
 // Bytes of LDS that a tile of 64 unpacked keys and values takes in the kernel for 128 rows: rows of keys and of features (16 bytes apart more
-// than they are long, so that their starts fall on all banks), the keys' further operand, the minima, the scales
-constexpr int wide_tile_bytes(int D, bool f32) { return 64 * (2 * D + 16) + D * 144 + 64 * 32 + D / 64 * (f32 ? 256 : 2 * 144) + D / 64 * 512; }
+// than they are long, so that their starts fall on all banks), the keys' further operand, the minima (bf16 tenants: in
+// two parts, and a row of zeros), the scales
+constexpr int wide_tile_bytes(int D, bool f32) { return 64 * (2 * D + 16) + D * 144 + 64 * 32 + (f32 ? D / 64 * 256 : (D / 64 * 2 + 1) * 144) + D / 64 * 512; }
 
 void launch_cache_attention_wide(const AttendArgs &b, int dtype, int D, int grid, hipStream_t s);      // rows of 128
 

@@ -7,19 +7,19 @@
 // order of the keys within that product is the one in which a lane holds them, and the values are stored in it.  As in the kernel for
 // few rows the scales are applied in fp32,
 //   q.k_j = sum over groups g of  s_jg * (sum_d q_d (c_jd - z)) + (m_jg + z s_jg) * sum_d q_d             (z = 8 or -16)
-//   out_d = sum_j (p_j s_jg) (c_jd - 8) + sum_j p_j (m_jg + 8 s_jg)
+//   out_d = sum_j w_jg (c_jd - 8) + sum_j w_jg (m_jg / s_jg + 8)                                        (w_jg = p_j s_jg)
 // with the second sum of the scores as a further matrix instruction: the pair (s, m) of a key, two bf16 numbers, times the sums of the queries
 // in three bf16 parts, and a one times the parts of minus the row's reference; that of the result likewise in bf16 tenants, the weights times
-// m + 8 s in two parts.  fp32 tenants have their queries and weights in three bf16 parts each, every part a matrix instruction, and add
-// p_j (m + 8 s) as it is.  In bf16 tenants the weights p_j s_jg are rounded to bf16 once: with codes around zero that is as much as the result's own
-// rounding adds (2.2e-3 of the result together, 1.7e-3 for the latter alone), and a second part would be 16 more matrix instructions per 64
-// keys and two more operations per weight.
+// m / s + 8 in two parts.  fp32 tenants have their queries and weights in three bf16 parts each, every part a matrix instruction, and add
+// p_j (m + 8 s) as it is.  In bf16 tenants the weights w are rounded to bf16 once, and both sums take them rounded, so that what rounding
+// does to a key is a factor, however far its values lie from its codes' middle: about as much as the result's own rounding adds, and a second part
+// would be 16 more matrix instructions per 64 keys and two more operations per weight.
 //
 // Bound by the two waves of a SIMD that 238 registers allow: each runs scores, exponentials and products one after another, and vector
 // instructions (52 % of the time), matrix instructions (32 %), LDS (35 %) and waits for LDS and barriers (39 %) fill each other's gaps only in part.  A
-// prompt of 4096 tokens, 32 heads of 128 features over 8 (bf16): 223 us = 617 TFLOP/s, where a large product reaches 1377.  256 rows a workgroup, which
-// halve the unpacking: 212 there, but 98 against 93 at 2048 tokens and 361 against 344 at 16 x 256 tokens after 4096 keys; two groups
-// of waves that take turns at the matrix cores, a barrier after each turn: 263.
+// prompt of 4096 tokens, 32 heads of 128 features over 8 (bf16): 230 us = 600 TFLOP/s, where a large product reaches 1377.  256 rows a workgroup, which
+// halve the unpacking: 5 % faster there, but 98 us against 93 at 2048 tokens and 361 against 344 at 16 x 256 tokens after 4096 keys; two groups
+// of waves that take turns at the matrix cores, a barrier after each turn: 17 % slower.
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include "cache_attention.h"
@@ -29,10 +29,10 @@ namespace gacer {
 template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 && D == 128 ? 1 : 2) void cache_attention_wide_kernel(AttendArgs a)
 {
     constexpr bool F32 = sizeof(T) == 4;
-    constexpr int QP = F32 ? 3 : 1, PP = F32 ? 3 : 1, MP = 2;                  // bf16 parts of queries, weights, and of the minima m + 8 s
+    constexpr int QP = F32 ? 3 : 1, PP = F32 ? 3 : 1, MP = 2;                  // bf16 parts of queries, weights, and of the minima (m + 8 s) / s
     constexpr float K_UNIT = F32 ? 16.f : 1.f, K_MIDDLE = F32 ? 8.f : -16.f;   // keys in LDS: (c - 8) / 16 or 16 + c; value of a step, of where they are zero
     constexpr int NG = D / 64, ROWS = 128, KROW = D * 2 + 16, VROW = 128 + 16, KROWS = 64 * KROW, VROWS = D * VROW;
-    constexpr int EXT_K = 64 * 32, EXT_V = F32 ? NG * 64 * 4 : MP * NG * VROW, BUF = wide_tile_bytes(D, F32);
+    constexpr int EXT_K = 64 * 32, EXT_V = F32 ? NG * 64 * 4 : (MP * NG + 1) * VROW, BUF = wide_tile_bytes(D, F32);
     constexpr int ITEMS = 64 * D / 32;                 // 16-byte pieces of a tile's key codes, and of its value codes
     __shared__ __align__(16) unsigned char lds[2 * BUF];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
@@ -109,14 +109,16 @@ template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 &&
                     scales[i * 64 + skey] = sc * K_UNIT * a.scale;
                     e[i] = sin[i];
                 } else {
-                    scales[(NG + i) * 64 + skey] = sc * 16.f;
-                    const float mm = fmaf(8.f, sc, m);
                     if constexpr (F32) {
-                        ((float *)(buf + KROWS + VROWS + EXT_K))[i * 64 + skey] = mm;
+                        scales[(NG + i) * 64 + skey] = sc * 16.f;
+                        ((float *)(buf + KROWS + VROWS + EXT_K))[i * 64 + skey] = fmaf(8.f, sc, m);
                         continue;
                     }
+                    // where the scale is nothing against the minimum, a small one: 15 of it are 2^-26 of the minimum
+                    const float tiny = fabsf(m) * 0x1p-30f, unit = tiny > sc ? tiny : sc;
+                    scales[(NG + i) * 64 + skey] = unit * 16.f;
                     unsigned part[MP];
-                    split_bf16<MP>(mm, part);
+                    split_bf16<MP>(unit == 0.f ? 0.f : fmaf(__fdiv_rn(m, unit), 0.0625f, 0.5f), part);       // in units of the codes' 16ths
 #pragma unroll
                     for (int k = 0; k < MP; ++k) *(unsigned short *)(buf + KROWS + VROWS + EXT_K + (MP * i + k) * VROW + slot * 2) = (unsigned short)(part[k] >> 16);
                 }
@@ -129,6 +131,7 @@ template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 &&
         }
     };
     if (lo < hi) load(lo);
+    if (!F32 && tid < 2 * VROW / 4) ((unsigned *)(lds + (tid >= VROW / 4) * BUF + KROWS + VROWS + EXT_K + MP * NG * VROW))[tid % (VROW / 4)] = 0u;
 
     // -- queries: lane & 31 = row; features 16 t + 8 half .. of step t, and the sums of each group as the operand of the pairs -----------
     bf16x8 q[QP][NG * 4], qx;
@@ -288,21 +291,22 @@ template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 &&
                     cr[i] += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
                 }
             } else {
-                bf16x8 mx = *(const bf16x8 *)(buf + KROWS + VROWS + EXT_K + min(l32, MP * NG - 1) * VROW + at_key);
-                if (edge) {                                // the same for their minima: an operand that holds no NaN
-                    uint4 u = __builtin_bit_cast(uint4, mx);
-                    unsigned *e = (unsigned *)&u;
-                    asm volatile("" : "+v"(e[0]));
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if ((e[i] & 0x7F80u) == 0x7F80u) e[i] &= 0xFFFF0000u;
-                        if ((e[i] & 0x7F800000u) == 0x7F800000u) e[i] &= 0xFFFFu;
+                for (int i = 0; i < NG; ++i) {             // the minima of a group meet the weights of that group
+                    bf16x8 mx = *(const bf16x8 *)(buf + KROWS + VROWS + EXT_K + (l32 / MP == i ? l32 : MP * NG) * VROW + at_key);
+                    if (edge) {                            // the same for them: an operand that holds no NaN
+                        uint4 u = __builtin_bit_cast(uint4, mx);
+                        unsigned *e = (unsigned *)&u;
+                        asm volatile("" : "+v"(e[0]));
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            if ((e[j] & 0x7F80u) == 0x7F80u) e[j] &= 0xFFFF0000u;
+                            if ((e[j] & 0x7F800000u) == 0x7F800000u) e[j] &= 0xFFFFu;
+                        }
+                        mx = __builtin_bit_cast(bf16x8, u);
                     }
-                    mx = __builtin_bit_cast(bf16x8, u);
+                    corr = mfma(mx, w[i][0], corr);
                 }
-                bf16x8 wp[1];
-                operands<1>(p + 8 * k, wp);
-                corr = mfma(mx, wp[0], corr);
             }
 #pragma unroll
             for (int c = 0; c < D / 32; ++c) {

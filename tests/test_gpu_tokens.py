@@ -669,3 +669,27 @@ def test_long_caches_are_averaged_without_bias(dtype, tokens, heads):
     err = (out.cpu().double().reshape(want.shape) - want).norm() / want.norm()
     assert err <= (2.0 ** -8 if dtype == "bf16" else 2.0 ** -17), float(err)
     s.close()
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("tokens", [1, 6, 12])                   # rows of 4, 24 and 48: every bf16 kernel
+def test_values_at_the_end_of_their_range(tokens, dim):
+    """Groups with a value far from all others: codes 0 and 1 of 16, around zero, so that the middle of the codes is 15 times what the values are.  Roundings
+    of weights must stay factors of the keys' own values: the norm of the error as in the test of long caches, 2^-8."""
+    page, heads, n_keys = 64, 4, 300
+    g = gen(dim + tokens)
+    ref = ref_cache(page, dim, 1, 1, g, n_keys)
+    ref.v &= 0x11
+    scale = 0.1 + 0.3 * torch.rand(ref.vs.shape, generator=g)
+    scale = scale.bfloat16().float()
+    ref.vs.copy_(R.pairs(scale, -0.5 * scale))
+    qkv = (0.2 * torch.randn(1, tokens, (heads + 2) * dim, generator=g)).bfloat16()
+    start = torch.tensor([n_keys - tokens], dtype=torch.int32)
+    want, _ = R.attention(ref, qkv, heads, start, None, dim ** -0.5, 0)
+    out = torch.empty(1, tokens, heads * dim, dtype=torch.bfloat16, device="cuda")
+    s = session(lambda o: o.cache_attention(dev(qkv), out, on_gpu(ref), dev(start), None, heads=heads), "bf16", 1)
+    s.enqueue()
+    torch.cuda.synchronize()
+    err = (out.cpu().double() - want).norm() / want.norm()
+    assert err <= 2.0 ** -8, float(err)
+    s.close()
