@@ -168,8 +168,8 @@ typedef struct {
  * count is taken as 0..S; a negative start or one beyond the pages makes it 0).
  *   Codes: groups of GACER_CACHE_GROUP features of one head and token share a pair of bf16 numbers (scale, minimum) in one
  * 32-bit word (scale in the low half); a code c in 0..15 stands for c * scale + minimum.  Writing a group of x takes
- * minimum = bf16(min x), scale = bf16((max x - min x) / 15), c = round((x - minimum) / scale) clamped to 0..15 (ties to even; 0 where scale
- * is 0), in fp32.  A group that holds an infinity or a NaN, or whose scale or minimum overflows, gets a NaN scale (0x7FC0) and reads back as NaN.
+ * minimum = bf16(min x), scale = bf16((max x - min x) * 0x1.111112p-4f) (1/15 in fp32), c = round((x - minimum) / scale) clamped to 0..15 (ties to
+ * even; 0 where scale is 0), in fp32.  A group that holds an infinity or a NaN, or whose scale or minimum overflows, gets a NaN scale (0x7FC0) and reads back as NaN.
  *   Layout: k_codes [page][kv head][token][head_dim/8 words], word i = features 8i..8i+7; v_codes [page][kv head][token / 32][feature][4 words],
  * word i = tokens 8i..8i+7 of the block of 32; the eight codes of a word start at bits 0, 16, 4, 20, 8, 24, 12, 28.
  * k_scales and v_scales [page][kv head][token][head_dim/GACER_CACHE_GROUP].

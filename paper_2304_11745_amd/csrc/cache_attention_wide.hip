@@ -115,7 +115,7 @@ template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 &&
                         continue;
                     }
                     // where the scale is nothing against the minimum, a small one: 15 of it are 2^-26 of the minimum
-                    const float tiny = fabsf(m) * 0x1p-30f, unit = tiny > sc ? tiny : sc;
+                    const float tiny = fabsf(m) * 0x1p-30f, unit = fabsf(sc) < tiny ? tiny : sc;
                     scales[(NG + i) * 64 + skey] = unit * 16.f;
                     unsigned part[MP];
                     split_bf16<MP>(unit == 0.f ? 0.f : fmaf(__fdiv_rn(m, unit), 0.0625f, 0.5f), part);       // in units of the codes' 16ths

@@ -230,7 +230,7 @@ __device__ __forceinline__ unsigned quantise(const float *v, unsigned &pair)
     }
     lo = group_min(lo == lo ? lo : -INFINITY);
     hi = group_max(hi);
-    const unsigned short low = to_bf16(lo), step = to_bf16(divided(__fsub_rn(hi, lo), 15.f, 1.f / 15.f));
+    const unsigned short low = to_bf16(lo), step = to_bf16(__fmul_rn(__fsub_rn(hi, lo), 1.f / 15.f));
     const float m = ld_f32(&low, 0) + 0.f, s = ld_f32(&step, 0);
     if (!(fabsf(s) < INFINITY && fabsf(m) < INFINITY)) {
         pair = 0x7FC0u;

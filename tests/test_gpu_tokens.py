@@ -693,3 +693,26 @@ def test_values_at_the_end_of_their_range(tokens, dim):
     err = (out.cpu().double() - want).norm() / want.norm()
     assert err <= 2.0 ** -8, float(err)
     s.close()
+
+
+@pytest.mark.parametrize("tokens", [1, 6, 12])                   # rows of 4, 24 and 48
+def test_groups_without_a_scale(tokens):
+    """Groups of equal values have scale 0, whatever their codes hold: they read as their minimum, beside groups that have a scale."""
+    page, dim, heads, n_keys = 64, 128, 4, 200
+    g = gen(40 + tokens)
+    ref = ref_cache(page, dim, 1, 1, g, n_keys)
+    scale = 0.1 + 0.3 * torch.rand(ref.vs.shape, generator=g)
+    scale[..., 0] = 0.0                                          # the first 64 features of every token, some of them zero altogether
+    low = torch.randn(ref.vs.shape, generator=g)
+    low[:, :, ::3, 0] = 0.0
+    for s in (ref.vs, ref.ks):
+        s.copy_(R.pairs(scale, low))
+    qkv = (0.2 * torch.randn(1, tokens, (heads + 2) * dim, generator=g)).bfloat16()
+    start = torch.tensor([n_keys - tokens], dtype=torch.int32)
+    want, weight = R.attention(ref, qkv, heads, start, None, dim ** -0.5, 0)
+    out = torch.empty(1, tokens, heads * dim, dtype=torch.bfloat16, device="cuda")
+    s = session(lambda o: o.cache_attention(dev(qkv), out, on_gpu(ref), dev(start), None, heads=heads), "bf16", 1)
+    s.enqueue()
+    torch.cuda.synchronize()
+    check_attention(out, want, weight, "bf16", dim)
+    s.close()

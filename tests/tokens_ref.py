@@ -38,7 +38,7 @@ def quantise(x):
     g = x.float().reshape(*x.shape[:-1], -1, GROUP)
     lo, hi = g.min(-1).values, g.max(-1).values
     bad = ~torch.isfinite(g).all(-1)
-    scale, low = bf16((hi - lo) / 15), bf16(lo) + 0.0                  # a minimum of zero is stored without a sign
+    scale, low = bf16((hi - lo) * torch.tensor(1 / 15, dtype=torch.float32)), bf16(lo) + 0.0                  # a minimum of zero is stored without a sign
     bad |= ~torch.isfinite(scale) | ~torch.isfinite(low)
     c = torch.round((g - low[..., None]) / scale[..., None]).clamp(0, 15)
     c = torch.where((scale > 0)[..., None] & ~bad[..., None], c, torch.zeros_like(c))
