@@ -696,7 +696,8 @@ template <typename T, bool PLAIN> __device__ __forceinline__ void sample_row(con
             draw_from_list(s, w, f, first, write);
         };
         if (sizeof(T) == 4 && f.top_k <= THREADS / 4) {
-            // top-k entries of the row are no smaller than the top-k of the threads' largest ones, and few others are
+            // the k largest entries are no smaller than the k largest of the threads' largest ones, and few others are: against the bins one row of 32000
+            // takes 10.9 us instead of 14.6 with k = 50, 19.3 instead of 22.6 with 256, but 34 instead of 32 with 500 and 119 instead of 65 with 900
             clear();
             to_bin(mine);
             __syncthreads();
