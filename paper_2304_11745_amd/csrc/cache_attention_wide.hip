@@ -15,7 +15,7 @@
 // does to a key is a factor, however far its values lie from its codes' middle: about as much as the result's own rounding adds, and a second part
 // would be 16 more matrix instructions per 64 keys and two more operations per weight.
 //
-// Bound by the two waves of a SIMD that 238 registers allow: each runs scores, exponentials and products one after another, and vector
+// Bound by the two waves of a SIMD that 254 registers allow: each runs scores, exponentials and products one after another, and vector
 // instructions (52 % of the time), matrix instructions (32 %), LDS (35 %) and waits for LDS and barriers (39 %) fill each other's gaps only in part.  A
 // prompt of 4096 tokens, 32 heads of 128 features over 8 (bf16): 232 us = 590 TFLOP/s, where a large product reaches 1377.  256 rows a workgroup, which
 // halve the unpacking: 5 % faster there, but 98 us against 93 at 2048 tokens and 361 against 344 at 16 x 256 tokens after 4096 keys; two groups
@@ -170,11 +170,13 @@ template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 &&
         qx = __builtin_bit_cast(bf16x8, half ? second : first);
     }
     const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    f32x16 o[D / 32], small[F32 ? D / 32 : 1], corr = zero;             // small: of the weights' second and third parts
+    f32x16 o[D / 32], small[F32 ? D / 32 : 1], corr[NG];                 // small: of the weights' second and third parts; corr: the minima's part of the result in bf16
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) o[c] = zero;
 #pragma unroll
     for (int c = 0; c < (F32 ? D / 32 : 1); ++c) small[c] = zero;
+#pragma unroll
+    for (int i = 0; i < NG; ++i) corr[i] = zero;
     float base = 0.f, l = 0.f, cr[NG];             // cr: the minima's part of the result, of the lane's keys (fp32) or at the end
 #pragma unroll
     for (int i = 0; i < NG; ++i) cr[i] = 0.f;
@@ -241,8 +243,12 @@ template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 &&
 #pragma unroll
             for (int i = 0; i < NG; ++i) cr[i] *= f;
 #pragma unroll
+            for (int i = 0; i < (F32 ? 0 : NG); ++i) {      // the two rows of a group's sums that are looked at
+                corr[i][2 * i] *= f;
+                corr[i][2 * i + 1] *= f;
+            }
+#pragma unroll
             for (int e = 0; e < 16; ++e) {
-                if constexpr (!F32) corr[e] *= f;
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c) {
                     o[c][e] *= f;
@@ -292,7 +298,7 @@ template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 &&
                 }
             } else {
 #pragma unroll
-                for (int i = 0; i < NG; ++i) {             // the minima of a group meet the weights of that group
+                for (int i = 0; i < NG; ++i) {             // the minima of a group meet the weights of that group, in sums of their own: the other group's may be NaN
                     bf16x8 mx = *(const bf16x8 *)(buf + KROWS + VROWS + EXT_K + (l32 / MP == i ? l32 : MP * NG) * VROW + at_key);
                     if (edge) {                            // the same for them: an operand that holds no NaN
                         uint4 u = __builtin_bit_cast(uint4, mx);
@@ -305,7 +311,7 @@ template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 &&
                         }
                         mx = __builtin_bit_cast(bf16x8, u);
                     }
-                    corr = mfma(mx, w[i][0], corr);
+                    corr[i] = mfma(mx, w[i][0], corr[i]);
                 }
             }
 #pragma unroll
@@ -348,7 +354,7 @@ template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 &&
     for (int i = 0; i < NG; ++i) {
         if constexpr (F32) cr[i] += __shfl_xor(cr[i], 32, 64);
         else {                                         // rows 2 i and 2 i + 1 of the product, in half 0
-            const float v = corr[2 * i] + corr[2 * i + 1], other = __shfl_xor(v, 32, 64);
+            const float v = corr[i][2 * i] + corr[i][2 * i + 1], other = __shfl_xor(v, 32, 64);
             cr[i] = half ? other : v;
         }
     }

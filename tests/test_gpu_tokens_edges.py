@@ -1,0 +1,46 @@
+"""Operators of a decoding tenant on the GPU where a mistake is easily overlooked.  References in 64 bits on the CPU."""
+import pytest
+import torch
+
+import tokens_ref as R
+from test_gpu_tokens import DT, dev, gen, on_gpu, ref_cache, session
+
+pytestmark = pytest.mark.gpu
+
+
+# -- values that are not finite ------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens,page,room", [(1, 64, 0), (3, 32, 0), (6, 64, 0), (12, 64, 0), (40, 32, 0), (12, 64, 16384), (40, 64, 16384)])      # rows of 4 to 160, keys in splits
+def test_a_value_group_that_is_not_finite_stays_in_its_features(dtype, tokens, page, room):
+    """A group of 64 features with an infinity or a NaN reads as NaN; a query that sees it has NaN in these features and its usual result in the others, one that does
+    not see it is untouched.  A key group that is not finite makes the key's score NaN, and with it the row."""
+    dim, heads, kv, starts = 128, 8, 2, [150, 0, 70]
+    g = gen(tokens + room)
+    ref = ref_cache(page, dim, kv, 3, g, 192)
+    if room:
+        ref.table = torch.cat((ref.table, torch.full((3, (room - 192) // page), -1, dtype=torch.int32)), 1)
+    qkv = (0.3 * torch.randn(3, tokens, (heads + 2 * kv) * dim, generator=g)).to(DT[dtype])
+    start = torch.tensor(starts, dtype=torch.int32)
+
+    def poison(scales, b, p, head, group):
+        at, o = ref.where(b, p)
+        scales[at, head, o, group] = 0x7FC0
+    poison(ref.vs, 0, 33, 0, 0)                                 # every token sees it
+    poison(ref.vs, 0, 149, 1, 1)
+    poison(ref.vs, 1, tokens // 2, 0, 1)                        # tokens before it do not
+    poison(ref.vs, 1, tokens - 1, 1, 0)
+    poison(ref.ks, 2, 70 + tokens // 2, 1, 0)
+    out = torch.full((3, tokens, heads * dim), 7.0, dtype=DT[dtype], device="cuda")
+    s = session(lambda o: o.cache_attention(dev(qkv), out, on_gpu(ref), dev(start), None, heads=heads), dtype, 3)
+    s.enqueue()
+    torch.cuda.synchronize()
+    got = out.cpu().double().reshape(3, tokens, heads, 2, 64)
+    want, weight = R.attention(ref, qkv, heads, start, None, dim ** -0.5, 0)
+    want, weight = (x.reshape(got.shape) for x in (want, weight))
+    assert torch.isnan(want).any() and not torch.isnan(want).all(-1).all()
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    score = 2 * 64 * 2.0 ** -24 * 16
+    relative = score + 2.0 ** -20 + (2.0 ** -8 if dtype == "bf16" else 0.0)
+    err = (got - want).nan_to_num().abs()
+    assert (err <= (relative * (weight + 6.5) + (2.0 ** -8 * want.abs() if dtype == "bf16" else 0.0)).nan_to_num()).all()
+    s.close()
