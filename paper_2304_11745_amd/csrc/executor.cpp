@@ -95,10 +95,13 @@ bool axis_legal(gacer_opkind kind, gacer_axis axis)
     return false;
 }
 
+// channels of an operator's output; an operator that writes none of the tenant's tensors counts as one channel
+static int out_channels(const Tenant &t, int oi) { return t.ops[oi].out < 0 ? 1 : (int)t.tensors[t.ops[oi].out].c; }
+
 int axis_extent(const Tenant &t, int op, gacer_axis axis)
 {
     if (axis == GACER_AXIS_BATCH) return t.batch;
-    if (axis == GACER_AXIS_COUT) return (int)t.tensors[t.ops[op].out].c;
+    if (axis == GACER_AXIS_COUT) return out_channels(t, op);
     return 1;
 }
 
@@ -110,9 +113,6 @@ void chunk_range(int extent, int factor, int j, int *lo, int *hi)
 }
 
 static int dt(const Tenant &t) { return t.dtype == GACER_BF16 ? DT_BF16 : DT_F32; }
-
-// channels of an operator's output; an operator that writes none of the tenant's tensors counts as one channel
-static int out_channels(const Tenant &t, int oi) { return t.ops[oi].out < 0 ? 1 : (int)t.tensors[t.ops[oi].out].c; }
 
 // The launch of an operator of a decoding tenant, sequences [b_lo, b_hi)
 static Launch make_token_launch(const Tenant &t, int oi, int b_lo, int b_hi)

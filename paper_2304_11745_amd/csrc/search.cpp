@@ -307,6 +307,11 @@ gacer_status build_model(Ctx *c, const gacer_prof *prof, size_t n, Model &m)
             c->err = "profile table row names a missing operator or an illegal (axis, factor)";
             return GACER_EINVAL;
         }
+        const gacer_opkind kind = c->tenants[p.tenant].ops[p.op].kind;
+        if (p.factor > 1 && is_token_op(kind) && !axis_legal(kind, p.axis)) {
+            c->err = "profile table row names an axis that an operator of a decoding tenant does not have";
+            return GACER_EINVAL;
+        }
         OpCosts &o = m.ops[p.tenant][p.op];
         Cost cost;
         cost.T = p.ms; cost.W = p.cu_share; cost.Wb = p.bw_share;

@@ -1,0 +1,24 @@
+// Geometry-only launcher of the operators of a decoding tenant, beside stub_kernels.cpp: the executor's own code runs, kernels do not.
+#include "../../paper_2304_11745_amd/csrc/kernels.h"
+#include "../../paper_2304_11745_amd/csrc/tokens_geom.h"
+#include "token_kernels.h"
+
+namespace gacer {
+TokenLaunches token_launches;
+LaunchInfo launch_tokens(const TokenArgs &a, hipStream_t, bool dry, int phase)
+{
+    LaunchInfo li;
+    li.workgroups = (a.b_hi - a.b_lo) * (a.op == TK_SAMPLE ? a.S : 1);
+    li.threads = 256; li.lds_bytes = 0; li.wg_per_cu = 8; li.kernel = phase == 2 ? "token_join" : "token";
+    li.phases = a.op == TK_CACHE_ATTENTION && attend_geom(a).splits > 1 ? 2 : 1;
+    if (!dry) {
+        ++token_launches.all;
+        if (a.op == TK_QKNORM_ROPE && a.x == a.y) {
+            token_launches.last_in_place = a.x;
+            ++token_launches.in_place;
+        }
+        if (token_ws_floats(a)) a.ws[token_ws_floats(a) - 1] = 1.f;      // the last float of the workspace is there
+    }
+    return li;
+}
+}  // namespace gacer
