@@ -361,7 +361,9 @@ gacer_status gacer_trace_run(gacer_ctx *ctx, int mode, int rounds, gacer_launch_
 /*
  * Builds the lookup table of Section 4.1 by timing, in isolation on the tenant's stream, every
  * operator unsplit and for every legal (axis, factor in {2,4,8}); plus the T_SW row.  Tenant
- * inputs must hold finite data (the call runs each tenant once first).  Writes up to `cap`
+ * inputs must hold finite data (the call runs each tenant once first).  What it leaves behind is what rounds leave: a decoding
+ * tenant's caches and tokens are written at the positions that its arrays hold, as gacer_run would (and gacer_refine, by its
+ * trial rounds); operators in place are timed on memory that the call allocates for itself.  Writes up to `cap`
  * rows to `out` (host) and the total number of rows to *n; call with cap = 0 to size.
  */
 gacer_status gacer_profile(gacer_ctx *ctx, gacer_prof *out, size_t cap, size_t *n);

@@ -113,7 +113,10 @@ int main()
         size_t n = 0;
         CHECK(gacer_profile(ctx, nullptr, 0, &n) == GACER_OK);
         std::vector<gacer_prof> table(n);
+        const long own_before = gacer::token_launches.in_place_at[at(1)];
         CHECK(gacer_profile(ctx, table.data(), n, &n) == GACER_OK);
+        // timed on other memory than the tenant's: on its own only in the rounds (one first, one more where a switch is timed)
+        CHECK(gacer::token_launches.in_place_at[at(1)] - own_before == (in_place ? (two ? 4 : 1) : 0));
         for (int k = 0; k < 6; ++k) {
             std::vector<gacer_prof> prof;
             std::uniform_real_distribution<float> uT(0.1f, 2.0f), uW(0.05f, 1.0f);

@@ -13,10 +13,7 @@ LaunchInfo launch_tokens(const TokenArgs &a, hipStream_t, bool dry, int phase)
     li.phases = a.op == TK_CACHE_ATTENTION && attend_geom(a).splits > 1 ? 2 : 1;
     if (!dry) {
         ++token_launches.all;
-        if (a.op == TK_QKNORM_ROPE && a.x == a.y) {
-            token_launches.last_in_place = a.x;
-            ++token_launches.in_place;
-        }
+        if (a.op == TK_QKNORM_ROPE && a.x == a.y) ++token_launches.in_place_at[a.x];
         if (token_ws_floats(a)) a.ws[token_ws_floats(a) - 1] = 1.f;      // the last float of the workspace is there
     }
     return li;

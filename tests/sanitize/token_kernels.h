@@ -1,6 +1,10 @@
 // What the geometry-only launcher of a decoding tenant's operators has been asked to do.
 #pragma once
+#include <map>
 namespace gacer {
-struct TokenLaunches { long all = 0, in_place = 0; const void *last_in_place = nullptr; };
+struct TokenLaunches {
+    long all = 0;
+    std::map<const void *, long> in_place_at;     // rotations in place, by their memory
+};
 extern TokenLaunches token_launches;
 }  // namespace gacer

@@ -1,9 +1,11 @@
 """Operators of a decoding tenant on the GPU where a mistake is easily overlooked.  References in 64 bits on the CPU."""
+import ctypes as C
+
 import pytest
 import torch
 
 import tokens_ref as R
-from test_gpu_tokens import DT, dev, gen, on_gpu, ref_cache, session
+from test_gpu_tokens import DT, dev, gen, on_gpu, ref_cache, same, session, small_tenant, snapshot
 
 pytestmark = pytest.mark.gpu
 
@@ -44,3 +46,54 @@ def test_a_value_group_that_is_not_finite_stays_in_its_features(dtype, tokens, p
     err = (got - want).nan_to_num().abs()
     assert (err <= (relative * (weight + 6.5) + (2.0 ** -8 * want.abs() if dtype == "bf16" else 0.0)).nan_to_num()).all()
     s.close()
+
+
+# -- profiles ------------------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lists", [1, 2])
+def test_a_profile_leaves_what_a_round_leaves(dtype, lists):
+    """Rotation in place, timed many times over, must not reach the cache or the tokens: after a profile everything is as after the round before it."""
+    from paper_2304_11745_amd import binding as B
+    from paper_2304_11745_amd import tokens as T
+    made = [small_tenant(dtype) for _ in range(lists)]
+    s = T.TokenSession([m[0] for m in made], [torch.cuda.Stream() for _ in made])
+    s.run()
+    everything = [t for m in made for t in m[1]] + [t for m in made for t, _ in m[0]._tensors]
+    want = snapshot(everything)
+    n = C.c_size_t()
+    B.check(s.ctx, B.gacer_profile(s.ctx, None, 0, C.byref(n)))
+    rows = (B.gacer_prof * n.value)()
+    B.check(s.ctx, B.gacer_profile(s.ctx, rows, n.value, C.byref(n)))
+    left = same(snapshot(everything), want)
+    assert left
+    s.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_profile_turns_the_tenants_input_no_further_than_a_round(dtype):
+    """A list that begins with a rotation in place of its own input (no earlier operator writes it anew): a profile turns it once, as the round that it runs first does."""
+    from paper_2304_11745_amd import binding as B
+    from paper_2304_11745_amd import tokens as T
+    n, t, heads, kv, dim = 4, 3, 4, 2, 64
+    g = gen(8)
+    x0 = torch.randn(n, t, (heads + 2 * kv) * dim, generator=g).to(DT[dtype])
+    angle = torch.rand(10, dim // 2, generator=g)
+    table, pos = dev(torch.stack((angle.cos(), angle.sin()), -1)), torch.full((n, t, 1), 7, dtype=torch.int32, device="cuda")
+
+    def make():
+        x, ops = dev(x0), T.OpList(DT[dtype], n)
+        ops.qknorm_rope(x, x, pos, table, heads=heads, kv_heads=kv, head_dim=dim)
+        return x, ops
+    (x, ops), (y, other) = make(), make()
+    once = T.TokenSession([other])
+    once.run()
+    want = y.clone()
+    s = T.TokenSession([ops])
+    size = C.c_size_t()
+    B.check(s.ctx, B.gacer_profile(s.ctx, None, 0, C.byref(size)))
+    rows = (B.gacer_prof * size.value)()
+    B.check(s.ctx, B.gacer_profile(s.ctx, rows, size.value, C.byref(size)))
+    turned_once = same(snapshot([x]), [want])
+    assert turned_once
+    s.close()
+    once.close()
