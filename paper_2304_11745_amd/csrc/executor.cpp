@@ -134,9 +134,12 @@ static Launch make_token_launch(const Tenant &t, int oi, int b_lo, int b_hi)
         k.op = TK_QKNORM_ROPE;
         k.heads = d.rope.heads; k.kv_heads = d.rope.kv_heads; k.D = d.rope.head_dim;
         k.gamma_q = op.scale; k.gamma_k = op.shift; k.eps = op.alpha;
-        k.table = d.rope.table; k.positions = d.rope.positions;
-        k.R = d.rope.rotary_dims; k.interleaved = d.rope.interleaved; k.axes = d.rope.n_axes; k.n_positions = d.rope.n_positions;
-        for (int i = 0; i < 3; ++i) k.sections[i] = i < d.rope.n_axes ? d.rope.sections[i] : 0;
+        k.R = d.rope.rotary_dims; k.interleaved = d.rope.interleaved;
+        if (k.R) {                                     // otherwise the fields of the rotation are not looked at
+            k.table = d.rope.table; k.positions = d.rope.positions;
+            k.axes = d.rope.n_axes; k.n_positions = d.rope.n_positions;
+            for (int i = 0; i < 3; ++i) k.sections[i] = i < d.rope.n_axes ? d.rope.sections[i] : 0;
+        }
     } else if (op.kind == GACER_SAMPLE) {
         k.op = TK_SAMPLE;
         k.vocab = (int)in->c;

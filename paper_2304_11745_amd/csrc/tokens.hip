@@ -72,9 +72,11 @@ template <typename T, int LPH, int IT> __global__ __launch_bounds__(256) void qk
             for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
         }
     }
-    int pos[3];                                        // the token's position on each axis (a missing one is not looked at)
+    int pos[3] = {0, 0, 0};                            // the token's position on each axis (a missing one is not looked at)
+    if (a.R > 0) {                                     // without rotated features there are no positions
 #pragma unroll
-    for (int i = 0; i < 3; ++i) pos[i] = fixed_int(a.positions, token * a.axes + min(i, a.axes - 1));
+        for (int i = 0; i < 3; ++i) pos[i] = fixed_int(a.positions, token * a.axes + min(i, a.axes - 1));
+    }
     float c[4], s[4];
     if (turned) {
         const int pair = sub * 4, half = a.R / 2;

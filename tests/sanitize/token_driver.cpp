@@ -27,6 +27,7 @@ struct Step {
     {
         const int kv = 1 + (int)(rng() % 3), heads = kv * (1 + (int)(rng() % 4)), dim = rng() % 2 ? 64 : 128, vocab = 1000 + (int)(rng() % 100);
         rope = {heads, kv, dim, dim, (int)(rng() % 2), 1, {dim / 2, 0, 0}, 100, (const float *)FAKE, (const int *)FAKE};
+        if (rng() % 4 == 0) rope.rotary_dims = 0, rope.n_axes = (int)rng(), rope.sections[1] = (int)rng();      // norms alone: the rotation's fields may hold anything
         cache = {heads, kv, dim, 64, 10, max_pages, (int)(rng() % 2) * 100, FAKE, FAKE, (unsigned *)FAKE, (unsigned *)FAKE, (const int *)FAKE, (const int *)FAKE, nullptr};
         sampling = {(const float *)FAKE, nullptr, nullptr, nullptr, nullptr, (int *)FAKE, nullptr};
         const int64_t w = (int64_t)(heads + 2 * kv) * dim;
@@ -153,6 +154,8 @@ int main()
         }
         gacer_destroy(ctx);
     }
+    gacer_ctx *ctx = nullptr;
+    CHECK(gacer::token_launches.stray_positions == 0);
     std::printf("token driver: all checks held\n");
     return 0;
 }

@@ -11,6 +11,7 @@ LaunchInfo launch_tokens(const TokenArgs &a, hipStream_t, bool dry, int phase)
     li.workgroups = (a.b_hi - a.b_lo) * (a.op == TK_SAMPLE ? a.S : 1);
     li.threads = 256; li.lds_bytes = 0; li.wg_per_cu = 8; li.kernel = phase == 2 ? "token_join" : "token";
     li.phases = a.op == TK_CACHE_ATTENTION && attend_geom(a).splits > 1 ? 2 : 1;
+    if (a.op == TK_QKNORM_ROPE && a.R == 0 && (a.positions || a.axes || a.table)) ++token_launches.stray_positions;
     if (!dry) {
         ++token_launches.all;
         if (a.op == TK_QKNORM_ROPE && a.x == a.y) ++token_launches.in_place_at[a.x];

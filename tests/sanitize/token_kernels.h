@@ -3,7 +3,7 @@
 #include <map>
 namespace gacer {
 struct TokenLaunches {
-    long all = 0;
+    long all = 0, stray_positions = 0;            // all: launches; rotations of no feature that were given positions all the same
     std::map<const void *, long> in_place_at;     // rotations in place, by their memory
 };
 extern TokenLaunches token_launches;

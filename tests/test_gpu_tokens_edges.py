@@ -10,6 +10,27 @@ from test_gpu_tokens import DT, dev, gen, on_gpu, ref_cache, same, session, smal
 pytestmark = pytest.mark.gpu
 
 
+# -- norms without a rotation --------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dim", [8, 64, 128, 512])
+def test_norms_alone_look_at_no_positions(dtype, dim):
+    """rotary_dims = 0 through the library's own descriptor: no table, no positions, no axes."""
+    from paper_2304_11745_amd import tokens as T
+    heads, kv, g = 3, 1, gen(dim)
+    qkv, gamma = torch.randn(2, 5, 5 * dim, generator=g).to(DT[dtype]), 1 + 0.1 * torch.randn(dim, generator=g)
+    x, out = dev(qkv), torch.zeros(2, 5, 5 * dim, dtype=DT[dtype], device="cuda")
+    ops = T.OpList(DT[dtype], 2)
+    ops.qknorm_rope(x, out, None, None, heads=heads, kv_heads=kv, head_dim=dim, gamma_q=dev(gamma), gamma_k=dev(gamma), eps=1e-5, rotary_dims=0)
+    ops._descs[0].n_axes, ops._descs[0].sections = 0, (C.c_int * 3)(-1, 2 ** 30, 7)
+    s = T.TokenSession([ops])
+    s.enqueue()
+    torch.cuda.synchronize()
+    want = R.qknorm_rope(qkv, heads, kv, dim, None, None, gamma, gamma, 1e-5, 0, [0], False)
+    err = (out.cpu().double() - want).abs()
+    assert (err <= (2.0 ** -8 if dtype == "bf16" else 0) * want.abs() + 2.0 ** -19 * want.abs().amax()).all()
+    s.close()
+
+
 # -- values that are not finite ------------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("tokens,page,room", [(1, 64, 0), (3, 32, 0), (6, 64, 0), (12, 64, 0), (40, 32, 0), (12, 64, 16384), (40, 64, 16384)])      # rows of 4 to 160, keys in splits
