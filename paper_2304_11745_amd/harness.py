@@ -35,6 +35,10 @@ class Session:
         self.dev = torch.device(device)
         torch.cuda.set_device(self.dev)
         extra = list(extra)
+        here = torch.device("cuda", torch.cuda.current_device())
+        for ops in extra:
+            if ops.device != here:
+                raise ValueError(f"the tensors of an operator list are on {ops.device}, the session on {here}")
         self.tenants = list(tenants) + extra
         self.ctx = C.c_void_p()
         B.check(self.ctx, B.gacer_create(C.byref(self.ctx)))

@@ -35,7 +35,7 @@ class Cache:
         _need(k_codes.dtype == torch.uint8 and v_codes.dtype == torch.uint8, "codes must be uint8")
         _need(page_table.dim() == 2 and page_table.dtype == torch.int32, "page_table must be int32 [batch, pages]")
         for t in (k_codes, v_codes, k_scales, v_scales, page_table):
-            _need(t.is_cuda and t.is_contiguous(), "the cache's tensors must be contiguous and on the GPU")
+            _need(t.is_cuda and t.is_contiguous() and t.device == k_codes.device, "the cache's tensors must be contiguous and on one GPU")
         self.k_codes, self.v_codes, self.k_scales, self.v_scales, self.page_table = k_codes, v_codes, k_scales, v_scales, page_table
         self.pages, self.kv_heads, self.page_tokens, self.head_dim = pages, heads, page, dim
 
@@ -147,6 +147,9 @@ class OpList:
     def _cache(self, cache, start, count, heads=0, kv_heads=None, head_dim=None, window=0):
         _need(kv_heads in (None, cache.kv_heads) and head_dim in (None, cache.head_dim), "heads do not match the cache's")
         _need(cache.page_table.shape[0] == self.batch, "the page table has a row per sequence")
+        if self.device is None:                      # a list that begins with a cache read
+            self.device = cache.k_codes.device
+        _need(cache.k_codes.device == self.device, "the cache must be on the tenant's GPU")
         st = self._array(start, torch.int32, (self.batch,), "start")
         ct = self._array(count, torch.int32, (self.batch,), "count")
         _need(st is not None, "start is missing")
@@ -208,6 +211,7 @@ class TokenSession:
             raise RuntimeError("a GPU is required: the library has no CPU fallback")
         self.lists = list(lists)
         self.device = self.lists[0].device
+        _need(all(l.device == self.device for l in self.lists), "the lists of a session are on one GPU")
         self.ctx = C.c_void_p()
         with torch.cuda.device(self.device):
             B.check(self.ctx, B.gacer_create(C.byref(self.ctx)))
