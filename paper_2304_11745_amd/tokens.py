@@ -222,20 +222,26 @@ class TokenSession:
     def enqueue(self, tenant=0, stream=None):
         """One round of a tenant on ``stream`` (default: PyTorch's current one), without waiting (gacer_enqueue)."""
         s = torch.cuda.current_stream(self.device) if stream is None else stream
-        st = B.gacer_enqueue(self.ctx, tenant, s.cuda_stream)
+        if torch.cuda.current_device() == self.device.index:
+            st = B.gacer_enqueue(self.ctx, tenant, s.cuda_stream)
+        else:                                        # kernels run on the current GPU; the null stream is each one's own
+            with torch.cuda.device(self.device):
+                st = B.gacer_enqueue(self.ctx, tenant, s.cuda_stream)
         if st:
             B.check(self.ctx, st)
 
     def run(self, mode=B.GACER_MODE_SEQUENTIAL, rounds=1):
         """Rounds of all tenants on their own streams (gacer_run); returns when they have finished."""
         ms = (C.c_float * rounds)()
-        B.check(self.ctx, B.gacer_run(self.ctx, mode, rounds, ms))
+        with torch.cuda.device(self.device):
+            B.check(self.ctx, B.gacer_run(self.ctx, mode, rounds, ms))
         return list(ms)
 
     def close(self):
         if self.ctx:
             torch.cuda.synchronize(self.device)
-            B.gacer_destroy(self.ctx)
+            with torch.cuda.device(self.device):
+                B.gacer_destroy(self.ctx)
             self.ctx = C.c_void_p()
 
     def __del__(self):
