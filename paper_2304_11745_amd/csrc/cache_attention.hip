@@ -23,6 +23,7 @@
 // and scores into weights bound it, and from 33 on (65 in fp32) the kernel for 128 rows takes over.
 #include <hip/hip_runtime.h>
 #include <limits.h>
+#include <algorithm>
 #include "cache_attention.h"
 #include "tokens_geom.h"
 
@@ -433,8 +434,11 @@ LaunchInfo launch_cache_attention(const TokenArgs &a, hipStream_t s, bool dry, i
     LaunchInfo li;
     li.workgroups = phase == 2 ? (join_by_groups(b, outputs) ? outputs : (int)(((int64_t)outputs * a.D + 1023) / 1024)) : grid;
     li.threads = phase == 2 ? 256 : g.waves * 64;
-    li.lds_bytes = phase == 2 ? 0 : g.rows == 128 ? 2 * wide_tile_bytes(a.D, a.dtype == DT_F32) : g.waves * g.rows * (a.D + 2) * 4;
-    li.wg_per_cu = phase == 2 ? 8 : g.per_cu;
+    const bool f32 = a.dtype == DT_F32, grouped = join_by_groups(b, outputs);
+    // up to 32 rows: the waves' patches of weights, or their results, and 12 bytes a row of them
+    const int few = g.waves * g.rows * (std::max(a.D / 64 * (f32 ? 3 : 2) * (128 + 16), a.D * 4) + 12);
+    li.lds_bytes = phase == 2 ? (grouped ? 4096 + 8192 / a.D : 0) : g.rows == 128 ? 2 * wide_tile_bytes(a.D, f32) : few;
+    li.wg_per_cu = phase == 2 ? (!grouped ? 7 : a.D == 64 ? 4 : 6) : g.per_cu;
     li.kernel = phase == 2 ? "cache_attention_join" : a.dtype == DT_BF16 ? "cache_attention_bf16" : "cache_attention_f32";
     li.phases = g.splits > 1 ? 2 : 1;
     if (dry || !grid) return li;

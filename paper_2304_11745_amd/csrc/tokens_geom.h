@@ -18,7 +18,9 @@ namespace gacer {
 //   splits  workgroups as many as the units hold at a time of a kernel with few rows (twice: one sequence of 131072 keys 49 against 41, four
 //           times 64), or with 128 (bf16 3 of 64 features, 2 of 128, fp32 2 and 1: 64 tokens of fp32 after 4 x 4096 keys 96 against 108
 //           with two), each with 1024 keys or 256 at least.
-struct AttendGeom { int rows, waves, row_tiles, splits, split_min, per_cu; };      // per_cu: workgroups that a unit holds
+// per_cu: workgroups that a unit holds, by the registers of their waves (4 waves: one workgroup of up to 512, two of 256, three of 168) and LDS.  8 waves of
+// 155 to 251 registers are one workgroup; of the kernels of 4 waves and up to 32 rows those of 64 features and up to 16 rows stay within 256, the others have 317 to 512.
+struct AttendGeom { int rows, waves, row_tiles, splits, split_min, per_cu; };
 inline AttendGeom attend_geom(const TokenArgs &a)
 {
     AttendGeom g;
@@ -29,7 +31,7 @@ inline AttendGeom attend_geom(const TokenArgs &a)
     const int64_t groups = (int64_t)a.batch * a.kv_heads * g.row_tiles;
     const int64_t most = std::min((int64_t)a.cache.max_pages << a.cache.page_shift, a.window > 0 ? (int64_t)a.window + a.S : (int64_t)1 << 40);
     const bool wide = g.rows == 128;
-    g.per_cu = wide ? (a.D == 64 ? 2 : 1) + (a.dtype == DT_BF16 ? 1 : 0) : 8 / g.waves;
+    g.per_cu = wide ? (a.D == 64 ? 2 : 1) + (a.dtype == DT_BF16 ? 1 : 0) : g.waves == 4 && a.D == 64 && g.rows <= 16 ? 2 : 1;
     const int want = 256 * (wide ? g.per_cu : 1), least = wide ? 256 : 1024;      // workgroups, keys of a split
     g.split_min = wide ? 4 : 8;
     g.splits = (int)std::min<int64_t>(std::min((want + groups - 1) / groups, std::max<int64_t>(1, most / least)), 128);
