@@ -20,6 +20,7 @@
 // logits, top-k 50 and top-p: 11 us, a chain of two passes, some twenty barriers and instructions that a single workgroup runs through once; by bins
 // 15, through the codes of bf16 as a first digit 21.
 #include <hip/hip_runtime.h>
+#include <algorithm>
 #include "device_util.h"
 #include "kernels.h"
 
@@ -37,6 +38,7 @@ struct SampleArgs {
     float *logp;
 };
 
+static constexpr int MOST_ROWS = 1 << 21;               // of a launch: a grid holds fewer than 2^32 threads
 static constexpr int THREADS = 1024, WAVES = THREADS / 64, BINS = 2048, LIST = 2048, CODES = 32768, GROUPS = 512, PEAKS = 768;
 // Entries that a list may hold where the alternative is another pass over the row: ranks by counting take n steps of a thread and more, a pass over 131072
 // entries what 600 of them take.
@@ -855,8 +857,11 @@ LaunchInfo launch_sample(const TokenArgs &a, hipStream_t s, bool dry, int)
     li.workgroups = (a.b_hi - a.b_lo) * a.S;
     li.threads = THREADS; li.lds_bytes = (int)sizeof(Shared); li.wg_per_cu = 1; li.kernel = a.dtype == DT_BF16 ? "sample_bf16" : "sample_f32"; li.phases = 1;
     if (dry || !li.workgroups) return li;
-    if (a.dtype == DT_BF16) GACER_LAUNCH(sample_kernel<unsigned short>, dim3(li.workgroups), dim3(THREADS), 0, s, b);
-    else GACER_LAUNCH(sample_kernel<float>, dim3(li.workgroups), dim3(THREADS), 0, s, b);
+    for (int at = 0; at < li.workgroups; at += MOST_ROWS, b.row_lo += MOST_ROWS) {
+        const dim3 grid(std::min(li.workgroups - at, MOST_ROWS));
+        if (a.dtype == DT_BF16) GACER_LAUNCH(sample_kernel<unsigned short>, grid, dim3(THREADS), 0, s, b);
+        else GACER_LAUNCH(sample_kernel<float>, grid, dim3(THREADS), 0, s, b);
+    }
     return li;
 }
 

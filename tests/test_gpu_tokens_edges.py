@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import tokens_ref as R
-from test_gpu_tokens import DT, dev, gen, on_gpu, ref_cache, same, session, small_tenant, snapshot
+from test_gpu_tokens import DT, dev, gen, on_gpu, ref_cache, sample, same, session, small_tenant, snapshot
 
 pytestmark = pytest.mark.gpu
 
@@ -67,6 +67,22 @@ def test_a_value_group_that_is_not_finite_stays_in_its_features(dtype, tokens, p
     err = (got - want).nan_to_num().abs()
     assert (err <= (relative * (weight + 6.5) + (2.0 ** -8 * want.abs() if dtype == "bf16" else 0.0)).nan_to_num()).all()
     s.close()
+
+
+# -- sampling ------------------------------------------------------------------------------------------------------------------------
+def test_sampling_of_more_rows_than_a_grid_holds():
+    """4194304 workgroups of 1024 threads are 2^32; the rows beyond are sampled too."""
+    n, v, g = 2 ** 22 + 5, 7, gen(17)
+    x, u = torch.randn(n, v, generator=g).bfloat16(), torch.rand(n, generator=g)
+    tokens, logp = sample("bf16", x, u)
+    w = torch.exp(x.double() - x.double().amax(-1, keepdim=True))
+    cum = w.cumsum(-1)
+    goal = u.double()[:, None] * cum[:, -1:]
+    far = (cum - goal).abs().amin(-1) > 1e-6 * cum[:, -1]
+    want = (cum <= goal).sum(-1)
+    assert far[-5:].any() and far.double().mean() > 0.99
+    assert torch.equal(tokens[far].long(), want[far])
+    assert (logp[far].double() - (w.gather(1, want[:, None])[:, 0] / cum[:, -1]).log()[far]).abs().max() < 1e-5
 
 
 # -- profiles ------------------------------------------------------------------------------------------------------------------------
