@@ -180,7 +180,9 @@ typedef struct {
  *   CACHE_ATTENTION: in0 = qkv (only its query heads are read), out = (n=batch, c=heads*head_dim, h=S, w=1): query t stands at
  * p = start[b]+t and sees the present keys j <= p, with window > 0 only those with j > p - window:
  * out = sum_j softmax_j(alpha * q.k_j) v_j.  Rows from count[b] on, and rows that see no key, are zeros.  CACHE_WRITE of the same tokens
- * comes first.  Scores, softmax and sums in fp32.
+ * comes first.  Scores, the softmax's maximum and sum, and all other sums are held in fp32.  A key's weight in the result: fp32 tenants, 24 bits; bf16
+ * tenants, with up to 32 rows (S * heads/kv_heads of the call) 15 bits or more, with more rows rounded to bf16 once, an error of at most 2^-8 of
+ * each weight, independent of one another, as the result's own rounding has.  A token's result may so differ in its last bits between calls of few and of many tokens.
  * head_dim: 64 or 128.  page_tokens: a power of two, 32..4096.  heads/kv_heads <= 64.
  */
 #define GACER_CACHE_GROUP 64

@@ -9,7 +9,7 @@
 // so neither keys nor values are ever rounded.  In bf16 tenants k = 16 + c, which is a shift and a mask per pair of codes; fp32 tenants pay more
 // instructions for k = c - 8, because sums of numbers that do not lie around zero lose what their differences need (attention over 1000 keys: relative
 // error 6.8e-6 with 16 + c).  Operands that are not whole numbers are split into bf16 parts: queries of fp32 tenants into
-// three, weights p_j s_jg into two (bf16 tenants: an error of 2^-16 against the result's own rounding of 2^-9; one part would add as much as
+// three, weights p_j s_jg into two (bf16 tenants: an error of at most 2^-15 against 2^-8 of the result's own rounding; one part would add as much as
 // that) or three.  Where rows leave room in the products' 32, the parts are rows of one product.  Weights pass through a patch of LDS, from
 // lane = key to the layout of an operand.
 //
@@ -403,8 +403,10 @@ template <typename T, int D, int GROUPS> __global__ __launch_bounds__(256) void 
     store_vec4((T *)a.y + ((int64_t)out + (int64_t)a.b_lo * a.S * a.heads) * D + lane * 4, v);
 }
 
-// Whether the splits of a row are joined by several groups of lanes in a workgroup of their own, or one after another.  Many splits of few rows:
-// 32768 keys for one token of 32 heads 18.5 us against 22.1; many rows: 4096 keys for 4 x 28 tokens of 32 heads (64 features) 25.1 us against 28.8 by groups.
+// Whether the splits of a row are joined by several groups of lanes in a workgroup of their own, or one after another; by groups against one after another, us of
+// the whole call (bf16, 128 features).  32 results after 131072 keys 41.3 against 43.9, 128 after 32768 25.2 against 28.6, 512 after 2 x 16384 32.7 against
+// 35.0, 896 after 16384 34.4 against 37.2; about where the line is 2048 after 8192 35.3 against 34.6; 3584 after 4 x 4096 34.2 against 32.6, 4096 after
+// 4096 36.6 against 35.0.  64 features: 1008 after 4 x 4096 18.5 against 19.2, 2160 of them 24.2 against 22.1.
 static bool join_by_groups(const AttendArgs &b, int outputs) { return b.splits > 8 && outputs <= 2048; }
 
 template <typename T, int D, int ROWS, int NW> static void attend(const AttendArgs &b, int grid, int outputs, hipStream_t s, int phase)

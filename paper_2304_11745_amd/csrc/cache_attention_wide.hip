@@ -16,8 +16,8 @@
 // would be 16 more matrix instructions per 64 keys and two more operations per weight.
 //
 // Bound by the two waves of a SIMD that 254 registers allow: each runs scores, exponentials and products one after another, and vector
-// instructions (52 % of the time), matrix instructions (32 %), LDS (35 %) and waits for LDS and barriers (39 %) fill each other's gaps only in part.  A
-// prompt of 4096 tokens, 32 heads of 128 features over 8 (bf16): 232 us = 590 TFLOP/s, where a large product reaches 1377.  256 rows a workgroup, which
+// instructions (52 % of the time), matrix instructions (32 %), LDS (35 %, 4 % more by conflicts of banks) and waits (35 % of the waves' time) fill each other's gaps only in part.  A
+// prompt of 4096 tokens, 32 heads of 128 features over 8 (bf16): 233 us = 590 TFLOP/s, where a large product reaches 1377.  256 rows a workgroup, which
 // halve the unpacking: 5 % faster there, but 98 us against 93 at 2048 tokens and 361 against 344 at 16 x 256 tokens after 4096 keys; two groups
 // of waves that take turns at the matrix cores, a barrier after each turn: 17 % slower.
 #include <hip/hip_runtime.h>

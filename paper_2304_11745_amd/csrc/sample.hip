@@ -15,8 +15,9 @@
 // scan, and few kept entries go into the list.  Otherwise only the last bin's entries need ranks, and the draw goes as for bf16.
 //   Where a list would not hold its entries or a counter its count (a flat row), the prefix's end is found digit by digit of the key instead.
 //
-// What bounds it, and what it takes.  256 rows of 131072 bf16 logits under top-p and min-p (67 MB, one row in each unit): 52 us, of which the first pass
-// takes 24 (20 without its counters; 67 MB at the rate of a large copy are 13), the scans of the counts 8, the draw 10.  One row of 32000 fp32
+// What bounds it, and what it takes.  256 rows of 131072 bf16 logits under top-p and min-p (67 MB, 13 us at the rate of a large copy; one row in each unit):
+// 51 us, which is the slowest row's time; an average row is done after 41.5: 7 until the counters are clear and the first loads there, 16 for the rest of the
+// first pass, 8 for the scans of the counts, 1 for the table, 9 for the draw, one after another.  One row of 32000 fp32
 // logits, top-k 50 and top-p: 11 us, a chain of two passes, some twenty barriers and instructions that a single workgroup runs through once; by bins
 // 15, through the codes of bf16 as a first digit 21.
 #include <hip/hip_runtime.h>
@@ -41,7 +42,8 @@ struct SampleArgs {
 static constexpr int MOST_ROWS = 1 << 21;               // of a launch: a grid holds fewer than 2^32 threads
 static constexpr int THREADS = 1024, WAVES = THREADS / 64, BINS = 2048, LIST = 2048, CODES = 32768, GROUPS = 512, PEAKS = 768;
 // Entries that a list may hold where the alternative is another pass over the row: ranks by counting take n steps of a thread and more, a pass over 131072
-// entries what 600 of them take.
+// entries what 600 of them take.  By a list against without, one row: 388 entries of 128256 49 us against 62, 136 of 32000 19 against 22, 523 of 32000 24 either
+// way (the line), 1243 of 32000 69 against 25; of a short row fewer would do, 397 of 8000 take 27 against 16.
 static constexpr int SHORT = 512;
 
 // numbers in an order of unsigned integers: -inf and NaN lowest, both zeros alike
@@ -698,8 +700,9 @@ template <typename T, bool PLAIN> __device__ __forceinline__ void sample_row(con
             draw_from_list(s, w, f, first, write);
         };
         if (sizeof(T) == 4 && f.top_k <= THREADS / 4) {
-            // the k largest entries are no smaller than the k largest of the threads' largest ones, and few others are: against the bins one row of 32000
-            // takes 10.9 us instead of 14.6 with k = 50, 19.3 instead of 22.6 with 256, but 34 instead of 32 with 500 and 119 instead of 65 with 900
+            // the k largest entries are no smaller than the k largest of the threads' largest ones, and few others are.  Against the bins, us: one row of 32000
+            // 11.0 and 14.7 with k = 50, 19.4 and 22.7 with 256, 26 and 28 with 384, but 34 and 32 with 500, 118 and 65 with 900; of 5000 9.0 and 9.9, 15.7 and 16.4,
+            // 20.6 and 20.8, 29 and 25, 150 and 54; of 128256 18 and 32, 27 and 41, 33 and 46, 44 and 51, 104 and 87; 64 rows of each alike
             clear();
             to_bin(mine);
             __syncthreads();

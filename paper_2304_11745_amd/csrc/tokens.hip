@@ -21,9 +21,11 @@ static LaunchInfo info(const char *name, int64_t workgroups, int lds)
 // A head is held by LPH lanes, eight features each: two runs of four, which are the two halves of the lane's pairs (i, i + R/2), so that
 // the rotation needs no other lane; beyond the rotated features, and for interleaved pairs, the two runs are neighbours.  Cosine and sine
 // depend on the token and the lane alone and are loaded once for all heads that a workgroup takes; the token's positions come through the scalar
-// cache.  Every element is read and written once: bound by the way to memory and back.  Three heads of a lane in flight: 3 x 4111
-// tokens of 28 + 4 + 4 heads of 128 features (bf16, 227 MB) 53 us = 4.3 TB/s; two 64, four 55 (few models' heads fill them), one 113 against 80 at
-// 16384 tokens of 32 + 8 + 8 heads, and no faster for a single token (5.8 us, a launch).
+// cache.  Every element is read and written once: bound by the way to memory and back (3 x 4111 tokens of 28 + 4 + 4 heads of 128 features, bf16, 227
+// MB: 52 us = 4.4 TB/s, vector instructions busy 73 % of it; fp32, 457 MB, 84 us = 5.5 TB/s).  A lane takes three heads; two take
+// 64 us, four 55 (few models' heads fill them), one 113 against 80 at 16384 tokens of 32 + 8 + 8 heads, and no faster for a single token (5 us, a launch).
+// In fp32 the loads of all three are in flight together; in bf16 they are converted where they are loaded, under the same condition, and each head's
+// loads are waited for before the next one's are issued.
 struct RopeArgs {
     const void *x;
     void *y;
@@ -170,8 +172,9 @@ LaunchInfo launch_qknorm_rope(const TokenArgs &a, hipStream_t s, bool dry)
 // keys, half values, eight features of a token per lane; a group's minimum and maximum go over the eight lanes that hold it.  Key codes
 // are one word per lane as they stand.  Of the values a wave takes eight tokens at a time, 64 features of each, and the eight lanes that
 // hold the same features transpose their 8 x 8 codes in three exchanges; where a word also has codes of tokens outside the call, those stay.
-// Nothing goes through LDS but the exchanges.  Bound by vector instructions, some 14 for an element, and the way from memory: 6 prompts of up to 5001
-// tokens, 8 kv heads of 128 features (bf16, 154 MB) 44 us = 3.5 TB/s; by divisions and with the transposition by LDS atomics 65.
+// Nothing goes through LDS but the exchanges.  6 prompts of up to 5001 tokens, 8 kv heads of 128 features (bf16, 154 MB) 44 us = 3.5 TB/s; by divisions and
+// with the transposition by LDS atomics 65.  Vector instructions, 18 for an element, are busy 70 % of that; the rest are waits: in bf16 a lane's loads, one for
+// each pass, are converted where they are loaded and so follow one another (in fp32 they are in flight together).
 // Reading is a copy that widens: value codes go through LDS to become rows of a token again.  The same prompts 25 us; 8 x 8192 tokens
 // (327 MB) 67 us = 4.9 TB/s, what a large copy reaches.
 struct CacheArgs {
