@@ -341,7 +341,8 @@ gacer_status gacer_run_static(gacer_ctx *ctx, int mode, int rounds);
  * One round of one tenant in the stream of the caller's own work: issues the tenant's operators, unsplit and fused as
  * gacer_set_fuse_affine says, on `stream` (a hipStream_t; NULL = null stream) and returns without waiting; ordinary stream order makes
  * the inputs' producers and the outputs' readers correct.  For decoding loops, where the host prepares the next step while this one
- * runs, and for callers that capture a step into a graph of their own (nothing is allocated, no event is recorded).  The tenant's
+ * runs, and for callers that capture a step into a graph of their own (nothing is allocated, no event is recorded).  The kernels run on the
+ * context's GPU, the one that was current in gacer_create, whichever is current now (a NULL stream is that GPU's).  The tenant's
  * split-K and attention workspaces belong to the context: two rounds of one tenant must not overlap, whichever calls issued them.  The
  * plan, the tenant's own stream and captured graphs play no part.  gacer_destroy and gacer_load_tenants do not wait for `stream`.
  */

@@ -1773,6 +1773,17 @@ gacer_status gacer_enqueue(gacer_ctx *c, int tenant, void *stream)
     if (tenant < 0 || tenant >= (int)c->tenants.size()) return fail(c, GACER_EINVAL, "gacer_enqueue: no tenant %d", tenant);
     if (!c->has_device) return fail(c, GACER_ESTATE, "the context was created without a GPU");
     if (c->ws_missing) return fail(c, GACER_EHIP, "split-K workspace could not be allocated when the tenants were loaded");
+    // launches go to the current GPU, and the null stream is each GPU's own: the context's becomes the current one while they are issued
+    struct Current {
+        int before = -1;
+        ~Current() { if (before >= 0) (void)hipSetDevice(before); }
+    } current;
+    int now = c->device;
+    HIPCHK(c, hipGetDevice(&now));
+    if (now != c->device) {
+        HIPCHK(c, hipSetDevice(c->device));
+        current.before = now;
+    }
     c->ws_run[tenant] = c->tenants[tenant].ws;
     const auto &ex = c->plain_exec[tenant];
     for (int i = 0; i < (int)ex.size(); ++i)

@@ -222,11 +222,7 @@ class TokenSession:
     def enqueue(self, tenant=0, stream=None):
         """One round of a tenant on ``stream`` (default: PyTorch's current one), without waiting (gacer_enqueue)."""
         s = torch.cuda.current_stream(self.device) if stream is None else stream
-        if torch.cuda.current_device() == self.device.index:
-            st = B.gacer_enqueue(self.ctx, tenant, s.cuda_stream)
-        else:                                        # kernels run on the current GPU; the null stream is each one's own
-            with torch.cuda.device(self.device):
-                st = B.gacer_enqueue(self.ctx, tenant, s.cuda_stream)
+        st = B.gacer_enqueue(self.ctx, tenant, s.cuda_stream)
         if st:
             B.check(self.ctx, st)
 

@@ -57,6 +57,7 @@ int main()
     std::mt19937 rng(5);
     for (int trial = 0; trial < 24; ++trial) {
         gacer_ctx *ctx = nullptr;
+        gacer::current_device = trial % 2;
         CHECK(gacer_create(&ctx) == GACER_OK);
         const bool in_place = trial % 2, two = trial % 3 == 0;
         const int batch = 1 + (int)(rng() % 9);
@@ -109,6 +110,10 @@ int main()
         for (int t = 0; t < NT; ++t) {
             const long before = gacer::token_launches.all;
             CHECK(gacer_enqueue(ctx, t, nullptr) == GACER_OK && gacer::token_launches.all == before + 5);
+            const int own = gacer::current_device, other = 1 - own;          // on the context's GPU while another one is current
+            gacer::current_device = other;
+            CHECK(gacer_enqueue(ctx, t, nullptr) == GACER_OK && gacer::token_launches.device == own && gacer::current_device == other);
+            gacer::current_device = own;
         }
         // the profile's own table, then random ones, with rows for axes that these operators do not have
         size_t n = 0;

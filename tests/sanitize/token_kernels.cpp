@@ -5,6 +5,7 @@
 
 namespace gacer {
 TokenLaunches token_launches;
+int current_device = 0;
 LaunchInfo launch_tokens(const TokenArgs &a, hipStream_t, bool dry, int phase)
 {
     LaunchInfo li;
@@ -14,9 +15,14 @@ LaunchInfo launch_tokens(const TokenArgs &a, hipStream_t, bool dry, int phase)
     if (a.op == TK_QKNORM_ROPE && a.R == 0 && (a.positions || a.axes || a.table)) ++token_launches.stray_positions;
     if (!dry) {
         ++token_launches.all;
+        token_launches.device = current_device;
         if (a.op == TK_QKNORM_ROPE && a.x == a.y) ++token_launches.in_place_at[a.x];
         if (token_ws_floats(a)) a.ws[token_ws_floats(a) - 1] = 1.f;      // the last float of the workspace is there
     }
     return li;
 }
 }  // namespace gacer
+
+// two devices (linked with --wrap)
+extern "C" hipError_t __wrap_hipGetDevice(int *d) { *d = gacer::current_device; return hipSuccess; }
+extern "C" hipError_t __wrap_hipSetDevice(int d) { gacer::current_device = d; return d < 2 ? hipSuccess : hipErrorInvalidDevice; }

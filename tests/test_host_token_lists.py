@@ -79,7 +79,7 @@ def test_lists_beside_other_tenants_are_on_the_sessions_gpu(monkeypatch):
 
 
 def test_a_session_runs_on_its_own_gpu_whichever_is_current(monkeypatch):
-    """The null stream of the library is that of the current GPU."""
+    """Rounds and the release of a session; gacer_enqueue sees to it itself."""
     now, seen = [0], []
 
     class device:
@@ -92,19 +92,14 @@ def test_a_session_runs_on_its_own_gpu_whichever_is_current(monkeypatch):
         def __exit__(self, *_):
             now[0] = self.before
 
-    class stream:
-        cuda_stream = 0
     monkeypatch.setattr(torch.cuda, "device", device)
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: now[0])
-    monkeypatch.setattr(torch.cuda, "current_stream", lambda d=None: stream)
     monkeypatch.setattr(torch.cuda, "synchronize", lambda d=None: None)
-    for call in ("gacer_enqueue", "gacer_run", "gacer_destroy"):
+    for call in ("gacer_run", "gacer_destroy"):
         monkeypatch.setattr(T.B, call, lambda *a, call=call: seen.append((call, now[0])) or 0)
     for gpu in (0, 1):
         for current in (0, 1):
             s, now[0], seen[:] = object.__new__(T.TokenSession), current, []
             s.device, s.ctx = torch.device("cuda", gpu), 1
-            s.enqueue()
             s.run()
             s.close()
-            assert seen == [("gacer_enqueue", gpu), ("gacer_run", gpu), ("gacer_destroy", gpu)] and now[0] == current
+            assert seen == [("gacer_run", gpu), ("gacer_destroy", gpu)] and now[0] == current

@@ -18,7 +18,7 @@ def test_a_decoding_tenant_is_walked_clean_under_asan_and_ubsan(tmp_path):
            "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
            "-Xarch_host", "-fsanitize=address,undefined", "-Xarch_host", "-fno-sanitize-recover=undefined",
            "-x", "hip", os.path.join(CSRC, "executor.cpp"), os.path.join(CSRC, "search.cpp")]
-    cmd += [os.path.join(HERE, "sanitize", f) for f in ("stub_kernels.cpp", "stub_hip.cpp", "token_kernels.cpp", "token_driver.cpp")] + ["-o", exe]
+    cmd += [os.path.join(HERE, "sanitize", f) for f in ("stub_kernels.cpp", "stub_hip.cpp", "token_kernels.cpp", "token_driver.cpp")] + ["-Wl,--wrap=hipGetDevice,--wrap=hipSetDevice", "-o", exe]
     built = subprocess.run(cmd, capture_output=True, text=True, timeout=600)
     assert built.returncode == 0, built.stderr[-4000:]
     env = dict(os.environ, ASAN_OPTIONS="detect_leaks=0:abort_on_error=0", UBSAN_OPTIONS="print_stacktrace=1")
