@@ -88,6 +88,19 @@ int main()
             (void)gacer_load_tenants(other, &bad.desc, 1);
             gacer_destroy(other);
         }
+        {   // a descriptor may stand at any address
+            Step odd = steps[0];
+            odd.desc.ops = odd.ops.data(); odd.desc.tensors = odd.tensors.data();
+            std::vector<char> bytes[3] = {std::vector<char>(sizeof odd.rope + 1), std::vector<char>(sizeof odd.cache + 1), std::vector<char>(sizeof odd.sampling + 1)};
+            std::memcpy(bytes[0].data() + 1, &odd.rope, sizeof odd.rope);
+            std::memcpy(bytes[1].data() + 1, &odd.cache, sizeof odd.cache);
+            std::memcpy(bytes[2].data() + 1, &odd.sampling, sizeof odd.sampling);
+            odd.ops[0].w = bytes[0].data() + 1; odd.ops[1].w = odd.ops[2].w = odd.ops[3].w = bytes[1].data() + 1; odd.ops[5].w = bytes[2].data() + 1;
+            gacer_ctx *other = nullptr;
+            CHECK(gacer_create(&other) == GACER_OK);
+            CHECK(gacer_load_tenants(other, &odd.desc, 1) == GACER_OK);
+            gacer_destroy(other);
+        }
         // every operator in two along the batch; none of them along its channels
         std::vector<gacer_split> sp;
         for (int i = 0; i < n_ops && batch >= 2; ++i) sp.push_back({0, i, GACER_AXIS_BATCH, 2, nullptr, 0});
