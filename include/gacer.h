@@ -66,17 +66,22 @@ typedef enum {
     GACER_SCALE = 12,     /* y[n,c,h,w] = act(in0[n,c,h,w] * in1[n,c]): squeeze-and-excitation gate */
     GACER_CONCAT = 13,    /* y[:, :cin] = in0, y[:, cin:] = in1 (channel concatenation)      */
     GACER_AVGPOOL = 14,   /* unpadded window mean (kh = kw, stride)                          */
-    /* operators of a decoding tenant; `w` is a HOST pointer to their descriptor, see gacer_rope / gacer_cache / gacer_sampling */
+    /* operators of a decoding tenant; `w` is a HOST pointer to their descriptor, see gacer_rope and what follows it */
     GACER_QKNORM_ROPE = 15,     /* RMS norm of every query and key head, then rotation by position */
     GACER_CACHE_WRITE = 16,     /* keys and values of new tokens into a paged 4-bit cache          */
     GACER_CACHE_READ = 17,      /* keys and values of cached tokens back in the tenant's type      */
     GACER_CACHE_ATTENTION = 18, /* causal attention of new tokens over that cache                  */
-    GACER_SAMPLE = 19           /* next token of every row of logits                               */
+    GACER_SAMPLE = 19,          /* next token of every row of logits                               */
+    GACER_RMSNORM_FP8 = 20,     /* residual, RMS norm and 8-bit rows, see gacer_fp8_norm           */
+    GACER_GEMM_FP8 = 21,        /* 8-bit rows times 8-bit weights, see gacer_fp8_gemm              */
+    GACER_GATED_FP8 = 22        /* gated feed-forward block of 8-bit rows, see gacer_fp8_gated     */
 } gacer_opkind;
 
-/* HSWISH(v) = v * HSIGMOID(v), HSIGMOID(v) = min(max(v + 3, 0), 6) / 6 */
+/* HSWISH(v) = v * HSIGMOID(v), HSIGMOID(v) = min(max(v + 3, 0), 6) / 6, SILU(v) = v / (1 + exp(-v)),
+ * GELU_TANH(v) = v / (1 + exp(-2 sqrt(2/pi) (v + 0.044715 v^3))); the last two are for GEMM_FP8 and GATED_FP8 only */
 typedef enum {
-    GACER_ACT_NONE = 0, GACER_ACT_RELU = 1, GACER_ACT_RELU6 = 2, GACER_ACT_GELU = 3, GACER_ACT_HSWISH = 4, GACER_ACT_HSIGMOID = 5
+    GACER_ACT_NONE = 0, GACER_ACT_RELU = 1, GACER_ACT_RELU6 = 2, GACER_ACT_GELU = 3, GACER_ACT_HSWISH = 4, GACER_ACT_HSIGMOID = 5,
+    GACER_ACT_SILU = 6, GACER_ACT_GELU_TANH = 7
 } gacer_act;
 
 /* Decomposition axis of an operator (Eq. 5 decomposes along batch; the output-channel
@@ -216,6 +221,60 @@ typedef struct {
     int *tokens;              /* device [rows]: the result */
     float *logp;              /* device [rows] or NULL */
 } gacer_sampling;
+
+/*
+ * Rows and weights in 8 bits, shared by RMSNORM_FP8, GEMM_FP8 and GATED_FP8.  A code is an e4m3 number (one sign, four exponent and three
+ * mantissa bits, largest 448, no infinities); it stands for itself times its scale.
+ *   Rows: `rows` = the tenant's batch times tokens per sequence, in that order; codes [rows][features], scales [ceil(features/128)][rows]: one
+ * for every row and block of 128 features (the last block may be shorter).  Rows are made by RMSNORM_FP8 and GATED_FP8 or by the caller; the
+ * library does not follow who writes them, the order of the list does.
+ *   Making a block of y (fp32): m = max(max |y|, 2^-60), scale = m / 448, code = e4m3(y * (448 / m)), the quotients and the code rounded to nearest even.
+ * A block that holds an infinity or a NaN gets a NaN scale and codes of 0: it stands for NaNs.
+ *   Weights: codes [out features][in features], scales [ceil(out/128)][ceil(in/128)]: one for every block of 128 by 128.
+ * features: a multiple of 16 for rows (and so for the inner extent of a product), 16..65536.  Codes 16-byte aligned, scales as float.
+ * codes < 2 GiB each.  What an operator writes must not share memory with what it reads.  These operators split along the batch.
+ */
+#define GACER_FP8_BLOCK 128
+typedef struct {
+    void *codes;   /* device [rows][features], e4m3 */
+    float *scales; /* device [ceil(features/128)][rows] */
+    int rows, features;
+} gacer_fp8_rows;
+typedef struct {
+    const void *codes;   /* device [out][in], e4m3 */
+    const float *scales; /* device [ceil(out/128)][ceil(in/128)] */
+} gacer_fp8_weight;
+
+/*
+ * RMSNORM_FP8: in0 = x (n a multiple of the batch, c = features; every position is a row), res = a tensor of the same shape or -1: written by an earlier
+ * operator, or by none of the list, then it is the caller's as the tenant's input is (so a list can begin behind a caller's own step).  In fp32, h = x + res;
+ * with norm != 0 y = h * rsqrt(mean(h^2) + alpha) * scale (scale = device [c] or NULL: ones), else y = h.
+ *   y.codes != NULL: y leaves as 8-bit rows, and out = h in the tenant's type, the residual stream behind the addition (-1: not kept).
+ *   y.codes == NULL: out = y in the tenant's type.
+ */
+typedef struct {
+    int norm;
+    gacer_fp8_rows y;
+} gacer_fp8_norm;
+
+/*
+ * GEMM_FP8: in0 = -1; out = (n a multiple of the batch, c = out features, h, w) with n*h*w = x.rows:
+ *   out[r][o] = act(sum_k x[r][k] w[o][k] + bias[o] + res[r][o]),  bias = device [c] or NULL, res = a tensor of out's shape or -1, as for RMSNORM_FP8.
+ * GATED_FP8: in0 = res = -1; with g = gate and u = up products of the same rows,
+ *   h[r][f] = act(sum_k x[r][k] g[f][k]) * (sum_k x[r][k] u[f][k]),
+ * as 8-bit rows (y.codes != NULL, out = -1, y.rows = x.rows) or as out in the tenant's type (y.codes == NULL; out as above, c = f).
+ * Products of codes are exact; blocks of 128 inner features are summed in fp32, scaled, and added in fp32, in an order that the number of rows of the
+ * whole operator fixes: a row's result may differ in its last bits between calls of few and of many rows, not between plans.
+ */
+typedef struct {
+    gacer_fp8_rows x;
+    gacer_fp8_weight w;
+} gacer_fp8_gemm;
+typedef struct {
+    gacer_fp8_rows x;
+    gacer_fp8_weight gate, up;
+    gacer_fp8_rows y;
+} gacer_fp8_gated;
 
 /* One tenant: its operator list in execution order, its tensors, and the stream it runs on. */
 typedef struct {

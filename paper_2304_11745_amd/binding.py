@@ -17,9 +17,11 @@ GACER_OK, GACER_EINVAL, GACER_ESHAPE, GACER_EPLAN, GACER_ESTATE, GACER_ENOMEM, G
 GACER_F32, GACER_BF16 = 0, 1
 (GACER_CONV2D, GACER_DWCONV2D, GACER_GEMM, GACER_BGEMM_QK, GACER_BGEMM_PV, GACER_MAXPOOL, GACER_GAVGPOOL,
  GACER_AFFINE_ACT, GACER_ADD, GACER_LAYERNORM, GACER_SOFTMAX, GACER_ACT, GACER_SCALE, GACER_CONCAT, GACER_AVGPOOL,
- GACER_QKNORM_ROPE, GACER_CACHE_WRITE, GACER_CACHE_READ, GACER_CACHE_ATTENTION, GACER_SAMPLE) = range(20)
+ GACER_QKNORM_ROPE, GACER_CACHE_WRITE, GACER_CACHE_READ, GACER_CACHE_ATTENTION, GACER_SAMPLE,
+ GACER_RMSNORM_FP8, GACER_GEMM_FP8, GACER_GATED_FP8) = range(23)
 GACER_CACHE_GROUP = 64
-GACER_ACT_NONE, GACER_ACT_RELU, GACER_ACT_RELU6, GACER_ACT_GELU, GACER_ACT_HSWISH, GACER_ACT_HSIGMOID = range(6)
+GACER_FP8_BLOCK = 128
+GACER_ACT_NONE, GACER_ACT_RELU, GACER_ACT_RELU6, GACER_ACT_GELU, GACER_ACT_HSWISH, GACER_ACT_HSIGMOID, GACER_ACT_SILU, GACER_ACT_GELU_TANH = range(8)
 GACER_AXIS_NONE, GACER_AXIS_BATCH, GACER_AXIS_COUT = range(3)
 GACER_MODE_PLAN, GACER_MODE_SEQUENTIAL, GACER_MODE_STREAM_PARALLEL = range(3)
 
@@ -57,6 +59,26 @@ class gacer_cache(C.Structure):
 class gacer_sampling(C.Structure):
     _fields_ = [("u", C.c_void_p), ("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p),
                 ("tokens", C.c_void_p), ("logp", C.c_void_p)]
+
+
+class gacer_fp8_rows(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("rows", C.c_int), ("features", C.c_int)]
+
+
+class gacer_fp8_weight(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p)]
+
+
+class gacer_fp8_norm(C.Structure):
+    _fields_ = [("norm", C.c_int), ("y", gacer_fp8_rows)]
+
+
+class gacer_fp8_gemm(C.Structure):
+    _fields_ = [("x", gacer_fp8_rows), ("w", gacer_fp8_weight)]
+
+
+class gacer_fp8_gated(C.Structure):
+    _fields_ = [("x", gacer_fp8_rows), ("gate", gacer_fp8_weight), ("up", gacer_fp8_weight), ("y", gacer_fp8_rows)]
 
 
 class gacer_tenant(C.Structure):

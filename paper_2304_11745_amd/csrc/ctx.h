@@ -24,8 +24,8 @@ struct Launch {
 // the cut of one operator's K range (see GemmArgs)
 struct KSplit { int ksplit = 1, kb_per_slice = 1 << 28, kwaves = 0, kb_per_wave = 0; bool stem = false, halo = false; };
 
-// descriptor of an operator of a decoding tenant (gacer_op.w), copied when the tenants are loaded; one of the three by the operator's kind
-struct TokenDesc { gacer_rope rope; gacer_cache cache; gacer_sampling sampling; };
+// descriptor of an operator of a decoding tenant (gacer_op.w), copied when the tenants are loaded; one of them by the operator's kind
+struct TokenDesc { gacer_rope rope; gacer_cache cache; gacer_sampling sampling; gacer_fp8_norm norm8; gacer_fp8_gemm gemm8; gacer_fp8_gated gated8; };
 
 struct Tenant {
     std::vector<gacer_op> ops;
@@ -96,6 +96,7 @@ struct Ctx {
 // axis extent and legality of a decomposition
 int axis_extent(const Tenant &t, int op, gacer_axis axis);
 inline bool is_token_op(gacer_opkind kind) { return kind >= GACER_QKNORM_ROPE; }
+inline bool is_fp8_op(gacer_opkind kind) { return kind >= GACER_RMSNORM_FP8; }
 bool axis_legal(gacer_opkind kind, gacer_axis axis);
 void chunk_range(int extent, int factor, int j, int *lo, int *hi);
 // builds the launch of operator `op` restricted to batch items [b_lo,b_hi) and channels [c_lo,c_hi)

@@ -128,8 +128,33 @@ static Launch make_token_launch(const Tenant &t, int oi, int b_lo, int b_hi)
     k.b_lo = b_lo; k.b_hi = b_hi; k.batch = t.batch;
     k.x = in ? in->dptr : nullptr;
     k.y = out ? out->dptr : nullptr;
-    k.S = (int)(in ? in->h : out->h);
     k.alpha = op.alpha;
+    if (is_fp8_op(op.kind)) {
+        auto rows = [](const gacer_fp8_rows &r) { return Fp8Rows{(unsigned char *)r.codes, r.scales, r.rows, r.features}; };
+        auto weight = [](const gacer_fp8_weight &w) { return Fp8Weight{(const unsigned char *)w.codes, w.scales}; };
+        k.res = op.res >= 0 ? t.tensors[op.res].dptr : nullptr;
+        k.act = (int)op.act;
+        if (op.kind == GACER_RMSNORM_FP8) {
+            k.op = TK_RMSNORM_FP8;
+            k.S = (int)((in->n / t.batch) * in->h * in->w);
+            k.features = (int)in->c;
+            k.norm = d.norm8.norm; k.gamma = op.scale; k.eps = op.alpha;
+            k.yq = rows(d.norm8.y);
+            return l;
+        }
+        if (op.kind == GACER_GEMM_FP8) {
+            k.op = TK_GEMM_FP8;
+            k.xq = rows(d.gemm8.x); k.w = weight(d.gemm8.w);
+            k.bias = op.bias;
+        } else {
+            k.op = TK_GATED_FP8;
+            k.xq = rows(d.gated8.x); k.w = weight(d.gated8.gate); k.w2 = weight(d.gated8.up); k.yq = rows(d.gated8.y);
+        }
+        k.S = k.xq.rows / t.batch;
+        k.features = out ? (int)out->c : k.yq.features;
+        return l;
+    }
+    k.S = (int)(in ? in->h : out->h);
     if (op.kind == GACER_QKNORM_ROPE) {
         k.op = TK_QKNORM_ROPE;
         k.heads = d.rope.heads; k.kv_heads = d.rope.kv_heads; k.D = d.rope.head_dim;
@@ -367,6 +392,94 @@ struct Written {
     }
 };
 
+// An operator on 8-bit rows: its descriptor against its tensors; copies the descriptor to *desc.
+static gacer_status check_fp8_op(Ctx *c, int ti, const gacer_tenant &t, int oi, const Written &written, TokenDesc *desc)
+{
+    const gacer_op &op = t.ops[oi];
+    auto bad = [&](const char *why) { return fail(c, GACER_ESHAPE, "tenant %d op %d: %s", ti, oi, why); };
+    auto inval = [&](const char *why) { return fail(c, GACER_EINVAL, "tenant %d op %d: %s", ti, oi, why); };
+    auto misaligned = [](const void *p, uintptr_t to) { return ((uintptr_t)p) % to != 0; };
+    const bool norm = op.kind == GACER_RMSNORM_FP8, gated = op.kind == GACER_GATED_FP8;
+    if (op.in1 >= 0) return bad("operators on 8-bit rows take no in1");
+    if (norm ? op.in0 < 0 || op.in0 >= t.n_tensors || !written.all(op.in0) : op.in0 >= 0) return bad(norm ? "in0 missing or not written by an earlier operator" : "products of 8-bit rows take no in0");
+    if (op.res >= 0) {                                       // the residual stream may come from outside: a tensor that no operator of the list writes
+        if (gated || op.res >= t.n_tensors) return bad("res index out of range, or of a gated block, which takes none");
+        bool outside = !t.tensors[op.res].pitch;
+        for (int i = 0; i < t.n_ops && outside; ++i) {
+            const int w = t.ops[i].out;
+            if (w >= 0 && w < t.n_tensors) outside = w != op.res && !(t.tensors[w].pitch && t.tensors[w].base == op.res);
+        }
+        if (!outside && !written.all(op.res)) return bad("res is written by a later operator of the list, or not whole");
+    }
+    if (norm && op.act != GACER_ACT_NONE) return bad("a norm takes no activation");
+    gacer_fp8_norm dn{};
+    gacer_fp8_gated dg{};
+    gacer_fp8_gemm dm{};
+    if (norm) std::memcpy(&dn, op.w, sizeof dn);             // host memory of any alignment
+    else if (gated) std::memcpy(&dg, op.w, sizeof dg);
+    else std::memcpy(&dm, op.w, sizeof dm);
+    const gacer_fp8_rows none{}, &x = norm ? none : gated ? dg.x : dm.x, &y = norm ? dn.y : dg.y;
+    const bool codes = y.codes != nullptr;
+    // out: always of a GEMM and where no rows are written; beside a norm's rows it is optional
+    if (op.out >= t.n_tensors || (op.out < 0 && !codes)) return bad("out index out of range");
+    if (op.out >= 0 && gated && codes) return bad("a gated block writes 8-bit rows or out, not both");
+    if (op.out >= 0 && !written.none(op.out)) return bad("out tensor is written twice");
+    const gacer_tensor *in = norm ? &t.tensors[op.in0] : nullptr, *out = op.out >= 0 ? &t.tensors[op.out] : nullptr, *res = op.res >= 0 ? &t.tensors[op.res] : nullptr;
+    for (const gacer_tensor *p : {in, out, res}) {
+        if (p && p->pitch) return bad("operators on 8-bit rows do not take channel windows");
+        if (p && p->n % t.batch) return bad("tensor n is not a multiple of the tenant batch");
+    }
+    auto positions = [](const gacer_tensor &p) { return p.n * p.h * p.w; };
+    if (norm && out && !same_shape(*in, *out)) return bad("out must have the shape of in0");
+    if (res && !same_shape(*res, norm ? *in : *out)) return bad("res shape differs");
+    if (norm && (!(op.alpha >= 0.f) || op.alpha > 1e30f)) return bad("alpha (the norm's epsilon) must be a finite number, not negative");
+    // 8-bit rows
+    auto bytes = [](const gacer_fp8_rows &r) { return (int64_t)r.rows * r.features; };
+    for (const gacer_fp8_rows *r : {norm ? nullptr : &x, codes ? &y : nullptr}) {
+        if (!r) continue;
+        if (!r->codes || !r->scales) return inval("null codes or scales");
+        if (misaligned(r->codes, 16) || misaligned(r->scales, 4)) return inval("codes must be 16-byte aligned, scales as float");
+        if (r->features < 16 || r->features > 65536 || r->features % 16) return bad("features of 8-bit rows must be a multiple of 16, 16..65536");
+        if (r->rows < 1 || r->rows % t.batch) return bad("rows must be a multiple of the tenant batch");
+        if (bytes(*r) >= (1ll << 31)) return bad("8-bit rows of 2 GiB or more");
+    }
+    if (norm && (in->c > 65536 || positions(*in) >= (1ll << 31))) return bad("more than 65536 features or 2^31 rows");
+    if (norm && codes && (y.features != in->c || y.rows != positions(*in))) return bad("8-bit rows do not match in0");
+    if (gated && codes && y.rows != x.rows) return bad("x and y must have the same number of rows");
+    if (!norm && out && positions(*out) != x.rows) return bad("out must have a position for every row");
+    const int64_t cout = norm ? 0 : out ? out->c : y.features;
+    if (cout > (1 << 24)) return bad("more than 2^24 output features");
+    const gacer_fp8_weight weights[2] = {gated ? dg.gate : dm.w, dg.up};
+    for (int i = 0; i < (norm ? 0 : gated ? 2 : 1); ++i) {
+        if (!weights[i].codes || !weights[i].scales) return inval("null weights");
+        if (misaligned(weights[i].codes, 16) || misaligned(weights[i].scales, 4)) return inval("codes must be 16-byte aligned, scales as float");
+        if (cout * x.features >= (1ll << 31)) return bad("weights of 2 GiB or more");
+    }
+    if (misaligned(op.scale, 4) || misaligned(op.bias, 4)) return inval("misaligned parameter");
+    // what is written against what is read, and against each other
+    struct Span { const void *p; int64_t n; };
+    const int64_t esz = t.dtype == GACER_BF16 ? 2 : 4;
+    auto blocks = [](int64_t f) { return (f + GACER_FP8_BLOCK - 1) / GACER_FP8_BLOCK; };
+    auto tensor = [&](const gacer_tensor *p) { return Span{p ? p->dptr : nullptr, p ? positions(*p) * p->c * esz : 0}; };
+    auto codes_of = [&](const gacer_fp8_rows &r) { return Span{r.codes, bytes(r)}; };
+    auto scales_of = [&](const gacer_fp8_rows &r) { return Span{r.scales, blocks(r.features) * r.rows * 4}; };
+    const Span writes[3] = {tensor(out), codes ? codes_of(y) : Span{}, codes ? scales_of(y) : Span{}};
+    Span reads[10] = {tensor(in), tensor(res), {op.scale, norm && op.scale ? in->c * 4 : 0}, {op.bias, !norm && !gated && op.bias ? cout * 4 : 0}, norm ? Span{} : codes_of(x), norm ? Span{} : scales_of(x)};
+    for (int i = 0; i < 2; ++i)
+        if (!norm && (i == 0 || gated)) { reads[6 + 2 * i] = {weights[i].codes, cout * x.features}; reads[7 + 2 * i] = {weights[i].scales, blocks(cout) * blocks(x.features) * 4}; }
+    auto meet = [](const Span &a, const Span &b) { return a.n && b.n && (uintptr_t)a.p < (uintptr_t)b.p + (uintptr_t)b.n && (uintptr_t)b.p < (uintptr_t)a.p + (uintptr_t)a.n; };
+    for (int i = 0; i < 3; ++i) {
+        for (const Span &r : reads)
+            if (meet(writes[i], r)) return bad("what the operator writes shares memory with what it reads");
+        for (int j = 0; j < i; ++j)
+            if (meet(writes[i], writes[j])) return bad("what the operator writes shares memory with itself");
+    }
+    if (norm) desc->norm8 = dn;
+    else if (gated) desc->gated8 = dg;
+    else desc->gemm8 = dm;
+    return GACER_OK;
+}
+
 // An operator of a decoding tenant: its descriptor against its tensors; copies the descriptor to *desc.
 static gacer_status check_token_op(Ctx *c, int ti, const gacer_tenant &t, int oi, const Written &written, TokenDesc *desc)
 {
@@ -376,6 +489,7 @@ static gacer_status check_token_op(Ctx *c, int ti, const gacer_tenant &t, int oi
     auto misaligned = [](const void *p, uintptr_t to) { return ((uintptr_t)p) % to != 0; };
     if (!launch_tokens) return inval("this build holds no kernels for operators of a decoding tenant");
     if (!op.w) return inval("null descriptor (w)");
+    if (is_fp8_op(op.kind)) return check_fp8_op(c, ti, t, oi, written, desc);
     if (op.act != GACER_ACT_NONE || op.in1 >= 0 || op.res >= 0) return bad("operators of a decoding tenant take no activation, in1 or res");
     if (op.kind == GACER_CACHE_READ) {
         if (op.in0 >= 0) return bad("cache read takes no in0");
@@ -458,8 +572,8 @@ static gacer_status check_op(Ctx *c, int ti, const gacer_tenant &t, int oi, cons
         if (i < 0) return !required;
         return i < t.n_tensors && written.all(i);
     };
-    if ((int)op.kind < 0 || (int)op.kind > (int)GACER_SAMPLE) return fail(c, GACER_EINVAL, "tenant %d op %d: unknown kind", ti, oi);
-    if ((int)op.act < 0 || (int)op.act > (int)GACER_ACT_HSIGMOID) return fail(c, GACER_EINVAL, "tenant %d op %d: unknown activation", ti, oi);
+    if ((int)op.kind < 0 || (int)op.kind > (int)GACER_GATED_FP8) return fail(c, GACER_EINVAL, "tenant %d op %d: unknown kind", ti, oi);
+    if ((int)op.act < 0 || (int)op.act > (int)(is_fp8_op(op.kind) ? GACER_ACT_GELU_TANH : GACER_ACT_HSIGMOID)) return fail(c, GACER_EINVAL, "tenant %d op %d: unknown activation", ti, oi);
     if (is_token_op(op.kind)) return check_token_op(c, ti, t, oi, written, desc);
     if (!idx_ok(op.in0, true)) return bad("in0 missing or not written by an earlier operator");
     if (!idx_ok(op.in1, false) || !idx_ok(op.res, false)) return bad("in1/res not written by an earlier operator");
@@ -1808,6 +1922,16 @@ static void launch_work(const Launch &l, double *flops, double *bytes)
             const double keys = k.window > 0 ? std::min(most, (double)k.window) : most;
             *flops = 4.0 * rows * q * keys;
             *bytes = rows * 2.0 * q * esz + (double)(k.b_hi - k.b_lo) * std::min(most, keys + k.S) * cached;
+            break;
+        }
+        case TK_RMSNORM_FP8: case TK_GEMM_FP8: case TK_GATED_FP8: {
+            const double f = k.features, K = k.xq.features, n = k.op == TK_GATED_FP8 ? 2.0 : 1.0, scale = 4.0 / FP8_BLOCK;
+            *bytes = rows * f * ((k.y ? esz : 0.0) + (k.yq.codes ? 1.0 + scale : 0.0) + (k.res ? esz : 0.0));
+            if (k.op == TK_RMSNORM_FP8) *bytes += rows * f * esz;
+            else {
+                *flops = 2.0 * n * rows * f * K;
+                *bytes += rows * K * (1.0 + scale) + n * f * K;
+            }
             break;
         }
         default: *bytes = rows * (k.vocab * esz + 8.0); break;

@@ -1,0 +1,59 @@
+// What the operators on 8-bit rows share: codes to operands and back, activations, the end of a product.
+#pragma once
+#include "device_util.h"
+
+namespace gacer {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+static constexpr float FP8_LEAST = 0x1p-60f, FP8_LARGEST = 448.f;
+
+// Eight e4m3 codes as bf16, which holds each of them exactly.
+__device__ __forceinline__ bf16x8 widen(unsigned lo, unsigned hi)
+{
+    uint4 v;
+    v.x = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false));
+    v.y = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true));
+    v.z = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false));
+    v.w = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true));
+    return __builtin_bit_cast(bf16x8, v);
+}
+
+// Four values times `inv` as e4m3 codes, rounded to nearest even.
+__device__ __forceinline__ unsigned to_codes(float a, float b, float c, float d, float inv)
+{
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
+    return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, w, true);
+}
+
+// A block's scale and the factor of its values, from the largest magnitude as bits (whole numbers keep a NaN the largest): (NaN, 0) where that is no number.
+__device__ __forceinline__ float2 scale_of_block(unsigned most)
+{
+    const float m = __builtin_fmaxf(__uint_as_float(most), FP8_LEAST);
+    return most >= 0x7F800000u ? make_float2(__uint_as_float(0x7FC00000u), 0.f) : make_float2(m / FP8_LARGEST, FP8_LARGEST / m);
+}
+__device__ __forceinline__ unsigned magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+// The activations of products, `act` uniform.
+__device__ __forceinline__ float activate8(float v, int act)
+{
+    if (act == ACT_SILU) return v / (1.f + __expf(-v));
+    if (act == ACT_GELU_TANH) return v / (1.f + __expf(-1.5957691216057308f * (v + 0.044715f * v * v * v)));
+    return activate(v, act);
+}
+
+// Arguments of the products (see gacer_fp8_gemm, gacer_fp8_gated)
+struct Fp8Args {
+    const unsigned char *x, *w, *w2;
+    const float *xs, *ws, *ws2;
+    const float *bias;
+    const void *res;
+    void *y;
+    unsigned char *yq;
+    float *ys, *part;
+    int K, KB, N, rows, r_lo, r_hi, act;     // KB: blocks of K; rows: of the whole operator; r_lo..r_hi: of this launch
+    int f_tiles, r_tiles, slices, per_slice; // tiles of this launch; slices of K of per_slice blocks
+};
+
+}  // namespace gacer

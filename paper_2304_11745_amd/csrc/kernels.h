@@ -13,7 +13,7 @@ enum { SLICES_PRE_MAX = 4096 };
 // most keys of an attention that runs as one launch
 enum { ATTENTION_KEYS_MAX = 128 };
 enum { DT_F32 = 0, DT_BF16 = 1 };
-enum { ACT_NONE = 0, ACT_RELU = 1, ACT_RELU6 = 2, ACT_GELU = 3, ACT_HSWISH = 4, ACT_HSIGMOID = 5 };
+enum { ACT_NONE = 0, ACT_RELU = 1, ACT_RELU6 = 2, ACT_GELU = 3, ACT_HSWISH = 4, ACT_HSIGMOID = 5, ACT_SILU = 6, ACT_GELU_TANH = 7 };
 
 struct StreamArgs;
 
@@ -101,7 +101,7 @@ struct StreamArgs {
 };
 
 // Operators of a decoding tenant.  Sub-range: sequences (SAMPLE: items) [b_lo, b_hi).
-enum TokenOp { TK_QKNORM_ROPE, TK_CACHE_WRITE, TK_CACHE_READ, TK_CACHE_ATTENTION, TK_SAMPLE };
+enum TokenOp { TK_QKNORM_ROPE, TK_CACHE_WRITE, TK_CACHE_READ, TK_CACHE_ATTENTION, TK_SAMPLE, TK_RMSNORM_FP8, TK_GEMM_FP8, TK_GATED_FP8 };
 // most query heads per key/value head
 enum { CACHE_GROUP = 64, CACHE_HEADS_PER_KV_MAX = 64 };
 
@@ -112,6 +112,11 @@ struct CacheView {
     const int *page_table, *start, *count;
     int kv_heads, D, page_shift, n_pages, max_pages;
 };
+
+// 8-bit rows: e4m3 codes [rows][features], a scale for each block of 128 features [block][rows]
+enum { FP8_BLOCK = 128 };
+struct Fp8Rows { unsigned char *codes; float *scales; int rows, features; };
+struct Fp8Weight { const unsigned char *codes; const float *scales; };
 
 struct TokenArgs {
     int op, dtype;
@@ -134,6 +139,12 @@ struct TokenArgs {
     const int *top_k;
     int *tokens;
     float *logp;
+    // 8-bit rows (S: rows per sequence): RMSNORM_FP8 x, res, gamma -> yq or y; products xq, w (gate), w2 (up) -> yq or y
+    Fp8Rows xq, yq;
+    Fp8Weight w, w2;
+    const float *bias, *gamma;
+    const void *res;
+    int norm, act, features;   // features: of the operator's result
     float *ws;                 // set per call: token_ws_floats() of the unsplit operator, indexed by sequence (chunks own disjoint parts)
 };
 
@@ -173,6 +184,8 @@ LaunchInfo launch_cache_write(const TokenArgs &a, hipStream_t s, bool dry);
 LaunchInfo launch_cache_read(const TokenArgs &a, hipStream_t s, bool dry);
 LaunchInfo launch_cache_attention(const TokenArgs &a, hipStream_t s, bool dry, int phase);
 LaunchInfo launch_sample(const TokenArgs &a, hipStream_t s, bool dry, int phase);
+LaunchInfo launch_rmsnorm_fp8(const TokenArgs &a, hipStream_t s, bool dry);
+LaunchInfo launch_gemm_fp8(const TokenArgs &a, hipStream_t s, bool dry, int phase);          // and the gated block
 // one wavefront that spins for `ticks` of the constant 100 MHz clock (stream placement probe)
 void launch_spin(hipStream_t s, unsigned long long ticks);
 

@@ -418,6 +418,8 @@ LaunchInfo launch_tokens(const TokenArgs &a, hipStream_t s, bool dry, int phase)
     case TK_CACHE_WRITE: return launch_cache_write(a, s, dry);
     case TK_CACHE_READ: return launch_cache_read(a, s, dry);
     case TK_CACHE_ATTENTION: return launch_cache_attention(a, s, dry, phase);
+    case TK_RMSNORM_FP8: return launch_rmsnorm_fp8(a, s, dry);
+    case TK_GEMM_FP8: case TK_GATED_FP8: return launch_gemm_fp8(a, s, dry, phase);
     default: return launch_sample(a, s, dry, phase);
     }
 }

@@ -38,12 +38,32 @@ inline AttendGeom attend_geom(const TokenArgs &a)
     return g;
 }
 
+// Products of 8-bit rows, by the unsplit operator's shape.
+struct Fp8Geom { int features, slices, blocks_per_slice; bool join; };
+inline Fp8Geom fp8_geom(const TokenArgs &a)
+{
+    Fp8Geom g;
+    const bool gated = a.op == TK_GATED_FP8;
+    g.features = gated ? 16 : 32;
+    const int64_t rows = (int64_t)a.batch * a.S, blocks = (a.xq.features + FP8_BLOCK - 1) / FP8_BLOCK;
+    const int64_t tiles = ((rows + 31) / 32) * ((a.features + g.features - 1) / g.features);
+    g.slices = (int)std::min<int64_t>(std::max<int64_t>(1, 512 / tiles), std::max<int64_t>(1, blocks / 16));
+    g.blocks_per_slice = (int)((blocks + g.slices - 1) / g.slices);
+    g.slices = (int)((blocks + g.blocks_per_slice - 1) / g.blocks_per_slice);
+    g.join = g.slices > 1 || (gated && a.yq.codes);
+    return g;
+}
+
 // Floats of workspace that the unsplit operator needs.
 inline size_t token_ws_floats(const TokenArgs &a)
 {
     if (a.op == TK_CACHE_ATTENTION) {
         const AttendGeom g = attend_geom(a);
         if (g.splits > 1) return (size_t)a.batch * a.kv_heads * g.row_tiles * g.splits * g.rows * (a.D + 2);
+    }
+    if (a.op == TK_GEMM_FP8 || a.op == TK_GATED_FP8) {
+        const Fp8Geom g = fp8_geom(a);
+        if (g.join) return (size_t)g.slices * a.batch * a.S * a.features * (a.op == TK_GATED_FP8 ? 2 : 1);
     }
     return 0;
 }

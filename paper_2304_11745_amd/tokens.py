@@ -1,9 +1,10 @@
-"""A decoding tenant over PyTorch tensors: operator lists, the paged 4-bit cache, and sessions that run them.
+"""A decoding tenant over PyTorch tensors: operator lists, the paged 4-bit cache, 8-bit rows and weights, and sessions that run them.
 
 ``OpList`` writes down a tenant's operators (``include/gacer.h`` has their definitions) over tensors that the caller owns;
 ``TokenSession`` loads one or several lists into a gacer context and enqueues or runs them; ``Cache`` holds the tensors of a
-paged cache.  ``harness.Session`` takes such lists beside its own tenants (``extra=``), so that a decoding tenant runs in
-the same regulated rounds as the others.  No arithmetic happens here; every operator runs inside libgacer.so.
+paged cache, ``Fp8Rows`` and ``Fp8Weight`` those of 8-bit operands.  ``harness.Session`` takes such lists beside its own tenants (``extra=``), so that a decoding tenant runs in
+the same regulated rounds as the others.  No arithmetic happens here but ``Fp8Weight.quantise``, which a program calls once; every operator runs
+inside libgacer.so.
 
 Activations are ``[batch, tokens, features]`` or ``[batch, features]``, contiguous, in the list's dtype.
 """
@@ -14,6 +15,7 @@ import torch
 from . import binding as B
 
 _ACT = {"none": B.GACER_ACT_NONE, "relu": B.GACER_ACT_RELU, "relu6": B.GACER_ACT_RELU6, "gelu": B.GACER_ACT_GELU}
+_ACT_FP8 = dict(_ACT, hard_swish=B.GACER_ACT_HSWISH, hard_sigmoid=B.GACER_ACT_HSIGMOID, silu=B.GACER_ACT_SILU, gelu_tanh=B.GACER_ACT_GELU_TANH)
 
 
 def _need(ok, why):
@@ -48,6 +50,69 @@ class Cache:
                    torch.zeros(pages, kv_heads, page_tokens // 32, head_dim, 16, dtype=torch.uint8, **z),
                    torch.zeros(pages, kv_heads, page_tokens, head_dim // B.GACER_CACHE_GROUP, dtype=torch.int32, **z),
                    torch.zeros(pages, kv_heads, page_tokens, head_dim // B.GACER_CACHE_GROUP, dtype=torch.int32, **z), page_table)
+
+
+def _blocks(features):
+    return -(-features // B.GACER_FP8_BLOCK)
+
+
+class Fp8Rows:
+    """8-bit rows (``gacer_fp8_rows``): codes float8_e4m3fn ``[batch, tokens, features]`` or ``[batch, features]`` and a float32 scale for each block of
+    128 features of each row, ``[ceil(features/128), batch * tokens]``.  A code stands for itself times its block's scale."""
+
+    def __init__(self, codes, scales):
+        _need(codes.dim() in (2, 3) and codes.dtype == torch.float8_e4m3fn, "codes must be float8_e4m3fn [batch, features] or [batch, tokens, features]")
+        self.batch, self.features = codes.shape[0], codes.shape[-1]
+        self.rows = self.batch * (codes.shape[1] if codes.dim() == 3 else 1)
+        _need(tuple(scales.shape) == (_blocks(self.features), self.rows) and scales.dtype == torch.float32, "scales must be float32 [ceil(features/128), batch * tokens]")
+        for t in (codes, scales):
+            _need(t.is_cuda and t.is_contiguous() and t.device == codes.device, "the tensors of 8-bit rows must be contiguous and on one GPU")
+        self.codes, self.scales, self.device = codes, scales, codes.device
+
+    @classmethod
+    def allocate(cls, batch, tokens, features, device="cuda"):
+        return cls(torch.zeros(batch, tokens, features, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn),
+                   torch.zeros(_blocks(features), batch * tokens, device=device))
+
+    def values(self):
+        """What the rows stand for, float32, in the shape of the codes."""
+        scale = self.scales.t().repeat_interleave(B.GACER_FP8_BLOCK, 1)[:, :self.features]
+        return self.codes.float() * scale.reshape(self.codes.shape)
+
+    def _struct(self):
+        return B.gacer_fp8_rows(self.codes.data_ptr(), self.scales.data_ptr(), self.rows, self.features)
+
+
+class Fp8Weight:
+    """8-bit weights (``gacer_fp8_weight``): codes float8_e4m3fn ``[out, in]``, scales float32 ``[ceil(out/128), ceil(in/128)]``."""
+
+    def __init__(self, codes, scales):
+        _need(codes.dim() == 2 and codes.dtype == torch.float8_e4m3fn, "codes must be float8_e4m3fn [out, in]")
+        self.out, self.cin = codes.shape
+        _need(tuple(scales.shape) == (_blocks(self.out), _blocks(self.cin)) and scales.dtype == torch.float32, "scales must be float32 [ceil(out/128), ceil(in/128)]")
+        for t in (codes, scales):
+            _need(t.is_cuda and t.is_contiguous() and t.device == codes.device, "the tensors of 8-bit weights must be contiguous and on one GPU")
+        self.codes, self.scales, self.device = codes, scales, codes.device
+
+    @classmethod
+    def quantise(cls, weight):
+        """The 8-bit weights next to ``weight`` ``[out, in]``: in each block the largest magnitude becomes 448."""
+        out, cin = weight.shape
+        n = B.GACER_FP8_BLOCK
+        w = torch.zeros(_blocks(out) * n, _blocks(cin) * n, dtype=torch.float32, device=weight.device)
+        w[:out, :cin] = weight
+        w = w.view(_blocks(out), n, _blocks(cin), n)
+        most = w.abs().amax((1, 3), keepdim=True).clamp_min(2.0 ** -60)
+        codes = (w * (448.0 / most)).to(torch.float8_e4m3fn).view(_blocks(out) * n, -1)[:out, :cin]
+        return cls(codes.contiguous(), (most / 448.0)[:, 0, :, 0].contiguous())
+
+    def values(self):
+        """What the weights stand for, float32."""
+        n = B.GACER_FP8_BLOCK
+        return self.codes.float() * self.scales.repeat_interleave(n, 0)[:self.out].repeat_interleave(n, 1)[:, :self.cin]
+
+    def _struct(self):
+        return B.gacer_fp8_weight(self.codes.data_ptr(), self.scales.data_ptr())
 
 
 class OpList:
@@ -92,6 +157,15 @@ class OpList:
             self._index[key] = self.input = self._register(t)
         return self._index[key]
 
+    def _residual(self, t):
+        """Index of the residual that an operator on 8-bit rows adds, -1 without one: it may also come from outside, beside the tenant's input."""
+        if t is None:
+            return -1
+        key = (t.data_ptr(), self._shape(t))
+        if key not in self._index and self.input is not None:
+            self._index[key] = self._register(t)
+        return self._read(t)
+
     def _write(self, t):
         i = self._register(t)
         self._index[(t.data_ptr(), self._shape(t))] = i
@@ -110,7 +184,8 @@ class OpList:
         if desc is not None:
             self._descs.append(desc)
             w = C.addressof(desc)
-        self.ops.append(B.gacer_op(kind, in0, in1, res, out, w, bias, scale, shift, cin, cout, 1, 1, 1, 0, 1, _ACT[act], alpha))
+        names = _ACT if kind < B.GACER_RMSNORM_FP8 else _ACT_FP8
+        self.ops.append(B.gacer_op(kind, in0, in1, res, out, w, bias, scale, shift, cin, cout, 1, 1, 1, 0, 1, names[act], alpha))
 
     # -- operators of any tenant that a decoder layer needs ----------------------------------------------------------------------
     def gemm(self, x, weight, out, bias=None, act="none", res=None):
@@ -186,11 +261,57 @@ class OpList:
                              self._array(logp, f, rows, "logp"))
         self._op(B.GACER_SAMPLE, i, desc=d)
 
+    # -- operators on 8-bit rows ---------------------------------------------------------------------------------------------------
+    def _fp8(self, x):
+        """8-bit rows or weights as an operator's operand."""
+        if self.device is None:                      # a list that begins with 8-bit rows
+            self.device = x.device
+        _need(x.device == self.device, "8-bit rows and weights must be on the tenant's GPU")
+        _need(not isinstance(x, Fp8Rows) or x.batch == self.batch, "8-bit rows have the tenant's batch")
+        self._keep.append(x)
+        return x._struct()
+
+    def _norm8(self, x, rows, out, gamma, eps, res, norm):
+        i, r = self._read(x), self._residual(res)
+        g = self._array(gamma, torch.float32, (x.shape[-1],), "gamma")
+        if rows is not None:
+            _need(tuple(rows.codes.shape) == tuple(x.shape), "the 8-bit rows must have the shape of x")
+        d = B.gacer_fp8_norm(int(norm), B.gacer_fp8_rows() if rows is None else self._fp8(rows))
+        self._op(B.GACER_RMSNORM_FP8, i, -1 if out is None else self._write(out), res=r, scale=g, alpha=eps, desc=d)
+
+    def rmsnorm_fp8(self, x, rows, gamma=None, *, eps=1e-6, res=None, sum=None):
+        """``rows`` (Fp8Rows) = RMS norm of x + res over the features, times gamma; ``sum`` = x + res in the list's dtype (GACER_RMSNORM_FP8)."""
+        self._norm8(x, rows, sum, gamma, eps, res, True)
+
+    def quantise_fp8(self, x, rows, *, res=None, sum=None):
+        """``rows`` (Fp8Rows) = x + res as they are; ``sum`` as in rmsnorm_fp8."""
+        self._norm8(x, rows, sum, None, 0.0, res, False)
+
+    def rmsnorm(self, x, gamma, out, *, eps=1e-6, res=None):
+        """RMS norm of x + res over the features, times gamma, in the list's dtype."""
+        self._norm8(x, None, out, gamma, eps, res, True)
+
+    def gemm_fp8(self, rows, weight, out, *, bias=None, act="none", res=None):
+        """out = act(rows @ weight.T + bias + res) of 8-bit rows and an Fp8Weight (GACER_GEMM_FP8)."""
+        _need((weight.out, weight.cin) == (out.shape[-1], rows.features), "the weight must be [out features, in features]")
+        r = self._residual(res)
+        b = self._array(bias, torch.float32, (weight.out,), "bias")
+        d = B.gacer_fp8_gemm(self._fp8(rows), self._fp8(weight))
+        self._op(B.GACER_GEMM_FP8, -1, self._write(out), res=r, bias=b, act=act, desc=d)
+
+    def gated_fp8(self, rows, gate, up, out, *, act="silu"):
+        """out = act(rows @ gate.T) * (rows @ up.T) of 8-bit rows and two Fp8Weights; ``out`` an Fp8Rows or a tensor of the list's dtype (GACER_GATED_FP8)."""
+        codes = isinstance(out, Fp8Rows)
+        features = out.features if codes else out.shape[-1]
+        _need(all((w.out, w.cin) == (features, rows.features) for w in (gate, up)), "gate and up must be [out features, in features]")
+        d = B.gacer_fp8_gated(self._fp8(rows), self._fp8(gate), self._fp8(up), self._fp8(out) if codes else B.gacer_fp8_rows())
+        self._op(B.GACER_GATED_FP8, -1, -1 if codes else self._write(out), act=act, desc=d)
+
     # -- descriptor ----------------------------------------------------------------------------------------------------------------
     def descriptor(self, stream=0):
         """The tenant's ``gacer_tenant``; the list must outlive the call that loads it, and its tensors the session."""
         _need(self.ops, "an empty operator list")
-        if self.input is None:                       # only cache reads: a tenant still names an input
+        if self.input is None:                       # only cache reads or 8-bit rows: a tenant still names an input
             self._tensors.append((torch.empty(self.batch, dtype=self.dtype, device=self.device), (self.batch, 1, 1, 1)))
             self.input = len(self._tensors) - 1
         tens = (B.gacer_tensor * len(self._tensors))()
