@@ -43,6 +43,35 @@ __device__ __forceinline__ float activate8(float v, int act)
     return activate(v, act);
 }
 
+__device__ __forceinline__ void store4(float *p, const float *v) { *(float4 *)p = make_float4(v[0], v[1], v[2], v[3]); }
+__device__ __forceinline__ void store4(unsigned short *p, const float *v) { *(uint2 *)p = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])); }
+
+__device__ __forceinline__ void store8(float *p, const float *v) { store4(p, v); store4(p + 4, v + 4); }
+__device__ __forceinline__ void store8(unsigned short *p, const float *v) { *(uint4 *)p = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])); }
+__device__ __forceinline__ void load8(const float *p, float *v)
+{
+    const float4 a = *(const float4 *)p, b = *(const float4 *)(p + 4);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ void load8(const unsigned short *p, float *v)
+{
+    const Vec<unsigned short, 8> r = ld_vec<unsigned short, 8>(p, 0);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = r.get(e);
+}
+
+// N values at once: one (uniform) branch for all of them.
+template <int N> __device__ __forceinline__ void activate8_n(float *v, int act)
+{
+    if (act == ACT_SILU) {
+#pragma unroll
+        for (int q = 0; q < N; ++q) v[q] = activate8(v[q], ACT_SILU);
+    } else if (act == ACT_GELU_TANH) {
+#pragma unroll
+        for (int q = 0; q < N; ++q) v[q] = activate8(v[q], ACT_GELU_TANH);
+    } else activate_n<N>(v, act);
+}
+
 // Arguments of the products (see gacer_fp8_gemm, gacer_fp8_gated)
 struct Fp8Args {
     const unsigned char *x, *w, *w2;

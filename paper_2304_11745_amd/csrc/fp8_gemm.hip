@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 #include <algorithm>
 #include "fp8.h"
+#include "gemm_util.h"
 #include "tokens_geom.h"
 
 namespace gacer {
@@ -84,6 +85,282 @@ template <typename T, bool GATED> __global__ __launch_bounds__(512) void fp8_few
     }
 }
 
+// ---- many rows -------------------------------------------------------------------------------------------------------------------------
+// Tiles of BF features and BT rows, WF x WT waves, 64x64 (or as the numbers say) of the tile each.  Blocks of 128 inner features travel from memory straight
+// into LDS, as codes, NS - 1 of them ahead; LDS rows are 128 bytes, chunks of 16 swapped by the row's lowest bits so that 16-byte reads meet no bank twice.
+// A wave reads its codes, widens them and adds up a block's 128 products in the matrix cores (`part`), then adds the block to its sums times the two scales.
+template <int N> __device__ __forceinline__ void meet()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// The end of eight neighbouring features of a row (v); width: features of a row of y and res.
+template <typename T> __device__ __forceinline__ void finish8(const Fp8Args &a, int64_t row, int f, float *v)
+{
+    const int64_t at = row * a.N + f;
+    if (a.N % 8) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) if (f + e < a.N) finish<T>(a, row, f + e, v[e]);
+        return;
+    }
+    if (f >= a.N) return;
+    if (a.bias) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += a.bias[f + e];
+    }
+    if (a.res) {
+        float r[8];
+        load8((const T *)a.res + at, r);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += r[e];
+    }
+    activate8_n<8>(v, a.act);
+    store8((T *)a.y + at, v);
+}
+
+template <typename T, bool GATED, int BF, int BT, int WF, int WT, int NS> __global__ __launch_bounds__(64 * WF * WT) void fp8_tile_kernel(Fp8Args a)
+{
+    constexpr int NW = WF * WT, NF = BF / WF / 32, NT = BT / WT / 32, STAGE = (BF + BT) * FP8_BLOCK;
+    constexpr int PW = BF / 8 / NW, PX = BT / 8 / NW;        // kilobytes of weights and rows that a wave moves for a block
+    constexpr int SCALES = NT + (GATED ? 2 : 1), BEHIND = (NS - 2) * (PW + PX + SCALES);
+    static_assert(PW * 8 * NW == BF && PX * 8 * NW == BT && (!GATED || NF % 2 == 0), "");
+    __shared__ __align__(1024) unsigned char s0[STAGE], s1[STAGE], s2[NS > 2 ? STAGE : 16];
+    auto stage_at = [&](int i) -> unsigned char * { return i == 0 ? s0 : i == 1 ? s1 : s2; };
+    const int tid = threadIdx.x, l = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = l & 31, half = l >> 5;
+    const int wf = wave % WF, wt = wave / WF;
+
+    // tile: each of the eight dies takes a run of them, in which four neighbouring feature tiles follow each other
+    int id = blockIdx.x;
+    const int slice = id % a.slices; id /= a.slices;
+    {
+        const int all = a.f_tiles * a.r_tiles, per = all / 8, more = all % 8, die = id % 8;
+        id = die * per + min(die, more) + id / 8;
+    }
+    int ft0, rt0;
+    {
+        const int group = id / (4 * a.r_tiles), in = id - group * 4 * a.r_tiles, wide = min(4, a.f_tiles - group * 4);
+        ft0 = group * 4 + in % wide; rt0 = in / wide;
+    }
+    constexpr int FT = GATED ? BF / 2 : BF;                  // features of the result per tile
+    const int f0 = ft0 * FT, r0 = a.r_lo + rt0 * BT;
+    const int lo = slice * a.per_slice, hi = min(lo + a.per_slice, a.KB);
+
+    // what a lane moves: 16 bytes of row 8 q + l / 8 of each of the wave's pieces q
+    const __amdgpu_buffer_rsrc_t xr = make_rsrc(a.x, (int64_t)a.rows * a.K), wr = make_rsrc(a.w, (int64_t)a.N * a.K), ur = GATED ? make_rsrc(a.w2, (int64_t)a.N * a.K) : wr;
+    const int chunk = ((l & 7) ^ (l >> 3)) * 16;
+    unsigned woff[PW], xoff[PX];
+#pragma unroll
+    for (int i = 0; i < PW; ++i) {
+        const int row = (i * NW + wave) * 8 + (l >> 3), f = f0 + (GATED && row >= BF / 2 ? row - BF / 2 : row);
+        woff[i] = f < a.N ? (unsigned)f * a.K + chunk : OOB;
+    }
+#pragma unroll
+    for (int i = 0; i < PX; ++i) {
+        const int row = r0 + (i * NW + wave) * 8 + (l >> 3);
+        xoff[i] = row < a.r_hi ? (unsigned)row * a.K + chunk : OOB;
+    }
+    auto request = [&](unsigned char *stage, int kb) {
+        const unsigned bad = kb >= hi || kb * FP8_BLOCK + chunk >= a.K ? OOB : 0u;
+        const int k = min(kb, a.KB) * FP8_BLOCK;
+#pragma unroll
+        for (int i = 0; i < PW; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(GATED && (i * NW) * 8 >= BF / 2 ? ur : wr, GACER_LDS(stage + (i * NW + wave) * 1024), 16, (int)(woff[i] | bad), k, 0, 0);
+#pragma unroll
+        for (int i = 0; i < PX; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(xr, GACER_LDS(stage + BF * FP8_BLOCK + (i * NW + wave) * 1024), 16, (int)(xoff[i] | bad), k, 0, 0);
+    };
+
+    // scales: a lane's rows, the wave's features
+    int row[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) row[t] = min(r0 + wt * (BT / WT) + t * 32 + r, a.r_hi - 1);
+    const int fw = f0 + wf * (FT / WF);                      // the wave's first feature
+    const float *ws = a.ws + (int64_t)(min(fw, a.N - 1) / FP8_BLOCK) * a.KB, *us = GATED ? a.ws2 + (int64_t)(min(fw, a.N - 1) / FP8_BLOCK) * a.KB : ws;
+    int zero = 0;
+    asm volatile("" : "+v"(zero));                           // weights' scales by vector loads: scalar ones share a counter with the reads of LDS and come in any order
+    struct Scale { float x[NT], w, u; };
+    auto scales = [&](int kb) {
+        Scale s;
+        kb = min(kb, a.KB - 1);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) s.x[t] = a.xs[(int64_t)kb * a.rows + row[t]];
+        s.w = ws[kb + zero];
+        s.u = GATED ? us[kb + zero] : s.w;
+        return s;
+    };
+
+    const unsigned wbase = (GATED ? wf * (BF / 2 / WF) : wf * (BF / WF)) * FP8_BLOCK + r * FP8_BLOCK;
+    const unsigned xbase = (BF + wt * (BT / WT)) * FP8_BLOCK + r * FP8_BLOCK;
+    const unsigned swap = (half ^ (r & 7)) * 16;
+    f32x16 acc[NF][NT];
+#pragma unroll
+    for (int f = 0; f < NF; ++f)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[f][t][i] = 0.f;
+
+    Scale next = scales(lo);
+    auto step = [&](const unsigned char *from, unsigned char *into, int kb) {
+        const Scale now = next;
+        next = scales(kb + 1);
+        request(into, kb + NS - 1);
+        f32x16 part[NF][NT];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const unsigned at = swap ^ (32 * j);
+            uint4 w[NF], x[NT];
+#pragma unroll
+            for (int f = 0; f < NF; ++f) {
+                const int lane_row = GATED ? (f % (NF / 2)) * 32 + (f / (NF / 2)) * (BF / 2) : f * 32;
+                w[f] = *(const uint4 *)(from + wbase + lane_row * FP8_BLOCK + at);
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t) x[t] = *(const uint4 *)(from + xbase + t * 32 * FP8_BLOCK + at);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                bf16x8 xb[NT];
+#pragma unroll
+                for (int t = 0; t < NT; ++t) xb[t] = h ? widen(x[t].z, x[t].w) : widen(x[t].x, x[t].y);
+#pragma unroll
+                for (int f = 0; f < NF; ++f) {
+                    const bf16x8 wb = h ? widen(w[f].z, w[f].w) : widen(w[f].x, w[f].y);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        if (j == 0 && h == 0) {
+                            f32x16 zero = {};
+                            part[f][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb, xb[t], zero, 0, 0, 0);
+                        } else part[f][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb, xb[t], part[f][t], 0, 0, 0);
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const float s = now.x[t] * (GATED && f >= NF / 2 ? now.u : now.w);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[f][t][i] = fmaf(part[f][t][i], s, acc[f][t][i]);
+            }
+    };
+#pragma unroll
+    for (int i = 0; i < NS - 1; ++i) request(stage_at(i), lo + i);
+    for (int kb = lo; kb < hi; kb += NS) {
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+            if (kb + i >= hi) break;
+            meet<BEHIND>();
+            step(stage_at(i), stage_at((i + NS - 1) % NS), kb + i);
+        }
+    }
+
+    meet<0>();                                               // requests behind the end, which write zeros, have landed
+    // accumulator i of lane l: feature 8 (i / 4) + 4 (l / 32) + i % 4 of its tile, row l % 32
+    constexpr int NO = GATED ? NF / 2 : NF, PITCH = NO * 32 + 4, LPR = NO * 4;       // result tiles of a wave; floats of a row of its patch; lanes that store one
+    static_assert((NW + 1) / 2 * 32 * PITCH * 4 <= STAGE, "patches fit");
+    float *patch = (float *)(wave < (NW + 1) / 2 ? s0 : s1) + (wave < (NW + 1) / 2 ? wave : wave - (NW + 1) / 2) * 32 * PITCH;
+    // features c0.. of the accumulators of row tile t, through the wave's patch: whole rows leave together; `end` takes eight features of a row
+    auto leave = [&](int t, int c0, auto end) {
+#pragma unroll
+        for (int f = 0; f < NO; ++f)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const f32x16 &c = acc[c0 + f][t];
+                *(float4 *)(patch + r * PITCH + f * 32 + 8 * q + 4 * half) = make_float4(c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]);
+            }
+        const int m0 = r0 + wt * (BT / WT) + t * 32;
+#pragma unroll 1
+        for (int e = l; e < 32 * LPR; e += 64) {
+            float v[8];
+            load8(patch + (e / LPR) * PITCH + (e % LPR) * 8, v);
+            if (m0 + e / LPR < a.r_hi) end((int64_t)(m0 + e / LPR), fw + (e % LPR) * 8, v);
+        }
+    };
+    if (a.part) {
+        const int64_t width = (int64_t)a.N * (GATED ? 2 : 1);
+        float *p = a.part + (int64_t)slice * a.rows * width;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int c = 0; c < NF / NO; ++c)
+                leave(t, c * NO, [&](int64_t m, int o, const float *v) {
+                    float *to = p + m * width + c * a.N + o;
+                    if (a.N % 4 == 0 && o + 8 <= a.N) { store4(to, v); store4(to + 4, v + 4); }
+                    else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) if (o + e < a.N) to[e] = v[e];
+                    }
+                });
+        return;
+    }
+    if constexpr (!GATED) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) leave(t, 0, [&](int64_t m, int o, float *v) { finish8<T>(a, m, o, v); });
+    } else {
+        constexpr int NG = NF / 2;
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                activate8_n<16>((float *)&acc[g][t], a.act);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[g][t][i] *= acc[g + NG][t][i];
+            }
+        if (!a.yq) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+                leave(t, 0, [&](int64_t m, int o, const float *v) {
+                    T *y = (T *)a.y + m * a.N + o;
+                    if (a.N % 8 == 0) { if (o < a.N) store8(y, v); }
+                    else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) if (o + e < a.N) st_f32(y, e, v[e]);
+                    }
+                });
+            return;
+        }
+        // the largest magnitude of each row's block of 128: a lane's, the other half's, the other waves'
+        static_assert(BF == 256, "a tile holds a block of 128 features");
+        unsigned *most = (unsigned *)s0;                     // [WF][BT]
+        unsigned char *codes = s1;                           // [BT][128 + 16]
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            unsigned m = 0;
+#pragma unroll
+            for (int g = 0; g < NG; ++g)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) m = max(m, fw + g * 32 + 8 * (i / 4) + 4 * half < a.N ? magnitude(acc[g][t][i]) : 0u);     // a.N is a multiple of 16 here
+            m = max(m, (unsigned)__shfl_xor((int)m, 32));
+            if (half == 0) most[wf * BT + wt * (BT / WT) + t * 32 + r] = m;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int at = wt * (BT / WT) + t * 32 + r;
+            unsigned m = most[at];
+#pragma unroll
+            for (int w = 1; w < WF; ++w) m = max(m, most[w * BT + at]);
+            const float2 s = scale_of_block(m);
+            if (wf == 0 && half == 0 && r0 + at < a.r_hi) a.ys[(int64_t)ft0 * a.rows + r0 + at] = s.x;
+#pragma unroll
+            for (int g = 0; g < NG; ++g)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const unsigned c = to_codes(acc[g][t][4 * q], acc[g][t][4 * q + 1], acc[g][t][4 * q + 2], acc[g][t][4 * q + 3], s.y);
+                    *(unsigned *)(codes + at * 144 + wf * (128 / WF) + g * 32 + 8 * q + 4 * half) = s.y == 0.f ? 0u : c;
+                }
+        }
+        __syncthreads();
+        for (int e = tid; e < BT * 8; e += 64 * NW) {
+            const int m = r0 + e / 8, o = f0 + (e % 8) * 16;
+            if (m < a.r_hi && o < a.N) *(uint4 *)(a.yq + (int64_t)m * a.N + o) = *(const uint4 *)(codes + (e / 8) * 144 + (e % 8) * 16);
+        }
+    }
+}
+
 // Adds the slices in order and ends the product: a wave per row and block of 128 features, two neighbouring features a lane.
 template <typename T, bool GATED> __global__ __launch_bounds__(256) void fp8_join_kernel(Fp8Args a)
 {
@@ -123,6 +400,15 @@ template <typename T, bool GATED> __global__ __launch_bounds__(256) void fp8_joi
     if (l == 0) a.ys[(int64_t)block * a.rows + row] = s.x;
 }
 
+template <typename T, bool GATED> static void launch_product(const Fp8Args &b, const Fp8Geom &g, int grid, int join, int phase, hipStream_t s)
+{
+    if (phase != 2) {
+        if (g.tile == FP8_FEW) GACER_LAUNCH((fp8_few_kernel<T, GATED>), dim3(grid), dim3(512), 0, s, b);
+        else if (g.tile == FP8_WIDE) GACER_LAUNCH((fp8_tile_kernel<T, GATED, 256, 128, 4, 2, 3>), dim3(grid), dim3(512), 0, s, b);
+    }
+    if (g.join && phase != 1) GACER_LAUNCH((fp8_join_kernel<T, GATED>), dim3(join), dim3(256), 0, s, b);
+}
+
 LaunchInfo launch_gemm_fp8(const TokenArgs &a, hipStream_t s, bool dry, int phase)
 {
     const Fp8Geom g = fp8_geom(a);
@@ -132,21 +418,17 @@ LaunchInfo launch_gemm_fp8(const TokenArgs &a, hipStream_t s, bool dry, int phas
     b.bias = a.bias; b.res = a.res; b.y = a.y; b.yq = a.yq.codes; b.ys = a.yq.scales; b.part = g.join ? a.ws : nullptr;
     b.K = a.xq.features; b.KB = (b.K + FP8_BLOCK - 1) / FP8_BLOCK; b.N = a.features; b.rows = a.batch * a.S; b.act = a.act;
     b.r_lo = a.b_lo * a.S; b.r_hi = a.b_hi * a.S;
-    b.f_tiles = (b.N + g.features - 1) / g.features; b.r_tiles = (b.r_hi - b.r_lo + 31) / 32; b.slices = g.slices; b.per_slice = g.blocks_per_slice;
+    b.f_tiles = (b.N + g.features - 1) / g.features; b.r_tiles = (b.r_hi - b.r_lo + g.rows - 1) / g.rows; b.slices = g.slices; b.per_slice = g.blocks_per_slice;
+    const int grid = b.f_tiles * b.r_tiles * b.slices;
     const int64_t units = (int64_t)(b.r_hi - b.r_lo) * ((b.N + FP8_BLOCK - 1) / FP8_BLOCK);
+    const int join = (int)((units + 3) / 4);
     LaunchInfo li;
-    li.workgroups = phase == 2 ? (int)((units + 3) / 4) : (int)((int64_t)b.f_tiles * b.r_tiles * b.slices);
+    li.workgroups = phase == 2 ? join : grid;
     li.threads = phase == 2 ? 256 : 512; li.lds_bytes = phase == 2 ? 0 : 8 * 16 * 65 * 4; li.wg_per_cu = phase == 2 ? 8 : 4; li.phases = g.join ? 2 : 1;
     li.kernel = phase == 2 ? "fp8_join" : gated ? "gated_fp8" : "gemm_fp8";
     if (dry || b.r_hi <= b.r_lo) return li;
-#define BOTH(T, GATED)                                                                                                               \
-    do {                                                                                                                             \
-        if (phase != 2) GACER_LAUNCH((fp8_few_kernel<T, GATED>), dim3((unsigned)((int64_t)b.f_tiles * b.r_tiles * b.slices)), dim3(512), 0, s, b); \
-        if (g.join && phase != 1) GACER_LAUNCH((fp8_join_kernel<T, GATED>), dim3((unsigned)((units + 3) / 4)), dim3(256), 0, s, b); \
-    } while (0)
-    if (a.dtype == DT_BF16) { if (gated) BOTH(unsigned short, true); else BOTH(unsigned short, false); }
-    else { if (gated) BOTH(float, true); else BOTH(float, false); }
-#undef BOTH
+    if (a.dtype == DT_BF16) { if (gated) launch_product<unsigned short, true>(b, g, grid, join, phase, s); else launch_product<unsigned short, false>(b, g, grid, join, phase, s); }
+    else { if (gated) launch_product<float, true>(b, g, grid, join, phase, s); else launch_product<float, false>(b, g, grid, join, phase, s); }
     return li;
 }
 

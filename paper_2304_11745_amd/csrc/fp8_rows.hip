@@ -21,8 +21,7 @@ template <bool WHOLE> __device__ __forceinline__ void load8(const float *p, int 
 {
     if constexpr (WHOLE) {
         if (n >= 8) {
-            const float4 a = *(const float4 *)p, b = *(const float4 *)(p + 4);
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+            load8(p, v);
             return;
         }
     }
@@ -33,9 +32,7 @@ template <bool WHOLE> __device__ __forceinline__ void load8(const unsigned short
 {
     if constexpr (WHOLE) {
         if (n >= 8) {
-            Vec<unsigned short, 8> r = ld_vec<unsigned short, 8>(p, 0);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = r.get(e);
+            load8(p, v);
             return;
         }
     }
@@ -45,8 +42,7 @@ template <bool WHOLE> __device__ __forceinline__ void load8(const unsigned short
 template <bool WHOLE> __device__ __forceinline__ void store8(float *p, int n, const float *v)
 {
     if (WHOLE && n >= 8) {
-        *(float4 *)p = make_float4(v[0], v[1], v[2], v[3]);
-        *(float4 *)(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+        store8(p, v);
         return;
     }
 #pragma unroll
@@ -55,9 +51,7 @@ template <bool WHOLE> __device__ __forceinline__ void store8(float *p, int n, co
 template <bool WHOLE> __device__ __forceinline__ void store8(unsigned short *p, int n, const float *v)
 {
     if (WHOLE && n >= 8) {
-        Vec<unsigned short, 8> r;
-        r.pack(v);
-        st_vec<unsigned short, 8>(p, 0, r);
+        store8(p, v);
         return;
     }
 #pragma unroll

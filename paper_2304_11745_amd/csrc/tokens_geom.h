@@ -38,19 +38,22 @@ inline AttendGeom attend_geom(const TokenArgs &a)
     return g;
 }
 
-// Products of 8-bit rows, by the unsplit operator's shape.
-struct Fp8Geom { int features, slices, blocks_per_slice; bool join; };
+// Products of 8-bit rows, by the unsplit operator's shape: tiles of `features` of the result and `rows`, `slices` of the inner extent.
+enum Fp8Tile { FP8_FEW, FP8_WIDE };
+struct Fp8Geom { Fp8Tile tile; int features, rows, slices, blocks_per_slice; bool join; };
 inline Fp8Geom fp8_geom(const TokenArgs &a)
 {
     Fp8Geom g;
     const bool gated = a.op == TK_GATED_FP8;
-    g.features = gated ? 16 : 32;
     const int64_t rows = (int64_t)a.batch * a.S, blocks = (a.xq.features + FP8_BLOCK - 1) / FP8_BLOCK;
-    const int64_t tiles = ((rows + 31) / 32) * ((a.features + g.features - 1) / g.features);
-    g.slices = (int)std::min<int64_t>(std::max<int64_t>(1, 512 / tiles), std::max<int64_t>(1, blocks / 16));
+    g.tile = rows > 64 && ((rows + 127) / 128) * ((a.features + (gated ? 127 : 255)) / (gated ? 128 : 256)) >= 64 ? FP8_WIDE : FP8_FEW;
+    g.features = (g.tile == FP8_WIDE ? 256 : 32) / (gated ? 2 : 1);
+    g.rows = g.tile == FP8_WIDE ? 128 : 32;
+    const int64_t tiles = ((rows + g.rows - 1) / g.rows) * ((a.features + g.features - 1) / g.features);
+    g.slices = g.tile == FP8_WIDE ? 1 : (int)std::min<int64_t>(std::max<int64_t>(1, 512 / tiles), std::max<int64_t>(1, blocks / 16));
     g.blocks_per_slice = (int)((blocks + g.slices - 1) / g.slices);
     g.slices = (int)((blocks + g.blocks_per_slice - 1) / g.blocks_per_slice);
-    g.join = g.slices > 1 || (gated && a.yq.codes);
+    g.join = g.slices > 1 || (gated && a.yq.codes && g.tile == FP8_FEW);
     return g;
 }
 
