@@ -96,6 +96,28 @@ template <int N> __device__ __forceinline__ void meet()
     asm volatile("" ::: "memory");
 }
 
+// Loads of 16 or 4 bytes a lane from memory to LDS (from `to` on, in order of lanes), counted by vmcnt.  The compiler, which would wait for all of them before
+// it reads LDS, does not see them; they have no result in registers, and nothing else in these kernels uses m0.
+__device__ __forceinline__ void load_to_lds16(unsigned to, unsigned off, i32x4 from, int base)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(off), "s"(from), "s"(base) : "memory");
+}
+__device__ __forceinline__ void load_to_lds4(unsigned to, unsigned off, i32x4 from, int base)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(to), "v"(off), "s"(from), "s"(base) : "memory");
+}
+// A buffer's descriptor in scalar registers, as the instructions take it.
+__device__ __forceinline__ i32x4 descriptor(const void *p, int64_t bytes)
+{
+    const uint64_t u = (uint64_t)p;
+    i32x4 d;
+    d.x = __builtin_amdgcn_readfirstlane((int)(unsigned)u);
+    d.y = __builtin_amdgcn_readfirstlane((int)(unsigned)(u >> 32));
+    d.z = __builtin_amdgcn_readfirstlane((int)(bytes > 0x7FFFFFFF ? 0x7FFFFFFF : bytes));
+    d.w = 0x00020000;
+    return d;
+}
+
 // The end of eight neighbouring features of a row (v); width: features of a row of y and res.
 template <typename T> __device__ __forceinline__ void finish8(const Fp8Args &a, int64_t row, int f, float *v)
 {
@@ -122,12 +144,13 @@ template <typename T> __device__ __forceinline__ void finish8(const Fp8Args &a, 
 
 template <typename T, bool GATED, int BF, int BT, int WF, int WT, int NS> __global__ __launch_bounds__(64 * WF * WT) void fp8_tile_kernel(Fp8Args a)
 {
-    constexpr int NW = WF * WT, NF = BF / WF / 32, NT = BT / WT / 32, STAGE = (BF + BT) * FP8_BLOCK;
+    constexpr int NW = WF * WT, NF = BF / WF / 32, NT = BT / WT / 32, CODES = (BF + BT) * FP8_BLOCK, STAGE = CODES + NW * 256;
     constexpr int PW = BF / 8 / NW, PX = BT / 8 / NW;        // kilobytes of weights and rows that a wave moves for a block
-    constexpr int SCALES = NT + (GATED ? 2 : 1), BEHIND = (NS - 2) * (PW + PX + SCALES);
-    static_assert(PW * 8 * NW == BF && PX * 8 * NW == BT && (!GATED || NF % 2 == 0), "");
-    __shared__ __align__(1024) unsigned char s0[STAGE], s1[STAGE], s2[NS > 2 ? STAGE : 16];
-    auto stage_at = [&](int i) -> unsigned char * { return i == 0 ? s0 : i == 1 ? s1 : s2; };
+    constexpr int REQUESTS = PW + PX + 1;
+    static_assert(PW * 8 * NW == BF && PX * 8 * NW == BT && NT <= 2 && (!GATED || NF % 2 == 0), "");
+    __shared__ __align__(1024) unsigned char stages[NS][STAGE];      // codes of weights, of rows; for each wave the scales of its rows
+    constexpr int OF = GATED ? 2 : (BF + FP8_BLOCK - 1) / FP8_BLOCK;  // blocks of 128 features in a tile (gated: of gate and of up)
+    __shared__ float wscale[OF][FP8_BLOCKS_MAX];                     // scales of the tile's weights
     const int tid = threadIdx.x, l = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = l & 31, half = l >> 5;
     const int wf = wave % WF, wt = wave / WF;
 
@@ -147,8 +170,9 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int NS> __glob
     const int f0 = ft0 * FT, r0 = a.r_lo + rt0 * BT;
     const int lo = slice * a.per_slice, hi = min(lo + a.per_slice, a.KB);
 
-    // what a lane moves: 16 bytes of row 8 q + l / 8 of each of the wave's pieces q
-    const __amdgpu_buffer_rsrc_t xr = make_rsrc(a.x, (int64_t)a.rows * a.K), wr = make_rsrc(a.w, (int64_t)a.N * a.K), ur = GATED ? make_rsrc(a.w2, (int64_t)a.N * a.K) : wr;
+    // what a lane moves: 16 bytes of row 8 q + l / 8 of each of the wave's pieces q, and the scale of a row
+    const i32x4 xr = descriptor(a.x, (int64_t)a.rows * a.K), wr = descriptor(a.w, (int64_t)a.N * a.K), ur = GATED ? descriptor(a.w2, (int64_t)a.N * a.K) : wr;
+    const i32x4 sr = descriptor(a.xs, (int64_t)a.rows * a.KB * 4);
     const int chunk = ((l & 7) ^ (l >> 3)) * 16;
     unsigned woff[PW], xoff[PX];
 #pragma unroll
@@ -161,35 +185,26 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int NS> __glob
         const int row = r0 + (i * NW + wave) * 8 + (l >> 3);
         xoff[i] = row < a.r_hi ? (unsigned)row * a.K + chunk : OOB;
     }
-    auto request = [&](unsigned char *stage, int kb) {
+    const unsigned soff = min(r0 + wt * (BT / WT) + l % (NT * 32), a.r_hi - 1) * 4;
+    const unsigned lds0 = (unsigned)(uintptr_t)GACER_LDS(&stages[0][0]);
+    // piece p of block kb; behind the end zeros
+    auto request = [&](int stage, int kb, int p) {
         const unsigned bad = kb >= hi || kb * FP8_BLOCK + chunk >= a.K ? OOB : 0u;
-        const int k = min(kb, a.KB) * FP8_BLOCK;
-#pragma unroll
-        for (int i = 0; i < PW; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(GATED && (i * NW) * 8 >= BF / 2 ? ur : wr, GACER_LDS(stage + (i * NW + wave) * 1024), 16, (int)(woff[i] | bad), k, 0, 0);
-#pragma unroll
-        for (int i = 0; i < PX; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(xr, GACER_LDS(stage + BF * FP8_BLOCK + (i * NW + wave) * 1024), 16, (int)(xoff[i] | bad), k, 0, 0);
+        const int k = min(kb, a.KB - 1);
+        const unsigned to = lds0 + stage * STAGE;
+        if (p < PW) load_to_lds16(to + (p * NW + wave) * 1024, woff[p] | bad, GATED && p * NW * 8 >= BF / 2 ? ur : wr, k * FP8_BLOCK);
+        else if (p < PW + PX) load_to_lds16(to + BF * FP8_BLOCK + ((p - PW) * NW + wave) * 1024, xoff[p - PW] | bad, xr, k * FP8_BLOCK);
+        else load_to_lds4(to + CODES + wave * 256, soff, sr, k * a.rows * 4);
     };
-
-    // scales: a lane's rows, the wave's features
-    int row[NT];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) row[t] = min(r0 + wt * (BT / WT) + t * 32 + r, a.r_hi - 1);
+    for (int i = 0; i < NS - 1; ++i)
+#pragma unroll
+        for (int p = 0; p < REQUESTS; ++p) request(i, lo + i, p);
     const int fw = f0 + wf * (FT / WF);                      // the wave's first feature
-    const float *ws = a.ws + (int64_t)(min(fw, a.N - 1) / FP8_BLOCK) * a.KB, *us = GATED ? a.ws2 + (int64_t)(min(fw, a.N - 1) / FP8_BLOCK) * a.KB : ws;
-    int zero = 0;
-    asm volatile("" : "+v"(zero));                           // weights' scales by vector loads: scalar ones share a counter with the reads of LDS and come in any order
-    struct Scale { float x[NT], w, u; };
-    auto scales = [&](int kb) {
-        Scale s;
-        kb = min(kb, a.KB - 1);
+    for (int k = lo + tid; k < hi; k += 64 * NW)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) s.x[t] = a.xs[(int64_t)kb * a.rows + row[t]];
-        s.w = ws[kb + zero];
-        s.u = GATED ? us[kb + zero] : s.w;
-        return s;
-    };
+        for (int i = 0; i < OF; ++i)
+            wscale[i][k] = (GATED && i ? a.ws2 : a.ws)[(int64_t)(min(f0 + (GATED ? 0 : i * FP8_BLOCK), a.N - 1) / FP8_BLOCK) * a.KB + k];
 
     const unsigned wbase = (GATED ? wf * (BF / 2 / WF) : wf * (BF / WF)) * FP8_BLOCK + r * FP8_BLOCK;
     const unsigned xbase = (BF + wt * (BT / WT)) * FP8_BLOCK + r * FP8_BLOCK;
@@ -202,31 +217,40 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int NS> __glob
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[f][t][i] = 0.f;
 
-    Scale next = scales(lo);
-    auto step = [&](const unsigned char *from, unsigned char *into, int kb) {
-        const Scale now = next;
-        next = scales(kb + 1);
-        request(into, kb + NS - 1);
+    auto step = [&](int stage, int kb) {
+        const unsigned char *from = stages[stage];
+        const int into = (stage + NS - 1) % NS;
         f32x16 part[NF][NT];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        uint4 w[2][NF], x[2][NT];
+        auto fragments = [&](int j) {
             const unsigned at = swap ^ (32 * j);
-            uint4 w[NF], x[NT];
 #pragma unroll
             for (int f = 0; f < NF; ++f) {
                 const int lane_row = GATED ? (f % (NF / 2)) * 32 + (f / (NF / 2)) * (BF / 2) : f * 32;
-                w[f] = *(const uint4 *)(from + wbase + lane_row * FP8_BLOCK + at);
+                w[j & 1][f] = *(const uint4 *)(from + wbase + lane_row * FP8_BLOCK + at);
             }
 #pragma unroll
-            for (int t = 0; t < NT; ++t) x[t] = *(const uint4 *)(from + xbase + t * 32 * FP8_BLOCK + at);
+            for (int t = 0; t < NT; ++t) x[j & 1][t] = *(const uint4 *)(from + xbase + t * 32 * FP8_BLOCK + at);
+        };
+        fragments(0);
+        float sx[NT], sw[GATED ? 2 : 1];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) sx[t] = *(const float *)(from + CODES + wave * 256 + (t * 32 + r) * 4);
+        sw[0] = wscale[GATED ? 0 : wf * (BF / WF) / FP8_BLOCK][kb];
+        if (GATED) sw[1] = wscale[1][kb];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (j < 3) fragments(j + 1);
+#pragma unroll
+            for (int p = j * REQUESTS / 4; p < (j + 1) * REQUESTS / 4; ++p) request(into, kb + NS - 1, p);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 bf16x8 xb[NT];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) xb[t] = h ? widen(x[t].z, x[t].w) : widen(x[t].x, x[t].y);
+                for (int t = 0; t < NT; ++t) xb[t] = h ? widen(x[j & 1][t].z, x[j & 1][t].w) : widen(x[j & 1][t].x, x[j & 1][t].y);
 #pragma unroll
                 for (int f = 0; f < NF; ++f) {
-                    const bf16x8 wb = h ? widen(w[f].z, w[f].w) : widen(w[f].x, w[f].y);
+                    const bf16x8 wb = h ? widen(w[j & 1][f].z, w[j & 1][f].w) : widen(w[j & 1][f].x, w[j & 1][f].y);
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
                         if (j == 0 && h == 0) {
@@ -241,27 +265,24 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int NS> __glob
         for (int f = 0; f < NF; ++f)
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                const float s = now.x[t] * (GATED && f >= NF / 2 ? now.u : now.w);
+                const float s = sx[t] * sw[GATED && f >= NF / 2 ? 1 : 0];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[f][t][i] = fmaf(part[f][t][i], s, acc[f][t][i]);
             }
     };
-#pragma unroll
-    for (int i = 0; i < NS - 1; ++i) request(stage_at(i), lo + i);
     for (int kb = lo; kb < hi; kb += NS) {
 #pragma unroll
         for (int i = 0; i < NS; ++i) {
             if (kb + i >= hi) break;
-            meet<BEHIND>();
-            step(stage_at(i), stage_at((i + NS - 1) % NS), kb + i);
+            meet<(NS - 2) * REQUESTS>();
+            step(i, kb + i);
         }
     }
-
     meet<0>();                                               // requests behind the end, which write zeros, have landed
     // accumulator i of lane l: feature 8 (i / 4) + 4 (l / 32) + i % 4 of its tile, row l % 32
     constexpr int NO = GATED ? NF / 2 : NF, PITCH = NO * 32 + 4, LPR = NO * 4;       // result tiles of a wave; floats of a row of its patch; lanes that store one
-    static_assert((NW + 1) / 2 * 32 * PITCH * 4 <= STAGE, "patches fit");
-    float *patch = (float *)(wave < (NW + 1) / 2 ? s0 : s1) + (wave < (NW + 1) / 2 ? wave : wave - (NW + 1) / 2) * 32 * PITCH;
+    static_assert(NW * 32 * PITCH * 4 <= NS * STAGE && WF * BT * 4 <= STAGE && BT * 144 <= STAGE, "patches, magnitudes and codes fit");
+    float *patch = (float *)&stages[0][0] + wave * 32 * PITCH;
     // features c0.. of the accumulators of row tile t, through the wave's patch: whole rows leave together; `end` takes eight features of a row
     auto leave = [&](int t, int c0, auto end) {
 #pragma unroll
@@ -324,8 +345,8 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int NS> __glob
         }
         // the largest magnitude of each row's block of 128: a lane's, the other half's, the other waves'
         static_assert(BF == 256, "a tile holds a block of 128 features");
-        unsigned *most = (unsigned *)s0;                     // [WF][BT]
-        unsigned char *codes = s1;                           // [BT][128 + 16]
+        unsigned *most = (unsigned *)stages[0];                     // [WF][BT]
+        unsigned char *codes = stages[1];                           // [BT][128 + 16]
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             unsigned m = 0;

@@ -114,7 +114,7 @@ struct CacheView {
 };
 
 // 8-bit rows: e4m3 codes [rows][features], a scale for each block of 128 features [block][rows]
-enum { FP8_BLOCK = 128 };
+enum { FP8_BLOCK = 128, FP8_BLOCKS_MAX = 512 };
 struct Fp8Rows { unsigned char *codes; float *scales; int rows, features; };
 struct Fp8Weight { const unsigned char *codes; const float *scales; };
 
