@@ -87,7 +87,8 @@ template <typename T, bool GATED> __global__ __launch_bounds__(512) void fp8_few
 
 // ---- many rows -------------------------------------------------------------------------------------------------------------------------
 // Tiles of BF features and BT rows, WF x WT waves, 64x64 (or as the numbers say) of the tile each.  Blocks of 128 inner features travel from memory straight
-// into LDS, as codes, NS - 1 of them ahead; LDS rows are 128 bytes, chunks of 16 swapped by the row's lowest bits so that 16-byte reads meet no bank twice.
+// into LDS, as codes, NS - 1 of them ahead; LDS rows are 128 bytes, chunks of 16 swapped by bits 1 to 3 of the row so that 16 neighbouring
+// rows' reads meet no bank twice.
 // A wave reads its codes, widens them and adds up a block's 128 products in the matrix cores (`part`), then adds the block to its sums times the two scales.
 template <int N> __device__ __forceinline__ void meet()
 {
@@ -173,7 +174,7 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int NS> __glob
     // what a lane moves: 16 bytes of row 8 q + l / 8 of each of the wave's pieces q, and the scale of a row
     const i32x4 xr = descriptor(a.x, (int64_t)a.rows * a.K), wr = descriptor(a.w, (int64_t)a.N * a.K), ur = GATED ? descriptor(a.w2, (int64_t)a.N * a.K) : wr;
     const i32x4 sr = descriptor(a.xs, (int64_t)a.rows * a.KB * 4);
-    const int chunk = ((l & 7) ^ (l >> 3)) * 16;
+    const int chunk = ((l & 7) ^ ((wave & 1) * 4 + (l >> 4))) * 16;      // pieces of a wave are an even number apart, so that row / 2 % 8 is the same in all
     unsigned woff[PW], xoff[PX];
 #pragma unroll
     for (int i = 0; i < PW; ++i) {
@@ -208,7 +209,7 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int NS> __glob
 
     const unsigned wbase = (GATED ? wf * (BF / 2 / WF) : wf * (BF / WF)) * FP8_BLOCK + r * FP8_BLOCK;
     const unsigned xbase = (BF + wt * (BT / WT)) * FP8_BLOCK + r * FP8_BLOCK;
-    const unsigned swap = (half ^ (r & 7)) * 16;
+    const unsigned swap = (half ^ (r >> 1 & 7)) * 16;
     f32x16 acc[NF][NT];
 #pragma unroll
     for (int f = 0; f < NF; ++f)
