@@ -148,12 +148,14 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int NS> __glob
     constexpr int NW = WF * WT, NF = BF / WF / 32, NT = BT / WT / 32, CODES = (BF + BT) * FP8_BLOCK, STAGE = CODES + NW * 256;
     constexpr int PW = BF / 8 / NW, PX = BT / 8 / NW;        // kilobytes of weights and rows that a wave moves for a block
     constexpr int REQUESTS = PW + PX + 1;
-    static_assert(PW * 8 * NW == BF && PX * 8 * NW == BT && NT <= 2 && (!GATED || NF % 2 == 0), "");
+    static_assert(PW * 8 * NW == BF && PX * 8 * NW == BT && NT <= 2 && (!GATED || (NF % 2 == 0 && PW % 2 == 0)), "");
     __shared__ __align__(1024) unsigned char stages[NS][STAGE];      // codes of weights, of rows; for each wave the scales of its rows
     constexpr int OF = GATED ? 2 : (BF + FP8_BLOCK - 1) / FP8_BLOCK;  // blocks of 128 features in a tile (gated: of gate and of up)
     __shared__ float wscale[OF][FP8_BLOCKS_MAX];                     // scales of the tile's weights
     const int tid = threadIdx.x, l = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = l & 31, half = l >> 5;
     const int wf = wave % WF, wt = wave / WF;
+    constexpr bool TURNS = NW == 8;                          // see the loop
+    const int late = TURNS && wave >= 4 ? 1 : 0;
 
     // tile: each of the eight dies takes a run of them, in which four neighbouring feature tiles follow each other
     int id = blockIdx.x;
@@ -175,41 +177,38 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int NS> __glob
     const i32x4 xr = descriptor(a.x, (int64_t)a.rows * a.K), wr = descriptor(a.w, (int64_t)a.N * a.K), ur = GATED ? descriptor(a.w2, (int64_t)a.N * a.K) : wr;
     const i32x4 sr = descriptor(a.xs, (int64_t)a.rows * a.KB * 4);
     const int chunk = ((l & 7) ^ ((wave & 1) * 4 + (l >> 4))) * 16;      // pieces of a wave are an even number apart, so that row / 2 % 8 is the same in all
-    unsigned woff[PW], xoff[PX];
-#pragma unroll
-    for (int i = 0; i < PW; ++i) {
-        const int row = (i * NW + wave) * 8 + (l >> 3), f = f0 + (GATED && row >= BF / 2 ? row - BF / 2 : row);
-        woff[i] = f < a.N ? (unsigned)f * a.K + chunk : OOB;
-    }
-#pragma unroll
-    for (int i = 0; i < PX; ++i) {
-        const int row = r0 + (i * NW + wave) * 8 + (l >> 3);
-        xoff[i] = row < a.r_hi ? (unsigned)row * a.K + chunk : OOB;
-    }
+    // a lane's row of piece 0, in bytes; rows behind the end repeat the last one, their results are not stored
+    const unsigned wrow0 = (unsigned)(f0 + wave * 8 + (l >> 3)) * a.K, xrow0 = (unsigned)(r0 + wave * 8 + (l >> 3)) * a.K;
+    const unsigned wlast = (unsigned)(a.N - 1) * a.K, xlast = (unsigned)(a.r_hi - 1) * a.K;
     const unsigned soff = min(r0 + wt * (BT / WT) + l % (NT * 32), a.r_hi - 1) * 4;
     const unsigned lds0 = (unsigned)(uintptr_t)GACER_LDS(&stages[0][0]);
     // piece p of block kb; behind the end zeros
     auto request = [&](int stage, int kb, int p) {
-        const unsigned bad = kb >= hi || kb * FP8_BLOCK + chunk >= a.K ? OOB : 0u;
+        unsigned row0 = p < PW ? wrow0 : xrow0;
+        asm volatile("" : "+v"(row0));                       // offsets are formed where they are used, not kept for every piece
+        const unsigned in = kb >= hi || kb * FP8_BLOCK + chunk >= a.K ? OOB : (unsigned)chunk;
         const int k = min(kb, a.KB - 1);
         const unsigned to = lds0 + stage * STAGE;
-        if (p < PW) load_to_lds16(to + (p * NW + wave) * 1024, woff[p] | bad, GATED && p * NW * 8 >= BF / 2 ? ur : wr, k * FP8_BLOCK);
-        else if (p < PW + PX) load_to_lds16(to + BF * FP8_BLOCK + ((p - PW) * NW + wave) * 1024, xoff[p - PW] | bad, xr, k * FP8_BLOCK);
+        const int q = p < PW ? (GATED ? p % (PW / 2) : p) : p - PW;
+        const unsigned row = min(row0 + (unsigned)(q * NW * 8) * a.K, p < PW ? wlast : xlast);
+        if (p < PW) load_to_lds16(to + (p * NW + wave) * 1024, row + in, GATED && p >= PW / 2 ? ur : wr, k * FP8_BLOCK);
+        else if (p < PW + PX) load_to_lds16(to + BF * FP8_BLOCK + (q * NW + wave) * 1024, row + in, xr, k * FP8_BLOCK);
         else load_to_lds4(to + CODES + wave * 256, soff, sr, k * a.rows * 4);
     };
 #pragma unroll
     for (int i = 0; i < NS - 1; ++i)
+        if (!TURNS || i <= late) {
 #pragma unroll
-        for (int p = 0; p < REQUESTS; ++p) request(i, lo + i, p);
+            for (int p = 0; p < REQUESTS; ++p) request(i, lo + i, p);
+        }
     const int fw = f0 + wf * (FT / WF);                      // the wave's first feature
     for (int k = lo + tid; k < hi; k += 64 * NW)
 #pragma unroll
         for (int i = 0; i < OF; ++i)
             wscale[i][k] = (GATED && i ? a.ws2 : a.ws)[(int64_t)(min(f0 + (GATED ? 0 : i * FP8_BLOCK), a.N - 1) / FP8_BLOCK) * a.KB + k];
 
-    const unsigned wbase = (GATED ? wf * (BF / 2 / WF) : wf * (BF / WF)) * FP8_BLOCK + r * FP8_BLOCK;
-    const unsigned xbase = (BF + wt * (BT / WT)) * FP8_BLOCK + r * FP8_BLOCK;
-    const unsigned swap = (half ^ (r >> 1 & 7)) * 16;
+    const int wbase = (GATED ? wf * (BF / 2 / WF) : wf * (BF / WF)) * FP8_BLOCK, xbase = (BF + wt * (BT / WT)) * FP8_BLOCK;
+    const unsigned at = r * FP8_BLOCK + (half ^ (r >> 1 & 7)) * 16;      // a lane's codes of group 0 within 32 rows; of group j: at ^ 32 j
     f32x16 acc[NF][NT];
 #pragma unroll
     for (int f = 0; f < NF; ++f)
@@ -218,67 +217,109 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int NS> __glob
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[f][t][i] = 0.f;
 
+    // A block's products stay in `part` until the next block's first products replace them, tile by tile: each tile is scaled just before.
+    f32x16 part[NF][NT];
+    float by[GATED ? 2 : 1][NT];                             // what they are scaled by
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        by[0][t] = 0.f;
+        if (GATED) by[1][t] = 0.f;
+#pragma unroll
+        for (int f = 0; f < NF; ++f) part[f][t] = acc[f][t];
+    }
+    auto scale = [&](int f, int t) {
+        const float s = by[GATED && f >= NF / 2 ? 1 : 0][t];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[f][t][i] = fmaf(part[f][t][i], s, acc[f][t][i]);
+    };
+    // The four groups of 32 inner features are halved: while the products of one half run, the operands of the next are widened, four instructions behind
+    // each product, and codes are read a group before.  The compiler keeps this order (sched_barrier) and so the registers that it needs.
     auto step = [&](int stage, int kb) {
-        const unsigned char *from = stages[stage];
-        const int into = (stage + NS - 1) % NS;
-        f32x16 part[NF][NT];
-        uint4 w[2][NF], x[2][NT];
+        const unsigned char *from = stages[0];
+        int begin = stage * STAGE;
+        unsigned mine = at;
+        asm volatile("" : "+s"(begin), "+v"(mine));          // addresses are formed where they are used: kept for all stages they would not fit the registers
+        const int ahead = TURNS ? 1 + late : NS - 1, into = TURNS ? (stage + 1) % NS + late * ((stage + 2) % NS - (stage + 1) % NS) : (stage + NS - 1) % NS;
+        uint4 raw[2][NF + NT];                               // codes: weights, rows
+        bf16x8 wide[2][NF + NT];
         auto fragments = [&](int j) {
-            const unsigned at = swap ^ (32 * j);
+            const unsigned wa = (mine ^ 32 * j) + (begin + wbase), xa = (mine ^ 32 * j) + (begin + xbase);
 #pragma unroll
             for (int f = 0; f < NF; ++f) {
                 const int lane_row = GATED ? (f % (NF / 2)) * 32 + (f / (NF / 2)) * (BF / 2) : f * 32;
-                w[j & 1][f] = *(const uint4 *)(from + wbase + lane_row * FP8_BLOCK + at);
+                raw[j & 1][f] = *(const uint4 *)(from + wa + lane_row * FP8_BLOCK);
             }
 #pragma unroll
-            for (int t = 0; t < NT; ++t) x[j & 1][t] = *(const uint4 *)(from + xbase + t * 32 * FP8_BLOCK + at);
+            for (int t = 0; t < NT; ++t) raw[j & 1][NF + t] = *(const uint4 *)(from + xa + t * 32 * FP8_BLOCK);
+        };
+        auto open = [&](int g, int i) {                      // operand i of half g
+            const uint4 &c = raw[g / 2 & 1][i];
+            wide[g & 1][i] = g & 1 ? widen(c.z, c.w) : widen(c.x, c.y);
+            asm volatile("" : "+v"(wide[g & 1][i]));         // here and no later
         };
         fragments(0);
-        float sx[NT], sw[GATED ? 2 : 1];
+        __builtin_amdgcn_sched_barrier(0);
+        scale(0, 0);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) sx[t] = *(const float *)(from + CODES + wave * 256 + (t * 32 + r) * 4);
-        sw[0] = wscale[GATED ? 0 : wf * (BF / WF) / FP8_BLOCK][kb];
-        if (GATED) sw[1] = wscale[1][kb];
+        for (int i = 0; i < NF + NT; ++i) open(0, i);
+        float sw = 0.f, su = 0.f, sx[NT];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (j < 3) fragments(j + 1);
+        for (int g = 0; g < 8; ++g) {
+            if (g % 2 == 0) {
+                if (g < 6) fragments(g / 2 + 1);
 #pragma unroll
-            for (int p = j * REQUESTS / 4; p < (j + 1) * REQUESTS / 4; ++p) request(into, kb + NS - 1, p);
+                for (int p = TURNS ? g / 2 * REQUESTS / 2 : g / 2 * REQUESTS / 4; p < (TURNS ? (g < 4 ? (g / 2 + 1) * REQUESTS / 2 : 0) : (g / 2 + 1) * REQUESTS / 4); ++p) request(into, kb + ahead, p);
+                if (TURNS && g == 4) __builtin_amdgcn_s_barrier();
+            }
+            if (g == 4) {
+                sw = wscale[GATED ? 0 : wf * (BF / WF) / FP8_BLOCK][kb];
+                if (GATED) su = wscale[1][kb];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                bf16x8 xb[NT];
+                for (int t = 0; t < NT; ++t) sx[t] = *(const float *)(from + (begin + CODES + wave * 256) + (t * 32 + r) * 4);
+            }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int t = 0; t < NT; ++t) xb[t] = h ? widen(x[j & 1][t].z, x[j & 1][t].w) : widen(x[j & 1][t].x, x[j & 1][t].y);
+            for (int m = 0; m < NF * NT; ++m) {
+                const int f = m / NT, t = m % NT;
+                if (g == 0) {
+                    if (m > 0) scale(f, t);
+                    __builtin_amdgcn_sched_barrier(0);
+                    f32x16 zero = {};
+                    part[f][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wide[0][f], wide[0][NF + t], zero, 0, 0, 0);
+                } else part[f][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wide[g & 1][f], wide[g & 1][NF + t], part[f][t], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+                if (g < 7) {
 #pragma unroll
-                for (int f = 0; f < NF; ++f) {
-                    const bf16x8 wb = h ? widen(w[j & 1][f].z, w[j & 1][f].w) : widen(w[j & 1][f].x, w[j & 1][f].y);
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        if (j == 0 && h == 0) {
-                            f32x16 zero = {};
-                            part[f][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb, xb[t], zero, 0, 0, 0);
-                        } else part[f][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb, xb[t], part[f][t], 0, 0, 0);
-                    }
+                    for (int i = m * (NF + NT) / (NF * NT); i < (m + 1) * (NF + NT) / (NF * NT); ++i) open(g + 1, i);
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
 #pragma unroll
-        for (int f = 0; f < NF; ++f)
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const float s = sx[t] * sw[GATED && f >= NF / 2 ? 1 : 0];
-#pragma unroll
-                for (int i = 0; i < 16; ++i) acc[f][t][i] = fmaf(part[f][t][i], s, acc[f][t][i]);
-            }
+        for (int t = 0; t < NT; ++t) {
+            by[0][t] = sx[t] * sw;
+            if (GATED) by[1][t] = sx[t] * su;
+        }
     };
+    // With eight waves, two to a SIMD, the second four are half a block late: while one wave of a SIMD scales its block's products, the other's keep the matrix
+    // core busy.  All meet twice a block.  When the early ones begin block n (their loads of it waited for; the late ones waited before their block n - 1, or
+    // before the first meeting), the late ones are amid block n - 1 and stage n - 2 is free: the early ones' loads of block n + 1 go there.  When the late ones
+    // begin block n, the early ones have left stage n - 1: the late ones' loads of block n + 2 go there.
+    if (late) meet<0>();
     for (int kb = lo; kb < hi; kb += NS) {
 #pragma unroll
         for (int i = 0; i < NS; ++i) {
             if (kb + i >= hi) break;
-            meet<(NS - 2) * REQUESTS>();
+            meet<TURNS ? 0 : (NS - 2) * REQUESTS>();
             step(i, kb + i);
         }
     }
+    if (TURNS && !late) __builtin_amdgcn_s_barrier();
+#pragma unroll
+    for (int f = 0; f < NF; ++f)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) scale(f, t);
     meet<0>();                                               // requests behind the end, which write zeros, have landed
     // accumulator i of lane l: feature 8 (i / 4) + 4 (l / 32) + i % 4 of its tile, row l % 32
     constexpr int NO = GATED ? NF / 2 : NF, PITCH = NO * 32 + 4, LPR = NO * 4;       // result tiles of a wave; floats of a row of its patch; lanes that store one
