@@ -19,69 +19,76 @@ template <typename T> __device__ __forceinline__ void finish(const Fp8Args &a, i
     st_f32((T *)a.y, row * a.N + f, activate8(v, a.act));
 }
 
-// One workgroup of eight waves per tile of 32 rows and 32 features (gated: 16 gate and 16 up features); the waves take the tile's blocks of 128 inner
-// features in turn and their sums are added in order.  Operands come straight from memory: lane l holds feature (row) l % 32, and of every
-// 32 inner features the 16 codes of half l / 32.
-template <typename T, bool GATED> __global__ __launch_bounds__(512) void fp8_few_kernel(Fp8Args a)
+// ---- few rows --------------------------------------------------------------------------------------------------------------------------
+// One workgroup of eight waves per tile of 32 features and 32 rows; the waves take the tile's blocks of 128 inner features in turn and their sums are added
+// in order.  Operands come straight from memory, three blocks of them in flight in registers: lane l holds feature (row) l % 32, and of every 32 inner
+// features the 16 codes of half l / 32.
+template <typename T> __global__ __launch_bounds__(512) void fp8_few_kernel(Fp8Args a)
 {
-    constexpr int W = 8, FT = GATED ? 16 : 32;
+    constexpr int W = 8, AHEAD = 3;
     __shared__ float red[W][16][65];
     const int tid = threadIdx.x, l = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = l & 31, half = l >> 5;
     int id = blockIdx.x;
     const int slice = id % a.slices; id /= a.slices;
-    const int f0 = (id % a.f_tiles) * FT, r0 = a.r_lo + (id / a.f_tiles) * 32;
-    const int row = min(r0 + r, a.r_hi - 1);            // rows and features beyond the end repeat the last one; their results are not stored
-    const unsigned char *x = a.x + (int64_t)row * a.K;
-    const unsigned char *w = GATED ? (r < 16 ? a.w : a.w2) + (int64_t)min(f0 + (r & 15), a.N - 1) * a.K : a.w + (int64_t)min(f0 + r, a.N - 1) * a.K;
-    const float *ws = a.ws + (int64_t)(f0 / FP8_BLOCK) * a.KB, *ws2 = GATED ? a.ws2 + (int64_t)(f0 / FP8_BLOCK) * a.KB : nullptr;
+    const int f0 = (id % a.f_tiles) * 32, r0 = a.r_lo + (id / a.f_tiles) * 32;
+    const int row = min(r0 + r, a.r_hi - 1);           // rows and features beyond the end repeat the last one; their results are not stored
+    const unsigned char *x = a.x + (int64_t)row * a.K, *w = a.w + (int64_t)min(f0 + r, a.N - 1) * a.K;
+    const float *ws = a.ws + (int64_t)(f0 / FP8_BLOCK) * a.KB;
     const int lo = slice * a.per_slice, hi = min(lo + a.per_slice, a.KB);
 
     f32x16 acc;
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[i] = 0.f;
-    for (int kb = lo + wave; kb < hi; kb += W) {
-        uint4 xv[4], wv[4];
+    struct Block { uint4 w[4], x[4]; float sx, sw; } blocks[AHEAD];
+    auto load = [&](Block &b, int kb) {                // behind the end one place for all lanes, which costs next to nothing
+        const bool on = kb < hi;
+        kb = on ? kb : lo;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int k = kb * FP8_BLOCK + 32 * j + 16 * half, at = min(k, a.K - 16);
-            wv[j] = *(const uint4 *)(w + at);
-            xv[j] = *(const uint4 *)(x + at);
-            if (k >= a.K) xv[j] = make_uint4(0, 0, 0, 0);       // behind the end
+            const int at = min(kb * FP8_BLOCK + 32 * j + 16 * half, a.K - 16);
+            b.w[j] = *(const uint4 *)(on ? w + at : a.w);
+            b.x[j] = *(const uint4 *)(on ? x + at : a.x);
         }
-        const float sx = a.xs[(int64_t)kb * a.rows + row], s = sx * ws[kb], s2 = GATED ? sx * ws2[kb] : s;
+        b.sw = ws[kb];
+        b.sx = a.xs[(int64_t)kb * a.rows + row];
+    };
+    auto multiply = [&](const Block &b, int kb) {
         f32x16 p;
 #pragma unroll
         for (int i = 0; i < 16; ++i) p[i] = 0.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            p = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(wv[j].x, wv[j].y), widen(xv[j].x, xv[j].y), p, 0, 0, 0);
-            p = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(wv[j].z, wv[j].w), widen(xv[j].z, xv[j].w), p, 0, 0, 0);
+            uint4 c = b.x[j];
+            if (kb == a.KB - 1 && kb * FP8_BLOCK + 32 * j + 16 * half >= a.K) c = make_uint4(0, 0, 0, 0);
+            p = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(b.w[j].x, b.w[j].y), widen(c.x, c.y), p, 0, 0, 0);
+            p = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(b.w[j].z, b.w[j].w), widen(c.z, c.w), p, 0, 0, 0);
         }
+        const float s = b.sx * b.sw;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) acc[i] = fmaf(p[i], GATED && i >= 8 ? s2 : s, acc[i]);
+        for (int i = 0; i < 16; ++i) acc[i] = fmaf(p[i], s, acc[i]);
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) load(blocks[i], lo + wave + i * W);
+    for (int kb = lo + wave; kb < hi; kb += W * AHEAD) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (kb + i * W < hi) multiply(blocks[i], kb + i * W);
+            load(blocks[i], kb + (i + AHEAD) * W);
+        }
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) red[wave][i][l] = acc[i];
     __syncthreads();
     // accumulator i of lane l: feature 8 (i / 4) + 4 (l / 32) + i % 4 of the tile, row l % 32
-    auto sum = [&](int f, int row) {
+    const int n = min(32, a.r_hi - r0);
+    for (int e = tid; e < 32 * n; e += 512) {
+        const int f = e % 32, m = e / 32;
+        if (f0 + f >= a.N) continue;
         float v = 0.f;
 #pragma unroll
-        for (int i = 0; i < W; ++i) v += red[i][(f >> 3) * 4 + (f & 3)][row + 32 * ((f >> 2) & 1)];
-        return v;
-    };
-    const int n = min(32, a.r_hi - r0);
-    for (int e = tid; e < FT * n; e += 512) {
-        const int f = e % FT, m = e / FT;
-        if (f0 + f >= a.N) continue;
-        const float v = sum(f, m), u = GATED ? sum(f + 16, m) : 0.f;
-        const int64_t at = r0 + m;
-        if (a.part) {
-            float *p = a.part + ((int64_t)slice * a.rows + at) * a.N * (GATED ? 2 : 1) + f0 + f;
-            p[0] = v;
-            if (GATED) p[a.N] = u;
-        } else if (GATED) st_f32((T *)a.y, at * a.N + f0 + f, activate8(v, a.act) * u);
-        else finish<T>(a, at, f0 + f, v);
+        for (int i = 0; i < W; ++i) v += red[i][(f >> 3) * 4 + (f & 3)][m + 32 * ((f >> 2) & 1)];
+        if (a.part) a.part[((int64_t)slice * a.rows + r0 + m) * a.N + f0 + f] = v;
+        else finish<T>(a, r0 + m, f0 + f, v);
     }
 }
 
@@ -143,18 +150,18 @@ template <typename T> __device__ __forceinline__ void finish8(const Fp8Args &a, 
     store8((T *)a.y + at, v);
 }
 
-template <typename T, bool GATED, int BF, int BT, int WF, int WT, int NS> __global__ __launch_bounds__(64 * WF * WT) void fp8_tile_kernel(Fp8Args a)
+template <typename T, bool GATED, int BF, int BT, int WF, int WT, int KH, int NS> __global__ __launch_bounds__(64 * WF * WT * KH) void fp8_tile_kernel(Fp8Args a)
 {
-    constexpr int NW = WF * WT, NF = BF / WF / 32, NT = BT / WT / 32, CODES = (BF + BT) * FP8_BLOCK, STAGE = CODES + NW * 256;
-    constexpr int PW = BF / 8 / NW, PX = BT / 8 / NW;        // kilobytes of weights and rows that a wave moves for a block
+    constexpr int NW = WF * WT * KH, GROUPS = 4 / KH, NF = BF / WF / 32, NT = BT / WT / 32, CODES = (BF + BT) * FP8_BLOCK, STAGE = CODES + NW * 256;
+    constexpr int PW = BF / 8 / NW, PX = (BT / 8 + NW - 1) / NW;        // kilobytes of weights and rows that a wave moves for a block
     constexpr int REQUESTS = PW + PX + 1;
-    static_assert(PW * 8 * NW == BF && PX * 8 * NW == BT && NT <= 2 && (!GATED || (NF % 2 == 0 && PW % 2 == 0)), "");
+    static_assert(PW * 8 * NW == BF && (PX * 8 * NW == BT || (PX == 1 && NW % (BT / 8) == 0)) && NW % 2 == 0 && NT <= 2 && (!GATED || (NF % 2 == 0 && PW % 2 == 0)), "");
     __shared__ __align__(1024) unsigned char stages[NS][STAGE];      // codes of weights, of rows; for each wave the scales of its rows
     constexpr int OF = GATED ? 2 : (BF + FP8_BLOCK - 1) / FP8_BLOCK;  // blocks of 128 features in a tile (gated: of gate and of up)
     __shared__ float wscale[OF][FP8_BLOCKS_MAX];                     // scales of the tile's weights
     const int tid = threadIdx.x, l = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = l & 31, half = l >> 5;
-    const int wf = wave % WF, wt = wave / WF;
-    constexpr bool TURNS = NW == 8;                          // see the loop
+    const int wf = wave % WF, wt = wave / WF % WT, kh = wave / (WF * WT);
+    constexpr bool TURNS = NW == 8 && KH == 1;               // see the loop
     const int late = TURNS && wave >= 4 ? 1 : 0;
 
     // tile: each of the eight dies takes a run of them, in which four neighbouring feature tiles follow each other
@@ -178,7 +185,7 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int NS> __glob
     const i32x4 sr = descriptor(a.xs, (int64_t)a.rows * a.KB * 4);
     const int chunk = ((l & 7) ^ ((wave & 1) * 4 + (l >> 4))) * 16;      // pieces of a wave are an even number apart, so that row / 2 % 8 is the same in all
     // a lane's row of piece 0, in bytes; rows behind the end repeat the last one, their results are not stored
-    const unsigned wrow0 = (unsigned)(f0 + wave * 8 + (l >> 3)) * a.K, xrow0 = (unsigned)(r0 + wave * 8 + (l >> 3)) * a.K;
+    const unsigned wrow0 = (unsigned)(f0 + wave * 8 + (l >> 3)) * a.K, xrow0 = (unsigned)(r0 + wave % (BT / 8) * 8 + (l >> 3)) * a.K;
     const unsigned wlast = (unsigned)(a.N - 1) * a.K, xlast = (unsigned)(a.r_hi - 1) * a.K;
     const unsigned soff = min(r0 + wt * (BT / WT) + l % (NT * 32), a.r_hi - 1) * 4;
     const unsigned lds0 = (unsigned)(uintptr_t)GACER_LDS(&stages[0][0]);
@@ -189,10 +196,10 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int NS> __glob
         const unsigned in = kb >= hi || kb * FP8_BLOCK + chunk >= a.K ? OOB : (unsigned)chunk;
         const int k = min(kb, a.KB - 1);
         const unsigned to = lds0 + stage * STAGE;
-        const int q = p < PW ? (GATED ? p % (PW / 2) : p) : p - PW;
+        const int q = p < PW ? p % (GATED ? (PW + 1) / 2 : PW) : p - PW, xwave = wave % (BT / 8);       // where there are more waves than pieces, several move the same one
         const unsigned row = min(row0 + (unsigned)(q * NW * 8) * a.K, p < PW ? wlast : xlast);
         if (p < PW) load_to_lds16(to + (p * NW + wave) * 1024, row + in, GATED && p >= PW / 2 ? ur : wr, k * FP8_BLOCK);
-        else if (p < PW + PX) load_to_lds16(to + BF * FP8_BLOCK + (q * NW + wave) * 1024, row + in, xr, k * FP8_BLOCK);
+        else if (p < PW + PX) load_to_lds16(to + BF * FP8_BLOCK + (q * NW + xwave) * 1024, row + in, xr, k * FP8_BLOCK);
         else load_to_lds4(to + CODES + wave * 256, soff, sr, k * a.rows * 4);
     };
 #pragma unroll
@@ -208,7 +215,7 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int NS> __glob
             wscale[i][k] = (GATED && i ? a.ws2 : a.ws)[(int64_t)(min(f0 + (GATED ? 0 : i * FP8_BLOCK), a.N - 1) / FP8_BLOCK) * a.KB + k];
 
     const int wbase = (GATED ? wf * (BF / 2 / WF) : wf * (BF / WF)) * FP8_BLOCK, xbase = (BF + wt * (BT / WT)) * FP8_BLOCK;
-    const unsigned at = r * FP8_BLOCK + (half ^ (r >> 1 & 7)) * 16;      // a lane's codes of group 0 within 32 rows; of group j: at ^ 32 j
+    const unsigned at = r * FP8_BLOCK + ((half ^ (r >> 1 & 7)) * 16 ^ 64 * kh);      // a lane's codes of group 0 within 32 rows; of group j: at ^ 32 j
     f32x16 acc[NF][NT];
 #pragma unroll
     for (int f = 0; f < NF; ++f)
@@ -223,7 +230,7 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int NS> __glob
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         by[0][t] = 0.f;
-        if (GATED) by[1][t] = 0.f;
+        if constexpr (GATED) by[1][t] = 0.f;
 #pragma unroll
         for (int f = 0; f < NF; ++f) part[f][t] = acc[f][t];
     }
@@ -246,7 +253,8 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int NS> __glob
             const unsigned wa = (mine ^ 32 * j) + (begin + wbase), xa = (mine ^ 32 * j) + (begin + xbase);
 #pragma unroll
             for (int f = 0; f < NF; ++f) {
-                const int lane_row = GATED ? (f % (NF / 2)) * 32 + (f / (NF / 2)) * (BF / 2) : f * 32;
+                constexpr int HALVES = GATED ? NF / 2 : NF;  // gate and up rows lie half a tile apart
+                const int lane_row = f % HALVES * 32 + f / HALVES * (BF / 2);
                 raw[j & 1][f] = *(const uint4 *)(from + wa + lane_row * FP8_BLOCK);
             }
 #pragma unroll
@@ -265,16 +273,16 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int NS> __glob
         for (int i = 0; i < NF + NT; ++i) open(0, i);
         float sw = 0.f, su = 0.f, sx[NT];
 #pragma unroll
-        for (int g = 0; g < 8; ++g) {
+        for (int g = 0; g < 2 * GROUPS; ++g) {
             if (g % 2 == 0) {
-                if (g < 6) fragments(g / 2 + 1);
+                if (g / 2 < GROUPS - 1) fragments(g / 2 + 1);
 #pragma unroll
-                for (int p = TURNS ? g / 2 * REQUESTS / 2 : g / 2 * REQUESTS / 4; p < (TURNS ? (g < 4 ? (g / 2 + 1) * REQUESTS / 2 : 0) : (g / 2 + 1) * REQUESTS / 4); ++p) request(into, kb + ahead, p);
+                for (int p = TURNS ? g / 2 * REQUESTS / 2 : g / 2 * REQUESTS / GROUPS; p < (TURNS ? (g < 4 ? (g / 2 + 1) * REQUESTS / 2 : 0) : (g / 2 + 1) * REQUESTS / GROUPS); ++p) request(into, kb + ahead, p);
                 if (TURNS && g == 4) __builtin_amdgcn_s_barrier();
             }
-            if (g == 4) {
+            if (g == GROUPS) {
                 sw = wscale[GATED ? 0 : wf * (BF / WF) / FP8_BLOCK][kb];
-                if (GATED) su = wscale[1][kb];
+                if constexpr (GATED) su = wscale[1][kb];
 #pragma unroll
                 for (int t = 0; t < NT; ++t) sx[t] = *(const float *)(from + (begin + CODES + wave * 256) + (t * 32 + r) * 4);
             }
@@ -289,7 +297,7 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int NS> __glob
                     part[f][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wide[0][f], wide[0][NF + t], zero, 0, 0, 0);
                 } else part[f][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wide[g & 1][f], wide[g & 1][NF + t], part[f][t], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
-                if (g < 7) {
+                if (g < 2 * GROUPS - 1) {
 #pragma unroll
                     for (int i = m * (NF + NT) / (NF * NT); i < (m + 1) * (NF + NT) / (NF * NT); ++i) open(g + 1, i);
                 }
@@ -299,7 +307,7 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int NS> __glob
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             by[0][t] = sx[t] * sw;
-            if (GATED) by[1][t] = sx[t] * su;
+            if constexpr (GATED) by[1][t] = sx[t] * su;
         }
     };
     // With eight waves, two to a SIMD, the second four are half a block late: while one wave of a SIMD scales its block's products, the other's keep the matrix
@@ -321,10 +329,35 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int NS> __glob
 #pragma unroll
         for (int t = 0; t < NT; ++t) scale(f, t);
     meet<0>();                                               // requests behind the end, which write zeros, have landed
+    if constexpr (KH == 2) {                                 // both halves of the blocks, in order
+        float4 *other = (float4 *)&stages[0][0] + (wave % (WF * WT)) * (NF * NT * 256) + l;
+        static_assert(WF * WT * NF * NT * 4096 <= NS * STAGE, "a half's sums fit");
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (kh == 1) other[(f * NT + t) * 256 + q * 64] = make_float4(acc[f][t][4 * q], acc[f][t][4 * q + 1], acc[f][t][4 * q + 2], acc[f][t][4 * q + 3]);
+        meet<0>();
+        if (kh == 0) {
+#pragma unroll
+            for (int f = 0; f < NF; ++f)
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const float4 v = other[(f * NT + t) * 256 + q * 64];
+                        acc[f][t][4 * q] += v.x; acc[f][t][4 * q + 1] += v.y; acc[f][t][4 * q + 2] += v.z; acc[f][t][4 * q + 3] += v.w;
+                    }
+        }
+        meet<0>();
+    }
+    const bool ends = KH == 1 || kh == 0;                    // the waves that hold the result
     // accumulator i of lane l: feature 8 (i / 4) + 4 (l / 32) + i % 4 of its tile, row l % 32
     constexpr int NO = GATED ? NF / 2 : NF, PITCH = NO * 32 + 4, LPR = NO * 4;       // result tiles of a wave; floats of a row of its patch; lanes that store one
-    static_assert(NW * 32 * PITCH * 4 <= NS * STAGE && WF * BT * 4 <= STAGE && BT * 144 <= STAGE, "patches, magnitudes and codes fit");
-    float *patch = (float *)&stages[0][0] + wave * 32 * PITCH;
+    static_assert(NW * 32 * PITCH * 4 <= NS * STAGE && (BF < 256 || (WF * BT * 4 <= STAGE && BT * 144 <= STAGE)), "patches, magnitudes and codes fit");
+    float *patch = (float *)&stages[0][0] + wave % (WF * WT) * 32 * PITCH;
     // features c0.. of the accumulators of row tile t, through the wave's patch: whole rows leave together; `end` takes eight features of a row
     auto leave = [&](int t, int c0, auto end) {
 #pragma unroll
@@ -343,6 +376,7 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int NS> __glob
         }
     };
     if (a.part) {
+        if (!ends) return;
         const int64_t width = (int64_t)a.N * (GATED ? 2 : 1);
         float *p = a.part + (int64_t)slice * a.rows * width;
 #pragma unroll
@@ -360,6 +394,7 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int NS> __glob
         return;
     }
     if constexpr (!GATED) {
+        if (!ends) return;
 #pragma unroll
         for (int t = 0; t < NT; ++t) leave(t, 0, [&](int64_t m, int o, float *v) { finish8<T>(a, m, o, v); });
     } else {
@@ -373,6 +408,7 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int NS> __glob
                 for (int i = 0; i < 16; ++i) acc[g][t][i] *= acc[g + NG][t][i];
             }
         if (!a.yq) {
+            if (!ends) return;
 #pragma unroll
             for (int t = 0; t < NT; ++t)
                 leave(t, 0, [&](int64_t m, int o, const float *v) {
@@ -385,41 +421,42 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int NS> __glob
                 });
             return;
         }
-        // the largest magnitude of each row's block of 128: a lane's, the other half's, the other waves'
-        static_assert(BF == 256, "a tile holds a block of 128 features");
-        unsigned *most = (unsigned *)stages[0];                     // [WF][BT]
-        unsigned char *codes = stages[1];                           // [BT][128 + 16]
+        if constexpr (BF == 256) {                           // narrower tiles leave codes through the workspace
+            // the largest magnitude of each row's block of 128: a lane's, the other half's, the other waves'
+            unsigned *most = (unsigned *)stages[0];                     // [WF][BT]
+            unsigned char *codes = stages[1];                           // [BT][128 + 16]
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            unsigned m = 0;
+            for (int t = 0; t < NT; ++t) {
+                unsigned m = 0;
 #pragma unroll
-            for (int g = 0; g < NG; ++g)
+                for (int g = 0; g < NG; ++g)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) m = max(m, fw + g * 32 + 8 * (i / 4) + 4 * half < a.N ? magnitude(acc[g][t][i]) : 0u);     // a.N is a multiple of 16 here
-            m = max(m, (unsigned)__shfl_xor((int)m, 32));
-            if (half == 0) most[wf * BT + wt * (BT / WT) + t * 32 + r] = m;
-        }
-        __syncthreads();
+                    for (int i = 0; i < 16; ++i) m = max(m, fw + g * 32 + 8 * (i / 4) + 4 * half < a.N ? magnitude(acc[g][t][i]) : 0u);     // a.N is a multiple of 16 here
+                m = max(m, (unsigned)__shfl_xor((int)m, 32));
+                if (ends && half == 0) most[wf * BT + wt * (BT / WT) + t * 32 + r] = m;
+            }
+            __syncthreads();
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const int at = wt * (BT / WT) + t * 32 + r;
-            unsigned m = most[at];
+            for (int t = 0; t < NT; ++t) {
+                const int at = wt * (BT / WT) + t * 32 + r;
+                unsigned m = most[at];
 #pragma unroll
-            for (int w = 1; w < WF; ++w) m = max(m, most[w * BT + at]);
-            const float2 s = scale_of_block(m);
-            if (wf == 0 && half == 0 && r0 + at < a.r_hi) a.ys[(int64_t)ft0 * a.rows + r0 + at] = s.x;
+                for (int w = 1; w < WF; ++w) m = max(m, most[w * BT + at]);
+                const float2 s = scale_of_block(m);
+                if (ends && wf == 0 && half == 0 && r0 + at < a.r_hi) a.ys[(int64_t)ft0 * a.rows + r0 + at] = s.x;
 #pragma unroll
-            for (int g = 0; g < NG; ++g)
+                for (int g = 0; g < NG; ++g)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const unsigned c = to_codes(acc[g][t][4 * q], acc[g][t][4 * q + 1], acc[g][t][4 * q + 2], acc[g][t][4 * q + 3], s.y);
-                    *(unsigned *)(codes + at * 144 + wf * (128 / WF) + g * 32 + 8 * q + 4 * half) = s.y == 0.f ? 0u : c;
-                }
-        }
-        __syncthreads();
-        for (int e = tid; e < BT * 8; e += 64 * NW) {
-            const int m = r0 + e / 8, o = f0 + (e % 8) * 16;
-            if (m < a.r_hi && o < a.N) *(uint4 *)(a.yq + (int64_t)m * a.N + o) = *(const uint4 *)(codes + (e / 8) * 144 + (e % 8) * 16);
+                    for (int q = 0; q < 4; ++q) {
+                        const unsigned c = to_codes(acc[g][t][4 * q], acc[g][t][4 * q + 1], acc[g][t][4 * q + 2], acc[g][t][4 * q + 3], s.y);
+                        if (ends) *(unsigned *)(codes + at * 144 + wf * (128 / WF) + g * 32 + 8 * q + 4 * half) = s.y == 0.f ? 0u : c;
+                    }
+            }
+            __syncthreads();
+            for (int e = tid; e < BT * 8; e += 64 * NW) {
+                const int m = r0 + e / 8, o = f0 + (e % 8) * 16;
+                if (m < a.r_hi && o < a.N) *(uint4 *)(a.yq + (int64_t)m * a.N + o) = *(const uint4 *)(codes + (e / 8) * 144 + (e % 8) * 16);
+            }
         }
     }
 }
@@ -463,14 +500,22 @@ template <typename T, bool GATED> __global__ __launch_bounds__(256) void fp8_joi
     if (l == 0) a.ys[(int64_t)block * a.rows + row] = s.x;
 }
 
-template <typename T, bool GATED> static void launch_product(const Fp8Args &b, const Fp8Geom &g, int grid, int join, int phase, hipStream_t s)
+#define FP8_TILE(TILE, GATED, BF, BT, WF, WT, KH, NS) if (g.tile == TILE) { GACER_LAUNCH((fp8_tile_kernel<T, GATED, BF, BT, WF, WT, KH, NS>), dim3(grid), dim3(64 * WF * WT * KH), 0, s, b); }
+template <typename T> static void launch_gemm(const Fp8Args &b, const Fp8Geom &g, int grid, hipStream_t s)
 {
-    if (phase != 2) {
-        if (g.tile == FP8_FEW) GACER_LAUNCH((fp8_few_kernel<T, GATED>), dim3(grid), dim3(512), 0, s, b);
-        else if (g.tile == FP8_WIDE) GACER_LAUNCH((fp8_tile_kernel<T, GATED, 256, 128, 4, 2, 3>), dim3(grid), dim3(512), 0, s, b);
-    }
-    if (g.join && phase != 1) GACER_LAUNCH((fp8_join_kernel<T, GATED>), dim3(join), dim3(256), 0, s, b);
+    if (g.tile == FP8_FEW) GACER_LAUNCH((fp8_few_kernel<T>), dim3(grid), dim3(512), 0, s, b);
+    else FP8_TILE(FP8_64x32, false, 64, 32, 2, 1, 2, 6)
+    else FP8_TILE(FP8_64x64, false, 64, 64, 2, 2, 2, 4)
+    else FP8_TILE(FP8_128x128, false, 128, 128, 4, 2, 1, 3)
+    else FP8_TILE(FP8_256x128, false, 256, 128, 4, 2, 1, 3)
 }
+template <typename T> static void launch_gated(const Fp8Args &b, const Fp8Geom &g, int grid, hipStream_t s)
+{
+    FP8_TILE(FP8_256x32, true, 256, 32, 4, 1, 2, 4)
+    else FP8_TILE(FP8_256x64, true, 256, 64, 4, 2, 1, 3)
+    else FP8_TILE(FP8_256x128, true, 256, 128, 4, 2, 1, 3)
+}
+#undef FP8_TILE
 
 LaunchInfo launch_gemm_fp8(const TokenArgs &a, hipStream_t s, bool dry, int phase)
 {
@@ -490,8 +535,15 @@ LaunchInfo launch_gemm_fp8(const TokenArgs &a, hipStream_t s, bool dry, int phas
     li.threads = phase == 2 ? 256 : 512; li.lds_bytes = phase == 2 ? 0 : 8 * 16 * 65 * 4; li.wg_per_cu = phase == 2 ? 8 : 4; li.phases = g.join ? 2 : 1;
     li.kernel = phase == 2 ? "fp8_join" : gated ? "gated_fp8" : "gemm_fp8";
     if (dry || b.r_hi <= b.r_lo) return li;
-    if (a.dtype == DT_BF16) { if (gated) launch_product<unsigned short, true>(b, g, grid, join, phase, s); else launch_product<unsigned short, false>(b, g, grid, join, phase, s); }
-    else { if (gated) launch_product<float, true>(b, g, grid, join, phase, s); else launch_product<float, false>(b, g, grid, join, phase, s); }
+    const bool bf16 = a.dtype == DT_BF16;
+    if (phase != 2) {
+        if (gated) bf16 ? launch_gated<unsigned short>(b, g, grid, s) : launch_gated<float>(b, g, grid, s);
+        else bf16 ? launch_gemm<unsigned short>(b, g, grid, s) : launch_gemm<float>(b, g, grid, s);
+    }
+    if (g.join && phase != 1) {
+        if (bf16) { if (gated) GACER_LAUNCH((fp8_join_kernel<unsigned short, true>), dim3(join), dim3(256), 0, s, b); else GACER_LAUNCH((fp8_join_kernel<unsigned short, false>), dim3(join), dim3(256), 0, s, b); }
+        else { if (gated) GACER_LAUNCH((fp8_join_kernel<float, true>), dim3(join), dim3(256), 0, s, b); else GACER_LAUNCH((fp8_join_kernel<float, false>), dim3(join), dim3(256), 0, s, b); }
+    }
     return li;
 }
 

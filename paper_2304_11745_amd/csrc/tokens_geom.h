@@ -38,22 +38,45 @@ inline AttendGeom attend_geom(const TokenArgs &a)
     return g;
 }
 
-// Products of 8-bit rows, by the unsplit operator's shape: tiles of `features` of the result and `rows`, `slices` of the inner extent.
-enum Fp8Tile { FP8_FEW, FP8_WIDE };
+// Products of 8-bit rows, by the unsplit operator's shape (so that every decomposition adds in the same order): tiles of `features` of the result and
+// `rows`, `slices` parts of the inner extent that a second kernel joins.  The choice with the least estimated time is taken: rounds of workgroups over the units,
+// times blocks of 128 inner features in a slice, times what a block takes in this tile, and for a join its launch and its way through memory.
+enum Fp8Tile { FP8_FEW, FP8_64x32, FP8_64x64, FP8_128x128, FP8_256x128, FP8_256x64, FP8_256x32 };      // rows of weights (a gated block: half gate, half up) x rows
+enum { FP8_WS_MAX = 16 << 20 };                                                      // bytes of workspace, of the 32 MiB that all tenants share in gacer_run_static
 struct Fp8Geom { Fp8Tile tile; int features, rows, slices, blocks_per_slice; bool join; };
 inline Fp8Geom fp8_geom(const TokenArgs &a)
 {
-    Fp8Geom g;
     const bool gated = a.op == TK_GATED_FP8;
-    const int64_t rows = (int64_t)a.batch * a.S, blocks = (a.xq.features + FP8_BLOCK - 1) / FP8_BLOCK;
-    g.tile = rows > 64 && ((rows + 127) / 128) * ((a.features + (gated ? 127 : 255)) / (gated ? 128 : 256)) >= 64 ? FP8_WIDE : FP8_FEW;
-    g.features = (g.tile == FP8_WIDE ? 256 : 32) / (gated ? 2 : 1);
-    g.rows = g.tile == FP8_WIDE ? 128 : 32;
-    const int64_t tiles = ((rows + g.rows - 1) / g.rows) * ((a.features + g.features - 1) / g.features);
-    g.slices = g.tile == FP8_WIDE ? 1 : (int)std::min<int64_t>(std::max<int64_t>(1, 512 / tiles), std::max<int64_t>(1, blocks / 16));
-    g.blocks_per_slice = (int)((blocks + g.slices - 1) / g.slices);
+    const int64_t rows = (int64_t)a.batch * a.S, blocks = (a.xq.features + FP8_BLOCK - 1) / FP8_BLOCK, N = a.features;
+    struct Shape { Fp8Tile tile; int features, rows; double us; int held; };             // us a block; workgroups that a unit works on at a time
+    static const Shape gemm[] = {{FP8_FEW, 32, 32, 0.0, 1}, {FP8_64x32, 64, 32, 0.32, 2}, {FP8_64x64, 64, 64, 0.37, 2}, {FP8_128x128, 128, 128, 1.05, 1}, {FP8_256x128, 256, 128, 1.5, 1}};
+    static const Shape block[] = {{FP8_256x32, 128, 32, 0.85, 1}, {FP8_256x64, 128, 64, 1.15, 1}, {FP8_256x128, 128, 128, 1.6, 1}};
+    Fp8Geom g = {};
+    double least = 0.0;
+    for (int i = 0; i < (gated ? 3 : 5); ++i) {
+        const Shape &s = gated ? block[i] : gemm[i];
+        const int64_t tiles = ((N + s.features - 1) / s.features) * ((rows + s.rows - 1) / s.rows);
+        if (s.tile == FP8_FEW && rows > 32) continue;
+        for (int slices = 1; slices <= 8; slices *= 2) {
+            const int64_t per = (blocks + slices - 1) / slices, bytes = slices * rows * N * (gated ? 8 : 4);
+            if ((slices > 1 && (per < 8 || bytes > FP8_WS_MAX)) || (s.tile == FP8_FEW && tiles * slices > 256)) break;
+            double rounds = (double)(tiles * slices) / 256.0;
+            if (s.held == 1) rounds = (double)((tiles * slices + 255) / 256);
+            if (rounds < 1.0) rounds = 1.0;
+            const double us = s.tile == FP8_FEW ? (rows <= 8 ? 1.05 : rows <= 16 ? 1.45 : 1.85) * (double)((per + 7) / 8) : s.us * (double)per;
+            const double all = rounds * us + (slices > 1 ? 3.5 + (double)bytes / 2.5e6 : 0.0);
+            if (least == 0.0 || all < least) {
+                least = all;
+                g = {s.tile, s.features, s.rows, slices, (int)per, slices > 1};
+            }
+        }
+    }
+#ifdef FP8_FORCE
+    auto is = [&](Fp8Tile tile, int f, int r) { g.tile = tile; g.features = f; g.rows = r; };
+    FP8_FORCE
+    g.blocks_per_slice = (int)((blocks + g.slices - 1) / g.slices); g.join = g.slices > 1;
+#endif
     g.slices = (int)((blocks + g.blocks_per_slice - 1) / g.blocks_per_slice);
-    g.join = g.slices > 1 || (gated && a.yq.codes && g.tile == FP8_FEW);
     return g;
 }
 
