@@ -126,28 +126,33 @@ __device__ __forceinline__ i32x4 descriptor(const void *p, int64_t bytes)
     return d;
 }
 
-// The end of eight neighbouring features of a row (v); width: features of a row of y and res.
+// The end of eight neighbouring features of a row.
 template <typename T> __device__ __forceinline__ void finish8(const Fp8Args &a, int64_t row, int f, float *v)
 {
-    const int64_t at = row * a.N + f;
-    if (a.N % 8) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) if (f + e < a.N) finish<T>(a, row, f + e, v[e]);
-        return;
-    }
     if (f >= a.N) return;
+    const int64_t at = row * a.N + f;
+    const int n = a.N - f;
+    const bool whole = a.N % 8 == 0;
     if (a.bias) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += a.bias[f + e];
+        for (int e = 0; e < 8; ++e) v[e] += a.bias[f + min(e, n - 1)];
     }
     if (a.res) {
         float r[8];
-        load8((const T *)a.res + at, r);
+        if (whole) load8((const T *)a.res + at, r);
+        else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) r[e] = ld_f32((const T *)a.res, at + min(e, n - 1));
+        }
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] += r[e];
     }
     activate8_n<8>(v, a.act);
-    store8((T *)a.y + at, v);
+    if (whole) store8((T *)a.y + at, v);
+    else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) if (e < n) st_f32((T *)a.y, at + e, v[e]);
+    }
 }
 
 template <typename T, bool GATED, int BF, int BT, int WF, int WT, int KH, int NS> __global__ __launch_bounds__(64 * WF * WT * KH) void fp8_tile_kernel(Fp8Args a)
