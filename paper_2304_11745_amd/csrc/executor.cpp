@@ -455,7 +455,7 @@ static gacer_status check_fp8_op(Ctx *c, int ti, const gacer_tenant &t, int oi, 
         if (misaligned(weights[i].codes, 16) || misaligned(weights[i].scales, 4)) return inval("codes must be 16-byte aligned, scales as float");
         if (cout * x.features >= (1ll << 31)) return bad("weights of 2 GiB or more");
     }
-    if (misaligned(op.scale, 4) || misaligned(op.bias, 4)) return inval("misaligned parameter");
+    if (misaligned(op.scale, 16) || misaligned(op.bias, 16)) return inval("parameter pointer not 16-byte aligned");
     // what is written against what is read, and against each other
     struct Span { const void *p; int64_t n; };
     const int64_t esz = t.dtype == GACER_BF16 ? 2 : 4;

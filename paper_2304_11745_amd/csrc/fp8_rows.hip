@@ -16,82 +16,83 @@ struct NormArgs {
     int r_lo, r_hi;
 };
 
-// eight values from p on, of which `n` are there
-template <bool WHOLE> __device__ __forceinline__ void load8(const float *p, int n, float *v)
+// Eight features as they lie in memory, behind a row's end zeros.  WHOLE: rows of a multiple of eight features, aligned vectors; otherwise one by one.
+template <typename T, bool WHOLE> struct Run;
+template <> struct Run<unsigned short, true> {
+    uint4 v;
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t row, int f) { v = buf_load16(row, f * 2); }
+    __device__ __forceinline__ float get(int e) const
+    {
+        const unsigned w = e / 2 == 0 ? v.x : e / 2 == 1 ? v.y : e / 2 == 2 ? v.z : v.w;
+        return __uint_as_float(e % 2 ? w & 0xFFFF0000u : w << 16);
+    }
+};
+template <> struct Run<float, true> {
+    uint4 a, b;
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t row, int f) { a = buf_load16(row, f * 4); b = buf_load16(row, f * 4 + 16); }
+    __device__ __forceinline__ float get(int e) const { return __uint_as_float(e == 0 ? a.x : e == 1 ? a.y : e == 2 ? a.z : e == 3 ? a.w : e == 4 ? b.x : e == 5 ? b.y : e == 6 ? b.z : b.w); }
+};
+template <typename T> struct Run<T, false> {
+    T v[8];
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t row, int f)
+    {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = buf_load1<T>(row, (f + e) * (int)sizeof(T));
+    }
+    __device__ __forceinline__ float get(int e) const { return ld_f32(&v[e], 0); }
+};
+template <typename T, bool WHOLE> __device__ __forceinline__ void store(T *row, int f, int C, const float *v)
 {
     if constexpr (WHOLE) {
-        if (n >= 8) {
-            load8(p, v);
-            return;
-        }
-    }
+        if (f < C) store8(row + f, v);
+    } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = e < n ? p[e] : 0.f;
-}
-template <bool WHOLE> __device__ __forceinline__ void load8(const unsigned short *p, int n, float *v)
-{
-    if constexpr (WHOLE) {
-        if (n >= 8) {
-            load8(p, v);
-            return;
-        }
+        for (int e = 0; e < 8; ++e) if (f + e < C) st_f32(row, f + e, v[e]);
     }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = e < n ? ld_f32(p, e) : 0.f;
-}
-template <bool WHOLE> __device__ __forceinline__ void store8(float *p, int n, const float *v)
-{
-    if (WHOLE && n >= 8) {
-        store8(p, v);
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) if (e < n) p[e] = v[e];
-}
-template <bool WHOLE> __device__ __forceinline__ void store8(unsigned short *p, int n, const float *v)
-{
-    if (WHOLE && n >= 8) {
-        store8(p, v);
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) if (e < n) p[e] = to_bf16(v[e]);
 }
 
-// A row is held by LANES threads in registers, R runs of eight features each; 16 neighbouring lanes hold a block of 128.  WHOLE: rows of a
-// multiple of eight features, whose runs are aligned vectors.
+// A row is held by LANES threads in registers, R runs of eight features each; 16 neighbouring lanes hold a block of 128.  All loads of a row are issued, through
+// descriptors that answer zeros behind the row, before the first is converted: under a condition each would be waited for where it stands.
 template <typename T, int LANES, int R, bool WHOLE> __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rmsnorm_fp8_kernel(NormArgs a)
 {
     constexpr int THREADS = LANES < 256 ? 256 : LANES, PER = THREADS / LANES;
     __shared__ float sums[LANES > 64 ? LANES / 64 : 1];
     const int tid = threadIdx.x, lane = tid % LANES;
     for (int64_t row = a.r_lo + (int64_t)blockIdx.x * PER + tid / LANES; row < a.r_hi; row += (int64_t)gridDim.x * PER) {
-        const T *x = (const T *)a.x + row * a.C, *res = a.res ? (const T *)a.res + row * a.C : nullptr;
-        float h[R][8];
-        float sum = 0.f;
+        const __amdgpu_buffer_rsrc_t xr = make_rsrc((const T *)a.x + row * a.C, a.C * (int64_t)sizeof(T));
+        Run<T, WHOLE> x[R], r[R];
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            const int f = (i * LANES + lane) * 8;
-            load8<WHOLE>(x + f, a.C - f, h[i]);
+        for (int i = 0; i < R; ++i) x[i].load(xr, (i * LANES + lane) * 8);
+        if (a.res) {
+            const __amdgpu_buffer_rsrc_t rr = make_rsrc((const T *)a.res + row * a.C, a.C * (int64_t)sizeof(T));
+#pragma unroll
+            for (int i = 0; i < R; ++i) r[i].load(rr, (i * LANES + lane) * 8);
         }
-        if (res) {
+        float h[R][8];
 #pragma unroll
-            for (int i = 0; i < R; ++i) {
-                const int f = (i * LANES + lane) * 8;
-                float r[8];
-                load8<WHOLE>(res + f, a.C - f, r);
+        for (int i = 0; i < R; ++i)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) h[i][e] += r[e];
-            }
+            for (int e = 0; e < 8; ++e) h[i][e] = x[i].get(e);
+        if (a.res) {
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) h[i][e] += r[i].get(e);
         }
         if (a.codes && a.y) {
 #pragma unroll
-            for (int i = 0; i < R; ++i) {
-                const int f = (i * LANES + lane) * 8;
-                store8<WHOLE>((T *)a.y + row * a.C + f, a.C - f, h[i]);
-            }
+            for (int i = 0; i < R; ++i) store<T, WHOLE>((T *)a.y + row * a.C, (i * LANES + lane) * 8, a.C, h[i]);
         }
         if (a.norm) {
+            // gamma comes with the row, but for the widest rows, whose registers it would not fit
+            constexpr bool EARLY = R <= 4;
+            const __amdgpu_buffer_rsrc_t gr = make_rsrc(a.gamma, a.gamma ? a.C * 4 : 0);
+            Run<float, WHOLE> g[EARLY ? R : 1];
+            if (EARLY && a.gamma) {
+#pragma unroll
+                for (int i = 0; i < (EARLY ? R : 1); ++i) g[i].load(gr, (i * LANES + lane) * 8);
+            }
+            float sum = 0.f;
 #pragma unroll
             for (int i = 0; i < R; ++i)
 #pragma unroll
@@ -104,32 +105,27 @@ template <typename T, int LANES, int R, bool WHOLE> __global__ __launch_bounds__
                 sum = 0.f;
 #pragma unroll
                 for (int i = 0; i < LANES / 64; ++i) sum += sums[i];
-                __syncthreads();
+                if (gridDim.x * PER < a.r_hi - a.r_lo) __syncthreads();      // another row follows
             }
-            const float by = 1.f / sqrtf(sum * a.inv_c + a.eps);
+            const float by = rsqrtf(sum * a.inv_c + a.eps);
 #pragma unroll
             for (int i = 0; i < R; ++i) {
-                const int f = (i * LANES + lane) * 8;
-                float g[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
-                if (a.gamma) load8<false>(a.gamma + f, a.C - f, g);
+                if (!EARLY && a.gamma) g[0].load(gr, (i * LANES + lane) * 8);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) h[i][e] = h[i][e] * by * g[e];
+                for (int e = 0; e < 8; ++e) h[i][e] = h[i][e] * by * (a.gamma ? g[EARLY ? i : 0].get(e) : 1.f);
             }
         }
         if (!a.codes) {
 #pragma unroll
-            for (int i = 0; i < R; ++i) {
-                const int f = (i * LANES + lane) * 8;
-                store8<WHOLE>((T *)a.y + row * a.C + f, a.C - f, h[i]);
-            }
+            for (int i = 0; i < R; ++i) store<T, WHOLE>((T *)a.y + row * a.C, (i * LANES + lane) * 8, a.C, h[i]);
             continue;
         }
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
+        for (int i = 0; i < R; ++i) {                      // codes: rows of a multiple of 16 features
             const int f = (i * LANES + lane) * 8;
             unsigned most = 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) most = max(most, f + e < a.C ? magnitude(h[i][e]) : 0u);
+            for (int e = 0; e < 8; ++e) most = max(most, magnitude(h[i][e]));
 #pragma unroll
             for (int d = 1; d < 16; d *= 2) most = max(most, (unsigned)__shfl_xor((int)most, d));
             const float2 s = scale_of_block(most);
@@ -156,7 +152,11 @@ LaunchInfo launch_rmsnorm_fp8(const TokenArgs &a, hipStream_t s, bool dry)
     n.x = a.x; n.res = a.res; n.gamma = a.gamma; n.y = a.y; n.codes = a.yq.codes; n.scales = a.yq.scales;
     n.eps = a.eps; n.C = a.features; n.inv_c = 1.f / (float)a.features; n.norm = a.norm; n.rows = a.batch * a.S;
     n.r_lo = a.b_lo * a.S; n.r_hi = a.b_hi * a.S;
-    const int runs = (a.features + 7) / 8, lanes = runs <= 128 ? 64 : runs <= 2048 ? 256 : 1024;
+    const int runs = (a.features + 7) / 8;
+    int lanes = runs <= 128 ? 64 : runs <= 1024 ? 256 : 1024;
+#ifdef FP8_FORCE
+    if (const char *e = getenv("NORM_LANES")) lanes = atoi(e);
+#endif
     const int per = lanes == 64 ? 4 : 1, each = (runs + lanes - 1) / lanes;
     LaunchInfo li;
     li.workgroups = (int)std::min<int64_t>(((int64_t)(n.r_hi - n.r_lo) + per - 1) / per, 1 << 20);
@@ -164,7 +164,7 @@ LaunchInfo launch_rmsnorm_fp8(const TokenArgs &a, hipStream_t s, bool dry)
     li.kernel = a.dtype == DT_BF16 ? "rmsnorm_fp8_bf16" : "rmsnorm_fp8_f32";
     if (dry || !li.workgroups) return li;
 #define NORM(LANES, R) if (lanes == LANES && each > R / 2 && each <= R) { if (a.dtype == DT_BF16) norm<unsigned short, LANES, R>(n, li.workgroups, s); else norm<float, LANES, R>(n, li.workgroups, s); }
-    NORM(64, 1) NORM(64, 2) NORM(256, 1) NORM(256, 2) NORM(256, 4) NORM(256, 8) NORM(1024, 4) NORM(1024, 8)
+    NORM(64, 1) NORM(64, 2) NORM(256, 1) NORM(256, 2) NORM(256, 4) NORM(1024, 2) NORM(1024, 4) NORM(1024, 8)
 #undef NORM
     return li;
 }
