@@ -104,11 +104,12 @@ template <int N> __device__ __forceinline__ void meet()
     asm volatile("" ::: "memory");
 }
 
-// Loads of 16 or 4 bytes a lane from memory to LDS (from `to` on, in order of lanes), counted by vmcnt.  The compiler, which would wait for all of them before
-// it reads LDS, does not see them; they have no result in registers, and nothing else in these kernels uses m0.
-__device__ __forceinline__ void load_to_lds16(unsigned to, unsigned off, i32x4 from, int base)
+// Loads of 16 or 4 bytes a lane from memory (at off | also, plus `base`) to LDS (from `to` on, in order of lanes), counted by vmcnt.  The compiler, which would
+// wait for all of them before it reads LDS, does not see them; they have no result in registers, and nothing else in these kernels uses m0.
+__device__ __forceinline__ void load_to_lds16(unsigned to, unsigned off, unsigned also, i32x4 from, int base)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(off), "s"(from), "s"(base) : "memory");
+    unsigned at;
+    asm volatile("s_mov_b32 m0, %1\n\tv_or_b32 %0, %2, %3\n\tbuffer_load_dwordx4 %0, %4, %5 offen lds" : "=&v"(at) : "s"(to), "v"(off), "v"(also), "s"(from), "s"(base) : "memory");
 }
 __device__ __forceinline__ void load_to_lds4(unsigned to, unsigned off, i32x4 from, int base)
 {
@@ -160,7 +161,7 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int KH, int NS
     constexpr int NW = WF * WT * KH, GROUPS = 4 / KH, NF = BF / WF / 32, NT = BT / WT / 32, CODES = (BF + BT) * FP8_BLOCK, STAGE = CODES + NW * 256;
     constexpr int PW = BF / 8 / NW, PX = (BT / 8 + NW - 1) / NW;        // kilobytes of weights and rows that a wave moves for a block
     constexpr int REQUESTS = PW + PX + 1;
-    static_assert(PW * 8 * NW == BF && (PX * 8 * NW == BT || (PX == 1 && NW % (BT / 8) == 0)) && NW % 2 == 0 && NT <= 2 && (!GATED || (NF % 2 == 0 && PW % 2 == 0)), "");
+    static_assert((PX * 8 * NW == BT || (PX == 1 && NW % (BT / 8) == 0)) && NW % 2 == 0 && NT <= 2 && (!GATED || NF % 2 == 0), "");
     __shared__ __align__(1024) unsigned char stages[NS][STAGE];      // codes of weights, of rows; for each wave the scales of its rows
     constexpr int OF = GATED ? 2 : (BF + FP8_BLOCK - 1) / FP8_BLOCK;  // blocks of 128 features in a tile (gated: of gate and of up)
     __shared__ float wscale[OF][FP8_BLOCKS_MAX];                     // scales of the tile's weights
@@ -189,22 +190,24 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int KH, int NS
     const i32x4 xr = descriptor(a.x, (int64_t)a.rows * a.K), wr = descriptor(a.w, (int64_t)a.N * a.K), ur = GATED ? descriptor(a.w2, (int64_t)a.N * a.K) : wr;
     const i32x4 sr = descriptor(a.xs, (int64_t)a.rows * a.KB * 4);
     const int chunk = ((l & 7) ^ ((wave & 1) * 4 + (l >> 4))) * 16;      // pieces of a wave are an even number apart, so that row / 2 % 8 is the same in all
-    // a lane's row of piece 0, in bytes; rows behind the end repeat the last one, their results are not stored
-    const unsigned wrow0 = (unsigned)(f0 + wave * 8 + (l >> 3)) * a.K, xrow0 = (unsigned)(r0 + wave % (BT / 8) * 8 + (l >> 3)) * a.K;
-    const unsigned wlast = (unsigned)(a.N - 1) * a.K, xlast = (unsigned)(a.r_hi - 1) * a.K;
+    // a lane's place in each piece; rows behind the end repeat the last one, their results are not stored; more waves than pieces: several move the same one
+    constexpr int PF = GATED ? PW / 2 : PW;                  // pieces of gate, and as many of up
+    static_assert(PW * 8 * NW == BF && (!GATED || 2 * PF == PW), "whole pieces");
+    const int xwave = wave % (BT / 8);
+    unsigned woff[PF], xoff[PX];
+#pragma unroll
+    for (int q = 0; q < PF; ++q) woff[q] = (unsigned)min(f0 + (q * NW + wave) * 8 + (l >> 3), a.N - 1) * a.K + chunk;
+#pragma unroll
+    for (int q = 0; q < PX; ++q) xoff[q] = (unsigned)min(r0 + (q * NW + xwave) * 8 + (l >> 3), a.r_hi - 1) * a.K + chunk;
     const unsigned soff = min(r0 + wt * (BT / WT) + l % (NT * 32), a.r_hi - 1) * 4;
     const unsigned lds0 = (unsigned)(uintptr_t)GACER_LDS(&stages[0][0]);
     // piece p of block kb; behind the end zeros
     auto request = [&](int stage, int kb, int p) {
-        unsigned row0 = p < PW ? wrow0 : xrow0;
-        asm volatile("" : "+v"(row0));                       // offsets are formed where they are used, not kept for every piece
-        const unsigned in = kb >= hi || kb * FP8_BLOCK + chunk >= a.K ? OOB : (unsigned)chunk;
+        const unsigned bad = kb >= hi || kb * FP8_BLOCK + chunk >= a.K ? OOB : 0u;
         const int k = min(kb, a.KB - 1);
         const unsigned to = lds0 + stage * STAGE;
-        const int q = p < PW ? p % (GATED ? (PW + 1) / 2 : PW) : p - PW, xwave = wave % (BT / 8);       // where there are more waves than pieces, several move the same one
-        const unsigned row = min(row0 + (unsigned)(q * NW * 8) * a.K, p < PW ? wlast : xlast);
-        if (p < PW) load_to_lds16(to + (p * NW + wave) * 1024, row + in, GATED && p >= PW / 2 ? ur : wr, k * FP8_BLOCK);
-        else if (p < PW + PX) load_to_lds16(to + BF * FP8_BLOCK + (q * NW + xwave) * 1024, row + in, xr, k * FP8_BLOCK);
+        if (p < PW) load_to_lds16(to + (p * NW + wave) * 1024, woff[p % PF], bad, GATED && p >= PF ? ur : wr, k * FP8_BLOCK);
+        else if (p < PW + PX) load_to_lds16(to + BF * FP8_BLOCK + ((p - PW) * NW + xwave) * 1024, xoff[p - PW], bad, xr, k * FP8_BLOCK);
         else load_to_lds4(to + CODES + wave * 256, soff, sr, k * a.rows * 4);
     };
 #pragma unroll
