@@ -376,8 +376,9 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int KH, int NS
                 *(float4 *)(patch + r * PITCH + f * 32 + 8 * q + 4 * half) = make_float4(c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]);
             }
         const int m0 = r0 + wt * (BT / WT) + t * 32;
-#pragma unroll 1
-        for (int e = l; e < 32 * LPR; e += 64) {
+#pragma unroll
+        for (int i = 0; i < LPR / 2; ++i) {
+            const int e = i * 64 + l;
             float v[8];
             load8(patch + (e / LPR) * PITCH + (e % LPR) * 8, v);
             if (m0 + e / LPR < a.r_hi) end((int64_t)(m0 + e / LPR), fw + (e % LPR) * 8, v);
@@ -508,6 +509,20 @@ template <typename T, bool GATED> __global__ __launch_bounds__(256) void fp8_joi
     if (l == 0) a.ys[(int64_t)block * a.rows + row] = s.x;
 }
 
+// What a launch of each tile is: threads, LDS bytes, workgroups that a unit holds (by their LDS: with these stages one or two).
+struct TileInfo { Fp8Tile tile; const char *name[2]; int threads, lds, held; };
+static constexpr int tile_lds(bool gated, int bf, int bt, int waves, int stages) { return stages * ((bf + bt) * FP8_BLOCK + waves * 256) + (gated ? 2 : (bf + FP8_BLOCK - 1) / FP8_BLOCK) * FP8_BLOCKS_MAX * 4; }
+static const TileInfo GEMM_TILES[] = {
+    {FP8_FEW, {"gemm_fp8_few_f32", "gemm_fp8_few_bf16"}, 512, 8 * 16 * 65 * 4, 1},
+    {FP8_64x32, {"gemm_fp8_64x32_f32", "gemm_fp8_64x32_bf16"}, 256, tile_lds(false, 64, 32, 4, 6), 2},
+    {FP8_64x64, {"gemm_fp8_64x64_f32", "gemm_fp8_64x64_bf16"}, 512, tile_lds(false, 64, 64, 8, 4), 2},
+    {FP8_128x128, {"gemm_fp8_128x128_f32", "gemm_fp8_128x128_bf16"}, 512, tile_lds(false, 128, 128, 8, 3), 1},
+    {FP8_256x128, {"gemm_fp8_256x128_f32", "gemm_fp8_256x128_bf16"}, 512, tile_lds(false, 256, 128, 8, 3), 1}};
+static const TileInfo GATED_TILES[] = {
+    {FP8_256x32, {"gated_fp8_256x32_f32", "gated_fp8_256x32_bf16"}, 512, tile_lds(true, 256, 32, 8, 4), 1},
+    {FP8_256x64, {"gated_fp8_256x64_f32", "gated_fp8_256x64_bf16"}, 512, tile_lds(true, 256, 64, 8, 3), 1},
+    {FP8_256x128, {"gated_fp8_256x128_f32", "gated_fp8_256x128_bf16"}, 512, tile_lds(true, 256, 128, 8, 3), 1}};
+
 #define FP8_TILE(TILE, GATED, BF, BT, WF, WT, KH, NS) if (g.tile == TILE) { GACER_LAUNCH((fp8_tile_kernel<T, GATED, BF, BT, WF, WT, KH, NS>), dim3(grid), dim3(64 * WF * WT * KH), 0, s, b); }
 template <typename T> static void launch_gemm(const Fp8Args &b, const Fp8Geom &g, int grid, hipStream_t s)
 {
@@ -538,12 +553,19 @@ LaunchInfo launch_gemm_fp8(const TokenArgs &a, hipStream_t s, bool dry, int phas
     const int grid = b.f_tiles * b.r_tiles * b.slices;
     const int64_t units = (int64_t)(b.r_hi - b.r_lo) * ((b.N + FP8_BLOCK - 1) / FP8_BLOCK);
     const int join = (int)((units + 3) / 4);
-    LaunchInfo li;
-    li.workgroups = phase == 2 ? join : grid;
-    li.threads = phase == 2 ? 256 : 512; li.lds_bytes = phase == 2 ? 0 : 8 * 16 * 65 * 4; li.wg_per_cu = phase == 2 ? 8 : 4; li.phases = g.join ? 2 : 1;
-    li.kernel = phase == 2 ? "fp8_join" : gated ? "gated_fp8" : "gemm_fp8";
-    if (dry || b.r_hi <= b.r_lo) return li;
     const bool bf16 = a.dtype == DT_BF16;
+    const TileInfo *t = gated ? GATED_TILES : GEMM_TILES;
+    while (t->tile != g.tile) ++t;
+    LaunchInfo li;
+    li.phases = g.join ? 2 : 1;
+    if (phase == 2) {
+        li.workgroups = join; li.threads = 256; li.lds_bytes = 0; li.wg_per_cu = 8;
+        li.kernel = bf16 ? "fp8_join_bf16" : "fp8_join_f32";
+    } else {
+        li.workgroups = grid; li.threads = t->threads; li.lds_bytes = t->lds; li.wg_per_cu = t->held;
+        li.kernel = t->name[bf16];
+    }
+    if (dry || b.r_hi <= b.r_lo) return li;
     if (phase != 2) {
         if (gated) bf16 ? launch_gated<unsigned short>(b, g, grid, s) : launch_gated<float>(b, g, grid, s);
         else bf16 ? launch_gemm<unsigned short>(b, g, grid, s) : launch_gemm<float>(b, g, grid, s);

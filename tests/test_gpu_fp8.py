@@ -183,6 +183,99 @@ def test_gated(dtype, codes, batch, tokens, cin, cout):
         assert ((out.cpu().double().view(n, cout) - want).abs() <= err + HALF[dtype] * (want.abs() + err)).all()
 
 
+# sizes that take the other tiles and the inner extent in slices (tests/test_host_fp8_dispatch.py sees that none is left out)
+WIDE_GEMMS = [(1, 1, 400, 70), (1, 17, 3088, 70), (3, 11, 3088, 71), (1, 1500, 4112, 70), (2, 1025, 144, 300), (3, 1000, 144, 1001), (4, 128, 14336, 4096), (50, 41, 144, 2068), (13, 5, 9616, 5520),
+              (7, 31, 6416, 2050)]
+WIDE_GATED = [(1, 1, 2000, 80), (2, 1500, 144, 304), (3, 1000, 144, 704), (5, 410, 4112, 80), (50, 41, 4112, 144), (3, 16, 5120, 2064)]
+
+
+def wide(g, rows, width, spread):
+    """8-bit operands made on the GPU: (float8 codes, scales, float64 values); blocks of rows (spread None) or of 128 by 128."""
+    codes = (torch.randn(rows, width, generator=g, device="cuda") * 60).clamp(-448, 448).to(torch.float8_e4m3fn)
+    if spread is None:
+        scales = (0.2 + torch.rand(R.blocks(width), rows, generator=g, device="cuda")) / 60
+        return codes, scales, codes.double() * scales.double().t().repeat_interleave(R.BLOCK, 1)[:, :width]
+    scales = (0.5 + torch.rand(R.blocks(rows), R.blocks(width), generator=g, device="cuda")) * spread / 60
+    return codes, scales, codes.double() * scales.double().repeat_interleave(R.BLOCK, 0)[:rows].repeat_interleave(R.BLOCK, 1)[:, :width]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("batch,tokens,cin,cout", WIDE_GEMMS)
+def test_gemm_in_every_tile(dtype, batch, tokens, cin, cout):
+    from paper_2304_11745_amd import tokens as T
+    g = torch.Generator(device="cuda").manual_seed(cin + cout)
+    n = batch * tokens
+    xc, xs, x = wide(g, n, cin, None)
+    wc, wsc, w = wide(g, cout, cin, cin ** -0.5)
+    bias, res = torch.randn(cout, generator=g, device="cuda"), torch.randn(batch, tokens, cout, generator=g, device="cuda").to(DT[dtype])
+    out = torch.full((batch, tokens, cout), 7.0, dtype=DT[dtype], device="cuda")
+    run(lambda o: o.gemm_fp8(T.Fp8Rows(xc.view(batch, tokens, cin), xs), T.Fp8Weight(wc, wsc), out, bias=bias, act="silu", res=res), dtype, batch)
+    y, e = R.product(x, w)
+    y, e = y + bias.double() + res.view(n, cout).double(), e + 2.0 ** -22 * (y.abs() + 8)
+    want = R.act(y, "silu")
+    assert ((out.double().view(n, cout) - want).abs() <= 1.5 * e + (HALF[dtype] + 2.0 ** -18) * (want.abs() + 1.5 * e)).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("codes", [True, False])
+@pytest.mark.parametrize("batch,tokens,cin,cout", WIDE_GATED)
+def test_gated_in_every_tile(dtype, codes, batch, tokens, cin, cout):
+    from paper_2304_11745_amd import tokens as T
+    g = torch.Generator(device="cuda").manual_seed(cin + cout)
+    n = batch * tokens
+    xc, xs, x = wide(g, n, cin, None)
+    (gc, gs, gv), (uc, us, uv) = wide(g, cout, cin, cin ** -0.5), wide(g, cout, cin, cin ** -0.5)
+    out = empty_rows(batch, tokens, cout) if codes else torch.full((batch, tokens, cout), 7.0, dtype=DT[dtype], device="cuda")
+    run(lambda o: o.gated_fp8(T.Fp8Rows(xc.view(batch, tokens, cin), xs), T.Fp8Weight(gc, gs), T.Fp8Weight(uc, us), out, act="gelu"), dtype, batch)
+    (a, ea), (b, eb) = R.product(x, gv), R.product(x, uv)
+    f = R.act(a, "gelu")
+    ea = 1.5 * ea + 2.0 ** -18 * (f.abs() + 1.5 * ea)
+    want = f * b
+    err = f.abs() * eb + b.abs() * ea + ea * eb
+    err = err + 2.0 ** -23 * (want.abs() + err)
+    if codes:
+        R.check_rows(out.codes.cpu().view(n, cout), out.scales.cpu(), want.cpu(), err.cpu())
+    else:
+        assert ((out.double().view(n, cout) - want).abs() <= err + HALF[dtype] * (want.abs() + err)).all()
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("tokens,cin,cout", [(1, 3088, 144), (1, 400, 70), (13, 3088, 144), (300, 4112, 144), (200, 144, 1008), (410, 144, 2064)])
+def test_plans_give_the_bits_of_the_whole(gated, tokens, cin, cout):
+    """Every tile, whole and in slices, with the batch cut unevenly, also over two streams."""
+    from paper_2304_11745_amd import binding as B
+    from paper_2304_11745_amd import tokens as T
+    g = torch.Generator(device="cuda").manual_seed(cin + tokens)
+    batch = 5
+    cout = -(-cout // 16) * 16 if gated else cout
+    xc, xs, _ = wide(g, batch * tokens, cin, None)
+    ws = [wide(g, cout, cin, cin ** -0.5)[:2] for _ in range(2)]
+    rows, out = T.Fp8Rows(xc.view(batch, tokens, cin), xs), empty_rows(batch, tokens, cout) if gated else torch.empty(batch, tokens, cout, dtype=torch.bfloat16, device="cuda")
+    ops = T.OpList(torch.bfloat16, batch)
+    if gated:
+        ops.gated_fp8(rows, T.Fp8Weight(*ws[0]), T.Fp8Weight(*ws[1]), out)
+    else:
+        ops.gemm_fp8(rows, T.Fp8Weight(*ws[0]), out)
+    state = [out.codes, out.scales] if gated else [out]
+    stream, sibling = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    s = T.TokenSession([ops], [stream])
+    d = (B.gacer_tenant * 1)(ops.descriptor(stream.cuda_stream))
+    d[0].sibling_stream = sibling.cuda_stream
+    B.check(s.ctx, B.gacer_load_tenants(s.ctx, d, 1))
+    s.run(B.GACER_MODE_SEQUENTIAL)
+    want = snapshot(state)
+    for sizes in ([2, 3], [1, 1, 1, 1, 1], [4, 1]):
+        for side in (0, 1):
+            arr = (C.c_int * len(sizes))(*sizes)
+            sp = (B.gacer_split * 1)(B.gacer_split(0, 0, B.GACER_AXIS_BATCH, len(sizes), arr, side))
+            B.check(s.ctx, B.gacer_set_plan(s.ctx, C.byref(B.gacer_plan(1, sp, 0, None))))
+            scrub(state)
+            s.run(B.GACER_MODE_PLAN)
+            assert same(snapshot(state), want), (sizes, side)
+    s.close()
+
+
 @pytest.mark.parametrize("tokens", [1, 40, 300])
 def test_a_row_or_block_that_is_no_number_stays_alone(tokens):
     """NaN scales of one row's block and of one weight block reach that row and those features, and nothing beside them."""
