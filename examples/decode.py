@@ -5,7 +5,10 @@ that takes a token of every sequence, and the head that turns hidden states into
 decoded with gacer_enqueue, step after step without waiting; then a decoding step and a ResNet-18 run in the same rounds, unsplit and with the
 batch of every operator cut in two.
 
-    python examples/decode.py [--steps 32] [--batch 6] [--dtype bf16]
+    python examples/decode.py [--steps 32] [--batch 6] [--dtype bf16] [--weights fp8]
+
+With --weights fp8 the projections and the feed-forward block hold 8-bit weights and read 8-bit rows: RMS norms with the residual's addition leave the rows, a
+gated block takes the place of the two products around an activation.
 """
 import argparse
 import os
@@ -22,7 +25,8 @@ from paper_2304_11745_amd import harness, tokens as T  # noqa: E402
 class Decoder:
     """Two lists over shared weights and caches: a pre-norm decoder of `layers` layers with `heads` query and `kv` key/value heads."""
 
-    def __init__(self, dtype=torch.bfloat16, batch=6, layers=2, heads=8, kv=2, dim=64, ffn=1024, vocab=8000, longest=160, page=32, seed=1):
+    def __init__(self, dtype=torch.bfloat16, batch=6, layers=2, heads=8, kv=2, dim=64, ffn=1024, vocab=8000, longest=160, page=32, seed=1, fp8=False):
+        self.fp8 = fp8
         self.dtype, self.batch, self.layers, self.heads, self.kv, self.dim, self.ffn, self.vocab = dtype, batch, layers, heads, kv, dim, ffn, vocab
         self.gen = torch.Generator(device="cuda").manual_seed(seed)
         width = self.width = heads * dim
@@ -30,6 +34,11 @@ class Decoder:
         self.layer = [dict(n1=self.norm(), n2=self.norm(), qkv=self.normal((heads + 2 * kv) * dim, width, scale=width ** -0.5), gq=torch.ones(dim, device="cuda"),
                            gk=torch.ones(dim, device="cuda"), o=self.normal(width, width, scale=width ** -0.5), up=self.normal(ffn, width, scale=width ** -0.5),
                            down=self.normal(width, ffn, scale=ffn ** -0.5)) for _ in range(layers)]
+        if fp8:
+            for p in self.layer:
+                p["gate"] = self.normal(ffn, width, scale=width ** -0.5)
+                for name in ("qkv", "o", "gate", "up", "down"):
+                    p[name] = T.Fp8Weight.quantise(p[name])
         self.last, self.out = self.norm(), self.normal(vocab, width, scale=3 * width ** -0.5)
         angle = torch.arange(longest, device="cuda", dtype=torch.float64)[:, None] * 10000.0 ** (-torch.arange(dim // 2, device="cuda", dtype=torch.float64) * 2 / dim)
         self.table = torch.stack((angle.cos(), angle.sin()), -1).float().contiguous()
@@ -53,6 +62,8 @@ class Decoder:
         x = first = self.empty(tokens, self.width)
         positions = torch.zeros(self.batch, tokens, 1, dtype=torch.int32, device="cuda")
         heads = dict(heads=self.heads, kv_heads=self.kv, head_dim=self.dim)
+        if self.fp8:
+            return ops, first, positions, self.body_fp8(ops, x, tokens, count, positions, heads)
         for p, cache in zip(self.layer, self.caches):
             h, qkv, ctx, y = self.empty(tokens, self.width), self.empty(tokens, (self.heads + 2 * self.kv) * self.dim), self.empty(tokens, self.width), self.empty(tokens, self.width)
             ops.layernorm(x, *p["n1"], h)
@@ -68,10 +79,32 @@ class Decoder:
             x = z
         return ops, first, positions, x
 
+    def body_fp8(self, ops, x, tokens, count, positions, heads):
+        """The layers with 8-bit rows and weights: every product reads the rows that the operator before it left."""
+        for p, cache in zip(self.layer, self.caches):
+            rows, qkv, ctx = T.Fp8Rows.allocate(self.batch, tokens, self.width), self.empty(tokens, (self.heads + 2 * self.kv) * self.dim), self.empty(tokens, self.width)
+            ops.rmsnorm_fp8(x, rows, p["n1"][0])
+            ops.gemm_fp8(rows, p["qkv"], qkv)
+            ops.qknorm_rope(qkv, qkv, positions, self.table, gamma_q=p["gq"], gamma_k=p["gk"], **heads)
+            ops.cache_write(qkv, cache, self.start, count, **heads)
+            ops.cache_attention(qkv, ctx, cache, self.start, count, **heads)
+            rows, y = T.Fp8Rows.allocate(self.batch, tokens, self.width), self.empty(tokens, self.width)
+            ops.quantise_fp8(ctx, rows)
+            ops.gemm_fp8(rows, p["o"], y)
+            rows, inner, h, z = T.Fp8Rows.allocate(self.batch, tokens, self.width), T.Fp8Rows.allocate(self.batch, tokens, self.ffn), self.empty(tokens, self.width), self.empty(tokens, self.width)
+            ops.rmsnorm_fp8(y, rows, p["n2"][0], res=x, sum=h)
+            ops.gated_fp8(rows, p["gate"], p["up"], inner)
+            ops.gemm_fp8(inner, p["down"], z, res=h)
+            x = z
+        return x
+
     def head(self, ops, x, token, u, **filters):
         """Final norm, logits and sampling of hidden states [batch, 1, width] at the end of a list."""
         h, logits = self.empty(1, self.width), self.empty(1, self.vocab)
-        ops.layernorm(x, *self.last, h)
+        if self.fp8:
+            ops.rmsnorm(x, self.last[0], h)
+        else:
+            ops.layernorm(x, *self.last, h)
         ops.gemm(h, self.out, logits)
         ops.sample(logits, token, u, **filters)
         return logits
@@ -134,7 +167,8 @@ if __name__ == "__main__":
     ap.add_argument("--steps", type=int, default=32)
     ap.add_argument("--batch", type=int, default=6)
     ap.add_argument("--dtype", choices=("bf16", "f32"), default="bf16")
+    ap.add_argument("--weights", choices=("full", "fp8"), default="full")
     a = ap.parse_args()
-    said, _ = serve(torch.bfloat16 if a.dtype == "bf16" else torch.float32, a.batch, a.steps)
+    said, _ = serve(torch.bfloat16 if a.dtype == "bf16" else torch.float32, a.batch, a.steps, fp8=a.weights == "fp8")
     for row in said.tolist():
         print(" ".join(map(str, row[:12])), "..." if len(row) > 12 else "")

@@ -509,6 +509,39 @@ def test_weights_are_quantised_to_the_nearest_codes():
     assert q.values().shape == w.shape
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_the_example_decodes_with_8_bit_weights(dtype):
+    """examples/decode.py --weights fp8: the last step's hidden states lie where a list that takes the same tokens as one prompt puts them.  A step's rows go through
+    other tiles than a prompt's, so that values next to a line between two codes may fall on either side: a step of e4m3 is 2^-3 of a value, of the 4-bit cache a
+    fifteenth of a group's range, and each is one of hundreds of addends of a hidden feature; a tenth of the largest is far beyond what they add up to."""
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import decode
+    from paper_2304_11745_amd import tokens as T
+    steps, batch = 5, 3
+    said, logits = decode.serve(DT[dtype], batch, steps, vision=True, fp8=True)
+    assert ((said >= 0) & (said < 8000)).all() and torch.isfinite(logits).all()
+    again, same_logits = decode.serve(DT[dtype], batch, steps, vision=False, fp8=True)
+    assert torch.equal(said, again) and torch.equal(logits, same_logits)
+    d = decode.Decoder(DT[dtype], batch, fp8=True)              # the same weights, by their seed
+    lengths = [1 + (7 * i) % 40 for i in range(batch)]
+    prompts = torch.randint(0, d.vocab, (batch, 40), generator=d.gen, device="cuda")
+    count = torch.tensor([n + steps for n in lengths], dtype=torch.int32, device="cuda")
+    ops, x, at, out = d.body(40 + steps, count)
+    s = T.TokenSession([ops])
+    ids = torch.zeros(batch, 40 + steps, dtype=torch.long, device="cuda")
+    for b, n in enumerate(lengths):
+        ids[b, :n], ids[b, n:n + steps] = prompts[b, :n], said[b, :steps].long()
+    x.copy_(d.embedding[ids])
+    at.copy_(torch.arange(40 + steps, device="cuda", dtype=torch.int32)[None, :, None].expand_as(at))
+    s.enqueue()
+    last = out[torch.arange(batch, device="cuda"), count.long() - 1].float()
+    want = (last * (last * last).mean(-1, keepdim=True).add(1e-6).rsqrt()) @ d.out.float().t()
+    assert (logits[:, 0].float() - want).abs().max() <= 0.1 * want.abs().max()
+    s.close()
+
+
 def test_operator_lists_refuse_what_they_can_see():
     from paper_2304_11745_amd import binding as B
     from paper_2304_11745_amd import tokens as T
