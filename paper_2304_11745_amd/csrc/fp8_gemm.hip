@@ -156,7 +156,7 @@ template <typename T> __device__ __forceinline__ void finish8(const Fp8Args &a, 
     }
 }
 
-template <typename T, bool GATED, int BF, int BT, int WF, int WT, int KH, int NS> __global__ __launch_bounds__(64 * WF * WT * KH) void fp8_tile_kernel(Fp8Args a)
+template <typename T, bool GATED, int BF, int BT, int WF, int WT, int KH, int NS, bool TURNS> __global__ __launch_bounds__(64 * WF * WT * KH) void fp8_tile_kernel(Fp8Args a)
 {
     constexpr int NW = WF * WT * KH, GROUPS = 4 / KH, NF = BF / WF / 32, NT = BT / WT / 32, CODES = (BF + BT) * FP8_BLOCK, STAGE = CODES + NW * 256;
     constexpr int PW = BF / 8 / NW, PX = (BT / 8 + NW - 1) / NW;        // kilobytes of weights and rows that a wave moves for a block
@@ -167,7 +167,7 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int KH, int NS
     __shared__ float wscale[OF][FP8_BLOCKS_MAX];                     // scales of the tile's weights
     const int tid = threadIdx.x, l = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = l & 31, half = l >> 5;
     const int wf = wave % WF, wt = wave / WF % WT, kh = wave / (WF * WT);
-    constexpr bool TURNS = NW == 8 && KH == 1;               // see the loop
+    static_assert(!TURNS || (NW == 8 && KH == 1 && NS == 3), "see the loop");
     const int late = TURNS && wave >= 4 ? 1 : 0;
 
     // tile: each of the eight dies takes a run of them, in which four neighbouring feature tiles follow each other
@@ -516,27 +516,27 @@ static const TileInfo GEMM_TILES[] = {
     {FP8_FEW, {"gemm_fp8_few_f32", "gemm_fp8_few_bf16"}, 512, 8 * 16 * 65 * 4, 1},
     {FP8_64x32, {"gemm_fp8_64x32_f32", "gemm_fp8_64x32_bf16"}, 256, tile_lds(false, 64, 32, 4, 6), 2},
     {FP8_64x64, {"gemm_fp8_64x64_f32", "gemm_fp8_64x64_bf16"}, 512, tile_lds(false, 64, 64, 8, 4), 2},
-    {FP8_128x128, {"gemm_fp8_128x128_f32", "gemm_fp8_128x128_bf16"}, 512, tile_lds(false, 128, 128, 8, 3), 1},
+    {FP8_128x128, {"gemm_fp8_128x128_f32", "gemm_fp8_128x128_bf16"}, 512, tile_lds(false, 128, 128, 8, 4), 1},
     {FP8_256x128, {"gemm_fp8_256x128_f32", "gemm_fp8_256x128_bf16"}, 512, tile_lds(false, 256, 128, 8, 3), 1}};
 static const TileInfo GATED_TILES[] = {
     {FP8_256x32, {"gated_fp8_256x32_f32", "gated_fp8_256x32_bf16"}, 512, tile_lds(true, 256, 32, 8, 4), 1},
     {FP8_256x64, {"gated_fp8_256x64_f32", "gated_fp8_256x64_bf16"}, 512, tile_lds(true, 256, 64, 8, 3), 1},
     {FP8_256x128, {"gated_fp8_256x128_f32", "gated_fp8_256x128_bf16"}, 512, tile_lds(true, 256, 128, 8, 3), 1}};
 
-#define FP8_TILE(TILE, GATED, BF, BT, WF, WT, KH, NS) if (g.tile == TILE) { GACER_LAUNCH((fp8_tile_kernel<T, GATED, BF, BT, WF, WT, KH, NS>), dim3(grid), dim3(64 * WF * WT * KH), 0, s, b); }
+#define FP8_TILE(TILE, GATED, BF, BT, WF, WT, KH, NS, TURNS) if (g.tile == TILE) { GACER_LAUNCH((fp8_tile_kernel<T, GATED, BF, BT, WF, WT, KH, NS, TURNS>), dim3(grid), dim3(64 * WF * WT * KH), 0, s, b); }
 template <typename T> static void launch_gemm(const Fp8Args &b, const Fp8Geom &g, int grid, hipStream_t s)
 {
     if (g.tile == FP8_FEW) GACER_LAUNCH((fp8_few_kernel<T>), dim3(grid), dim3(512), 0, s, b);
-    else FP8_TILE(FP8_64x32, false, 64, 32, 2, 1, 2, 6)
-    else FP8_TILE(FP8_64x64, false, 64, 64, 2, 2, 2, 4)
-    else FP8_TILE(FP8_128x128, false, 128, 128, 4, 2, 1, 3)
-    else FP8_TILE(FP8_256x128, false, 256, 128, 4, 2, 1, 3)
+    else FP8_TILE(FP8_64x32, false, 64, 32, 2, 1, 2, 6, false)
+    else FP8_TILE(FP8_64x64, false, 64, 64, 2, 2, 2, 4, false)
+    else FP8_TILE(FP8_128x128, false, 128, 128, 4, 2, 1, 4, false)
+    else FP8_TILE(FP8_256x128, false, 256, 128, 4, 2, 1, 3, true)
 }
 template <typename T> static void launch_gated(const Fp8Args &b, const Fp8Geom &g, int grid, hipStream_t s)
 {
-    FP8_TILE(FP8_256x32, true, 256, 32, 4, 1, 2, 4)
-    else FP8_TILE(FP8_256x64, true, 256, 64, 4, 2, 1, 3)
-    else FP8_TILE(FP8_256x128, true, 256, 128, 4, 2, 1, 3)
+    FP8_TILE(FP8_256x32, true, 256, 32, 4, 1, 2, 4, false)
+    else FP8_TILE(FP8_256x64, true, 256, 64, 4, 2, 1, 3, false)
+    else FP8_TILE(FP8_256x128, true, 256, 128, 4, 2, 1, 3, true)
 }
 #undef FP8_TILE
 

@@ -49,8 +49,8 @@ inline Fp8Geom fp8_geom(const TokenArgs &a)
     const bool gated = a.op == TK_GATED_FP8;
     const int64_t rows = (int64_t)a.batch * a.S, blocks = (a.xq.features + FP8_BLOCK - 1) / FP8_BLOCK, N = a.features;
     struct Shape { Fp8Tile tile; int features, rows; double us; int held; };             // us a block; workgroups that a unit works on at a time
-    static const Shape gemm[] = {{FP8_FEW, 32, 32, 0.0, 1}, {FP8_64x32, 64, 32, 0.32, 2}, {FP8_64x64, 64, 64, 0.37, 2}, {FP8_128x128, 128, 128, 1.05, 1}, {FP8_256x128, 256, 128, 1.5, 1}};
-    static const Shape block[] = {{FP8_256x32, 128, 32, 0.85, 1}, {FP8_256x64, 128, 64, 1.15, 1}, {FP8_256x128, 128, 128, 1.6, 1}};
+    static const Shape gemm[] = {{FP8_FEW, 32, 32, 0.0, 1}, {FP8_64x32, 64, 32, 0.32, 2}, {FP8_64x64, 64, 64, 0.37, 2}, {FP8_128x128, 128, 128, 0.95, 1}, {FP8_256x128, 256, 128, 1.5, 1}};
+    static const Shape block[] = {{FP8_256x32, 128, 32, 0.85, 1}, {FP8_256x64, 128, 64, 1.05, 1}, {FP8_256x128, 128, 128, 1.6, 1}};
     Fp8Geom g = {};
     double least = 0.0;
     for (int i = 0; i < (gated ? 3 : 5); ++i) {
