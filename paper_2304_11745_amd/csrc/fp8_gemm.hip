@@ -127,33 +127,39 @@ __device__ __forceinline__ i32x4 descriptor(const void *p, int64_t bytes)
     return d;
 }
 
-// The end of eight neighbouring features of a row.
-template <typename T> __device__ __forceinline__ void finish8(const Fp8Args &a, int64_t row, int f, float *v)
+// Eight values on their way out: neighbouring features of a row, or, where rows are no multiple of eight features, of neighbouring rows, so that neighbouring
+// lanes store neighbouring features.
+struct Eight {
+    int64_t at;                                              // of the first, in elements of the result
+    int step, n;                                             // to the next; how many are there
+};
+template <typename T> __device__ __forceinline__ void store_eight(T *to, const Eight &p, const float *v)
 {
-    if (f >= a.N) return;
-    const int64_t at = row * a.N + f;
-    const int n = a.N - f;
-    const bool whole = a.N % 8 == 0;
+    if (p.step == 1) store8(to + p.at, v);
+    else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) if (e < p.n) st_f32(to, p.at + (int64_t)e * p.step, v[e]);
+    }
+}
+// The end of a product: bias, residual, activation, one rounding.  f: the first value's feature.
+template <typename T> __device__ __forceinline__ void finish_eight(const Fp8Args &a, const Eight &p, int f, float *v)
+{
     if (a.bias) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += a.bias[f + min(e, n - 1)];
+        for (int e = 0; e < 8; ++e) v[e] += a.bias[p.step == 1 ? f + e : f];
     }
     if (a.res) {
         float r[8];
-        if (whole) load8((const T *)a.res + at, r);
+        if (p.step == 1) load8((const T *)a.res + p.at, r);
         else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) r[e] = ld_f32((const T *)a.res, at + min(e, n - 1));
+            for (int e = 0; e < 8; ++e) r[e] = ld_f32((const T *)a.res, p.at + (int64_t)min(e, p.n - 1) * p.step);
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] += r[e];
     }
     activate8_n<8>(v, a.act);
-    if (whole) store8((T *)a.y + at, v);
-    else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) if (e < n) st_f32((T *)a.y, at + e, v[e]);
-    }
+    store_eight((T *)a.y, p, v);
 }
 
 template <typename T, bool GATED, int BF, int BT, int WF, int WT, int KH, int NS, bool TURNS> __global__ __launch_bounds__(64 * WF * WT * KH) void fp8_tile_kernel(Fp8Args a)
@@ -366,8 +372,9 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int KH, int NS
     constexpr int NO = GATED ? NF / 2 : NF, PITCH = NO * 32 + 4, LPR = NO * 4;       // result tiles of a wave; floats of a row of its patch; lanes that store one
     static_assert(NW * 32 * PITCH * 4 <= NS * STAGE && (BF < 256 || (WF * BT * 4 <= STAGE && BT * 144 <= STAGE)), "patches, magnitudes and codes fit");
     float *patch = (float *)&stages[0][0] + wave % (WF * WT) * 32 * PITCH;
-    // features c0.. of the accumulators of row tile t, through the wave's patch: whole rows leave together; `end` takes eight features of a row
-    auto leave = [&](int t, int c0, auto end) {
+    // features c0.. of the accumulators of row tile t, through the wave's patch: whole rows leave together, in rows of `width`; `end` takes eight values
+    const bool whole = a.N % 8 == 0;
+    auto leave = [&](int t, int c0, int width, auto end) {
 #pragma unroll
         for (int f = 0; f < NO; ++f)
 #pragma unroll
@@ -380,32 +387,32 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int KH, int NS
         for (int i = 0; i < LPR / 2; ++i) {
             const int e = i * 64 + l;
             float v[8];
-            load8(patch + (e / LPR) * PITCH + (e % LPR) * 8, v);
-            if (m0 + e / LPR < a.r_hi) end((int64_t)(m0 + e / LPR), fw + (e % LPR) * 8, v);
+            if (whole) {
+                const int m = m0 + e / LPR, o = fw + e % LPR * 8;
+                load8(patch + e / LPR * PITCH + e % LPR * 8, v);
+                if (m < a.r_hi && o < a.N) end(Eight{(int64_t)m * width + o, 1, 8}, o, v);
+            } else {
+                const int m = m0 + e / (NO * 32) * 8, o = fw + e % (NO * 32);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = patch[(e / (NO * 32) * 8 + k) * PITCH + e % (NO * 32)];
+                if (m < a.r_hi && o < a.N) end(Eight{(int64_t)m * width + o, width, a.r_hi - m}, o, v);
+            }
         }
     };
     if (a.part) {
         if (!ends) return;
-        const int64_t width = (int64_t)a.N * (GATED ? 2 : 1);
+        const int width = a.N * (GATED ? 2 : 1);
         float *p = a.part + (int64_t)slice * a.rows * width;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int c = 0; c < NF / NO; ++c)
-                leave(t, c * NO, [&](int64_t m, int o, const float *v) {
-                    float *to = p + m * width + c * a.N + o;
-                    if (a.N % 4 == 0 && o + 8 <= a.N) { store4(to, v); store4(to + 4, v + 4); }
-                    else {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) if (o + e < a.N) to[e] = v[e];
-                    }
-                });
+            for (int c = 0; c < NF / NO; ++c) leave(t, c * NO, width, [&](const Eight &e, int, const float *v) { store_eight(p + c * a.N, e, v); });
         return;
     }
     if constexpr (!GATED) {
         if (!ends) return;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) leave(t, 0, [&](int64_t m, int o, float *v) { finish8<T>(a, m, o, v); });
+        for (int t = 0; t < NT; ++t) leave(t, 0, a.N, [&](const Eight &e, int o, float *v) { finish_eight<T>(a, e, o, v); });
     } else {
         constexpr int NG = NF / 2;
 #pragma unroll
@@ -419,15 +426,7 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int KH, int NS
         if (!a.yq) {
             if (!ends) return;
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-                leave(t, 0, [&](int64_t m, int o, const float *v) {
-                    T *y = (T *)a.y + m * a.N + o;
-                    if (a.N % 8 == 0) { if (o < a.N) store8(y, v); }
-                    else {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) if (o + e < a.N) st_f32(y, e, v[e]);
-                    }
-                });
+            for (int t = 0; t < NT; ++t) leave(t, 0, a.N, [&](const Eight &e, int, const float *v) { store_eight((T *)a.y, e, v); });
             return;
         }
         if constexpr (BF == 256) {                           // narrower tiles leave codes through the workspace
