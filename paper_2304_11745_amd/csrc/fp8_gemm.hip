@@ -115,7 +115,8 @@ __device__ __forceinline__ void load_to_lds4(unsigned to, unsigned off, i32x4 fr
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(to), "v"(off), "s"(from), "s"(base) : "memory");
 }
-// A buffer's descriptor in scalar registers, as the instructions take it.
+// A buffer's descriptor in scalar registers, as the instructions take it: five states after the vector unit wrote them, which the compiler, not seeing the loads,
+// does not see to.
 __device__ __forceinline__ i32x4 descriptor(const void *p, int64_t bytes)
 {
     const uint64_t u = (uint64_t)p;
@@ -124,6 +125,7 @@ __device__ __forceinline__ i32x4 descriptor(const void *p, int64_t bytes)
     d.y = __builtin_amdgcn_readfirstlane((int)(unsigned)(u >> 32));
     d.z = __builtin_amdgcn_readfirstlane((int)(bytes > 0x7FFFFFFF ? 0x7FFFFFFF : bytes));
     d.w = 0x00020000;
+    asm volatile("s_nop 4" : "+s"(d));
     return d;
 }
 
@@ -415,6 +417,7 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int KH, int NS
         for (int t = 0; t < NT; ++t) leave(t, 0, a.N, [&](const Eight &e, int o, float *v) { finish_eight<T>(a, e, o, v); });
     } else {
         constexpr int NG = NF / 2;
+        static_assert(BF == 256, "a tile holds whole blocks of the result");
 #pragma unroll
         for (int g = 0; g < NG; ++g)
 #pragma unroll
@@ -429,83 +432,104 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int KH, int NS
             for (int t = 0; t < NT; ++t) leave(t, 0, a.N, [&](const Eight &e, int, const float *v) { store_eight((T *)a.y, e, v); });
             return;
         }
-        if constexpr (BF == 256) {                           // narrower tiles leave codes through the workspace
-            // the largest magnitude of each row's block of 128: a lane's, the other half's, the other waves'
-            unsigned *most = (unsigned *)stages[0];                     // [WF][BT]
-            unsigned char *codes = stages[1];                           // [BT][128 + 16]
+        // the largest magnitude of each row's block of 128: a lane's, the other half's, the other waves'
+        unsigned *most = (unsigned *)stages[0];                     // [WF][BT]
+        unsigned char *codes = stages[1];                           // [BT][128 + 16]
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                unsigned m = 0;
+        for (int t = 0; t < NT; ++t) {
+            unsigned m = 0;
 #pragma unroll
-                for (int g = 0; g < NG; ++g)
+            for (int g = 0; g < NG; ++g)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) m = max(m, fw + g * 32 + 8 * (i / 4) + 4 * half < a.N ? magnitude(acc[g][t][i]) : 0u);     // a.N is a multiple of 16 here
-                m = max(m, (unsigned)__shfl_xor((int)m, 32));
-                if (ends && half == 0) most[wf * BT + wt * (BT / WT) + t * 32 + r] = m;
-            }
-            __syncthreads();
+                for (int i = 0; i < 16; ++i) m = max(m, fw + g * 32 + 8 * (i / 4) + 4 * half < a.N ? magnitude(acc[g][t][i]) : 0u);     // a.N is a multiple of 16 here
+            m = max(m, (unsigned)__shfl_xor((int)m, 32));
+            if (ends && half == 0) most[wf * BT + wt * (BT / WT) + t * 32 + r] = m;
+        }
+        __syncthreads();
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const int at = wt * (BT / WT) + t * 32 + r;
-                unsigned m = most[at];
+        for (int t = 0; t < NT; ++t) {
+            const int at = wt * (BT / WT) + t * 32 + r;
+            unsigned m = most[at];
 #pragma unroll
-                for (int w = 1; w < WF; ++w) m = max(m, most[w * BT + at]);
-                const float2 s = scale_of_block(m);
-                if (ends && wf == 0 && half == 0 && r0 + at < a.r_hi) a.ys[(int64_t)ft0 * a.rows + r0 + at] = s.x;
+            for (int w = 1; w < WF; ++w) m = max(m, most[w * BT + at]);
+            const float2 s = scale_of_block(m);
+            if (ends && wf == 0 && half == 0 && r0 + at < a.r_hi) a.ys[(int64_t)ft0 * a.rows + r0 + at] = s.x;
 #pragma unroll
-                for (int g = 0; g < NG; ++g)
+            for (int g = 0; g < NG; ++g)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const unsigned c = to_codes(acc[g][t][4 * q], acc[g][t][4 * q + 1], acc[g][t][4 * q + 2], acc[g][t][4 * q + 3], s.y);
-                        if (ends) *(unsigned *)(codes + at * 144 + wf * (128 / WF) + g * 32 + 8 * q + 4 * half) = s.y == 0.f ? 0u : c;
-                    }
-            }
-            __syncthreads();
-            for (int e = tid; e < BT * 8; e += 64 * NW) {
-                const int m = r0 + e / 8, o = f0 + (e % 8) * 16;
-                if (m < a.r_hi && o < a.N) *(uint4 *)(a.yq + (int64_t)m * a.N + o) = *(const uint4 *)(codes + (e / 8) * 144 + (e % 8) * 16);
-            }
+                for (int q = 0; q < 4; ++q) {
+                    const unsigned c = to_codes(acc[g][t][4 * q], acc[g][t][4 * q + 1], acc[g][t][4 * q + 2], acc[g][t][4 * q + 3], s.y);
+                    if (ends) *(unsigned *)(codes + at * 144 + wf * (128 / WF) + g * 32 + 8 * q + 4 * half) = s.y == 0.f ? 0u : c;
+                }
+        }
+        __syncthreads();
+        for (int e = tid; e < BT * 8; e += 64 * NW) {
+            const int m = r0 + e / 8, o = f0 + (e % 8) * 16;
+            if (m < a.r_hi && o < a.N) *(uint4 *)(a.yq + (int64_t)m * a.N + o) = *(const uint4 *)(codes + (e / 8) * 144 + (e % 8) * 16);
         }
     }
 }
 
-// Adds the slices in order and ends the product: a wave per row and block of 128 features, two neighbouring features a lane.
-template <typename T, bool GATED> __global__ __launch_bounds__(256) void fp8_join_kernel(Fp8Args a)
+// Adds the slices in order and ends the product: a wave per row and block of 128 features, two neighbouring features a lane.  All slices are requested before the
+// first is added; those that fill up SLICES repeat the last one and add nothing.
+template <typename T, bool GATED, int SLICES> __global__ __launch_bounds__(256) void fp8_join_kernel(Fp8Args a)
 {
     const int l = threadIdx.x & 63, blocks = (a.N + FP8_BLOCK - 1) / FP8_BLOCK;
-    const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), row = a.r_lo + id / blocks;
+    const int id = blockIdx.x * 4 + (threadIdx.x >> 6), row = a.r_lo + id / blocks;
     if (row >= a.r_hi) return;
-    const int block = (int)(id % blocks), f = block * FP8_BLOCK + 2 * l;
-    const int64_t width = (int64_t)a.N * (GATED ? 2 : 1), step = a.rows * width;
-    float v[2] = {0.f, 0.f}, u[2] = {0.f, 0.f};
+    const int block = id % blocks, f = block * FP8_BLOCK + 2 * l, width = a.N * (GATED ? 2 : 1);
+    const int64_t step = (int64_t)a.rows * width;
+    const float *p = a.part + (int64_t)row * width + min(f, a.N - 1);
+    const bool pair = a.N % 2 == 0;                        // then both features are there, or neither
+    float2 g[SLICES], h[GATED ? SLICES : 1];
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        if (f + e >= a.N) continue;
-        const float *p = a.part + row * width + f + e;
-        for (int i = 0; i < a.slices; ++i) {
-            v[e] += p[i * step];
-            if (GATED) u[e] += p[i * step + a.N];
+    for (int i = 0; i < SLICES; ++i) {
+        const float *q = p + min(i, a.slices - 1) * step;
+        if (pair) {
+            g[i] = *(const float2 *)(f < a.N ? q : a.part);
+            if constexpr (GATED) h[i] = *(const float2 *)(f < a.N ? q + a.N : a.part);
+        } else {
+            g[i] = make_float2(q[0], q[f + 1 < a.N ? 1 : 0]);
+            if constexpr (GATED) h[i] = make_float2(q[a.N], q[a.N + (f + 1 < a.N ? 1 : 0)]);
         }
     }
-    if (!GATED) {
+    float v[2] = {0.f, 0.f}, u[2] = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < SLICES; ++i) {
+        const bool on = i < a.slices;
+        v[0] += on ? g[i].x : 0.f;
+        v[1] += on ? g[i].y : 0.f;
+        if constexpr (GATED) {
+            u[0] += on ? h[i].x : 0.f;
+            u[1] += on ? h[i].y : 0.f;
+        }
+    }
+    if constexpr (!GATED) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) if (f + e < a.N) finish<T>(a, row, f + e, v[e]);
-        return;
+    } else {
+        activate8_n<2>(v, a.act);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) v[e] *= u[e];
+        if (!a.yq) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) if (f + e < a.N) st_f32((T *)a.y, (int64_t)row * a.N + f + e, v[e]);
+            return;
+        }
+        unsigned most = f < a.N ? max(magnitude(v[0]), magnitude(v[1])) : 0u;      // a.N is a multiple of 16 here
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) most = max(most, (unsigned)__shfl_xor((int)most, d));
+        const float2 s = scale_of_block(most);
+        const unsigned c = s.y == 0.f ? 0u : to_codes(v[0], v[1], 0.f, 0.f, s.y);
+        if (f < a.N) *(unsigned short *)(a.yq + (int64_t)row * a.N + f) = (unsigned short)c;
+        if (l == 0) a.ys[(int64_t)block * a.rows + row] = s.x;
     }
-#pragma unroll
-    for (int e = 0; e < 2; ++e) v[e] = activate8(v[e], a.act) * u[e];
-    if (!a.yq) {
-#pragma unroll
-        for (int e = 0; e < 2; ++e) if (f + e < a.N) st_f32((T *)a.y, row * a.N + f + e, v[e]);
-        return;
-    }
-    unsigned most = max(f < a.N ? magnitude(v[0]) : 0u, f + 1 < a.N ? magnitude(v[1]) : 0u);
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) most = max(most, (unsigned)__shfl_xor((int)most, d));
-    const float2 s = scale_of_block(most);
-    const unsigned c = s.y == 0.f ? 0u : to_codes(v[0], v[1], 0.f, 0.f, s.y);
-    if (f < a.N) *(unsigned short *)(a.yq + row * a.N + f) = (unsigned short)c;      // a.N is even here
-    if (l == 0) a.ys[(int64_t)block * a.rows + row] = s.x;
+}
+template <typename T, bool GATED> static void launch_join(const Fp8Args &b, int grid, hipStream_t s)
+{
+    if (b.slices <= 2) GACER_LAUNCH((fp8_join_kernel<T, GATED, 2>), dim3(grid), dim3(256), 0, s, b);
+    else if (b.slices <= 4) GACER_LAUNCH((fp8_join_kernel<T, GATED, 4>), dim3(grid), dim3(256), 0, s, b);
+    else GACER_LAUNCH((fp8_join_kernel<T, GATED, 8>), dim3(grid), dim3(256), 0, s, b);
 }
 
 // What a launch of each tile is: threads, LDS bytes, workgroups that a unit holds (by their LDS: with these stages one or two).
@@ -545,7 +569,7 @@ LaunchInfo launch_gemm_fp8(const TokenArgs &a, hipStream_t s, bool dry, int phas
     const bool gated = a.op == TK_GATED_FP8;
     Fp8Args b;
     b.x = a.xq.codes; b.xs = a.xq.scales; b.w = a.w.codes; b.ws = a.w.scales; b.w2 = a.w2.codes; b.ws2 = a.w2.scales;
-    b.bias = a.bias; b.res = a.res; b.y = a.y; b.yq = a.yq.codes; b.ys = a.yq.scales; b.part = g.join ? a.ws : nullptr;
+    b.bias = a.bias; b.res = a.res; b.y = a.y; b.yq = a.yq.codes; b.ys = a.yq.scales; b.part = g.slices > 1 ? a.ws : nullptr;
     b.K = a.xq.features; b.KB = (b.K + FP8_BLOCK - 1) / FP8_BLOCK; b.N = a.features; b.rows = a.batch * a.S; b.act = a.act;
     b.r_lo = a.b_lo * a.S; b.r_hi = a.b_hi * a.S;
     b.f_tiles = (b.N + g.features - 1) / g.features; b.r_tiles = (b.r_hi - b.r_lo + g.rows - 1) / g.rows; b.slices = g.slices; b.per_slice = g.blocks_per_slice;
@@ -556,7 +580,7 @@ LaunchInfo launch_gemm_fp8(const TokenArgs &a, hipStream_t s, bool dry, int phas
     const TileInfo *t = gated ? GATED_TILES : GEMM_TILES;
     while (t->tile != g.tile) ++t;
     LaunchInfo li;
-    li.phases = g.join ? 2 : 1;
+    li.phases = g.slices > 1 ? 2 : 1;
     if (phase == 2) {
         li.workgroups = join; li.threads = 256; li.lds_bytes = 0; li.wg_per_cu = 8;
         li.kernel = bf16 ? "fp8_join_bf16" : "fp8_join_f32";
@@ -569,9 +593,9 @@ LaunchInfo launch_gemm_fp8(const TokenArgs &a, hipStream_t s, bool dry, int phas
         if (gated) bf16 ? launch_gated<unsigned short>(b, g, grid, s) : launch_gated<float>(b, g, grid, s);
         else bf16 ? launch_gemm<unsigned short>(b, g, grid, s) : launch_gemm<float>(b, g, grid, s);
     }
-    if (g.join && phase != 1) {
-        if (bf16) { if (gated) GACER_LAUNCH((fp8_join_kernel<unsigned short, true>), dim3(join), dim3(256), 0, s, b); else GACER_LAUNCH((fp8_join_kernel<unsigned short, false>), dim3(join), dim3(256), 0, s, b); }
-        else { if (gated) GACER_LAUNCH((fp8_join_kernel<float, true>), dim3(join), dim3(256), 0, s, b); else GACER_LAUNCH((fp8_join_kernel<float, false>), dim3(join), dim3(256), 0, s, b); }
+    if (g.slices > 1 && phase != 1) {
+        if (gated) bf16 ? launch_join<unsigned short, true>(b, join, s) : launch_join<float, true>(b, join, s);
+        else bf16 ? launch_join<unsigned short, false>(b, join, s) : launch_join<float, false>(b, join, s);
     }
     return li;
 }

@@ -43,7 +43,7 @@ inline AttendGeom attend_geom(const TokenArgs &a)
 // times blocks of 128 inner features in a slice, times what a block takes in this tile, and for a join its launch and its way through memory.
 enum Fp8Tile { FP8_FEW, FP8_64x32, FP8_64x64, FP8_128x128, FP8_256x128, FP8_256x64, FP8_256x32 };      // rows of weights (a gated block: half gate, half up) x rows
 enum { FP8_WS_MAX = 16 << 20 };                                                      // bytes of workspace, of the 32 MiB that all tenants share in gacer_run_static
-struct Fp8Geom { Fp8Tile tile; int features, rows, slices, blocks_per_slice; bool join; };
+struct Fp8Geom { Fp8Tile tile; int features, rows, slices, blocks_per_slice; };
 inline Fp8Geom fp8_geom(const TokenArgs &a)
 {
     const bool gated = a.op == TK_GATED_FP8;
@@ -67,16 +67,10 @@ inline Fp8Geom fp8_geom(const TokenArgs &a)
             const double all = rounds * us + (slices > 1 ? 3.5 + (double)bytes / 2.5e6 : 0.0);
             if (least == 0.0 || all < least) {
                 least = all;
-                g = {s.tile, s.features, s.rows, slices, (int)per, slices > 1};
+                g = {s.tile, s.features, s.rows, slices, (int)per};
             }
         }
     }
-#ifdef FP8_FORCE
-    auto is = [&](Fp8Tile tile, int f, int r) { g.tile = tile; g.features = f; g.rows = r; };
-    FP8_FORCE
-    g.blocks_per_slice = (int)((blocks + g.slices - 1) / g.slices); g.join = g.slices > 1;
-#endif
-    g.slices = (int)((blocks + g.blocks_per_slice - 1) / g.blocks_per_slice);
     return g;
 }
 
@@ -89,7 +83,7 @@ inline size_t token_ws_floats(const TokenArgs &a)
     }
     if (a.op == TK_GEMM_FP8 || a.op == TK_GATED_FP8) {
         const Fp8Geom g = fp8_geom(a);
-        if (g.join) return (size_t)g.slices * a.batch * a.S * a.features * (a.op == TK_GATED_FP8 ? 2 : 1);
+        if (g.slices > 1) return (size_t)g.slices * a.batch * a.S * a.features * (a.op == TK_GATED_FP8 ? 2 : 1);
     }
     return 0;
 }

@@ -40,13 +40,13 @@ int main(int argc, char **argv)
         const std::string type = dtype == DT_F32 ? "f" : "t";
         for (int gated : {0, 1})
             for (int rows : {1, 20, 40, 64, 128, 300, 512, 1024, 4096})
-                for (int cin : {128, 1024, 14336})
-                    for (int cout : {512, 4096, 14336}) {
+                for (int cin : {128, 1024, 3088, 8208, 14336})
+                    for (int cout : {80, 512, 4096, 14336}) {
                         const TokenArgs a = product(gated, rows, cin, cout, gated, dtype);
                         const Fp8Geom g = fp8_geom(a);
                         const std::string name = g.tile == FP8_FEW ? "fp8_few_kernelI" + type + "E" : "fp8_tile_kernelI" + type + "Lb" + std::to_string(gated) + "E" + tiles[g.tile];
                         tell(name, launch_gemm_fp8(a, nullptr, true, 1));
-                        if (g.join) tell("fp8_join_kernelI" + type + "Lb" + std::to_string(gated) + "E", launch_gemm_fp8(a, nullptr, true, 2));
+                        if (g.slices > 1) tell("fp8_join_kernelI" + type + "Lb" + std::to_string(gated) + "ELi" + std::to_string(g.slices <= 2 ? 2 : g.slices <= 4 ? 4 : 8) + "E", launch_gemm_fp8(a, nullptr, true, 2));
                     }
         for (int runs : {128, 129, 1024, 1025, 2048, 4096, 8192, 1, 64, 65, 256, 257, 512})
             for (int odd : {0, 1}) {
