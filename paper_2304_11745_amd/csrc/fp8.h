@@ -83,6 +83,7 @@ struct Fp8Args {
     float *ys, *part;
     int K, KB, N, rows, r_lo, r_hi, act;     // KB: blocks of K; rows: of the whole operator; r_lo..r_hi: of this launch
     int f_tiles, r_tiles, slices, per_slice; // tiles of this launch; slices of K of per_slice blocks
+    int whole;                               // tiles that are not done in halves
 };
 
 }  // namespace gacer

@@ -164,32 +164,19 @@ template <typename T> __device__ __forceinline__ void finish_eight(const Fp8Args
     store_eight((T *)a.y, p, v);
 }
 
-template <typename T, bool GATED, int BF, int BT, int WF, int WT, int KH, int NS, bool TURNS> __global__ __launch_bounds__(64 * WF * WT * KH) void fp8_tile_kernel(Fp8Args a)
+static constexpr int tile_stage(int bf, int bt, int waves) { return (bf + bt) * FP8_BLOCK + waves * 256; }      // codes of weights, of rows; for each wave the scales of its rows
+template <typename T, bool GATED, int BF, int BT, int WF, int WT, int KH, int NS, bool TURNS> __device__ __forceinline__ void fp8_tile(const Fp8Args &a, unsigned char *lds, float (*wscale)[FP8_BLOCKS_MAX], int slice, int ft0, int rt0)
 {
-    constexpr int NW = WF * WT * KH, GROUPS = 4 / KH, NF = BF / WF / 32, NT = BT / WT / 32, CODES = (BF + BT) * FP8_BLOCK, STAGE = CODES + NW * 256;
+    constexpr int NW = WF * WT * KH, GROUPS = 4 / KH, NF = BF / WF / 32, NT = BT / WT / 32, CODES = (BF + BT) * FP8_BLOCK, STAGE = tile_stage(BF, BT, NW);
     constexpr int PW = BF / 8 / NW, PX = (BT / 8 + NW - 1) / NW;        // kilobytes of weights and rows that a wave moves for a block
     constexpr int REQUESTS = PW + PX + 1;
     static_assert((PX * 8 * NW == BT || (PX == 1 && NW % (BT / 8) == 0)) && NW % 2 == 0 && NT <= 2 && (!GATED || NF % 2 == 0), "");
-    __shared__ __align__(1024) unsigned char stages[NS][STAGE];      // codes of weights, of rows; for each wave the scales of its rows
+    unsigned char (*stages)[STAGE] = (unsigned char (*)[STAGE])lds;
     constexpr int OF = GATED ? 2 : (BF + FP8_BLOCK - 1) / FP8_BLOCK;  // blocks of 128 features in a tile (gated: of gate and of up)
-    __shared__ float wscale[OF][FP8_BLOCKS_MAX];                     // scales of the tile's weights
     const int tid = threadIdx.x, l = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = l & 31, half = l >> 5;
     const int wf = wave % WF, wt = wave / WF % WT, kh = wave / (WF * WT);
     static_assert(!TURNS || (NW == 8 && KH == 1 && NS == 3), "see the loop");
     const int late = TURNS && wave >= 4 ? 1 : 0;
-
-    // tile: each of the eight dies takes a run of them, in which four neighbouring feature tiles follow each other
-    int id = blockIdx.x;
-    const int slice = id % a.slices; id /= a.slices;
-    {
-        const int all = a.f_tiles * a.r_tiles, per = all / 8, more = all % 8, die = id % 8;
-        id = die * per + min(die, more) + id / 8;
-    }
-    int ft0, rt0;
-    {
-        const int group = id / (4 * a.r_tiles), in = id - group * 4 * a.r_tiles, wide = min(4, a.f_tiles - group * 4);
-        ft0 = group * 4 + in % wide; rt0 = in / wide;
-    }
     constexpr int FT = GATED ? BF / 2 : BF;                  // features of the result per tile
     const int f0 = ft0 * FT, r0 = a.r_lo + rt0 * BT;
     const int lo = slice * a.per_slice, hi = min(lo + a.per_slice, a.KB);
@@ -470,6 +457,31 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int KH, int NS
     }
 }
 
+// Tiles in the order of workgroups: each of the eight dies takes a run of them, in which four neighbouring feature tiles follow each other.  TAIL: those behind
+// a.whole, a last round that would leave half of the units or more without work, are done in halves of their rows by as many workgroups; results are the same.
+template <typename T, bool GATED, int BF, int BT, int WF, int WT, int KH, int NS, bool TURNS, bool TAIL> __global__ __launch_bounds__(64 * WF * WT * KH) void fp8_tile_kernel(Fp8Args a)
+{
+    __shared__ __align__(1024) unsigned char lds[NS * tile_stage(BF, BT, WF * WT * KH)];
+    __shared__ float wscale[GATED ? 2 : (BF + FP8_BLOCK - 1) / FP8_BLOCK][FP8_BLOCKS_MAX];      // scales of the tile's weights
+    int id = blockIdx.x;
+    const int slice = id % a.slices; id /= a.slices;
+    const int part = TAIL && id >= a.whole ? 1 + (id - a.whole) % 2 : 0;
+    if (part) id = a.whole + (id - a.whole) / 2;
+    else {
+        const int per = a.whole / 8, more = a.whole % 8, die = id % 8;
+        id = die * per + min(die, more) + id / 8;
+    }
+    const int group = id / (4 * a.r_tiles), in = id - group * 4 * a.r_tiles, wide = min(4, a.f_tiles - group * 4);
+    const int ft = group * 4 + in % wide, rt = in / wide;
+    if constexpr (TAIL) {
+        if (part) {
+            if (a.r_lo + rt * BT + (part - 1) * (BT / 2) < a.r_hi) fp8_tile<T, GATED, BF, BT / 2, WF, WT, KH, NS, false>(a, lds, wscale, slice, ft, 2 * rt + part - 1);
+            return;
+        }
+    }
+    fp8_tile<T, GATED, BF, BT, WF, WT, KH, NS, TURNS>(a, lds, wscale, slice, ft, rt);
+}
+
 // Adds the slices in order and ends the product: a wave per row and block of 128 features, two neighbouring features a lane.  All slices are requested before the
 // first is added; those that fill up SLICES repeat the last one and add nothing.
 template <typename T, bool GATED, int SLICES> __global__ __launch_bounds__(256) void fp8_join_kernel(Fp8Args a)
@@ -534,7 +546,7 @@ template <typename T, bool GATED> static void launch_join(const Fp8Args &b, int 
 
 // What a launch of each tile is: threads, LDS bytes, workgroups that a unit holds (by their LDS: with these stages one or two).
 struct TileInfo { Fp8Tile tile; const char *name[2]; int threads, lds, held; };
-static constexpr int tile_lds(bool gated, int bf, int bt, int waves, int stages) { return stages * ((bf + bt) * FP8_BLOCK + waves * 256) + (gated ? 2 : (bf + FP8_BLOCK - 1) / FP8_BLOCK) * FP8_BLOCKS_MAX * 4; }
+static constexpr int tile_lds(bool gated, int bf, int bt, int waves, int stages) { return stages * tile_stage(bf, bt, waves) + (gated ? 2 : (bf + FP8_BLOCK - 1) / FP8_BLOCK) * FP8_BLOCKS_MAX * 4; }
 static const TileInfo GEMM_TILES[] = {
     {FP8_FEW, {"gemm_fp8_few_f32", "gemm_fp8_few_bf16"}, 512, 8 * 16 * 65 * 4, 1},
     {FP8_64x32, {"gemm_fp8_64x32_f32", "gemm_fp8_64x32_bf16"}, 256, tile_lds(false, 64, 32, 4, 6), 2},
@@ -546,20 +558,20 @@ static const TileInfo GATED_TILES[] = {
     {FP8_256x64, {"gated_fp8_256x64_f32", "gated_fp8_256x64_bf16"}, 512, tile_lds(true, 256, 64, 8, 3), 1},
     {FP8_256x128, {"gated_fp8_256x128_f32", "gated_fp8_256x128_bf16"}, 512, tile_lds(true, 256, 128, 8, 3), 1}};
 
-#define FP8_TILE(TILE, GATED, BF, BT, WF, WT, KH, NS, TURNS) if (g.tile == TILE) { GACER_LAUNCH((fp8_tile_kernel<T, GATED, BF, BT, WF, WT, KH, NS, TURNS>), dim3(grid), dim3(64 * WF * WT * KH), 0, s, b); }
+#define FP8_TILE(TILE, GATED, BF, BT, WF, WT, KH, NS, TURNS, TAIL) if (g.tile == TILE) { GACER_LAUNCH((fp8_tile_kernel<T, GATED, BF, BT, WF, WT, KH, NS, TURNS, TAIL>), dim3(grid), dim3(64 * WF * WT * KH), 0, s, b); }
 template <typename T> static void launch_gemm(const Fp8Args &b, const Fp8Geom &g, int grid, hipStream_t s)
 {
     if (g.tile == FP8_FEW) GACER_LAUNCH((fp8_few_kernel<T>), dim3(grid), dim3(512), 0, s, b);
-    else FP8_TILE(FP8_64x32, false, 64, 32, 2, 1, 2, 6, false)
-    else FP8_TILE(FP8_64x64, false, 64, 64, 2, 2, 2, 4, false)
-    else FP8_TILE(FP8_128x128, false, 128, 128, 4, 2, 1, 4, false)
-    else FP8_TILE(FP8_256x128, false, 256, 128, 4, 2, 1, 3, true)
+    else FP8_TILE(FP8_64x32, false, 64, 32, 2, 1, 2, 6, false, false)
+    else FP8_TILE(FP8_64x64, false, 64, 64, 2, 2, 2, 4, false, false)
+    else FP8_TILE(FP8_128x128, false, 128, 128, 4, 2, 1, 4, false, false)
+    else FP8_TILE(FP8_256x128, false, 256, 128, 4, 2, 1, 3, true, true)
 }
 template <typename T> static void launch_gated(const Fp8Args &b, const Fp8Geom &g, int grid, hipStream_t s)
 {
-    FP8_TILE(FP8_256x32, true, 256, 32, 4, 1, 2, 4, false)
-    else FP8_TILE(FP8_256x64, true, 256, 64, 4, 2, 1, 3, false)
-    else FP8_TILE(FP8_256x128, true, 256, 128, 4, 2, 1, 3, true)
+    FP8_TILE(FP8_256x32, true, 256, 32, 4, 1, 2, 4, false, false)
+    else FP8_TILE(FP8_256x64, true, 256, 64, 4, 2, 1, 3, false, false)
+    else FP8_TILE(FP8_256x128, true, 256, 128, 4, 2, 1, 3, true, true)
 }
 #undef FP8_TILE
 
@@ -573,7 +585,9 @@ LaunchInfo launch_gemm_fp8(const TokenArgs &a, hipStream_t s, bool dry, int phas
     b.K = a.xq.features; b.KB = (b.K + FP8_BLOCK - 1) / FP8_BLOCK; b.N = a.features; b.rows = a.batch * a.S; b.act = a.act;
     b.r_lo = a.b_lo * a.S; b.r_hi = a.b_hi * a.S;
     b.f_tiles = (b.N + g.features - 1) / g.features; b.r_tiles = (b.r_hi - b.r_lo + g.rows - 1) / g.rows; b.slices = g.slices; b.per_slice = g.blocks_per_slice;
-    const int grid = b.f_tiles * b.r_tiles * b.slices;
+    const int tiles = b.f_tiles * b.r_tiles, halves = g.tile == FP8_256x128 ? fp8_halves(tiles, b.slices) : 0;
+    b.whole = tiles - halves;
+    const int grid = (tiles + halves) * b.slices;
     const int64_t units = (int64_t)(b.r_hi - b.r_lo) * ((b.N + FP8_BLOCK - 1) / FP8_BLOCK);
     const int join = (int)((units + 3) / 4);
     const bool bf16 = a.dtype == DT_BF16;

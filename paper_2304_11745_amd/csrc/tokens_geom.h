@@ -44,13 +44,15 @@ inline AttendGeom attend_geom(const TokenArgs &a)
 enum Fp8Tile { FP8_FEW, FP8_64x32, FP8_64x64, FP8_128x128, FP8_256x128, FP8_256x64, FP8_256x32 };      // rows of weights (a gated block: half gate, half up) x rows
 enum { FP8_WS_MAX = 16 << 20 };                                                      // bytes of workspace, of the 32 MiB that all tenants share in gacer_run_static
 struct Fp8Geom { Fp8Tile tile; int features, rows, slices, blocks_per_slice; };
+// Tiles of a last round that are done in halves of their rows, by twice as many workgroups: where these are one round too.
+inline int fp8_halves(int64_t tiles, int slices) { return slices == 1 && tiles > 256 && tiles % 256 <= 128 ? (int)(tiles % 256) : 0; }
 inline Fp8Geom fp8_geom(const TokenArgs &a)
 {
     const bool gated = a.op == TK_GATED_FP8;
     const int64_t rows = (int64_t)a.batch * a.S, blocks = (a.xq.features + FP8_BLOCK - 1) / FP8_BLOCK, N = a.features;
-    struct Shape { Fp8Tile tile; int features, rows; double us; int held; };             // us a block; workgroups that a unit works on at a time
-    static const Shape gemm[] = {{FP8_FEW, 32, 32, 0.0, 1}, {FP8_64x32, 64, 32, 0.32, 2}, {FP8_64x64, 64, 64, 0.37, 2}, {FP8_128x128, 128, 128, 0.95, 1}, {FP8_256x128, 256, 128, 1.5, 1}};
-    static const Shape block[] = {{FP8_256x32, 128, 32, 0.85, 1}, {FP8_256x64, 128, 64, 1.05, 1}, {FP8_256x128, 128, 128, 1.6, 1}};
+    struct Shape { Fp8Tile tile; int features, rows; double us; int held; double half; };      // us a block; workgroups that a unit works on at a time; us a block in halves
+    static const Shape gemm[] = {{FP8_FEW, 32, 32, 0.0, 1, 0.0}, {FP8_64x32, 64, 32, 0.32, 2, 0.0}, {FP8_64x64, 64, 64, 0.37, 2, 0.0}, {FP8_128x128, 128, 128, 0.95, 1, 0.0}, {FP8_256x128, 256, 128, 1.5, 1, 1.1}};
+    static const Shape block[] = {{FP8_256x32, 128, 32, 0.85, 1, 0.0}, {FP8_256x64, 128, 64, 1.05, 1, 0.0}, {FP8_256x128, 128, 128, 1.6, 1, 1.05}};
     Fp8Geom g = {};
     double least = 0.0;
     for (int i = 0; i < (gated ? 3 : 5); ++i) {
@@ -63,6 +65,7 @@ inline Fp8Geom fp8_geom(const TokenArgs &a)
             double rounds = (double)(tiles * slices) / 256.0;
             if (s.held == 1) rounds = (double)((tiles * slices + 255) / 256);
             if (rounds < 1.0) rounds = 1.0;
+            if (s.half > 0.0 && fp8_halves(tiles, slices)) rounds += s.half / s.us - 1.0;
             const double us = s.tile == FP8_FEW ? (rows <= 8 ? 1.05 : rows <= 16 ? 1.45 : 1.85) * (double)((per + 7) / 8) : s.us * (double)per;
             const double all = rounds * us + (slices > 1 ? 3.5 + (double)bytes / 2.5e6 : 0.0);
             if (least == 0.0 || all < least) {

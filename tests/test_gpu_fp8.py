@@ -185,8 +185,8 @@ def test_gated(dtype, codes, batch, tokens, cin, cout):
 
 # sizes that take the other tiles and the inner extent in slices (tests/test_host_fp8_dispatch.py sees that none is left out)
 WIDE_GEMMS = [(1, 1, 400, 70), (1, 17, 3088, 70), (3, 11, 3088, 71), (1, 1500, 4112, 70), (2, 1025, 144, 300), (3, 1000, 144, 1001), (4, 128, 14336, 4096), (50, 41, 144, 2068), (13, 5, 9616, 5520),
-              (7, 31, 6416, 2050)]
-WIDE_GATED = [(1, 1, 2000, 80), (2, 1500, 144, 304), (3, 1000, 144, 704), (5, 410, 4112, 80), (50, 41, 4112, 144), (3, 16, 5120, 2064)]
+              (7, 31, 6416, 2050), (8, 165, 160, 6650), (5, 264, 656, 6656)]      # the last two end in tiles of half the rows, some of them empty
+WIDE_GATED = [(1, 1, 2000, 80), (2, 1500, 144, 304), (3, 1000, 144, 704), (5, 410, 4112, 80), (50, 41, 4112, 144), (3, 16, 5120, 2064), (5, 264, 656, 3328)]
 
 
 def wide(g, rows, width, spread):
@@ -240,7 +240,7 @@ def test_gated_in_every_tile(dtype, codes, batch, tokens, cin, cout):
 
 
 @pytest.mark.parametrize("gated", [False, True])
-@pytest.mark.parametrize("tokens,cin,cout", [(1, 3088, 144), (1, 400, 70), (13, 3088, 144), (300, 4112, 144), (200, 144, 1008), (410, 144, 2064)])
+@pytest.mark.parametrize("tokens,cin,cout", [(1, 3088, 144), (1, 400, 70), (13, 3088, 144), (300, 4112, 144), (200, 144, 1008), (410, 144, 2064), (264, 656, 6656)])
 def test_plans_give_the_bits_of_the_whole(gated, tokens, cin, cout):
     """Every tile, whole and in slices, with the batch cut unevenly, also over two streams."""
     from paper_2304_11745_amd import binding as B
