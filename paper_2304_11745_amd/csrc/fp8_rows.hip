@@ -1,7 +1,7 @@
 // Residual, RMS norm and 8-bit rows: h = x + res, y = h * rsqrt(mean(h^2) + eps) * gamma, then e4m3 codes with a scale for each row and block of 128 features.
 //
 // Every element is read and written once, the row in between in registers: bound by the way to memory.  4101 rows of 4096 features, bf16, with residual (118 MB):
-// 25.4 us = 4.6 TB/s; codes alone of 8192 rows of 8192 (203 MB) 39.7 us = 5.1 TB/s, what a large copy reaches; 1018 rows of 5008 in fp32 9.2 us, one row 5.3, of which a
+// 25.4 us = 4.6 TB/s; codes alone of 8192 rows of 8192 (203 MB) 39.7 us = 5.1 TB/s, what a large copy reaches; 1018 rows of 5008 in fp32 8.5 us, one row 5.3, of which a
 // launch in a stream of launches is 4.  With the loads under conditions, each waited for where it stood, they took 47, 54 and 16 us.
 #include <hip/hip_runtime.h>
 #include <algorithm>
@@ -57,50 +57,55 @@ template <typename T, bool WHOLE> __device__ __forceinline__ void store(T *row, 
 
 // A row is held by LANES threads in registers, R runs of eight features each; 16 neighbouring lanes hold a block of 128.  All loads of a row are issued, through
 // descriptors that answer zeros behind the row, before the first is converted: under a condition each would be waited for where it stands.
-template <typename T, int LANES, int R, bool WHOLE> __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rmsnorm_fp8_kernel(NormArgs a)
+// LONG: a row that the registers do not fit goes through them in pieces of LANES * R * 8 features, with a norm twice; the second time it comes from the caches.
+template <typename T, int LANES, int R, bool WHOLE, bool LONG> __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rmsnorm_fp8_kernel(NormArgs a)
 {
-    constexpr int THREADS = LANES < 256 ? 256 : LANES, PER = THREADS / LANES;
+    constexpr int THREADS = LANES < 256 ? 256 : LANES, PER = THREADS / LANES, PIECE = LANES * R * 8;
     __shared__ float sums[LANES > 64 ? LANES / 64 : 1];
     const int tid = threadIdx.x, lane = tid % LANES;
+    const __amdgpu_buffer_rsrc_t gr = make_rsrc(a.gamma, a.gamma ? a.C * 4 : 0);
     for (int64_t row = a.r_lo + (int64_t)blockIdx.x * PER + tid / LANES; row < a.r_hi; row += (int64_t)gridDim.x * PER) {
         const __amdgpu_buffer_rsrc_t xr = make_rsrc((const T *)a.x + row * a.C, a.C * (int64_t)sizeof(T));
-        Run<T, WHOLE> x[R], r[R];
-#pragma unroll
-        for (int i = 0; i < R; ++i) x[i].load(xr, (i * LANES + lane) * 8);
-        if (a.res) {
-            const __amdgpu_buffer_rsrc_t rr = make_rsrc((const T *)a.res + row * a.C, a.C * (int64_t)sizeof(T));
-#pragma unroll
-            for (int i = 0; i < R; ++i) r[i].load(rr, (i * LANES + lane) * 8);
-        }
         float h[R][8];
+        auto fetch = [&](int from) {
+            Run<T, WHOLE> x[R], r[R];
 #pragma unroll
-        for (int i = 0; i < R; ++i)
+            for (int i = 0; i < R; ++i) x[i].load(xr, from + (i * LANES + lane) * 8);
+            if (a.res) {
+                const __amdgpu_buffer_rsrc_t rr = make_rsrc((const T *)a.res + row * a.C, a.C * (int64_t)sizeof(T));
 #pragma unroll
-            for (int e = 0; e < 8; ++e) h[i][e] = x[i].get(e);
-        if (a.res) {
+                for (int i = 0; i < R; ++i) r[i].load(rr, from + (i * LANES + lane) * 8);
+            }
 #pragma unroll
             for (int i = 0; i < R; ++i)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) h[i][e] += r[i].get(e);
-        }
-        if (a.codes && a.y) {
+                for (int e = 0; e < 8; ++e) h[i][e] = x[i].get(e);
+            if (a.res) {
 #pragma unroll
-            for (int i = 0; i < R; ++i) store<T, WHOLE>((T *)a.y + row * a.C, (i * LANES + lane) * 8, a.C, h[i]);
-        }
-        if (a.norm) {
-            // gamma comes with the row, but for the widest rows, whose registers it would not fit
-            constexpr bool EARLY = R <= 4;
-            const __amdgpu_buffer_rsrc_t gr = make_rsrc(a.gamma, a.gamma ? a.C * 4 : 0);
-            Run<float, WHOLE> g[EARLY ? R : 1];
-            if (EARLY && a.gamma) {
+                for (int i = 0; i < R; ++i)
 #pragma unroll
-                for (int i = 0; i < (EARLY ? R : 1); ++i) g[i].load(gr, (i * LANES + lane) * 8);
+                    for (int e = 0; e < 8; ++e) h[i][e] += r[i].get(e);
             }
-            float sum = 0.f;
+        };
+        auto keep = [&](int from) {                        // in the tenant's type
+#pragma unroll
+            for (int i = 0; i < R; ++i) store<T, WHOLE>((T *)a.y + row * a.C, from + (i * LANES + lane) * 8, a.C, h[i]);
+        };
+        Run<float, WHOLE> g[R];
+        auto fetch_gamma = [&](int from) {
+            if (!a.gamma) return;
+#pragma unroll
+            for (int i = 0; i < R; ++i) g[i].load(gr, from + (i * LANES + lane) * 8);
+        };
+        float sum = 0.f;
+        auto squares = [&] {
 #pragma unroll
             for (int i = 0; i < R; ++i)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum = fmaf(h[i][e], h[i][e], sum);
+        };
+        float by = 1.f;
+        auto factor = [&] {
 #pragma unroll
             for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
             if constexpr (LANES > 64) {
@@ -111,43 +116,68 @@ template <typename T, int LANES, int R, bool WHOLE> __global__ __launch_bounds__
                 for (int i = 0; i < LANES / 64; ++i) sum += sums[i];
                 if (gridDim.x * PER < a.r_hi - a.r_lo) __syncthreads();      // another row follows
             }
-            const float by = rsqrtf(sum * a.inv_c + a.eps);
+            by = rsqrtf(sum * a.inv_c + a.eps);
+        };
+        auto leave = [&](int from) {
+            if (a.norm) {
 #pragma unroll
-            for (int i = 0; i < R; ++i) {
-                if (!EARLY && a.gamma) g[0].load(gr, (i * LANES + lane) * 8);
+                for (int i = 0; i < R; ++i)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) h[i][e] = h[i][e] * by * (a.gamma ? g[EARLY ? i : 0].get(e) : 1.f);
+                    for (int e = 0; e < 8; ++e) h[i][e] = h[i][e] * by * (a.gamma ? g[i].get(e) : 1.f);
             }
-        }
-        if (!a.codes) {
+            if (!a.codes) {
+                keep(from);
+                return;
+            }
 #pragma unroll
-            for (int i = 0; i < R; ++i) store<T, WHOLE>((T *)a.y + row * a.C, (i * LANES + lane) * 8, a.C, h[i]);
-            continue;
-        }
+            for (int i = 0; i < R; ++i) {                  // codes: rows of a multiple of 16 features
+                const int f = from + (i * LANES + lane) * 8;
+                unsigned most = 0;
 #pragma unroll
-        for (int i = 0; i < R; ++i) {                      // codes: rows of a multiple of 16 features
-            const int f = (i * LANES + lane) * 8;
-            unsigned most = 0;
+                for (int e = 0; e < 8; ++e) most = max(most, magnitude(h[i][e]));
 #pragma unroll
-            for (int e = 0; e < 8; ++e) most = max(most, magnitude(h[i][e]));
-#pragma unroll
-            for (int d = 1; d < 16; d *= 2) most = max(most, (unsigned)__shfl_xor((int)most, d));
-            const float2 s = scale_of_block(most);
-            uint2 c = make_uint2(to_codes(h[i][0], h[i][1], h[i][2], h[i][3], s.y), to_codes(h[i][4], h[i][5], h[i][6], h[i][7], s.y));
-            if (s.y == 0.f) c = make_uint2(0, 0);
-            if (f < a.C) {
-                *(uint2 *)(a.codes + row * a.C + f) = c;
-                if (lane % 16 == 0) a.scales[(int64_t)(f / FP8_BLOCK) * a.rows + row] = s.x;
+                for (int d = 1; d < 16; d *= 2) most = max(most, (unsigned)__shfl_xor((int)most, d));
+                const float2 s = scale_of_block(most);
+                uint2 c = make_uint2(to_codes(h[i][0], h[i][1], h[i][2], h[i][3], s.y), to_codes(h[i][4], h[i][5], h[i][6], h[i][7], s.y));
+                if (s.y == 0.f) c = make_uint2(0, 0);
+                if (f < a.C) {
+                    *(uint2 *)(a.codes + row * a.C + f) = c;
+                    if (lane % 16 == 0) a.scales[(int64_t)(f / FP8_BLOCK) * a.rows + row] = s.x;
+                }
+            }
+        };
+        if constexpr (!LONG) {
+            fetch(0);
+            if (a.codes && a.y) keep(0);
+            if (a.norm) {
+                fetch_gamma(0);
+                squares();
+                factor();
+            }
+            leave(0);
+        } else {
+            if (a.norm) {
+                for (int from = 0; from < a.C; from += PIECE) {
+                    fetch(from);
+                    squares();
+                }
+                factor();
+            }
+            for (int from = 0; from < a.C; from += PIECE) {
+                fetch(from);
+                if (a.norm) fetch_gamma(from);
+                if (a.codes && a.y) keep(from);
+                leave(from);
             }
         }
     }
 }
 
-template <typename T, int LANES, int R> static void norm(const NormArgs &a, int grid, hipStream_t s)
+template <typename T, int LANES, int R, bool LONG> static void norm(const NormArgs &a, int grid, hipStream_t s)
 {
     const dim3 g(grid), b(LANES < 256 ? 256 : LANES);
-    if (a.C % 8 == 0) GACER_LAUNCH((rmsnorm_fp8_kernel<T, LANES, R, true>), g, b, 0, s, a);
-    else GACER_LAUNCH((rmsnorm_fp8_kernel<T, LANES, R, false>), g, b, 0, s, a);
+    if (a.C % 8 == 0) GACER_LAUNCH((rmsnorm_fp8_kernel<T, LANES, R, true, LONG>), g, b, 0, s, a);
+    else GACER_LAUNCH((rmsnorm_fp8_kernel<T, LANES, R, false, LONG>), g, b, 0, s, a);
 }
 
 LaunchInfo launch_rmsnorm_fp8(const TokenArgs &a, hipStream_t s, bool dry)
@@ -158,19 +188,20 @@ LaunchInfo launch_rmsnorm_fp8(const TokenArgs &a, hipStream_t s, bool dry)
     n.r_lo = a.b_lo * a.S; n.r_hi = a.b_hi * a.S;
     // lanes of a row: a wave up to 1024 features, four up to 8192, else sixteen.  Measured, us with 64 / 256 / 1024 lanes, bf16, with residual: 8192 rows of 512
     // 7.6 / 12.1 / 40, 8192 of 1024 11.4 / 14.0 / 40, 4101 of 4096 29.7 / 25.2 / 29.1, 2048 of 8192 - / 26.5 / 26.0, 1000 of 16384 - / 17.4 / 16.0.  Beyond
-    // 32768 features a row does not fit the registers whole (500 rows of 65536 80 us, of 32768 13).
+    // 16384 features in pieces, us whole (in registers and, in part, scratch memory) / in pieces, with residual: 500 rows of 65536 121 / 67, of 32768 24 / 27, in fp32
+    // 214 / 121 and 54 / 60, one row of 65536 30 / 12; a product's inner extent of that size is rare, and one kernel does them all.
     const int runs = (a.features + 7) / 8, lanes = runs <= 128 ? 64 : runs <= 1024 ? 256 : 1024;
     const int per = lanes == 64 ? 4 : 1, each = (runs + lanes - 1) / lanes;
     // workgroups that a unit holds, by the registers of (64, 1), (64, 2), (256, 1), (256, 2), (256, 4) and wider
-    static const int held[2][2][6] = {{{8, 5, 8, 5, 3, 1}, {8, 6, 8, 5, 3, 1}}, {{8, 5, 8, 5, 2, 1}, {8, 7, 8, 6, 4, 1}}};
+    static const int held[2][2][6] = {{{8, 6, 8, 5, 3, 1}, {8, 7, 8, 7, 4, 1}}, {{8, 4, 8, 4, 2, 1}, {8, 8, 8, 7, 4, 1}}};
     LaunchInfo li;
     li.workgroups = (int)std::min<int64_t>(((int64_t)(n.r_hi - n.r_lo) + per - 1) / per, 1 << 20);
     li.threads = std::max(256, lanes); li.lds_bytes = lanes == 64 ? 0 : lanes / 16; li.phases = 1;
     li.wg_per_cu = held[a.dtype == DT_BF16][a.features % 8 == 0][lanes == 64 ? each - 1 : lanes == 256 ? (each > 2 ? 4 : each + 1) : 5];
     li.kernel = a.dtype == DT_BF16 ? "rmsnorm_fp8_bf16" : "rmsnorm_fp8_f32";
     if (dry || !li.workgroups) return li;
-#define NORM(LANES, R) if (lanes == LANES && each > R / 2 && each <= R) { if (a.dtype == DT_BF16) norm<unsigned short, LANES, R>(n, li.workgroups, s); else norm<float, LANES, R>(n, li.workgroups, s); }
-    NORM(64, 1) NORM(64, 2) NORM(256, 1) NORM(256, 2) NORM(256, 4) NORM(1024, 2) NORM(1024, 4) NORM(1024, 8)
+#define NORM(LANES, R, LONG) if (lanes == LANES && (LONG ? each > R : each > R / 2 && each <= R)) { if (a.dtype == DT_BF16) norm<unsigned short, LANES, R, LONG>(n, li.workgroups, s); else norm<float, LANES, R, LONG>(n, li.workgroups, s); }
+    NORM(64, 1, false) NORM(64, 2, false) NORM(256, 1, false) NORM(256, 2, false) NORM(256, 4, false) NORM(1024, 2, false) NORM(1024, 2, true)
 #undef NORM
     return li;
 }

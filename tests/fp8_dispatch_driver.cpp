@@ -53,8 +53,8 @@ int main(int argc, char **argv)
                 TokenArgs a;
                 std::memset(&a, 0, sizeof a);
                 a.dtype = dtype; a.op = TK_RMSNORM_FP8; a.b_hi = a.batch = 5; a.S = 1; a.features = runs * 8 - odd; a.x = a.y = (void *)0x10000;
-                const int lanes = runs <= 128 ? 64 : runs <= 1024 ? 256 : 1024, each = (runs + lanes - 1) / lanes, r = each <= 1 ? 1 : each <= 2 ? 2 : each <= 4 ? 4 : 8;
-                tell("rmsnorm_fp8_kernelI" + type + "Li" + std::to_string(lanes) + "ELi" + std::to_string(r) + "ELb" + std::to_string(!odd) + "E", launch_rmsnorm_fp8(a, nullptr, true));
+                const int lanes = runs <= 128 ? 64 : runs <= 1024 ? 256 : 1024, each = (runs + lanes - 1) / lanes, r = each <= 1 ? 1 : each <= 2 || lanes == 1024 ? 2 : 4;
+                tell("rmsnorm_fp8_kernelI" + type + "Li" + std::to_string(lanes) + "ELi" + std::to_string(r) + "ELb" + std::to_string(!odd) + "ELb" + std::to_string(lanes == 1024 && each > 2) + "E", launch_rmsnorm_fp8(a, nullptr, true));
             }
     }
     return 0;

@@ -55,6 +55,8 @@ def empty_rows(batch, tokens, features, fill=0x55):
     (1, 2, 12288, False, False, False, False),
     (1, 2, 16400, True, True, True, True),         # the large workgroup
     (1, 1, 65536, True, True, True, True),
+    (3, 2, 40976, True, True, True, False),        # in pieces, the last one short
+    (1, 3, 32784, False, False, True, True),
 ])
 def test_norm_and_codes(dtype, batch, tokens, width, norm, gamma, res, total):
     g = gen(width + tokens)
@@ -80,7 +82,7 @@ def test_norm_and_codes(dtype, batch, tokens, width, norm, gamma, res, total):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("tokens,width", [(1, 1), (3, 7), (5, 129), (2, 1000), (3, 4097), (2, 20001)])
+@pytest.mark.parametrize("tokens,width", [(1, 1), (3, 7), (5, 129), (2, 1000), (3, 4097), (2, 20001), (5, 49999), (1, 32768)])
 def test_norm_in_the_tenants_type(dtype, tokens, width):
     g = gen(width)
     x, r, gm = (torch.randn(2, tokens, width, generator=g) * 4).to(DT[dtype]), torch.randn(2, tokens, width, generator=g).to(DT[dtype]), 1 + 0.2 * torch.randn(width, generator=g)
