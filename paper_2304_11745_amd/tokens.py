@@ -3,8 +3,8 @@
 ``OpList`` writes down a tenant's operators (``include/gacer.h`` has their definitions) over tensors that the caller owns;
 ``TokenSession`` loads one or several lists into a gacer context and enqueues or runs them; ``Cache`` holds the tensors of a
 paged cache, ``Fp8Rows`` and ``Fp8Weight`` those of 8-bit operands.  ``harness.Session`` takes such lists beside its own tenants (``extra=``), so that a decoding tenant runs in
-the same regulated rounds as the others.  No arithmetic happens here but ``Fp8Weight.quantise``, which a program calls once; every operator runs
-inside libgacer.so.
+the same regulated rounds as the others.  No arithmetic happens here but ``Fp8Weight.quantise``, which a program calls once, and
+``values()``, what 8-bit operands stand for; every operator runs inside libgacer.so.
 
 Activations are ``[batch, tokens, features]`` or ``[batch, features]``, contiguous, in the list's dtype.
 """
@@ -64,6 +64,7 @@ class Fp8Rows:
         _need(codes.dim() in (2, 3) and codes.dtype == torch.float8_e4m3fn, "codes must be float8_e4m3fn [batch, features] or [batch, tokens, features]")
         self.batch, self.features = codes.shape[0], codes.shape[-1]
         self.rows = self.batch * (codes.shape[1] if codes.dim() == 3 else 1)
+        _need(self.rows * self.features < 2 ** 31, "8-bit rows of 2 GiB or more")
         _need(tuple(scales.shape) == (_blocks(self.features), self.rows) and scales.dtype == torch.float32, "scales must be float32 [ceil(features/128), batch * tokens]")
         for t in (codes, scales):
             _need(t.is_cuda and t.is_contiguous() and t.device == codes.device, "the tensors of 8-bit rows must be contiguous and on one GPU")
@@ -89,6 +90,7 @@ class Fp8Weight:
     def __init__(self, codes, scales):
         _need(codes.dim() == 2 and codes.dtype == torch.float8_e4m3fn, "codes must be float8_e4m3fn [out, in]")
         self.out, self.cin = codes.shape
+        _need(self.out * self.cin < 2 ** 31, "weights of 2 GiB or more")
         _need(tuple(scales.shape) == (_blocks(self.out), _blocks(self.cin)) and scales.dtype == torch.float32, "scales must be float32 [ceil(out/128), ceil(in/128)]")
         for t in (codes, scales):
             _need(t.is_cuda and t.is_contiguous() and t.device == codes.device, "the tensors of 8-bit weights must be contiguous and on one GPU")

@@ -72,3 +72,11 @@ def test_what_a_list_writes_down():
         o.gemm_fp8(n, weight(70, 144), tensor(70), act="no such")
     with pytest.raises(KeyError):
         T.OpList(F32, 3)._op(B.GACER_GEMM, act="silu")          # an activation of products of 8-bit rows alone
+
+
+def test_operands_of_2_gib_are_refused():
+    """The library's structures hold their extents in 32 bits."""
+    for make in (lambda: rows(16, batch=2 ** 20, tokens=4096 + 1), lambda: rows(16, batch=2, tokens=2 ** 26), lambda: weight(2 ** 20, 2048), lambda: weight(2 ** 32 + 128, 16)):
+        with pytest.raises(ValueError, match="2 GiB"):
+            make()
+    assert rows(16, batch=1, tokens=2 ** 27 - 1).rows == 2 ** 27 - 1
