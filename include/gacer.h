@@ -260,7 +260,7 @@ typedef struct {
 /*
  * GEMM_FP8: in0 = -1; out = (n a multiple of the batch, c = out features, h, w) with n*h*w = x.rows:
  *   out[r][o] = act(sum_k x[r][k] w[o][k] + bias[o] + res[r][o]),  bias = device [c] or NULL, res = a tensor of out's shape or -1, as for RMSNORM_FP8.
- * GATED_FP8: in0 = res = -1; with g = gate and u = up products of the same rows,
+ * GATED_FP8: in0 = res = -1, no bias; with g = gate and u = up products of the same rows,
  *   h[r][f] = act(sum_k x[r][k] g[f][k]) * (sum_k x[r][k] u[f][k]),
  * as 8-bit rows (y.codes != NULL, out = -1, y.rows = x.rows) or as out in the tenant's type (y.codes == NULL; out as above, c = f).
  * Products of codes are exact; blocks of 128 inner features are summed in fp32, scaled, and added in fp32, in an order that the number of rows of the

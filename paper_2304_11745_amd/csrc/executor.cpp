@@ -412,6 +412,7 @@ static gacer_status check_fp8_op(Ctx *c, int ti, const gacer_tenant &t, int oi, 
         if (!outside && !written.all(op.res)) return bad("res is written by a later operator of the list, or not whole");
     }
     if (norm && op.act != GACER_ACT_NONE) return bad("a norm takes no activation");
+    if ((norm || gated) && op.bias) return bad("only a product of 8-bit rows takes a bias");
     gacer_fp8_norm dn{};
     gacer_fp8_gated dg{};
     gacer_fp8_gemm dm{};

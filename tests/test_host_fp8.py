@@ -126,6 +126,12 @@ def test_a_gated_block_refuses(ctx, status, kw):
     assert b"tenant 0 op 0" in B.gacer_last_error(ctx)
 
 
+@pytest.mark.parametrize("kind", [N, A])
+def test_norms_and_gated_blocks_refuse_a_bias(ctx, kind):
+    assert load(ctx, kind, bias=AT[13]) == S, B.gacer_last_error(ctx)
+    assert b"tenant 0 op 0" in B.gacer_last_error(ctx) and b"bias" in B.gacer_last_error(ctx)
+
+
 def test_other_operators_take_no_new_activation(ctx):
     t = (B.gacer_tensor * 2)(*[B.gacer_tensor(BATCH, 16, 1, 1, AT[i], 0, 0, 0) for i in range(2)])
     for act, status in ((5, B.GACER_OK), (6, B.GACER_EINVAL), (7, B.GACER_EINVAL)):
