@@ -27,7 +27,7 @@ template <typename T> __device__ __forceinline__ void finish(const Fp8Args &a, i
 // in order.  Operands come straight from memory, three blocks of them in flight in registers: lane l holds feature (row) l % 32, and of every 32 inner
 // features the 16 codes of half l / 32.  Nothing is shared between waves, so that LDS and its barriers would only add to the chain of a load, eight
 // products and the join.  One row 4096 -> 6144 (25 MB of weights): 9.3 us, 8.8 of them in the kernel, 2.8 TB/s: 192 of 256 units, each
-// with 128 KB to fetch; all loads at once, or the inner extent in two slices (12.1 with the join), are no faster.  In tiles through LDS it takes 12.
+// with 128 KB to fetch; all loads at once are no faster, and in tiles through LDS, 64x32 in two slices, it takes 12.1.
 template <typename T> __global__ __launch_bounds__(512) void fp8_few_kernel(Fp8Args a)
 {
     constexpr int W = 8, AHEAD = 3;
@@ -105,8 +105,8 @@ template <typename T> __global__ __launch_bounds__(512) void fp8_few_kernel(Fp8A
 //   256x128 (gated: 128 features of gate and up), where there are tiles enough: 32 matrix instructions a block and wave against 128 that widen, 64 that scale and 25
 // others.  8192^3: matrix cores busy 60 %, vector instructions 61 %, LDS 17 % (conflicts 1 % of it), waves waiting 29 % of their time.  Of the 3218 clocks a block takes
 // (2048 on the matrix cores) the scaling costs 620, loads 300, widening 150.
-//   128x128, 64x64, 64x32 (gated 64 and 32 rows), where there are not: more units at work and more blocks ahead (NS); KH: with four waves in a tile the two halves
-// of each block are shared between two groups of waves, added at the end.
+//   128x128, 64x64, 64x32 (gated 64 and 32 rows), where there are not: more units at work and more blocks ahead (NS); KH = 2: two groups of waves share
+// the tile, each takes its half of every block, and the sums of the two are added at the end.
 template <int N> __device__ __forceinline__ void meet()
 {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
@@ -326,8 +326,8 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int KH, int NS
     // TURNS: with eight waves, two to a SIMD, the second four are half a block late: while one wave of a SIMD scales its block's products, the other's keep the matrix
     // core busy.  All meet twice a block.  When the early ones begin block n (their loads of it waited for; the late ones waited before their block n - 1, or
     // before the first meeting), the late ones are amid block n - 1 and stage n - 2 is free: the early ones' loads of block n + 1 go there.  When the late ones
-    // begin block n, the early ones have left stage n - 1: the late ones' loads of block n + 2 go there.  8192^3 901 us
-    // with turns, 1045 without (and then the registers spill), a gated block of 4096 rows 826 and 878; with a tile of half the rows, whose blocks are short, two
+    // begin block n, the early ones have left stage n - 1: the late ones' loads of block n + 2 go there.  8192^3 901 us with
+    // turns, 1045 without (and then the registers spill), a gated block of 4096 rows 826 and 878; with a tile of half the rows, whose blocks are short, two
     // meetings cost more than the turns give (48 gated rows 44 with, 42 without).
     if (late) meet<0>();
     for (int kb = lo; kb < hi; kb += NS) {

@@ -75,6 +75,7 @@ inline Fp8Geom fp8_geom(const TokenArgs &a)
             if (s.held == 1) rounds = (double)((tiles * slices + 255) / 256);
             if (rounds < 1.0) rounds = 1.0;
             if (s.half > 0.0 && fp8_halves(tiles, slices)) rounds += s.half / s.us - 1.0;
+            // few rows: a round of eight blocks, one a wave, longer by the rows that are read beside the weights
             const double us = s.tile == FP8_FEW ? (rows <= 8 ? 1.05 : rows <= 16 ? 1.45 : 1.85) * (double)((per + 7) / 8) : s.us * (double)per;
             const double all = rounds * us + (slices > 1 ? 3.5 + (double)bytes / 2.5e6 : 0.0);
             if (least == 0.0 || all < least) {
