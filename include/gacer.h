@@ -233,6 +233,7 @@ typedef struct {
  *   Weights: codes [out features][in features], scales [ceil(out/128)][ceil(in/128)]: one for every block of 128 by 128.
  * features: a multiple of 16 for rows (and so for the inner extent of a product), 16..65536.  Codes 16-byte aligned, scales as float.
  * codes < 2 GiB each.  What an operator writes must not share memory with what it reads.  These operators split along the batch.
+ * bias, scale and shift are NULL but where an operator below names them; another parameter is refused (GACER_ESHAPE), never left out.
  */
 #define GACER_FP8_BLOCK 128
 typedef struct {
@@ -248,7 +249,7 @@ typedef struct {
 /*
  * RMSNORM_FP8: in0 = x (n a multiple of the batch, c = features; every position is a row), res = a tensor of the same shape or -1: written by an earlier
  * operator, or by none of the list, then it is the caller's as the tenant's input is (so a list can begin behind a caller's own step).  In fp32, h = x + res;
- * with norm != 0 y = h * rsqrt(mean(h^2) + alpha) * scale (scale = device [c] or NULL: ones), else y = h.
+ * with norm != 0 y = h * rsqrt(mean(h^2) + alpha) * scale (scale = device [c] or NULL: ones), else y = h (scale is not read).
  *   y.codes != NULL: y leaves as 8-bit rows, and out = h in the tenant's type, the residual stream behind the addition (-1: not kept).
  *   y.codes == NULL: out = y in the tenant's type.
  */

@@ -413,6 +413,8 @@ static gacer_status check_fp8_op(Ctx *c, int ti, const gacer_tenant &t, int oi, 
     }
     if (norm && op.act != GACER_ACT_NONE) return bad("a norm takes no activation");
     if ((norm || gated) && op.bias) return bad("only a product of 8-bit rows takes a bias");
+    if (op.shift) return bad("operators on 8-bit rows take no shift");
+    if (!norm && op.scale) return bad("products of 8-bit rows take no scale beside those of their codes");
     gacer_fp8_norm dn{};
     gacer_fp8_gated dg{};
     gacer_fp8_gemm dm{};
