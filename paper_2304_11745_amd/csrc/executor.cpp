@@ -2267,13 +2267,21 @@ gacer_status gacer_profile(gacer_ctx *c, gacer_prof *out, size_t cap, size_t *n_
 }
 
 
-// Rough cost of one tenant for stream placement: matrix-core time of its convolutions / GEMMs plus a fixed cost per
+// Rough cost of one tenant for stream placement: matrix-core time of its convolutions, GEMMs and products of 8-bit rows plus a fixed cost per
 // operator launch.  Only the ranking matters.
 static double tenant_weight(const gacer_tenant &t)
 {
-    double macs = 0;
+    double macs = 0, macs8 = 0;                              // macs8: of 8-bit rows, on the bf16 matrix instructions whatever the tenant's type
     for (int i = 0; i < t.n_ops; ++i) {
         const gacer_op &op = t.ops[i];
+        if ((op.kind == GACER_GEMM_FP8 || op.kind == GACER_GATED_FP8) && op.w) {             // the result may be 8-bit rows instead of a tensor
+            const bool gated = op.kind == GACER_GATED_FP8;
+            gacer_fp8_gated d{};
+            std::memcpy((void *)&d, op.w, gated ? sizeof d : sizeof(gacer_fp8_gemm));        // both begin with the rows they read
+            const double features = op.out >= 0 && op.out < t.n_tensors ? (double)t.tensors[op.out].c : gated ? (double)d.y.features : 0.0;
+            macs8 += (gated ? 2.0 : 1.0) * (double)d.x.rows * (double)d.x.features * features;
+            continue;
+        }
         if (op.out < 0 || op.out >= t.n_tensors) continue;
         const gacer_tensor &y = t.tensors[op.out];
         const double outs = (double)y.n * y.c * y.h * y.w;
@@ -2283,7 +2291,7 @@ static double tenant_weight(const gacer_tenant &t)
         default: break;
         }
     }
-    return 2.0 * macs / (t.dtype == GACER_BF16 ? 4.0e14 : 1.0e14) + 6e-6 * t.n_ops;
+    return 2.0 * macs / (t.dtype == GACER_BF16 ? 4.0e14 : 1.0e14) + 2.0 * macs8 / 4.0e14 + 6e-6 * t.n_ops;
 }
 
 gacer_status gacer_place_streams(const gacer_tenant *tenants, int n, void *const *candidates, int n_cand, int *chosen, int *queue_of,
