@@ -229,7 +229,7 @@ typedef struct {
  * for every row and block of 128 features (the last block may be shorter).  Rows are made by RMSNORM_FP8 and GATED_FP8 or by the caller; the
  * library does not follow who writes them, the order of the list does.
  *   Making a block of y (fp32): m = max(max |y|, 2^-60), scale = m / 448, code = e4m3(y * (448 / m)), the quotients and the code rounded to nearest even.
- * A block that holds an infinity or a NaN gets a NaN scale and codes of 0: it stands for NaNs.
+ * A block that holds an infinity or a NaN gets a NaN scale and codes of 0: it stands for NaNs, and every activation of a product keeps them.
  *   Weights: codes [out features][in features], scales [ceil(out/128)][ceil(in/128)]: one for every block of 128 by 128.
  * features: a multiple of 16 for rows (and so for the inner extent of a product), 16..65536.  Codes 16-byte aligned, scales as float.
  * codes < 2 GiB each.  What an operator writes must not share memory with what it reads.  These operators split along the batch.

@@ -35,9 +35,17 @@ __device__ __forceinline__ float2 scale_of_block(unsigned most)
 }
 __device__ __forceinline__ unsigned magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 
-// The activations of products, `act` uniform.
+// The activations of products, `act` uniform.  A row or block that is no number has to stay none: the bounds of ReLU and the hard activations are comparisons, which
+// keep a NaN (the maximum and the median that activate() takes return a bound for it) and give the same bits for every number.
+__device__ __forceinline__ float between(float v, float most) { return v <= 0.f ? 0.f : v >= most ? most : v; }
 __device__ __forceinline__ float activate8(float v, int act)
 {
+    if (act == ACT_RELU) return v <= 0.f ? 0.f : v;
+    if (act == ACT_RELU6) return between(v, 6.f);
+    if (act == ACT_HSWISH || act == ACT_HSIGMOID) {
+        const float s = __fmul_rn(between(__fadd_rn(v, 3.f), 6.f), 0.16666667163372039794921875f);
+        return act == ACT_HSWISH ? __fmul_rn(v, s) : s;
+    }
     if (act == ACT_SILU) return v / (1.f + __expf(-v));
     if (act == ACT_GELU_TANH) return v / (1.f + __expf(-1.5957691216057308f * (v + 0.044715f * v * v * v)));
     return activate(v, act);
@@ -61,15 +69,21 @@ __device__ __forceinline__ void load8(const unsigned short *p, float *v)
 }
 
 // N values at once: one (uniform) branch for all of them.
+template <int N, int ACT> __device__ __forceinline__ void activate8_all(float *v)
+{
+#pragma unroll
+    for (int q = 0; q < N; ++q) v[q] = activate8(v[q], ACT);
+}
 template <int N> __device__ __forceinline__ void activate8_n(float *v, int act)
 {
-    if (act == ACT_SILU) {
-#pragma unroll
-        for (int q = 0; q < N; ++q) v[q] = activate8(v[q], ACT_SILU);
-    } else if (act == ACT_GELU_TANH) {
-#pragma unroll
-        for (int q = 0; q < N; ++q) v[q] = activate8(v[q], ACT_GELU_TANH);
-    } else activate_n<N>(v, act);
+    if (act == ACT_NONE) return;
+    if (act == ACT_SILU) activate8_all<N, ACT_SILU>(v);
+    else if (act == ACT_GELU_TANH) activate8_all<N, ACT_GELU_TANH>(v);
+    else if (act == ACT_GELU) activate8_all<N, ACT_GELU>(v);
+    else if (act == ACT_RELU) activate8_all<N, ACT_RELU>(v);
+    else if (act == ACT_RELU6) activate8_all<N, ACT_RELU6>(v);
+    else if (act == ACT_HSWISH) activate8_all<N, ACT_HSWISH>(v);
+    else activate8_all<N, ACT_HSIGMOID>(v);
 }
 
 // Arguments of the products (see gacer_fp8_gemm, gacer_fp8_gated)
