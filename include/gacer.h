@@ -264,7 +264,8 @@ typedef struct {
  * GATED_FP8: in0 = res = -1, no bias; with g = gate and u = up products of the same rows,
  *   h[r][f] = act(sum_k x[r][k] g[f][k]) * (sum_k x[r][k] u[f][k]),
  * as 8-bit rows (y.codes != NULL, out = -1, y.rows = x.rows) or as out in the tenant's type (y.codes == NULL; out as above, c = f).
- * Products of codes are exact; blocks of 128 inner features are summed in fp32, scaled, and added in fp32, in an order that the number of rows of the
+ * Products of codes are exact; blocks of 128 inner features are summed in fp32, scaled (by the product of their two scales; by one after the other, the larger
+ * first, where that product is infinite or subnormal; below 2^-150 it is 0), and added in fp32, in an order that the number of rows of the
  * whole operator fixes: a row's result may differ in its last bits between calls of few and of many rows, not between plans.
  */
 typedef struct {

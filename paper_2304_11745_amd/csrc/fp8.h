@@ -86,6 +86,23 @@ template <int N> __device__ __forceinline__ void activate8_n(float *v, int act)
     else activate8_all<N, ACT_HSIGMOID>(v);
 }
 
+// The two scales of a block's sums.  Their product does for both, but where it leaves the range or loses bits below 2^-126: there it would turn sums of 0 into NaN and
+// small results into rough ones, and the scales are taken one after the other, the larger first.  (A product below 2^-150, or of a scale of 0, is 0.)  Which way a row
+// goes is up to its own scales, so that it has the same bits whichever rows lie beside it.
+static constexpr int CLASS_ODD = 0x294;                      // bits of the class instruction: infinite or subnormal, either sign
+__device__ __forceinline__ float2 factors(float a, float b)
+{
+    if (!__builtin_amdgcn_classf(a * b, CLASS_ODD)) return make_float2(1.f, a * b);
+    return __builtin_fabsf(a) > __builtin_fabsf(b) ? make_float2(a, b) : make_float2(b, a);
+}
+// Lanes whose product is such a one (the builtin beneath a ballot would become a number a lane first, then a mask again).
+__device__ __forceinline__ uint64_t odd_lanes(float product)
+{
+    uint64_t lanes;
+    asm("v_cmp_class_f32_e64 %0, %1, %2" : "=s"(lanes) : "v"(product), "s"(CLASS_ODD));
+    return lanes;
+}
+
 // Arguments of the products (see gacer_fp8_gemm, gacer_fp8_gated)
 struct Fp8Args {
     const unsigned char *x, *w, *w2;

@@ -57,7 +57,7 @@ template <typename T> __global__ __launch_bounds__(512) void fp8_few_kernel(Fp8A
         b.sw = ws[kb];
         b.sx = a.xs[(int64_t)kb * a.rows + row];
     };
-    auto multiply = [&](const Block &b, int kb) {
+    auto sums = [&](const Block &b, int kb) {
         f32x16 p;
 #pragma unroll
         for (int i = 0; i < 16; ++i) p[i] = 0.f;
@@ -68,7 +68,13 @@ template <typename T> __global__ __launch_bounds__(512) void fp8_few_kernel(Fp8A
             p = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(b.w[j].x, b.w[j].y), widen(c.x, c.y), p, 0, 0, 0);
             p = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(b.w[j].z, b.w[j].w), widen(c.z, c.w), p, 0, 0, 0);
         }
+        return p;
+    };
+    uint64_t odd = 0;                                  // lanes whose two scales have no ordinary product, in any block
+    auto multiply = [&](const Block &b, int kb) {
+        const f32x16 p = sums(b, kb);
         const float s = b.sx * b.sw;
+        odd |= odd_lanes(s);
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[i] = fmaf(p[i], s, acc[i]);
     };
@@ -79,6 +85,17 @@ template <typename T> __global__ __launch_bounds__(512) void fp8_few_kernel(Fp8A
         for (int i = 0; i < AHEAD; ++i) {
             if (kb + i * W < hi) multiply(blocks[i], kb + i * W);
             load(blocks[i], kb + (i + AHEAD) * W);
+        }
+    }
+    if (__builtin_expect(odd != 0, 0)) {               // once more, with two scales; one row 4096 -> 6144 with this watch 9.22 us, 9.18 without, 9.31 with a branch in the loop
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[i] = 0.f;
+        for (int kb = lo + wave; kb < hi; kb += W) {
+            load(blocks[0], kb);
+            const f32x16 p = sums(blocks[0], kb);
+            const float2 s = factors(blocks[0].sx, blocks[0].sw);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[i] = fmaf(p[i] * s.x, s.y, acc[i]);
         }
     }
 #pragma unroll
@@ -240,6 +257,7 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int KH, int NS
     // A block's products stay in `part` until the next block's first products replace them, tile by tile: each tile is scaled just before.
     f32x16 part[NF][NT];
     float by[GATED ? 2 : 1][NT];                             // what they are scaled by
+    uint64_t odd = 0;                                        // lanes whose two scales have no ordinary product, in any block
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         by[0][t] = 0.f;
@@ -320,7 +338,11 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int KH, int NS
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             by[0][t] = sx[t] * sw;
-            if constexpr (GATED) by[1][t] = sx[t] * su;
+            odd |= odd_lanes(by[0][t]);
+            if constexpr (GATED) {
+                by[1][t] = sx[t] * su;
+                odd |= odd_lanes(by[1][t]);
+            }
         }
     };
     // TURNS: with eight waves, two to a SIMD, the second four are half a block late: while one wave of a SIMD scales its block's products, the other's keep the matrix
@@ -343,6 +365,54 @@ template <typename T, bool GATED, int BF, int BT, int WF, int WT, int KH, int NS
     for (int f = 0; f < NF; ++f)
 #pragma unroll
         for (int t = 0; t < NT; ++t) scale(f, t);
+    // Scales that no one product stands for: the wave adds its blocks up once more, with the two scales one after the other, straight from memory; the sums are
+    // those of the loop above, bit by bit, for every row whose scales have an ordinary product.  A way around the loop's own scaling instead made it spill (21 to 57
+    // registers of 256).  What the watch costs where there is nothing to mend, us with / without, two states in turn: gated block of 777 rows 2064 -> 5520 52.6 / 51.8, of
+    // 48 rows 41.0 / 40.8, of 4096 rows 818 / 824; 64 rows 14336 -> 4096 18.8 / 18.7, 333 rows 2000 -> 1111 11.8 / 12.3, 8192^3 925 / 924 (a card that runs it in 924).
+    if (__builtin_expect(odd != 0, 0)) {
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[f][t][i] = 0.f;
+        for (int kb = lo; kb < hi; ++kb) {
+#pragma unroll
+            for (int f = 0; f < NF; ++f)
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) part[f][t][i] = 0.f;
+#pragma unroll 1
+            for (int j = 0; j < GROUPS; ++j) {
+                const int k = kb * FP8_BLOCK + (half + 2 * j + 4 * kh) * 16;
+                uint4 c[NF + NT];
+#pragma unroll
+                for (int f = 0; f < NF + NT; ++f) {
+                    constexpr int HALVES = GATED ? NF / 2 : NF;
+                    const unsigned char *from = f >= NF ? a.x : GATED && f >= HALVES ? a.w2 : a.w;
+                    const int line = f >= NF ? min(r0 + wt * (BT / WT) + (f - NF) * 32 + r, a.r_hi - 1) : min(fw + f % HALVES * 32 + r, a.N - 1);
+                    c[f] = k < a.K ? *(const uint4 *)(from + (int64_t)line * a.K + k) : make_uint4(0, 0, 0, 0);
+                }
+#pragma unroll
+                for (int f = 0; f < NF; ++f)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        part[f][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(c[f].x, c[f].y), widen(c[NF + t].x, c[NF + t].y), part[f][t], 0, 0, 0);
+                        part[f][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(c[f].z, c[f].w), widen(c[NF + t].z, c[NF + t].w), part[f][t], 0, 0, 0);
+                    }
+            }
+#pragma unroll
+            for (int f = 0; f < NF; ++f)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const float w = wscale[GATED ? f / (NF / 2) : wf * (BF / WF) / FP8_BLOCK][kb];
+                    const float2 s = factors(a.xs[(int64_t)kb * a.rows + min(r0 + wt * (BT / WT) + t * 32 + r, a.r_hi - 1)], w);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[f][t][i] = fmaf(part[f][t][i] * s.x, s.y, acc[f][t][i]);
+                }
+        }
+    }
     meet<0>();                                               // requests behind the end, which write zeros, have landed
     if constexpr (KH == 2) {                                 // both halves of the blocks, in order
         float4 *other = (float4 *)&stages[0][0] + (wave % (WF * WT)) * (NF * NT * 256) + l;
