@@ -132,7 +132,8 @@ template <int N> __device__ __forceinline__ void meet()
 }
 
 // Loads of 16 or 4 bytes a lane from memory (at off | also, plus `base`) to LDS (from `to` on, in order of lanes), counted by vmcnt.  The compiler, which would
-// wait for all of them before it reads LDS, does not see them; they have no result in registers, and nothing else in these kernels uses m0.
+// wait for all of them before it reads LDS, does not see them; they have no result in registers, and nothing else in these kernels uses m0, which a
+// clobber list does not take (tests/test_host_fp8_assembly.py reads that from the machine code).
 __device__ __forceinline__ void load_to_lds16(unsigned to, unsigned off, unsigned also, i32x4 from, int base)
 {
     unsigned at;
