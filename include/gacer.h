@@ -404,7 +404,7 @@ gacer_status gacer_run_static(gacer_ctx *ctx, int mode, int rounds);
  * the inputs' producers and the outputs' readers correct.  For decoding loops, where the host prepares the next step while this one
  * runs, and for callers that capture a step into a graph of their own (nothing is allocated, no event is recorded).  The kernels run on the
  * context's GPU, the one that was current in gacer_create, whichever is current now (a NULL stream is that GPU's).  The tenant's
- * split-K and attention workspaces belong to the context: two rounds of one tenant must not overlap, whichever calls issued them.  The
+ * split-K, attention and 8-bit products' workspaces belong to the context: two rounds of one tenant must not overlap, whichever calls issued them.  The
  * plan, the tenant's own stream and captured graphs play no part.  gacer_destroy and gacer_load_tenants do not wait for `stream`.
  */
 gacer_status gacer_enqueue(gacer_ctx *ctx, int tenant, void *stream);

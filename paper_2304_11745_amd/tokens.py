@@ -97,6 +97,7 @@ class Fp8Weight:
         self.codes, self.scales, self.device = codes, scales, codes.device
 
     @classmethod
+    @torch.no_grad()
     def quantise(cls, weight):
         """The 8-bit weights next to ``weight`` ``[out, in]``: in each block the largest magnitude becomes 448."""
         out, cin = weight.shape
