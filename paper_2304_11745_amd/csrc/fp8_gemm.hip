@@ -5,7 +5,7 @@
 // and more below it: an error of 1.5e-5 of the result on bell-shaped rows of 128 (4.8e-5 with an outlier), where this way it is 1e-8.
 //
 // Few rows are bound by the way of the weights to the units, many rows by the matrix cores and the power they may draw: 8192 rows of 8192 to 8192 features 880 to
-// 920 us = 1.25 PFLOP/s at 1.97 GHz, zeros instead of numbers 735 us at 2.4 GHz; a plain bf16 product of that size, with nothing to widen or scale, 670.
+// 950 us by the card = 1.25 to 1.16 PFLOP/s at about 1.97 GHz, zeros instead of numbers 735 us at 2.4 GHz; a plain bf16 product of that size, with nothing to widen or scale, 670.
 #include <hip/hip_runtime.h>
 #include <algorithm>
 #include "fp8.h"
@@ -26,7 +26,7 @@ template <typename T> __device__ __forceinline__ void finish(const Fp8Args &a, i
 // One workgroup of eight waves per tile of 32 features and 32 rows; the waves take the tile's blocks of 128 inner features in turn and their sums are added
 // in order.  Operands come straight from memory, three blocks of them in flight in registers: lane l holds feature (row) l % 32, and of every 32 inner
 // features the 16 codes of half l / 32.  Nothing is shared between waves, so that LDS and its barriers would only add to the chain of a load, eight
-// products and the join.  One row 4096 -> 6144 (25 MB of weights): 9.3 us, 8.8 of them in the kernel, 2.8 TB/s: 192 of 256 units, each
+// products and the join.  One row 4096 -> 6144 (25 MB of weights): 9.2 us, 9.0 of them in the kernel, 2.8 TB/s: 192 of 256 units, each
 // with 128 KB to fetch; all loads at once are no faster, and in tiles through LDS, 64x32 in two slices, it takes 12.1.
 template <typename T> __global__ __launch_bounds__(512) void fp8_few_kernel(Fp8Args a)
 {

@@ -1,7 +1,7 @@
 // Residual, RMS norm and 8-bit rows: h = x + res, y = h * rsqrt(mean(h^2) + eps) * gamma, then e4m3 codes with a scale for each row and block of 128 features.
 //
 // Every element is read and written once, the row in between in registers: bound by the way to memory.  4101 rows of 4096 features, bf16, with residual (118 MB):
-// 25.4 us = 4.6 TB/s; codes alone of 8192 rows of 8192 (203 MB) 39.7 us = 5.1 TB/s, what a large copy reaches; 1018 rows of 5008 in fp32 8.5 us, one row 5.3, of which a
+// 25.3 us = 4.7 TB/s; codes alone of 8192 rows of 8192 (203 MB) 39.4 us = 5.1 TB/s, what a large copy reaches; 1018 rows of 5008 in fp32 8.3 us, one row 5.3, of which a
 // launch in a stream of launches is 4.  With the loads under conditions, each waited for where it stood, they took 47, 54 and 16 us.
 #include <hip/hip_runtime.h>
 #include <algorithm>
@@ -186,10 +186,12 @@ LaunchInfo launch_rmsnorm_fp8(const TokenArgs &a, hipStream_t s, bool dry)
     n.x = a.x; n.res = a.res; n.gamma = a.gamma; n.y = a.y; n.codes = a.yq.codes; n.scales = a.yq.scales;
     n.eps = a.eps; n.C = a.features; n.inv_c = 1.f / (float)a.features; n.norm = a.norm; n.rows = a.batch * a.S;
     n.r_lo = a.b_lo * a.S; n.r_hi = a.b_hi * a.S;
-    // lanes of a row: a wave up to 1024 features, four up to 8192, else sixteen.  Measured, us with 64 / 256 / 1024 lanes, bf16, with residual: 8192 rows of 512
-    // 7.6 / 12.1 / 40, 8192 of 1024 11.4 / 14.0 / 40, 4101 of 4096 29.7 / 25.2 / 29.1, 2048 of 8192 - / 26.5 / 26.0, 1000 of 16384 - / 17.4 / 16.0.  Beyond
-    // 16384 features in pieces, us whole (in registers and, in part, scratch memory) / in pieces, with residual: 500 rows of 65536 121 / 67, of 32768 24 / 27, in fp32
-    // 214 / 121 and 54 / 60, one row of 65536 30 / 12; a product's inner extent of that size is rare, and one kernel does them all.
+    // lanes of a row: a wave up to 1024 features, four up to 8192, else sixteen.  Measured, us with 64 / 256 / 1024 lanes, codes and sum with residual, buffers of 1.5 GB in
+    // turn, so that the last-level cache holds none (the same ones again take up to 25 % less): bf16 8192 rows of 512 9.2 / 14.4 / 43, of 1024 14.9 / 17.5 / 45, of 1536
+    // 21.1 / 21.2 / 46, 4101 of 4096 30.4 / 26.3 / 30.5, 2048 of 8192 - / 27.6 / 26.8, of 12288 - / 44 / 41, 1000 of 16384 - / 30.4 / 29.5; fp32 8192 of 1024 25.1 / 26.7 / 62, of
+    // 1536 35.4 / 32.9 / 66, 4101 of 4096 51 / 44.5 / 50, 2048 of 8192 - / 45.7 / 44.2, of 12288 - / 68 / 75, 1000 of 16384 - / 49.4 / 48.0.  Beyond 16384 features in pieces, us whole (in
+    // registers and, from 65536 on, scratch memory) / in pieces: bf16 500 rows of 65536 113 / 68, one row 32 / 14, 500 of 32768 30 / 35, 2000 of 32768 99 / 117; fp32 200 / 120, 54 / 21,
+    // 48 / 60, 172 / 216; a product's inner extent of that size is rare, and one kernel does them all.
     const int runs = (a.features + 7) / 8, lanes = runs <= 128 ? 64 : runs <= 1024 ? 256 : 1024;
     const int per = lanes == 64 ? 4 : 1, each = (runs + lanes - 1) / lanes;
     // workgroups that a unit holds, by the registers of (64, 1), (64, 2), (256, 1), (256, 2), (256, 4) and wider

@@ -41,13 +41,16 @@ inline AttendGeom attend_geom(const TokenArgs &a)
 // Products of 8-bit rows, by the unsplit operator's shape (so that every decomposition adds in the same order): tiles of `features` of the result and
 // `rows`, `slices` parts of the inner extent that a second kernel joins.  The choice with the least estimated time is taken: rounds of workgroups over the units,
 // times blocks of 128 inner features in a slice, times what a block takes in this tile, and for a join its launch and its way through memory.
-// Measured, us, the choice first (bf16):
+// Measured, us, the choice first (bf16; operands of three calls in turn, 75 to 350 MB, of which the last-level cache keeps a part):
 //   4096 -> 6144: 1 row few 9.3, 64x32 in two slices 12.1; 32 rows few 12.1, 64x32 12.7; 64 rows 64x32 14.2, 64x64 15.2, in two 13.5; 128 rows 64x64 15.0, 128x128 34;
 //   512 rows 128x128 31, 64x64 37, 256x128 50; 1024 rows 256x128 53, 128x128 70.  4096 -> 32000: 1 row 64x32 29, few 37.
 //   14336 -> 4096: 1 row few in two 15.6, 64x32 in four 16.3, few whole 19.7; 32 rows 64x32 in four 16.5, few 20.5; 64 rows 64x64 in four 18.3, whole 44; 128 rows
 //   128x128 in eight 27.5, 64x64 in two 28.5, whole 44; 512 rows 128x128 in two 69, 64x64 82; 2048 rows 256x128 206, 128x128 253.
 //   gated, 4096 -> 14336: 1 row 256x32 in two 26.2, whole 32; 48 rows 256x64 in two 34.2, whole 35, 256x32 32; 128 rows 256x64 41, 256x128 51; 256 rows 256x128 64,
 //   256x64 80.
+// The constants below stand for these: a round's time less a launch of 4, over its blocks, is 0.32 for 64x32 (64 rows 4096 -> 6144), 0.34 for 64x64 (128), 0.84 for 128x128 (512), 1.53 for
+// 256x128 (1024), and gated, 4096 -> 14336, 0.88 for 256x32 (48 rows), 1.16 for 256x64 (128), 1.88 for 256x128 (256); they differ from it by up to 15 %.  The choice is within 7 % of the
+// best at the sizes above, and not the best at all of them (64 rows 4096 -> 6144, 48 gated rows).
 // Numbers of slices between the powers of two gain nothing (64 rows 4096 -> 6144 14.9 and in three 15.1, gated 128 rows 5120 -> 5120 27.7 and 26.7, 333 rows
 // 8192 -> 2048 25.0 and in five 25.5).
 enum Fp8Tile { FP8_FEW, FP8_64x32, FP8_64x64, FP8_128x128, FP8_256x128, FP8_256x64, FP8_256x32 };      // rows of weights (a gated block: half gate, half up) x rows
